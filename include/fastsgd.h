@@ -272,6 +272,119 @@ uint64_t fastsgd_key_encode_paper_bound(uint64_t d, uint32_t flag_bits);
 int fastsgd_key_encode_paper(const uint32_t* keys, uint64_t d, uint32_t flag_bits,
                              void* out, uint64_t out_bytes, void* stream);
 
+/* ---- where a worker's gradient begins: losses on logits, and their data as key-value pairs ----------
+ * (No counterpart in the paper, whose models end in a logistic or linear loss: these are the losses of
+ * models whose gradients are compressed today.)  All of them only enqueue kernels on `stream`.
+ */
+
+/* element types of logits and of their gradients */
+#define FASTSGD_F32  0
+#define FASTSGD_BF16 1
+#define FASTSGD_F16  2
+
+/* rows of logits, or of their gradient (host struct, device data) */
+typedef struct fastsgd_matrix {
+    void*    data;        /* aligned to its type; rows may begin at any element               */
+    uint64_t rows;        /* 0 .. 2^31 - 1; no row: the call checks its arguments and does nothing else */
+    uint64_t cols;        /* 1 .. 2^31 - 1                                                    */
+    uint64_t row_stride;  /* elements from one row to the next, cols .. 2^31 - 1; what lies between is not touched */
+    uint32_t type;        /* FASTSGD_F32, FASTSGD_BF16 or FASTSGD_F16                          */
+    uint32_t reserved;    /* must be 0                                                        */
+} fastsgd_matrix;
+
+/*
+ * The k largest of each row as (key, value) pairs: the top logits of a teacher, the experts that a router selects.
+ *   logits  rows x V
+ *   k       1 .. min(V, 1024)
+ *   keys    device, rows * k: column numbers in descending order of their values, equal values in ascending order of
+ *           their columns (NaN above everything, -0 equal to +0)
+ *   values  device, rows * k, the logits' type: their values
+ *   lse     device, rows floats, or NULL: log sum_j exp(z_j / temperature) of the row
+ *   tail    device, rows floats, or NULL: the share of that sum outside the k pairs (formed from them alone: no
+ *           difference of nearly equal numbers)
+ *   temperature  2^-20 .. 2^20; bears on lse and tail only
+ * A row of -inf has lse = -inf and tail = 0; NaN or +inf in a row makes both NaN.
+ */
+int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperature, int32_t* keys, void* values,
+                       float* lse, float* tail, void* stream);
+
+/* a teacher's top logits of every row (host struct, device data), as fastsgd_top_logits makes them */
+typedef struct fastsgd_pairs {
+    const int32_t* keys;    /* rows * k; a key outside [0, V) marks a pair that is not there    */
+    const void*    values;  /* rows * k, of `type`; -inf: a pair of no probability              */
+    const float*   tail;    /* rows, or NULL (0): the teacher's probability outside the pairs, 0 .. 1 */
+    uint32_t       k;       /* 1 .. 1024                                                        */
+    uint32_t       type;    /* of the values                                                    */
+} fastsgd_pairs;
+
+/*
+ * Distillation loss of a student's logits z against a teacher's top logits, and its gradient.  With q = softmax(z / T),
+ * the teacher's p_i = (1 - tail) softmax(values / T)_i over the pairs of the row that are there, and rest = the sum of q_j
+ * over the classes that are no key of the row:
+ *   loss[r]    = weight[r] T^2 ( sum_i p_i (log p_i - log q_key_i) + tail (log tail - log rest) )       (0 log 0 = 0)
+ *   grad[r, j] = d loss[r] / d z[r, j] = weight[r] T ( q_j - sum of p_i over the pairs with key_i = j )  for a key j
+ *                                        weight[r] T q_j (1 - tail / rest)                               else
+ * Without a tail the teacher's probability is that of the pairs alone, and the loss is the divergence from them to q.
+ *   student  rows x V, V <= 2^20 (else FASTSGD_E_NOT_IMPLEMENTED)
+ *   temperature  T, 2^-20 .. 2^20
+ *   weight   device, rows floats, or NULL (1): 1 / rows for the mean; a row of weight 0 (padding) is not read
+ *   loss     device, rows floats, or NULL
+ *   stats    device, 2 * rows floats, or NULL: what fastsgd_distill_loss_backward takes (of the logits that the sum runs over
+ *            -- all, or with a tail > 0 those that are no key -- one that is near the largest, and the sum of
+ *            exp((z - it) / T))
+ *   grad     rows x V, or NULL: of the logits' type, or fp32, as fastsgd_compress takes it; it may be the logits' own
+ *            place (same data, type and stride), otherwise apart from them
+ * At least one of loss, stats and grad is wanted.
+ * A row of weight 0, without a pair that is there, whose pairs all have value -inf, or whose logits are all -inf counts for
+ * nothing: loss 0, gradient 0.  Where the student rules out (-inf) what the teacher gives probability to, the loss is +inf.
+ * Pairs may come in any order, and keys may repeat.  One launch; the sums' order depends on the sizes and alignment alone.
+ */
+int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
+                         float* loss, float* stats, const fastsgd_matrix* grad, void* stream);
+
+/*
+ * The gradient alone, times the gradient of each row's loss, from what fastsgd_distill_loss kept: reads the logits once.
+ *   stats      as fastsgd_distill_loss wrote them for the same student, teacher, temperature and weight
+ *   grad_loss  device, rows floats, or NULL (1): grad[r, j] = grad_loss[r] d loss[r] / d z[r, j]
+ * Other arguments as there.
+ */
+int fastsgd_distill_loss_backward(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
+                                  const float* stats, const float* grad_loss, const fastsgd_matrix* grad, void* stream);
+
+/*
+ * How often each expert was selected, per segment of tokens.
+ *   selected  device, tokens * k, k <= experts: expert numbers; one outside [0, experts) was dropped and counts nowhere
+ *   experts   1 .. 1024; tokens < 2^31, tokens * k < 2^32
+ *   mask      device, tokens bytes, or NULL: tokens whose byte is 0 (padding) count nowhere
+ *   offsets   device, segments + 1 ascending token numbers: segment s is [offsets[s], offsets[s + 1]); NULL: one segment of
+ *             all tokens.  Tokens before the first and behind the last segment belong to none.
+ *   counts    device, segments * experts: written
+ *   counted   device, segments: the segment's tokens that the mask lets count
+ * Both add up over workers (Sec. 2.1): fastsgd_balance_loss takes the sums where the loss is that of all workers' tokens.
+ */
+int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, uint32_t experts, const uint8_t* mask,
+                          const uint64_t* offsets, uint32_t segments, uint32_t* counts, uint32_t* counted, void* stream);
+
+/*
+ * The balance loss of a router's logits x (tokens x experts) and its gradient.  Per segment s, with f_e = counts[s, e] / sum of
+ * counts[s, :], p_t = softmax(x_t) and the tokens t of the segment that the mask lets count:
+ *   loss[s]    = coef experts / counted[s] sum_t sum_e f_e p_te
+ *   grad[t, e] = grad_loss[s] coef experts / counted[s] p_te (f_e - sum_e' f_e' p_te')
+ * (the counts are constants of the gradient).  With the counts of all workers, loss[s] is this worker's part of the loss: the
+ * parts add up.
+ *   logits     cols = experts, 1 .. 1024
+ *   mask, offsets, segments (1 .. 2^24), counts, counted   as for fastsgd_expert_counts
+ *   grad_loss  device, segments floats, or NULL (1)
+ *   loss       device, segments floats, or NULL; needs a workspace of 2 MiB + 8 (2048 + segments) bytes, whatever the tokens
+ *   grad       tokens x experts, or NULL: type and place as for fastsgd_distill_loss.  Zero for tokens that do not count; rows
+ *              of tokens that belong to no segment are left as they are.
+ * A segment without counted tokens or without selections has loss 0 and gradient 0; so has a token whose logits are all -inf.
+ * One launch; the order of the sums depends on the sizes and offsets alone.
+ */
+int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, const uint64_t* offsets, uint32_t segments,
+                         const uint32_t* counts, const uint32_t* counted, float coef, const float* grad_loss,
+                         float* loss, const fastsgd_matrix* grad, void* stream);
+
 /* ---- helpers, not on the timed path (no counterpart in the paper) ---------- */
 
 /* worst-case stream size in bytes (every entry kept, every delta at the widest
@@ -284,6 +397,7 @@ uint64_t fastsgd_compress_bound(uint64_t n, const fastsgd_params* params);
  * 237 MB for 25.6 M, 619 MB for 2^26, 1.29 GB from 403 M on.
  * Any call is accepted with the part of it that it uses:
  *   decoder, model update     2 MiB, whatever n
+ *   fastsgd_balance_loss      2 MiB + 8 bytes for each of 2048 + segments
  *   fastsgd_abs_sum           2 MiB + 8 bytes per 2^14 entries
  *   fastsgd_compress_kv       2 MiB + 8 bytes per group
  *   fastsgd_compress          3 MiB + 2432 bytes per 2^14 entries + 12 per group

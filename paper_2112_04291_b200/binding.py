@@ -30,6 +30,7 @@ EXPORTS = [
     "fastsgd_strerror", "fastsgd_version", "fastsgd_kernel_timing_enable", "fastsgd_kernel_timing_read", "fastsgd_abs_sum_noalloc",
     "fastsgd_sparse_adam_update_batch", "fastsgd_sparse_adam_update_packed_batch", "fastsgd_key_encode_paper", "fastsgd_key_encode_paper_bound",
     "fastsgd_compress_kv",
+    "fastsgd_top_logits", "fastsgd_distill_loss", "fastsgd_distill_loss_backward", "fastsgd_expert_counts", "fastsgd_balance_loss",
     "fastsgd_debug_set_wait_limits", "fastsgd_debug_layout", "fastsgd_debug_set_grid",
     "fastsgd_debug_decoder_route",
 ]
@@ -42,6 +43,19 @@ class Params(C.Structure):
 
 class Adam(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("row_stride", C.c_uint64),
+                ("type", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class Pairs(C.Structure):
+    _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p), ("tail", C.c_void_p), ("k", C.c_uint32), ("type", C.c_uint32)]
+
+
+F32, BF16, F16 = 0, 1, 2
+TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
 def params(base: float, tau: int = 128, flag_bits: int = 2, group_log2: int = 14) -> Params:
@@ -86,6 +100,17 @@ def lib():
         L.fastsgd_sparse_adam_update_batch.argtypes = [C.POINTER(vp), u64p, C.c_uint32, u64, PP, C.POINTER(Adam), vp, vp, vp, vp, vp]
         L.fastsgd_sparse_adam_update_packed_batch.restype = C.c_int
         L.fastsgd_sparse_adam_update_packed_batch.argtypes = [C.POINTER(vp), u64p, C.c_uint32, u64, PP, C.POINTER(Adam), vp, vp]
+        MP, TP = C.POINTER(Matrix), C.POINTER(Pairs)
+        L.fastsgd_top_logits.restype = C.c_int
+        L.fastsgd_top_logits.argtypes = [MP, C.c_uint32, C.c_float, vp, vp, vp, vp, vp]
+        L.fastsgd_distill_loss.restype = C.c_int
+        L.fastsgd_distill_loss.argtypes = [MP, TP, C.c_float, vp, vp, vp, MP, vp]
+        L.fastsgd_distill_loss_backward.restype = C.c_int
+        L.fastsgd_distill_loss_backward.argtypes = [MP, TP, C.c_float, vp, vp, vp, MP, vp]
+        L.fastsgd_expert_counts.restype = C.c_int
+        L.fastsgd_expert_counts.argtypes = [vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp, vp]
+        L.fastsgd_balance_loss.restype = C.c_int
+        L.fastsgd_balance_loss.argtypes = [MP, vp, vp, C.c_uint32, vp, vp, C.c_float, vp, vp, MP, vp]
         L.fastsgd_compress_bound.restype = u64
         L.fastsgd_compress_bound.argtypes = [u64, PP]
         L.fastsgd_workspace_bytes.restype = u64
@@ -258,6 +283,108 @@ def key_encode_paper(keys: torch.Tensor, flag_bits: int, out: torch.Tensor, stre
     assert out.is_cuda and out.dtype == torch.uint8 and out.is_contiguous()
     return lib().fastsgd_key_encode_paper(keys.data_ptr() if keys.numel() else None, keys.numel(), int(flag_bits),
                                           out.data_ptr(), out.numel(), _stream_handle(stream))
+
+
+# ---- losses on logits, and their data as key-value pairs ----------------------------------------
+
+def _matrix(t: torch.Tensor) -> Matrix:
+    """Rows of logits or of a gradient: unit stride along a row, any stride between rows."""
+    assert t.is_cuda and t.dim() == 2 and t.dtype in TYPES and (t.stride(1) == 1 or t.shape[1] == 1)
+    rows, cols = t.shape
+    return Matrix(t.data_ptr() if rows else None, rows, cols, t.stride(0) if rows > 1 else cols, TYPES[t.dtype], 0)
+
+
+def _beside(t, like: torch.Tensor, dtypes, shape):
+    """Address of a contiguous tensor of the given type(s) and shape on the device of `like` (None: 0)."""
+    if t is None:
+        return None
+    assert t.device == like.device and t.dtype in dtypes and t.is_contiguous() and t.shape == shape
+    return t.data_ptr()
+
+
+_F32, _I32 = (torch.float32,), (torch.int32,)
+
+
+def _here(t: torch.Tensor) -> None:
+    assert t.device.index == torch.cuda.current_device(), "tensors live on the current device"
+
+
+def top_logits(logits: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, temperature: float = 1.0, lse: torch.Tensor = None,
+               tail: torch.Tensor = None, stream=None) -> int:
+    """fastsgd_top_logits: the k largest of each row as (key, value) pairs; keys and values are [rows, k]."""
+    m = _matrix(logits)
+    _here(logits)
+    rows, k = keys.shape
+    assert rows == m.rows
+    return lib().fastsgd_top_logits(C.byref(m), k, temperature, _beside(keys, logits, _I32, keys.shape),
+                                    _beside(values, logits, (logits.dtype,), keys.shape), _beside(lse, logits, _F32, (rows,)),
+                                    _beside(tail, logits, _F32, (rows,)), _stream_handle(stream))
+
+
+def _teacher(student, keys, values, tail) -> Pairs:
+    rows, k = keys.shape
+    assert rows == student.shape[0]
+    return Pairs(_beside(keys, student, _I32, keys.shape), _beside(values, student, tuple(TYPES), keys.shape),
+                 _beside(tail, student, _F32, (rows,)), k, TYPES[values.dtype])
+
+
+def _gradient(grad, logits):
+    if grad is None:
+        return None
+    assert grad.device == logits.device
+    return C.byref(_matrix(grad))
+
+
+def distill_loss(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
+                 temperature: float = 1.0, tail: torch.Tensor = None, weight: torch.Tensor = None, stats: torch.Tensor = None, stream=None) -> int:
+    """fastsgd_distill_loss: loss [rows] of student logits against a teacher's pairs [rows, k], and its gradient."""
+    m, rows = _matrix(student), student.shape[0]
+    _here(student)
+    t = _teacher(student, keys, values, tail)
+    return lib().fastsgd_distill_loss(C.byref(m), C.byref(t), temperature, _beside(weight, student, _F32, (rows,)),
+                                      _beside(loss, student, _F32, (rows,)), _beside(stats, student, _F32, (rows, 2)),
+                                      _gradient(grad, student), _stream_handle(stream))
+
+
+def distill_loss_backward(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, stats: torch.Tensor, grad: torch.Tensor,
+                          grad_loss: torch.Tensor = None, temperature: float = 1.0, tail: torch.Tensor = None, weight: torch.Tensor = None,
+                          stream=None) -> int:
+    """fastsgd_distill_loss_backward: the gradient from the stats [rows, 2] of a forward call, times grad_loss [rows]."""
+    m, rows = _matrix(student), student.shape[0]
+    _here(student)
+    t = _teacher(student, keys, values, tail)
+    return lib().fastsgd_distill_loss_backward(C.byref(m), C.byref(t), temperature, _beside(weight, student, _F32, (rows,)),
+                                               _beside(stats, student, _F32, (rows, 2)), _beside(grad_loss, student, _F32, (rows,)),
+                                               _gradient(grad, student), _stream_handle(stream))
+
+
+def _tokens(like, tokens, mask, offsets, segments):
+    assert offsets is not None or segments == 1
+    return (_beside(mask, like, (torch.bool, torch.uint8), (tokens,)), _beside(offsets, like, (torch.int64,), (segments + 1,)))
+
+
+def expert_counts(selected: torch.Tensor, counts: torch.Tensor, counted: torch.Tensor, mask: torch.Tensor = None, offsets: torch.Tensor = None,
+                  stream=None) -> int:
+    """fastsgd_expert_counts: selected [tokens, k] -> counts [segments, experts], counted [segments] (int32 tensors)."""
+    assert counts.is_cuda
+    _here(counts)
+    (tokens, k), (segments, experts) = selected.shape, counts.shape
+    at_mask, at_offsets = _tokens(counts, tokens, mask, offsets, segments)
+    return lib().fastsgd_expert_counts(_beside(selected, counts, _I32, (tokens, k)), tokens, k, experts, at_mask, at_offsets, segments,
+                                       _beside(counts, counts, _I32, (segments, experts)), _beside(counted, counts, _I32, (segments,)),
+                                       _stream_handle(stream))
+
+
+def balance_loss(logits: torch.Tensor, counts: torch.Tensor, counted: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
+                 coef: float = 1.0, mask: torch.Tensor = None, offsets: torch.Tensor = None, grad_loss: torch.Tensor = None, stream=None) -> int:
+    """fastsgd_balance_loss: loss [segments] of router logits [tokens, experts] for given counts, and its gradient."""
+    m = _matrix(logits)
+    _here(logits)
+    (tokens, experts), segments = logits.shape, counts.shape[0]
+    at_mask, at_offsets = _tokens(logits, tokens, mask, offsets, segments)
+    return lib().fastsgd_balance_loss(C.byref(m), at_mask, at_offsets, segments, _beside(counts, logits, _I32, (segments, experts)),
+                                      _beside(counted, logits, _I32, (segments,)), coef, _beside(grad_loss, logits, _F32, (segments,)),
+                                      _beside(loss, logits, _F32, (segments,)), _gradient(grad, logits), _stream_handle(stream))
 
 
 def stream_info(stream_in: torch.Tensor, stream=None):

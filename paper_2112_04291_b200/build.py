@@ -14,7 +14,7 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-fast-math",
     "--fmad=false", "--ftz=false", "--prec-div=true", "--prec-sqrt=true",
-    "-cudart", "static",
+    "-cudart", "static", "--threads", "4",
 ]
 
 

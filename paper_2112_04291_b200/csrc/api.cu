@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "host.cuh"
 #include "sum.cuh"
 #include "bits.cuh"
 #include "prims.cuh"
@@ -240,19 +241,6 @@ int ensure_device_setup() {
     return FASTSGD_OK;
 }
 
-// A launch whose blocks may move onto the GPU while the previous kernel of the stream drains (programmatic dependent launch): the
-// kernel itself waits (wait_for_previous_kernels) before it reads or writes memory.
-cudaError_t launch_overlapped(const void* fn, unsigned grid, unsigned threads, size_t smem, void** kargs, cudaStream_t st) {
-    cudaLaunchConfig_t c;
-    std::memset(&c, 0, sizeof(c));
-    c.gridDim = dim3(grid); c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = at; c.numAttrs = 1;
-    return cudaLaunchKernelExC(&c, fn, kargs);
-}
-
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // 1 / b^k (kernels multiply with it where that gives the quotient's rounding)
@@ -275,6 +263,35 @@ int launch_sum(const float* grad, uint64_t n, Control* ctl, double* partials, do
 }
 
 }  // namespace
+
+// What other translation units see of the state (host.cuh).
+namespace fsg {
+
+int device_view(DeviceView* out) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    FSG_DEVICE_STATE();
+    const int rc = ensure_device_setup();
+    if (rc) return rc;
+    out->ws = g_state.ws; out->ws_bytes = g_state.ws_bytes; out->sm_count = g_state.sm_count;
+    return FASTSGD_OK;
+}
+
+void count_launches(uint64_t launches) { g_launches.fetch_add(launches, std::memory_order_relaxed); }
+
+cudaError_t launch_overlapped(const void* fn, unsigned grid, unsigned threads, size_t smem, void** kargs, cudaStream_t st, unsigned cluster) {
+    cudaLaunchConfig_t c;
+    std::memset(&c, 0, sizeof(c));
+    c.gridDim = dim3(grid); c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    c.attrs = at; c.numAttrs = cluster > 1u ? 2 : 1;
+    return cudaLaunchKernelExC(&c, fn, kargs);
+}
+
+}  // namespace fsg
 
 extern "C" {
 

@@ -11,6 +11,7 @@ constexpr uint32_t kMagic       = 0x31475346u;   // "FSG1"
 constexpr uint32_t kVersion     = 1u;
 constexpr uint32_t kHeaderBytes = 64u;
 constexpr int      kMaxTau      = 128;
+constexpr unsigned kFullMask    = 0xFFFFFFFFu;
 
 // The sum tree is cut into aligned chunks of 2^14 entries: one fp64 partial per chunk.
 constexpr int      kChunkLog2   = 14;
@@ -32,7 +33,7 @@ struct Control {
     unsigned int       done;           // blocks of the sum kernel that have finished (self-resetting)
     unsigned int       pad0;
     unsigned int       error;          // encode: non-zero once a bounded wait ran out
-    unsigned int       pad1;
+    unsigned int       loss_done;      // blocks of the balance loss that have finished (self-resetting)
     unsigned long long decode_status;  // min over failures of (group << 32 | key index << 8 | status)
     double             sum;            // S
     unsigned int       bar_gen;        // launches of the kernels whose blocks wait for one another that have finished

@@ -1,0 +1,225 @@
+// C-ABI entries of the operators that a worker's gradient begins with: top logits, the distillation loss, the balance loss.
+// Argument checks and launches on the caller's stream, as in api.cu.
+#include "../../include/fastsgd.h"
+
+#include <cmath>
+
+#include "host.cuh"
+#include "top.cuh"
+#include "distill.cuh"
+#include "balance.cuh"
+
+namespace {
+
+using namespace fsg;
+
+constexpr double kLog2E = 1.4426950408889634;
+constexpr float  kLeastTemperature = 1.f / 1048576.f, kMostTemperature = 1048576.f;
+
+uint32_t size_of(uint32_t type) { return type == FASTSGD_F32 ? 4u : 2u; }
+bool is_type(uint32_t type) { return type == FASTSGD_F32 || type == FASTSGD_BF16 || type == FASTSGD_F16; }
+bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool is_temperature(float t) { return t >= kLeastTemperature && t <= kMostTemperature; }
+
+int check_matrix(const fastsgd_matrix* m) {
+    if (!m) return FASTSGD_E_NULL;
+    if (!is_type(m->type) || m->reserved) return FASTSGD_E_BAD_PARAM;
+    if (m->rows >= (1ull << 31) || m->cols == 0 || m->cols >= (1ull << 31)) return FASTSGD_E_BAD_N;
+    if (m->row_stride < m->cols || m->row_stride >= (1ull << 31)) return FASTSGD_E_BAD_PARAM;
+    if (m->rows && !m->data) return FASTSGD_E_NULL;
+    if (!aligned_to(m->data, size_of(m->type))) return FASTSGD_E_ALIGN;
+    return FASTSGD_OK;
+}
+
+uint64_t span_bytes(const fastsgd_matrix* m) { return m->rows ? ((m->rows - 1) * m->row_stride + m->cols) * size_of(m->type) : 0; }
+
+// A gradient: of the logits' shape, in their type or fp32; the logits' own place, element for element, or apart from them.
+int check_grad(const fastsgd_matrix* grad, const fastsgd_matrix* logits) {
+    const int rc = check_matrix(grad);
+    if (rc) return rc;
+    if (grad->rows != logits->rows || grad->cols != logits->cols) return FASTSGD_E_BAD_PARAM;
+    if (grad->type != logits->type && grad->type != FASTSGD_F32) return FASTSGD_E_BAD_PARAM;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(grad->data), b = reinterpret_cast<uintptr_t>(logits->data);
+    const bool same = a == b && grad->type == logits->type && grad->row_stride == logits->row_stride;
+    if (!same && a < b + span_bytes(logits) && b < a + span_bytes(grad)) return FASTSGD_E_BAD_PARAM;
+    return FASTSGD_OK;
+}
+
+int launched(cudaError_t err, uint64_t launches = 1) {
+    if (err != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
+    count_launches(launches);
+    return FASTSGD_OK;
+}
+
+// blocks of a kernel that stay on the GPU at once
+int resident_blocks(const void* fn, int threads, size_t smem, const DeviceView& dev, uint64_t* out) {
+    int per_sm = 0;
+    if (smem > 16u * 1024u && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, threads, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); return FASTSGD_E_CUDA; }
+    *out = (uint64_t)per_sm * (uint64_t)dev.sm_count;
+    return FASTSGD_OK;
+}
+
+template <int MODE> const void* distill_kernel(uint32_t z, uint32_t g) {
+    if (z == FASTSGD_F32) return (const void*)k_distill<float, float, MODE>;
+    if (z == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_distill<__nv_bfloat16, float, MODE> : (const void*)k_distill<__nv_bfloat16, __nv_bfloat16, MODE>;
+    return g == FASTSGD_F32 ? (const void*)k_distill<__half, float, MODE> : (const void*)k_distill<__half, __half, MODE>;
+}
+const void* balance_kernel(uint32_t x, uint32_t g) {
+    if (x == FASTSGD_F32) return (const void*)k_balance<float, float>;
+    if (x == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_balance<__nv_bfloat16, float> : (const void*)k_balance<__nv_bfloat16, __nv_bfloat16>;
+    return g == FASTSGD_F32 ? (const void*)k_balance<__half, float> : (const void*)k_balance<__half, __half>;
+}
+
+int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
+            float* loss, float* stats_out, const float* stats_in, const float* grad_loss, const fastsgd_matrix* grad, void* stream) {
+    int rc = check_matrix(student);
+    if (rc) return rc;
+    if (!teacher) return FASTSGD_E_NULL;
+    if (!is_type(teacher->type) || teacher->k < 1u || teacher->k > kDistillMaxPairs || !is_temperature(temperature)) return FASTSGD_E_BAD_PARAM;
+    if (student->rows && (!teacher->keys || !teacher->values)) return FASTSGD_E_NULL;
+    if (!aligned_to(teacher->keys, 4) || !aligned_to(teacher->values, size_of(teacher->type)) || !aligned_to(teacher->tail, 4) || !aligned_to(weight, 4)
+        || !aligned_to(loss, 4) || !aligned_to(stats_out, 4) || !aligned_to(stats_in, 4) || !aligned_to(grad_loss, 4)) return FASTSGD_E_ALIGN;
+    if (grad) { rc = check_grad(grad, student); if (rc) return rc; }
+    if (student->cols > kDistillMaxCols) return FASTSGD_E_NOT_IMPLEMENTED;
+    if (!student->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    DistillArgs a{};
+    a.z = student->data; a.rows = student->rows; a.cols = (uint32_t)student->cols; a.z_stride = student->row_stride;
+    if (grad) { a.grad = grad->data; a.grad_stride = grad->row_stride; }
+    a.keys = teacher->keys; a.values = teacher->values; a.tail = teacher->tail; a.k = teacher->k; a.values_type = teacher->type;
+    a.weight = weight; a.grad_loss = grad_loss; a.stats_in = stats_in; a.loss = loss; a.stats_out = stats_out;
+    a.temperature = temperature; a.inv_t = 1.f / temperature; a.c = (float)(kLog2E / (double)temperature); a.slack = exp_slack(a.c);
+    const uint32_t gt = grad ? grad->type : student->type;
+    const void* fn = mode == kLossOnly ? distill_kernel<kLossOnly>(student->type, gt)
+                   : mode == kLossAndGrad ? distill_kernel<kLossAndGrad>(student->type, gt) : distill_kernel<kGradOnly>(student->type, gt);
+    const size_t smem = 4u * ((a.cols + 31u) / 32u + 1u);
+    uint64_t grid = 0;
+    rc = resident_blocks(fn, kDistillThreads, smem, dev, &grid);
+    if (rc) return rc;
+    if (grid > a.rows) grid = a.rows;
+    void* kargs[] = {&a};
+    return launched(launch_overlapped(fn, (unsigned)grid, kDistillThreads, smem, kargs, static_cast<cudaStream_t>(stream)));
+}
+
+// tokens a block of the router's kernels takes, and the blocks
+uint32_t rows_per_block(uint64_t tokens, uint64_t least, uint64_t blocks) {
+    uint64_t rows = (tokens + blocks - 1) / blocks;
+    return (uint32_t)(rows < least ? least : rows);
+}
+
+int check_tokens(uint64_t tokens, uint32_t segments, const uint64_t* offsets) {
+    if (tokens >= (1ull << 31)) return FASTSGD_E_BAD_N;
+    if (segments < 1u || segments > (1u << 24)) return FASTSGD_E_BAD_PARAM;
+    if (!offsets && segments != 1u) return FASTSGD_E_NULL;
+    return aligned_to(offsets, 8) ? FASTSGD_OK : FASTSGD_E_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperature, int32_t* keys, void* values,
+                       float* lse, float* tail, void* stream) {
+    int rc = check_matrix(logits);
+    if (rc) return rc;
+    if (k < 1u || k > kTopMaxPairs || k > logits->cols || !is_temperature(temperature)) return FASTSGD_E_BAD_PARAM;
+    if (logits->rows && (!keys || !values)) return FASTSGD_E_NULL;
+    if (!aligned_to(keys, 4) || !aligned_to(values, size_of(logits->type)) || !aligned_to(lse, 4) || !aligned_to(tail, 4)) return FASTSGD_E_ALIGN;
+    if (!logits->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    TopArgs a{};
+    a.z = logits->data; a.rows = logits->rows; a.cols = (uint32_t)logits->cols; a.z_stride = logits->row_stride;
+    a.keys = keys; a.values = values; a.lse = lse; a.tail = tail; a.k = k;
+    a.temperature = temperature; a.c = (float)(kLog2E / (double)temperature);
+    const void* fn = logits->type == FASTSGD_F32 ? (const void*)k_top<float> : logits->type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16> : (const void*)k_top<__half>;
+    uint64_t grid = 0;
+    rc = resident_blocks(fn, kTopThreads, 0, dev, &grid);
+    if (rc) return rc;
+    if (grid > a.rows) grid = a.rows;
+    void* kargs[] = {&a};
+    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, 0, kargs, static_cast<cudaStream_t>(stream)));
+}
+
+int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
+                         float* loss, float* stats, const fastsgd_matrix* grad, void* stream) {
+    if (!loss && !stats && !grad) return FASTSGD_E_NULL;
+    return distill(grad ? kLossAndGrad : kLossOnly, student, teacher, temperature, weight, loss, stats, nullptr, nullptr, grad, stream);
+}
+
+int fastsgd_distill_loss_backward(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
+                                  const float* stats, const float* grad_loss, const fastsgd_matrix* grad, void* stream) {
+    if (!grad) return FASTSGD_E_NULL;
+    if (student && student->rows && !stats) return FASTSGD_E_NULL;
+    return distill(kGradOnly, student, teacher, temperature, weight, nullptr, nullptr, stats, grad_loss, grad, stream);
+}
+
+int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, uint32_t experts, const uint8_t* mask,
+                          const uint64_t* offsets, uint32_t segments, uint32_t* counts, uint32_t* counted, void* stream) {
+    int rc = check_tokens(tokens, segments, offsets);
+    if (rc) return rc;
+    if (experts < 1u || experts > kBalanceMaxExperts || k < 1u || k > experts) return FASTSGD_E_BAD_PARAM;
+    if (!counts || !counted || (tokens && !selected)) return FASTSGD_E_NULL;
+    if (!aligned_to(selected, 4) || !aligned_to(counts, 4) || !aligned_to(counted, 4)) return FASTSGD_E_ALIGN;
+    if (tokens * k >= (1ull << 32)) return FASTSGD_E_BAD_N;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cudaMemsetAsync(counts, 0, 4ull * segments * experts, st) != cudaSuccess || cudaMemsetAsync(counted, 0, 4ull * segments, st) != cudaSuccess) {
+        cudaGetLastError();
+        return FASTSGD_E_CUDA;
+    }
+    if (!tokens) return FASTSGD_OK;
+    CountArgs a{};
+    a.selected = selected; a.mask = mask; a.offsets = offsets; a.counts = counts; a.counted = counted;
+    a.tokens = tokens; a.k = k; a.experts = experts; a.segments = segments;
+    a.rows_per_block = rows_per_block(tokens, 64u, 4ull * (uint64_t)dev.sm_count);
+    void* kargs[] = {&a};
+    const unsigned grid = (unsigned)((tokens + a.rows_per_block - 1) / a.rows_per_block);
+    return launched(cudaLaunchKernel((const void*)k_expert_counts, dim3(grid), dim3(kBalanceThreads), kargs, 0, st));
+}
+
+int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, const uint64_t* offsets, uint32_t segments,
+                         const uint32_t* counts, const uint32_t* counted, float coef, const float* grad_loss,
+                         float* loss, const fastsgd_matrix* grad, void* stream) {
+    int rc = check_matrix(logits);
+    if (rc) return rc;
+    rc = check_tokens(logits->rows, segments, offsets);
+    if (rc) return rc;
+    if ((!loss && !grad) || !counts || !counted) return FASTSGD_E_NULL;
+    if (logits->cols > kBalanceMaxExperts || !std::isfinite(coef)) return FASTSGD_E_BAD_PARAM;
+    if (!aligned_to(counts, 4) || !aligned_to(counted, 4) || !aligned_to(grad_loss, 4) || !aligned_to(loss, 4)) return FASTSGD_E_ALIGN;
+    if (grad) { rc = check_grad(grad, logits); if (rc) return rc; }
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (loss && (!dev.ws || dev.ws_bytes < kPartialsOffset + 8ull * (kBalanceMaxBlocks + (uint64_t)segments))) return FASTSGD_E_NO_WORKSPACE;
+    if (!logits->rows) {
+        if (loss && cudaMemsetAsync(loss, 0, 4ull * segments, st) != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
+        return FASTSGD_OK;
+    }
+    BalanceArgs a{};
+    a.x = logits->data; a.x_stride = logits->row_stride; a.tokens = logits->rows; a.experts = (uint32_t)logits->cols;
+    if (grad) { a.grad = grad->data; a.grad_stride = grad->row_stride; }
+    a.mask = mask; a.offsets = offsets; a.segments = segments; a.counts = counts; a.counted = counted; a.grad_loss = grad_loss;
+    a.loss = loss; a.coef = coef;
+    a.partials = reinterpret_cast<double*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset);
+    a.done = loss ? &static_cast<Control*>(dev.ws)->loss_done : nullptr;
+    const void* fn = balance_kernel(logits->type, grad ? grad->type : logits->type);
+    uint64_t blocks = 0;
+    rc = resident_blocks(fn, kBalanceThreads, 0, dev, &blocks);
+    if (rc) return rc;
+    if (blocks > kBalanceMaxBlocks) blocks = kBalanceMaxBlocks;
+    a.rows_per_block = rows_per_block(a.tokens, kBalanceWarps, blocks);
+    void* kargs[] = {&a};
+    const unsigned grid = (unsigned)((a.tokens + a.rows_per_block - 1) / a.rows_per_block);
+    return launched(launch_overlapped(fn, grid, kBalanceThreads, 0, kargs, st));
+}
+
+}  // extern "C"

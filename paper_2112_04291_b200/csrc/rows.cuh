@@ -1,0 +1,198 @@
+// Rows of logits: element types, 16-byte loads and stores at any row alignment, sums of exponentials relative to a running
+// maximum, and block-wide reductions.  Shared by the kernels on top logits, the distillation loss and the balance loss.
+//
+// exp(x / T) is taken as 2^(x c), c = log2(e) / T, always of a difference (x - m): a difference of two logits is exact where it
+// matters, whereas x c - m c would carry the rounding of m c (and overflow for a row of the type's lowest value).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace fsg {
+
+constexpr uint32_t kTypeF32 = 0u, kTypeBf16 = 1u, kTypeF16 = 2u;
+constexpr float    kLowest  = -3.402823466e+38f;
+
+__device__ __forceinline__ float exp2_fast(float x) {       // relative error 2^-22; results below 2^-126 are zero
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <class T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// element i of an array whose type is known at run time only
+__device__ __forceinline__ float load_typed(const void* p, uint64_t i, uint32_t type) {
+    return type == kTypeF32 ? static_cast<const float*>(p)[i]
+         : type == kTypeBf16 ? to_float(static_cast<const __nv_bfloat16*>(p)[i]) : to_float(static_cast<const __half*>(p)[i]);
+}
+
+// 16 bytes that are read once by one thread
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, uint4 v) {
+    asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// The elements of a 16-byte vector of T.
+template <class T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void unpack(uint4 v, float (&f)[4]) {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ float max(uint4 v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ float max(uint4 v) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__bfloat162float(m.x), __bfloat162float(m.y));
+    }
+};
+template <> struct Vec<__half> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 x = __half22float2(h[i]); f[2 * i] = x.x; f[2 * i + 1] = x.y; }
+    }
+    static __device__ __forceinline__ float max(uint4 v) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+        const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__half2float(m.x), __half2float(m.y));
+    }
+};
+
+// N consecutive values to an array of T, in 16-byte stores (wide) or one by one.
+template <int N> __device__ __forceinline__ void store_values(float* p, const float (&f)[N], bool wide) {
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            store16(p + i, make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = f[i];
+    }
+}
+template <class T> __device__ __forceinline__ uint32_t pack_two(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack_two<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack_two<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <class T, int N> __device__ __forceinline__ void store_values(T* p, const float (&f)[N], bool wide) {
+    static_assert(N == 8, "a vector of 16-bit values");
+    if (wide) store16(p, make_uint4(pack_two<T>(f[0], f[1]), pack_two<T>(f[2], f[3]), pack_two<T>(f[4], f[5]), pack_two<T>(f[6], f[7])));
+    else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = from_float<T>(f[i]);
+    }
+}
+
+// A run of n elements from p on: `head` single elements up to a 16-byte boundary, `vecs` vectors, `tail` single elements.
+struct Span {
+    uint32_t head, vecs, tail;
+};
+template <class T> __device__ __forceinline__ Span span_of(const T* p, uint32_t n) {
+    Span s;
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (uint32_t)sizeof(T);
+    s.head = off ? (uint32_t)Vec<T>::N - off : 0u;
+    if (s.head > n) s.head = n;
+    s.vecs = (n - s.head) / (uint32_t)Vec<T>::N;
+    s.tail = n - s.head - s.vecs * (uint32_t)Vec<T>::N;
+    return s;
+}
+
+// sum of 2^((x - m) c) over the values added so far.  m is one of them, or the lowest value; it follows the largest only once that
+// is 2^40 times what m gives, so that the sum is hardly ever rescaled and stays far from overflow.  Infinite values of -inf add
+// nothing; NaN and +inf make the sum NaN.
+struct ExpSum {
+    float m, s;
+    __device__ __forceinline__ ExpSum() : m(kLowest), s(0.f) {}
+    __device__ __forceinline__ void raise(float top, float c, float slack) {
+        if (top > m + slack) { s *= exp2_fast((m - top) * c); m = top; }
+    }
+    __device__ __forceinline__ void add(float x, float c, float slack) {
+        raise(x, c, slack);
+        s += exp2_fast((x - m) * c);
+    }
+    __device__ __forceinline__ void join(float m2, float s2, float c) {
+        const float top = fmaxf(m, m2);
+        s = s * exp2_fast((m - top) * c) + s2 * exp2_fast((m2 - top) * c);
+        m = top;
+    }
+};
+// 40 powers of two, in logits (bounded: m + slack has to stay below any value when m is the lowest)
+__host__ __device__ __forceinline__ float exp_slack(float c) { return fminf(40.f / c, 1e30f); }
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFullMask, v, o));
+    return v;
+}
+template <class F> __device__ __forceinline__ F warp_sum(F v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFullMask, v, o);
+    return v;
+}
+__device__ __forceinline__ ExpSum warp_join(ExpSum e, float c) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float m2 = __shfl_xor_sync(kFullMask, e.m, o), s2 = __shfl_xor_sync(kFullMask, e.s, o);
+        e.join(m2, s2, c);
+    }
+    return e;
+}
+
+// Block-wide, the result in every thread; `s` holds a value per warp and is free again once the next barrier has passed.
+template <int WARPS> __device__ __forceinline__ float block_max(float v, float* s) {
+    v = warp_max(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    return warp_max(lane < WARPS ? s[lane] : -INFINITY);
+}
+template <int WARPS, class F> __device__ __forceinline__ F block_sum(F v, F* s) {
+    v = warp_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    return warp_sum(lane < WARPS ? s[lane] : (F)0);
+}
+template <int WARPS> __device__ __forceinline__ ExpSum block_join(ExpSum e, float2* s, float c) {
+    e = warp_join(e, c);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(e.m, e.s);
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    ExpSum r;
+    if (lane < WARPS) { r.m = s[lane].x; r.s = s[lane].y; }
+    return warp_join(r, c);
+}
+
+}  // namespace fsg

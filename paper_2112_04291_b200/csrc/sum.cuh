@@ -13,7 +13,6 @@
 namespace fsg {
 
 constexpr int kSumThreads = 512;
-constexpr unsigned kFullMask = 0xFFFFFFFFu;
 
 __device__ __forceinline__ double abs_sum4(float4 v) {
     double a = (double)fabsf(v.x), b = (double)fabsf(v.y), c = (double)fabsf(v.z), d = (double)fabsf(v.w);
