@@ -51,7 +51,7 @@ int launched(cudaError_t err, uint64_t launches = 1) {
     return FASTSGD_OK;
 }
 
-// blocks of a kernel that stay on the GPU at once
+// Blocks of a kernel that stay on the GPU at once.
 int resident_blocks(const void* fn, int threads, size_t smem, const DeviceView& dev, uint64_t* out) {
     int per_sm = 0;
     if (smem > 16u * 1024u && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
@@ -69,6 +69,14 @@ const void* balance_kernel(uint32_t x, uint32_t g) {
     if (x == FASTSGD_F32) return (const void*)k_balance<float, float>;
     if (x == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_balance<__nv_bfloat16, float> : (const void*)k_balance<__nv_bfloat16, __nv_bfloat16>;
     return g == FASTSGD_F32 ? (const void*)k_balance<__half, float> : (const void*)k_balance<__half, __half>;
+}
+
+template <class T> const void* top_rows_kernel_of(uint32_t cols) {
+    return cols <= 32u ? (const void*)k_top_rows<T, 1> : cols <= 64u ? (const void*)k_top_rows<T, 2> : cols <= 128u ? (const void*)k_top_rows<T, 4>
+         : cols <= 256u ? (const void*)k_top_rows<T, 8> : cols <= 512u ? (const void*)k_top_rows<T, 16> : (const void*)k_top_rows<T, 32>;
+}
+const void* top_rows_kernel(uint32_t type, uint32_t cols) {
+    return type == FASTSGD_F32 ? top_rows_kernel_of<float>(cols) : type == FASTSGD_BF16 ? top_rows_kernel_of<__nv_bfloat16>(cols) : top_rows_kernel_of<__half>(cols);
 }
 
 int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
@@ -135,14 +143,23 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
     TopArgs a{};
     a.z = logits->data; a.rows = logits->rows; a.cols = (uint32_t)logits->cols; a.z_stride = logits->row_stride;
     a.keys = keys; a.values = values; a.lse = lse; a.tail = tail; a.k = k;
-    a.temperature = temperature; a.c = (float)(kLog2E / (double)temperature);
-    const void* fn = logits->type == FASTSGD_F32 ? (const void*)k_top<float> : logits->type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16> : (const void*)k_top<__half>;
-    uint64_t grid = 0;
-    rc = resident_blocks(fn, kTopThreads, 0, dev, &grid);
-    if (rc) return rc;
-    if (grid > a.rows) grid = a.rows;
+    a.temperature = temperature; a.c = (float)(kLog2E / (double)temperature); a.slack = exp_slack(a.c);
     void* kargs[] = {&a};
-    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, 0, kargs, static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.cols <= kTopRowsMaxCols && k <= kTopRowsMaxPairs) {
+        const unsigned grid = (unsigned)((a.rows + kTopRowsThreads / 32 - 1) / (kTopRowsThreads / 32));
+        return launched(launch_overlapped(top_rows_kernel(logits->type, a.cols), grid, kTopRowsThreads, 0, kargs, st));
+    }
+    const void* fn = logits->type == FASTSGD_F32 ? (const void*)k_top<float> : logits->type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16> : (const void*)k_top<__half>;
+    uint64_t resident = 0;
+    rc = resident_blocks(fn, kTopThreads, sizeof(TopShared), dev, &resident);
+    if (rc) return rc;
+    // few rows: a cluster of up to 8 blocks shares each, as long as a block has two tiles' worth of 16-bit values for every four threads
+    unsigned blocks = 1u;
+    while (blocks < 8u && a.rows * blocks * 2u <= resident && a.cols / (2u * blocks) >= 8192u) blocks *= 2u;
+    a.slice = ((a.cols + blocks - 1u) / blocks + 63u) & ~63u;
+    uint64_t grid = a.rows * blocks < resident ? a.rows * blocks : resident / blocks * blocks;
+    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, sizeof(TopShared), kargs, st, blocks));
 }
 
 int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,

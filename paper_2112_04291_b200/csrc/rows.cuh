@@ -45,7 +45,13 @@ __device__ __forceinline__ void store16(void* p, uint4 v) {
     asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// The elements of a 16-byte vector of T.
+__device__ __forceinline__ float nan_or_max(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+// The elements of a 16-byte vector of T, and their maximum (without NaN, or NaN if there is one).
 template <class T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int N = 4;
@@ -54,6 +60,9 @@ template <> struct Vec<float> {
     }
     static __device__ __forceinline__ float max(uint4 v) {
         return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    static __device__ __forceinline__ float max_nan(uint4 v) {
+        return nan_or_max(nan_or_max(__uint_as_float(v.x), __uint_as_float(v.y)), nan_or_max(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
 };
 template <> struct Vec<__nv_bfloat16> {
@@ -68,6 +77,11 @@ template <> struct Vec<__nv_bfloat16> {
         const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
         return fmaxf(__bfloat162float(m.x), __bfloat162float(m.y));
     }
+    static __device__ __forceinline__ float max_nan(uint4 v) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        return nan_or_max(__bfloat162float(m.x), __bfloat162float(m.y));
+    }
 };
 template <> struct Vec<__half> {
     static constexpr int N = 8;
@@ -80,6 +94,11 @@ template <> struct Vec<__half> {
         const __half2* h = reinterpret_cast<const __half2*>(&v);
         const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
         return fmaxf(__half2float(m.x), __half2float(m.y));
+    }
+    static __device__ __forceinline__ float max_nan(uint4 v) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+        const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        return nan_or_max(__half2float(m.x), __half2float(m.y));
     }
 };
 
