@@ -41,6 +41,12 @@ __device__ __forceinline__ uint4 load16(const void* p) {
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
+// 16 bytes from global to shared memory without a register in between.  Each thread waits for, and reads, what it has copied itself.
+__device__ __forceinline__ void copy16_async(void* smem, const void* p) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(__cvta_generic_to_global(p)) : "memory");
+}
+__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 __device__ __forceinline__ void store16(void* p, uint4 v) {
     asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -162,6 +168,54 @@ struct ExpSum {
         const float top = fmaxf(m, m2);
         s = s * exp2_fast((m - top) * c) + s2 * exp2_fast((m2 - top) * c);
         m = top;
+    }
+};
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(unsigned long long p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add_pairs(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long mul_pairs(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// The same sum, of vectors: four partial sums, two operations at a time.
+struct ExpSums {
+    float m;
+    unsigned long long s[2];
+    __device__ __forceinline__ ExpSums() : m(kLowest), s{0ull, 0ull} {}
+    // the N values of a vector whose maximum is `top` (NaN apart)
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float top, float c, float slack) {
+        if (top > m + slack) {
+            const float f = exp2_fast((m - top) * c);
+            s[0] = mul_pairs(s[0], pair_of(f, f)); s[1] = mul_pairs(s[1], pair_of(f, f));
+            m = top;
+        }
+        const unsigned long long minus_m = pair_of(-m, -m), cc = pair_of(c, c);
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = halves(mul_pairs(add_pairs(pair_of(x[i], x[i + 1]), minus_m), cc));
+            s[i / 2 & 1] = add_pairs(s[i / 2 & 1], pair_of(exp2_fast(y.x), exp2_fast(y.y)));
+        }
+    }
+    __device__ __forceinline__ ExpSum whole() const {
+        const float2 p = halves(add_pairs(s[0], s[1]));
+        ExpSum e;
+        e.m = m; e.s = p.x + p.y;
+        return e;
     }
 };
 // 40 powers of two, in logits (bounded: m + slack has to stay below any value when m is the lowest)
