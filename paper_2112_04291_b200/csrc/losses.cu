@@ -71,6 +71,9 @@ const void* balance_kernel(uint32_t x, uint32_t g) {
     return g == FASTSGD_F32 ? (const void*)k_balance<__half, float> : (const void*)k_balance<__half, __half>;
 }
 
+template <uint32_t MOST> const void* top_kernel(uint32_t type) {
+    return type == FASTSGD_F32 ? (const void*)k_top<float, MOST> : type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16, MOST> : (const void*)k_top<__half, MOST>;
+}
 template <class T> const void* top_rows_kernel_of(uint32_t cols) {
     return cols <= 32u ? (const void*)k_top_rows<T, 1> : cols <= 64u ? (const void*)k_top_rows<T, 2> : cols <= 128u ? (const void*)k_top_rows<T, 4>
          : cols <= 256u ? (const void*)k_top_rows<T, 8> : cols <= 512u ? (const void*)k_top_rows<T, 16> : (const void*)k_top_rows<T, 32>;
@@ -150,16 +153,17 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
         const unsigned grid = (unsigned)((a.rows + kTopRowsThreads / 32 - 1) / (kTopRowsThreads / 32));
         return launched(launch_overlapped(top_rows_kernel(logits->type, a.cols), grid, kTopRowsThreads, 0, kargs, st));
     }
-    const void* fn = logits->type == FASTSGD_F32 ? (const void*)k_top<float> : logits->type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16> : (const void*)k_top<__half>;
+    const void* fn = k <= kTopFewPairs ? top_kernel<kTopFewPairs>(logits->type) : top_kernel<kTopMaxPairs>(logits->type);
+    const size_t smem = k <= kTopFewPairs ? sizeof(TopShared<kTopFewPairs>) : sizeof(TopShared<kTopMaxPairs>);
     uint64_t resident = 0;
-    rc = resident_blocks(fn, kTopThreads, sizeof(TopShared), dev, &resident);
+    rc = resident_blocks(fn, kTopThreads, smem, dev, &resident);
     if (rc) return rc;
     // few rows: a cluster of up to 8 blocks shares each, as long as a block has two tiles' worth of 16-bit values for every four threads
     unsigned blocks = 1u;
     while (blocks < 8u && a.rows * blocks * 2u <= resident && a.cols / (2u * blocks) >= 8192u) blocks *= 2u;
     a.slice = ((a.cols + blocks - 1u) / blocks + 63u) & ~63u;
     uint64_t grid = a.rows * blocks < resident ? a.rows * blocks : resident / blocks * blocks;
-    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, sizeof(TopShared), kargs, st, blocks));
+    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, smem, kargs, st, blocks));
 }
 
 int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,

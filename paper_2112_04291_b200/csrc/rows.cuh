@@ -61,6 +61,7 @@ __device__ __forceinline__ float nan_or_max(float a, float b) {
 template <class T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int N = 4;
+    static constexpr uint32_t kMinusInf = 0xFF800000u;      // a word of -inf
     static __device__ __forceinline__ void unpack(uint4 v, float (&f)[4]) {
         f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
     }
@@ -73,6 +74,7 @@ template <> struct Vec<float> {
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
+    static constexpr uint32_t kMinusInf = 0xFF80FF80u;
     static __device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -91,6 +93,7 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<__half> {
     static constexpr int N = 8;
+    static constexpr uint32_t kMinusInf = 0xFC00FC00u;
     static __device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
         const __half2* h = reinterpret_cast<const __half2*>(&v);
 #pragma unroll
@@ -192,18 +195,19 @@ __device__ __forceinline__ unsigned long long mul_pairs(unsigned long long a, un
     return r;
 }
 
-// The same sum, of vectors: four partial sums, two operations at a time.
+// The same sum, of vectors: four partial sums, two operations at a time.  raise() before add(), with the maximum of what is added.
 struct ExpSums {
     float m;
     unsigned long long s[2];
     __device__ __forceinline__ ExpSums() : m(kLowest), s{0ull, 0ull} {}
-    // the N values of a vector whose maximum is `top` (NaN apart)
-    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float top, float c, float slack) {
+    __device__ __forceinline__ void raise(float top, float c, float slack) {
         if (top > m + slack) {
             const float f = exp2_fast((m - top) * c);
             s[0] = mul_pairs(s[0], pair_of(f, f)); s[1] = mul_pairs(s[1], pair_of(f, f));
             m = top;
         }
+    }
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float c) {
         const unsigned long long minus_m = pair_of(-m, -m), cc = pair_of(c, c);
 #pragma unroll
         for (int i = 0; i < N; i += 2) {

@@ -11,7 +11,7 @@
 
 namespace fsg {
 
-constexpr int kTopThreads = 512;
+constexpr int kTopThreads = 256;
 constexpr int kTopWarps   = kTopThreads / 32;
 constexpr uint32_t kTopMaxPairs = 1024u;
 
@@ -90,32 +90,32 @@ __global__ void __launch_bounds__(kTopRowsThreads) k_top_rows(TopArgs a) {
 
 // ---- many columns: a block or a cluster of blocks per row -----------------------------------------
 // One pass over the row in tiles.  A vector of 16 bytes whose maximum is below the bar cannot hold one of the k pairs: its
-// exponentials are summed and it is forgotten.  The others are kept as they are in shared memory; when they are many, and at the
-// end, their elements above the bar become candidates, and the rest of them joins the sum.  When there are many candidates, the k-th largest
-// is found by histograms of eight bits, the smaller ones join the sum and the bar rises to it.
+// exponentials are summed and it is forgotten.  The others are listed, warp by warp; their elements above the bar become candidates,
+// and the rest of them joins the sum.  At the end the k-th largest candidate is found by histograms of eight bits, and the smaller
+// ones join the sum.
 //
-// The first tile is a sample of the row (its 512-byte pieces lie apart as many pieces as there are tiles).  The first bar is the
-// maximum of one of its vectors, of the place from above that the k-th of the row has in the sample, five standard deviations
-// lower.  Where that turns out too high (fewer than k candidates at the end: values in an order that the sample does not
-// meet), the row is gone through again with a bar that is a lower bound for sure: the k-th largest maximum of the first tile.
+// The first tile is a sample of the row (its 512-byte pieces lie apart as many pieces as there are tiles), and the bar is the
+// maximum of one of its vectors: the one whose place from above the k-th of the row has among them, four standard deviations lower.
+// With a bar that turns out too high (fewer than k candidates) or too low (no room for them: values in an order that the sample
+// does not meet, or many equal ones) the row is gone through again step by step: from a bar that is a lower bound for sure, the
+// k-th largest maximum of the first tile, which rises to the k-th candidate whenever there are many.
 constexpr int kTopTile = 4;                                // vectors a thread takes per tile
 constexpr uint32_t kTopTileVecs = kTopTile * kTopThreads;
-constexpr uint32_t kTopKeep = 256u;                        // vectors kept before they are gone through
-constexpr uint32_t kTopRoom = kTopKeep + kTopTileVecs + 2u;
+constexpr uint32_t kTopList = 256u;                        // vectors a warp lists
 constexpr uint32_t kTopHead = 0xFFFFFFFEu, kTopTail = 0xFFFFFFFFu;
-constexpr uint32_t kTopStep = 256u;                        // kept vectors gone through at a time
-constexpr uint32_t kTopBurst = 8u * kTopStep;              // candidates that they can add
-constexpr uint32_t kTopCands = kTopMaxPairs + kTopBurst;
-constexpr uint32_t kTopByCount = 384u;                     // candidates that are sorted by counting the larger ones
+constexpr uint32_t kTopBurst = 8u * kTopThreads + 16u;     // candidates that a step of the careful way can add
+constexpr uint32_t kTopByCount = 256u;                     // candidates that are sorted by counting the larger ones
+constexpr uint32_t kTopFewPairs = 128u;                    // k up to here: less shared memory
 
-struct TopShared {
-    unsigned long long cand[kTopCands];
-    unsigned long long sorted[kTopMaxPairs];
+// MOST: the largest k
+template <uint32_t MOST> struct TopShared {
+    static constexpr uint32_t kRoom = MOST + kTopBurst;
+    unsigned long long cand[kRoom];
+    unsigned long long sorted[MOST < kTopByCount ? kTopByCount : MOST];
     uint4    ring[2][kTopTile][kTopThreads];               // the tile at hand and the next one
-    uint32_t vec[kTopRoom];                                // vectors that are kept, by number; kTopHead, kTopTail: the elements around them
-    unsigned long long head[2], tail[2];                   // those elements, as vectors
+    uint32_t list[kTopWarps][kTopList];                    // vectors by number; kTopHead, kTopTail: the elements around them
     uint32_t hist[256];
-    uint32_t kept, cands, taken, bin, above, equal;
+    uint32_t cands, taken, bin, above, equal;              // (cands may count more than there is room for)
     float2   join[kTopWarps];
     float4   cluster[8];                                   // in the first block: m, rest and in of every block
     uint32_t count;                                        // for the neighbours: entries of `sorted`
@@ -123,7 +123,8 @@ struct TopShared {
 
 // The bin that holds the `need`-th entry counted from the last bin down, how many lie in later bins and in it.  One warp; there are
 // at least `need`.
-__device__ __forceinline__ void find_bin(TopShared& s, uint32_t need) {
+template <class S>
+__device__ __forceinline__ void find_bin(S& s, uint32_t need) {
     const int lane = threadIdx.x & 31;
     uint32_t h[8], sum = 0u;
 #pragma unroll
@@ -141,12 +142,13 @@ __device__ __forceinline__ void find_bin(TopShared& s, uint32_t need) {
     }
 }
 
-// One step of a selection: the histogram of the eight bits at `shift` of the words whose bits above are those of `word`.  Afterwards the
-// need-th largest word begins with `word`; true when as many begin with it as are still needed.
-template <class W, class EACH>
-__device__ __forceinline__ bool select_step(TopShared& s, W& word, uint32_t& need, int shift, W fixed, EACH each) {
+// One step of a selection: the histogram of the eight bits at `shift` of the words whose `fixed` bits are those of `word` (they may
+// overlap those eight).  Afterwards the need-th largest word begins with `word`; true when as many begin with it as are still needed.
+template <class S, class W, class EACH>
+__device__ __forceinline__ bool select_step(S& s, W& word, uint32_t& need, int shift, W fixed, EACH each) {
     __syncthreads();
-    if (threadIdx.x < 256u) s.hist[threadIdx.x] = 0u;
+    s.hist[threadIdx.x] = 0u;
+    static_assert(kTopThreads == 256, "a bin a thread");
     __syncthreads();
     each([&](W w) { if ((w & fixed) == word) atomicAdd(&s.hist[(uint32_t)(w >> shift) & 255u], 1u); });
     __syncthreads();
@@ -157,21 +159,28 @@ __device__ __forceinline__ bool select_step(TopShared& s, W& word, uint32_t& nee
     return need == s.equal;
 }
 
-// The k largest of the n candidates (more than k of them) stay; the others join the sum.  Returns a lower bound of them all: the bar.
-template <class T>
-__device__ __noinline__ unsigned long long cut_candidates(TopShared& s, uint32_t n, uint32_t k, uint32_t cols, ExpSum* sum, float c, float slack) {
-    const uint32_t tid = threadIdx.x;
-    unsigned long long word = 0ull;
+// The k largest of the n candidates (more than k of them, none below `floor`) stay; the others join the sum.  Returns a lower bound of
+// them all: the bar.  The histograms begin with the highest bit in which the candidates' distances from `floor` differ.
+template <class T, class S>
+__device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor, ExpSum* sum, float c, float slack) {
+    const uint32_t tid = threadIdx.x, base = (uint32_t)(floor >> 32);
+    const unsigned long long low = (unsigned long long)base << 32;
+    uint32_t most = 0u;
+    for (uint32_t i = tid; i < n; i += kTopThreads) most = max(most, (uint32_t)(s.cand[i] >> 32) - base);
+    most = __reduce_max_sync(kFullMask, most);
+    __syncthreads();
+    if ((tid & 31u) == 0u) s.hist[tid >> 5] = most;
+    __syncthreads();
+    for (int w = 0; w < kTopWarps; ++w) most = max(most, s.hist[w]);
+    unsigned long long word = 0ull, fixed = 0ull;
     uint32_t need = k;
-    auto each = [&](auto put) { for (uint32_t i = tid; i < n; i += kTopThreads) put(s.cand[i]); };
-    bool done = false;
-    for (int shift = 32 + 8 * ((Rank<T>::kBits - 1) / 8); shift >= 32 && !done; shift -= 8)
-        done = select_step(s, word, need, shift, shift + 8 > 63 ? 0ull : ~0ull << (shift + 8), each);
-    if (!done) {                                           // of the equals, those of the least keys (the bits that no key has are all set)
-        const int passes = cols > 1u << 24 ? 4 : cols > 1u << 16 ? 3 : cols > 1u << 8 ? 2 : 1;
-        if (passes < 4) word |= 0xFFFFFFFFull & ~0ull << (8 * passes);
-        for (int shift = 8 * passes - 8; shift >= 0 && !done; shift -= 8) done = select_step(s, word, need, shift, ~0ull << (shift + 8), each);
+    int shift = 64 - __clz((int)most) - 8;                 // (0 or more: without a difference in rank, the keys' upper bits)
+    shift = shift < 24 ? 24 : shift;
+    while (!select_step(s, word, need, shift, fixed, [&](auto put) { for (uint32_t i = tid; i < n; i += kTopThreads) put(s.cand[i] - low); }) && shift) {
+        fixed = ~0ull << shift;
+        shift = shift > 8 ? shift - 8 : 0;
     }
+    word += low;
     if (tid == 0) s.taken = 0u;
     __syncthreads();
     ExpSum e = *sum;
@@ -188,48 +197,44 @@ __device__ __noinline__ unsigned long long cut_candidates(TopShared& s, uint32_t
     return word;
 }
 
-// The kept vectors' elements above the bar become candidates, the others join the sum.
-template <class T>
-__device__ __noinline__ unsigned long long go_through(TopShared& s, const T* z, uint32_t k, unsigned long long cut, uint32_t first_key, uint32_t begin, uint32_t end, uint32_t cols,
-                                                      ExpSum* sum, float c, float slack) {
-    constexpr int N = Vec<T>::N;
-    const uint32_t tid = threadIdx.x, kept = s.kept;
-    uint32_t n = s.cands;
-    __syncthreads();
-    for (uint32_t h0 = 0; h0 < kept; h0 += kTopStep) {
-        if (n > kTopMaxPairs) cut = cut_candidates<T>(s, n, k, cols, sum, c, slack);
-        const uint32_t h = h0 + tid / 2u, part = tid & 1u;      // two threads a vector
-        if (h < kept) {
-            ExpSum e = *sum;
-            const uint32_t v = s.vec[h];
-            uint32_t base = v == kTopHead ? first_key - N : v == kTopTail ? end - (end - first_key) % N : first_key + v * N;
-            unsigned long long raw = v == kTopHead ? s.head[part] : v == kTopTail ? s.tail[part] : *(reinterpret_cast<const unsigned long long*>(z + base) + part);
-            const T* x = reinterpret_cast<const T*>(&raw);
-            base += part * (N / 2);
+// A warp's listed vectors: their elements above the bar become candidates (as far as there is room), the others join the sum.  Two
+// lanes a vector.
+template <class T, uint32_t MOST>
+__device__ __noinline__ void go_through(TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long cut, uint32_t first_key, uint32_t begin, uint32_t end,
+                                        ExpSum* sum, float c, float slack) {
+    constexpr int N = Vec<T>::N, H = N / 2;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, part = lane & 1u;
+    ExpSum e = *sum;
+    __syncwarp();
+    for (uint32_t h = lane >> 1; h < listed; h += 16u) {
+        const uint32_t v = s.list[warp][h];
+        const uint32_t base = (v == kTopHead ? first_key - N : v == kTopTail ? end - (end - first_key) % N : first_key + v * N) + part * H;
+        T x[H];
+        if (v < kTopHead) *reinterpret_cast<unsigned long long*>(x) = *reinterpret_cast<const unsigned long long*>(z + base);
+        else {
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                if (base + i - begin >= end - begin) continue;
-                const unsigned long long w = candidate(rank_of<T>(to_float(x[i])), base + i);
-                if (w >= cut) s.cand[atomicAdd(&s.cands, 1u)] = w;
-                else e.add(to_float(x[i]), c, slack);
-            }
-            *sum = e;
+            for (int i = 0; i < H; ++i) x[i] = base + i - begin < end - begin ? z[base + i] : from_float<T>(0.f);
         }
-        __syncthreads();
-        n = s.cands;
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            if (base + i - begin >= end - begin) continue;
+            const float y = to_float(x[i]);
+            const unsigned long long w = candidate(rank_of<T>(y), base + i);
+            if (w >= cut) {
+                const uint32_t n = atomicAdd(&s.cands, 1u);
+                if (n < TopShared<MOST>::kRoom) s.cand[n] = w;
+            } else e.add(y, c, slack);
+        }
     }
-    if (n > 2u * k + 256u) cut = cut_candidates<T>(s, n, k, cols, sum, c, slack);
-    if (tid == 0) s.kept = 0u;
-    __syncthreads();
-    return cut;
+    __syncwarp();
+    *sum = e;
 }
 
 // The k largest of n candidates (all, if there are no more) in descending order to `sorted`; the others join the sum.
-template <class T>
-__device__ __noinline__ uint32_t sort_candidates(TopShared& s, uint32_t n, uint32_t k, uint32_t cols, ExpSum* sum, float c, float slack) {
+template <class T, class S>
+__device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor, ExpSum* sum, float c, float slack) {
     const uint32_t tid = threadIdx.x;
-    if (n > kTopByCount && n > k) { cut_candidates<T>(s, n, k, cols, sum, c, slack); n = k; }
+    if (n > k + k / 2u + 32u || (n > kTopByCount && n > k)) { cut_candidates<T>(s, n, k, floor, sum, c, slack); n = k; }
     if (n <= kTopByCount) {                                // a candidate's place is the number of larger ones
         constexpr uint32_t kParts = 8u;                    // threads of a candidate, next to each other
         for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads / kParts) {
@@ -245,7 +250,7 @@ __device__ __noinline__ uint32_t sort_candidates(TopShared& s, uint32_t n, uint3
             }
         }
     } else {                                               // n <= k: a bitonic network
-        uint32_t size2 = 512u;
+        uint32_t size2 = 2u * kTopByCount;
         while (size2 < n) size2 <<= 1;
         for (uint32_t i = tid; i < size2; i += kTopThreads) s.sorted[i] = i < n ? s.cand[i] : 0ull;
         for (uint32_t size = 2u; size <= size2; size <<= 1)
@@ -262,18 +267,99 @@ __device__ __noinline__ uint32_t sort_candidates(TopShared& s, uint32_t n, uint3
     return n < k ? n : k;
 }
 
-// The elements of a slice that lie before its first vector or behind its last: kept as a vector whose other elements lie outside.
-template <class T>
-__device__ __forceinline__ void keep_edge(TopShared& s, const T* z, uint32_t which, uint32_t base, uint32_t begin, uint32_t end) {
-    T* x = reinterpret_cast<T*>(which == kTopHead ? s.head : s.tail);
-    for (int i = 0; i < Vec<T>::N; ++i) x[i] = base + i - begin < end - begin ? z[base + i] : from_float<T>(0.f);
-    s.vec[atomicAdd(&s.kept, 1u)] = which;
+// The slice of a row as vectors: in pieces of 32, piece p in tile p % tiles.  A thread's vector u of tile t is number first + 32 t + step u.
+struct TopSlice { uint32_t head, tail, vecs, tiles, first, step; };
+template <class T> __device__ __forceinline__ TopSlice top_slice(const T* z, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const Span sp = span_of(z, n);
+    TopSlice q;
+    q.head = sp.head; q.tail = sp.tail; q.vecs = sp.vecs;
+    q.tiles = sp.vecs ? (sp.vecs + kTopTileVecs - 1u) / kTopTileVecs : 1u;
+    q.first = warp * q.tiles * 32u + lane; q.step = kTopWarps * q.tiles * 32u;
+    return q;
+}
+// of the four vectors of tile t, those that there are
+__device__ __forceinline__ uint32_t vectors_of(const TopSlice& q, uint32_t t) {
+    const uint32_t v = q.first + 32u * t;
+    return v + (kTopTile - 1u) * q.step < q.vecs ? kTopTile : v < q.vecs ? (q.vecs - 1u - v) / q.step + 1u : 0u;
+}
+// a lower bound of the need-th largest rank among the maxima of the first tile's vectors (16 of its bits)
+template <class T, class S>
+__device__ __forceinline__ unsigned long long first_bar(S& s, uint32_t need, uint32_t mine, const float (&top)[kTopTile]) {
+    constexpr int kTopBit = 8 * ((Rank<T>::kBits - 1) / 8);
+    uint32_t word = 0u;
+    auto each = [&](auto put) {
+#pragma unroll
+        for (int u = 0; u < kTopTile; ++u) if ((uint32_t)u < mine) put(rank_of<T>(top[u]));
+    };
+    if (!select_step(s, word, need, kTopBit, 0u, each)) {
+        const bool done = select_step(s, word, need, kTopBit - 8, ~0u << kTopBit, each);
+        // (of 19 bits the first eight are three: the last step, too)
+        if (kTopBit == 16 && !done) select_step(s, word, need, 0, ~0u << 8, each);
+    }
+    return (unsigned long long)word << 32;
 }
 
-template <class T>
-__global__ void __launch_bounds__(kTopThreads, 2) k_top(TopArgs a) {
+// The bar as a value, for whole vectors: nothing above it may be missed.
+template <class T> __device__ __forceinline__ float bar_value(unsigned long long cut) {
+    const uint32_t lo = (uint32_t)(cut >> 32);
+    return lo > rank_of<T>(INFINITY) ? INFINITY : value_of_rank<T>(lo);      // (nothing is below NaN, the value of 0)
+}
+
+// The careful way through a slice.
+template <class T, uint32_t MOST>
+__device__ __noinline__ unsigned long long top_carefully(TopShared<MOST>& s, const T* z, const TopSlice& q, uint32_t there, uint32_t k, uint32_t begin, uint32_t end, ExpSum* sum, float c, float slack) {
+    constexpr int N = Vec<T>::N;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, first_key = begin + q.head;
+    const uint4* body = reinterpret_cast<const uint4*>(z + first_key);
+    unsigned long long cut = 0ull;
+    if (tid == 0) s.cands = 0u;
+    for (uint32_t t = 0; t < q.tiles; ++t) {
+        const uint32_t v = q.first + 32u * t, mine = vectors_of(q, t);
+        if (t == 0u) {
+            float top[kTopTile];
+#pragma unroll
+            for (int u = 0; u < kTopTile; ++u) top[u] = (uint32_t)u < mine ? Vec<T>::max_nan(load16(body + v + u * q.step)) : 0.f;
+            if (k <= there) cut = first_bar<T>(s, k, mine, top);
+        }
+        __syncthreads();
+        for (uint32_t u = 0; u < (uint32_t)kTopTile; ++u) {
+            const float bar = bar_value<T>(cut);
+            uint32_t listed = 0u;
+            if (t == 0u && u == 0u && warp == 0u) {
+                if (q.head) { if (lane == 0) s.list[0][listed] = kTopHead; ++listed; }
+                if (q.tail) { if (lane == 0) s.list[0][listed] = kTopTail; ++listed; }
+            }
+            bool hit = false;
+            if (u < mine) {
+                const uint4 raw = load16(body + v + u * q.step);
+                const float top = Vec<T>::max_nan(raw);
+                hit = !(top < bar) && !(top == bar && first_key + (v + u * q.step) * N > ~(uint32_t)cut);
+                if (!hit) {
+                    float x[N];
+                    Vec<T>::unpack(raw, x);
+                    ExpSum e = *sum;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) e.add(x[i], c, slack);
+                    *sum = e;
+                }
+            }
+            const unsigned hits = __ballot_sync(kFullMask, hit);
+            if (hit) s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = v + u * q.step;
+            go_through<T>(s, z, listed + __popc(hits), cut, first_key, begin, end, sum, c, slack);
+            __syncthreads();
+            const uint32_t n = s.cands;
+            __syncthreads();
+            if (n > MOST) cut = cut_candidates<T>(s, n, k, cut, sum, c, slack);
+        }
+    }
+    return cut;
+}
+
+template <class T, uint32_t MOST>
+__global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
     extern __shared__ __align__(16) unsigned char top_smem[];
-    TopShared& s = *reinterpret_cast<TopShared*>(top_smem);
+    TopShared<MOST>& s = *reinterpret_cast<TopShared<MOST>*>(top_smem);
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     constexpr int N = Vec<T>::N;
@@ -281,117 +367,111 @@ __global__ void __launch_bounds__(kTopThreads, 2) k_top(TopArgs a) {
     const bool sums = a.lse || a.tail;
     const uint32_t begin = rank * a.slice < a.cols ? rank * a.slice : a.cols, end = begin + a.slice < a.cols ? begin + a.slice : a.cols;
     const uint64_t stride = gridDim.x / blocks;
-    // The slice of a row as vectors: in pieces of 32, piece p in tile p % tiles.
-    struct Slice { const T* z; const T* body; Span sp; uint32_t pieces, tiles; };
-    auto slice_of = [&](uint64_t row) {
-        Slice q;
-        q.z = static_cast<const T*>(a.z) + row * a.z_stride;
-        q.sp = span_of(q.z + begin, end - begin);
-        q.body = q.z + begin + q.sp.head;
-        q.pieces = (q.sp.vecs + 31u) / 32u;
-        q.tiles = q.pieces ? (q.pieces + kTopTileVecs / 32u - 1u) / (kTopTileVecs / 32u) : 1u;
-        return q;
-    };
-    // vector u of this thread's in tile t
-    auto place_of = [&](const Slice& q, uint32_t t, int u) { return ((warp + (uint32_t)u * kTopWarps) * q.tiles + t) * 32u + lane; };
-    auto fetch = [&](const Slice& q, uint32_t t, uint32_t slot) {
+    auto fetch = [&](const T* z, const TopSlice& q, uint32_t t, uint32_t slot) {
+        const uint4* body = reinterpret_cast<const uint4*>(z + begin + q.head);
+        uint32_t v = q.first + 32u * t;
 #pragma unroll
-        for (int u = 0; u < kTopTile; ++u) {
-            const uint32_t v = place_of(q, t, u);
-            if (v < q.sp.vecs) copy16_async(&s.ring[slot][u][tid], q.body + (uint64_t)v * N);
-        }
+        for (int u = 0; u < kTopTile; ++u, v += q.step) if (v < q.vecs) copy16_async(&s.ring[slot][u][tid], body + v);
         copies_end_group();
     };
     wait_for_previous_kernels();
     uint32_t slot = 0u;
     uint64_t row = blockIdx.x / blocks;
-    Slice q = slice_of(row < a.rows ? row : 0);
-    if (row < a.rows) fetch(q, 0u, slot);
+    const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
+    TopSlice q{};
+    if (row < a.rows) { q = top_slice(z + begin, end - begin); fetch(z, q, 0u, slot); }
     for (; row < a.rows; row += stride) {
-        if (row != blockIdx.x / blocks) q = slice_of(row);
-        const T* z = q.z;
-        const uint32_t first_key = begin + q.sp.head;
+        const T* next_z = z + stride * a.z_stride;
+        TopSlice next{};
+        const uint32_t first_key = begin + q.head;
         // vectors in the first tile: of its pieces all but the row's last are whole
-        const uint32_t there = q.pieces ? (q.pieces + q.tiles - 1u) / q.tiles * 32u - ((q.pieces - 1u) % q.tiles ? 0u : q.pieces * 32u - q.sp.vecs) : 0u;
-        const float expect = (float)k * (float)there / (float)max(q.sp.vecs, 1u);
-        const uint32_t guess = (uint32_t)(expect + 5.f * sqrtf(expect) + 3.f);
+        const uint32_t pieces = (q.vecs + 31u) / 32u;
+        const uint32_t there = pieces ? (pieces + q.tiles - 1u) / q.tiles * 32u - ((pieces - 1u) % q.tiles ? 0u : pieces * 32u - q.vecs) : 0u;
+        const float expect = (float)k * (float)there / (float)max(q.vecs, 1u);
+        const uint32_t guess = min(k, (uint32_t)(expect + 5.f * sqrtf(expect) + 5.f));
+        ExpSums es;
         ExpSum e;
-        for (bool sure = guess >= k, again = false;; sure = again = true) {
-            ExpSums es;
-            e = ExpSum();
-            unsigned long long cut = 0ull;
-            float bar = 0.f;
-            uint32_t key_bar = 0u;
-            auto vector_at = [&](uint32_t t, int u) { return again ? load16(q.body + (uint64_t)place_of(q, t, u) * N) : s.ring[slot][u][tid]; };
-            auto set_bar = [&]() {
-                const uint32_t lo = (uint32_t)(cut >> 32);
-                bar = lo > rank_of<T>(INFINITY) ? INFINITY : value_of_rank<T>(lo);      // (nothing is below NaN, the value of 0)
-                key_bar = ~(uint32_t)cut;
-            };
-            __syncthreads();
-            if (tid == 0) { s.kept = 0u; s.cands = 0u; }
-            for (uint32_t t = 0; t < q.tiles; ++t) {
-                if (!again) {
-                    if (t + 1u < q.tiles) fetch(q, t + 1u, slot ^ 1u);
-                    else if (row + stride < a.rows) fetch(slice_of(row + stride), 0u, slot ^ 1u);
-                    else copies_end_group();
-                    wait_copies<1>();
-                }
-                if (t == 0u) {
-                    uint32_t need = sure ? k : guess;
-                    if (need <= there) {
-                        uint32_t word = 0u;
-                        for (int shift = 8 * ((Rank<T>::kBits - 1) / 8); shift >= 0; shift -= 8) {
-                            if (select_step(s, word, need, shift, shift == 24 ? 0u : ~0u << (shift + 8), [&](auto put) {
-#pragma unroll 1
-                                    for (int u = 0; u < kTopTile; ++u) if (place_of(q, 0u, u) < q.sp.vecs) put(rank_of<T>(Vec<T>::max_nan(vector_at(0u, u))));
-                                })) break;
-                        }
-                        cut = (unsigned long long)word << 32;
-                    } else __syncthreads();
-                    set_bar();
-                    if (tid == 0 && q.sp.head) keep_edge(s, z, kTopHead, first_key - N, begin, end);
-                    if (tid == 1 && q.sp.tail) keep_edge(s, z, kTopTail, end - q.sp.tail, begin, end);
-                }
-                bool many = false;
+        unsigned long long cut = 0ull;
+        float bar = 0.f;
+        uint32_t listed = 0u;
+        __syncthreads();
+        if (tid == 0) s.cands = 0u;
+        for (uint32_t t = 0; t < q.tiles; ++t) {
+            if (t + 1u < q.tiles) fetch(z, q, t + 1u, slot ^ 1u);
+            else if (row + stride < a.rows) { next = top_slice(next_z + begin, end - begin); fetch(next_z, next, 0u, slot ^ 1u); }
+            else copies_end_group();
+            wait_copies<1>();
+            uint4 raw[kTopTile];
+            float top[kTopTile];
 #pragma unroll
-                for (int u = 0; u < kTopTile; ++u) {
-                    const uint32_t v = place_of(q, t, u), key = first_key + v * N;
-                    if (v >= q.sp.vecs) break;
-                    const uint4 raw = vector_at(t, u);
-                    const float top = Vec<T>::max_nan(raw);
-                    if (!(top < bar) && !(top == bar && key > key_bar)) {
-                        const uint32_t h = atomicAdd(&s.kept, 1u);
-                        s.vec[h] = v;
-                        many |= h >= kTopKeep;
-                    } else if (sums) {
-                        float x[N];
-                        Vec<T>::unpack(raw, x);
-                        es.add(x, top, a.c, a.slack);
+            for (int u = 0; u < kTopTile; ++u) raw[u] = s.ring[slot][u][tid];
+            slot ^= 1u;
+            const uint32_t v = q.first + 32u * t, mine = vectors_of(q, t);
+            if (mine < kTopTile) {                         // (the last tiles may be short)
+#pragma unroll
+                for (int u = 0; u < kTopTile; ++u)
+                    if ((uint32_t)u >= mine) raw[u] = make_uint4(Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf);
+            }
+#pragma unroll
+            for (int u = 0; u < kTopTile; ++u) top[u] = Vec<T>::max_nan(raw[u]);
+            if (t == 0u) {
+                if (guess <= there) cut = first_bar<T>(s, guess, mine, top);
+                else __syncthreads();
+                bar = bar_value<T>(cut);
+                if (warp == 0u && q.head) { if (lane == 0) s.list[0][listed] = kTopHead; ++listed; }
+                if (warp == 0u && q.tail) { if (lane == 0) s.list[0][listed] = kTopTail; ++listed; }
+            }
+#pragma unroll
+            for (int u = 0; u < kTopTile; ++u) {
+                const bool hit = (uint32_t)u < mine && !(top[u] < bar);
+                const unsigned hits = __ballot_sync(kFullMask, hit);
+                if (hits) {
+                    if (hit) {
+                        s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = v + u * q.step;
+                        raw[u] = make_uint4(Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf);      // (summed later)
+                        top[u] = -INFINITY;
                     }
-                }
-                if (!again) slot ^= 1u;
-                if (__syncthreads_or(many) || t == q.tiles - 1u) {
-                    cut = go_through<T>(s, z, k, cut, first_key, begin, end, a.cols, &e, a.c, a.slack);
-                    set_bar();
+                    listed += __popc(hits);
                 }
             }
-            const ExpSum w = es.whole();
-            e.join(w.m, w.s, a.c);
-            if (s.cands >= k || sure) break;
+            if (sums) {
+                es.raise(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), a.c, a.slack);
+#pragma unroll
+                for (int u = 0; u < kTopTile; ++u) {
+                    float x[N];
+                    Vec<T>::unpack(raw[u], x);
+                    es.add(x, a.c);
+                }
+            }
+            if (listed > kTopList - 32u * kTopTile || t == q.tiles - 1u) {
+                go_through<T>(s, z, listed, cut, first_key, begin, end, &e, a.c, a.slack);
+                listed = 0u;
+            }
         }
-        const uint32_t have = sort_candidates<T>(s, s.cands, k, a.cols, &e, a.c, a.slack);
+        const ExpSum streamed = es.whole();
+        e.join(streamed.m, streamed.s, a.c);
+        __syncthreads();
+        uint32_t n = s.cands;
+        if (n > TopShared<MOST>::kRoom || (n < k && cut)) {
+            __syncthreads();
+            e = ExpSum();
+            cut = top_carefully<T>(s, z, q, there, k, begin, end, &e, a.c, a.slack);
+            n = s.cands;
+        }
+        const uint32_t have = sort_candidates<T>(s, n, k, cut, &e, a.c, a.slack);
 
         // ---- the pairs: a candidate's place is how many of the whole row's are larger -----------------
         if (tid == 0) s.count = have;
         if (blocks > 1u) cluster.sync();
-        ExpSum in;
+        // (of all that this block has seen, the first is the largest)
+        const float m = have ? fmaxf(value_of_rank<T>((uint32_t)(s.sorted[0] >> 32)), kLowest) : kLowest;
+        float in = 0.f;
         for (uint32_t i = tid; i < have; i += kTopThreads) {
             const unsigned long long w = s.sorted[i];
             uint32_t place = i;
             for (uint32_t b = 0; b < blocks; ++b) {
                 if (b == rank) continue;
-                const TopShared& o = *cluster.map_shared_rank(&s, b);
+                const TopShared<MOST>& o = *cluster.map_shared_rank(&s, b);
                 uint32_t l = 0u, h = o.count;
                 while (l < h) { const uint32_t mid = (l + h) >> 1; if (o.sorted[mid] > w) l = mid + 1u; else h = mid; }
                 place += l;
@@ -401,28 +481,33 @@ __global__ void __launch_bounds__(kTopThreads, 2) k_top(TopArgs a) {
                 const uint32_t key = ~(uint32_t)w;
                 a.keys[row * k + place] = (int32_t)key;
                 static_cast<T*>(a.values)[row * k + place] = z[key];
-                in.add(x, a.c, a.slack);
+                in += exp2_fast((x - m) * a.c);
             } else e.add(x, a.c, a.slack);
         }
         if (sums) {
-            e = block_join<kTopWarps>(e, s.join, a.c);
-            in = block_join<kTopWarps>(in, s.join, a.c);
-            const float top = fmaxf(e.m, in.m);
-            const float4 sum = make_float4(top, e.s * exp2_fast((e.m - top) * a.c), in.s * exp2_fast((in.m - top) * a.c), 0.f);
-            if (tid == 0) cluster.map_shared_rank(&s, 0)->cluster[rank] = sum;
+            float rest = warp_sum(e.s * exp2_fast((e.m - m) * a.c));
+            in = warp_sum(in);
+            if (lane == 0) s.join[warp] = make_float2(rest, in);
+            __syncthreads();
+            if (warp == 0u) {
+                const float2 p = lane < (uint32_t)kTopWarps ? s.join[lane] : make_float2(0.f, 0.f);
+                rest = warp_sum(p.x); in = warp_sum(p.y);
+                if (lane == 0) cluster.map_shared_rank(&s, 0)->cluster[rank] = make_float4(m, rest, in, 0.f);
+            }
         }
         if (blocks > 1u) cluster.sync(); else __syncthreads();
         if (sums && rank == 0u && tid == 0) {
-            float m = kLowest, rest = 0.f, inside = 0.f;
-            for (uint32_t b = 0; b < blocks; ++b) m = fmaxf(m, s.cluster[b].x);
+            float top = kLowest, rest = 0.f, inside = 0.f;
+            for (uint32_t b = 0; b < blocks; ++b) top = fmaxf(top, s.cluster[b].x);
             for (uint32_t b = 0; b < blocks; ++b) {
-                const float f = exp2_fast((s.cluster[b].x - m) * a.c);
+                const float f = exp2_fast((s.cluster[b].x - top) * a.c);
                 rest += s.cluster[b].y * f; inside += s.cluster[b].z * f;
             }
             const bool none = rest + inside == 0.f;        // every logit is -inf
-            if (a.lse) a.lse[row] = none ? -INFINITY : m / a.temperature + logf(rest + inside);
+            if (a.lse) a.lse[row] = none ? -INFINITY : top / a.temperature + logf(rest + inside);
             if (a.tail) a.tail[row] = none ? 0.f : rest / (rest + inside);
         }
+        z = next_z; q = next;
     }
 }
 
