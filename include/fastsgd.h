@@ -354,7 +354,7 @@ int fastsgd_distill_loss_backward(const fastsgd_matrix* student, const fastsgd_p
 /*
  * How often each expert was selected, per segment of tokens.
  *   selected  device, tokens * k, k <= experts: expert numbers; one outside [0, experts) was dropped and counts nowhere
- *   experts   1 .. 1024; tokens < 2^31, tokens * k < 2^32
+ *   experts   1 .. 1024; tokens * k < 2^31
  *   mask      device, tokens bytes, or NULL: tokens whose byte is 0 (padding) count nowhere
  *   offsets   device, segments + 1 ascending token numbers: segment s is [offsets[s], offsets[s + 1]); NULL: one segment of
  *             all tokens.  Tokens before the first and behind the last segment belong to none.

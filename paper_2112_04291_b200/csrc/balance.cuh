@@ -6,12 +6,15 @@
 // gradient and, as the sum over the tokens of sum_e f_e p_te, the loss.
 #pragma once
 
+#include <cooperative_groups.h>
+
 #include "rows.cuh"
 
 namespace fsg {
 
 constexpr int kBalanceThreads = 256;
 constexpr int kBalanceWarps   = kBalanceThreads / 32;
+constexpr int kCountThreads   = 512;
 constexpr uint32_t kBalanceMaxExperts = 1024u;
 constexpr uint32_t kBalanceMaxBlocks  = 2048u;
 
@@ -44,9 +47,71 @@ struct Segments {
     }
 };
 
-// A block per run of tokens: a histogram per segment in shared memory, added to the counts (cleared before) with integer atomics,
-// whose order changes nothing.
-__global__ void __launch_bounds__(kBalanceThreads) k_expert_counts(CountArgs a) {
+// The selections of `n` tokens into a histogram in shared memory.
+__device__ __forceinline__ void count_tokens(const CountArgs& a, uint64_t from, uint32_t n, uint32_t* hist, uint32_t* tokens_in) {
+    const uint32_t tid = threadIdx.x;
+    if (a.mask) {
+        uint32_t mine = 0u;
+        for (uint32_t t = tid; t < n; t += kCountThreads) mine += a.mask[from + t] != 0;
+        mine = __reduce_add_sync(kFullMask, mine);
+        if ((tid & 31u) == 0u && mine) atomicAdd(tokens_in, mine);
+    } else if (tid == 0) *tokens_in = n;
+    const int32_t* sel = a.selected + from * a.k;
+    const uint32_t all = n * a.k;
+    auto put = [&](int e, uint32_t i) {
+        if (e >= 0 && (uint32_t)e < a.experts && (!a.mask || a.mask[from + i / a.k])) atomicAdd(&hist[e], 1u);
+    };
+    constexpr uint32_t U = 4u;
+    for (uint32_t i = tid; i < all; i += U * kCountThreads) {
+        int e[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) e[u] = i + u * kCountThreads < all ? sel[i + u * kCountThreads] : -1;
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) put(e[u], i + u * kCountThreads);
+    }
+}
+
+// A cluster of blocks per segment: a histogram each, added up over the cluster's shared memory.  Writes every count, so that nothing is
+// cleared before.
+__global__ void __launch_bounds__(kCountThreads) k_expert_counts(CountArgs a) {
+    namespace cg = cooperative_groups;
+    __shared__ uint32_t hist[kBalanceMaxExperts], tokens_in;
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t tid = threadIdx.x, blocks = cluster.num_blocks(), rank = cluster.block_rank();
+    wait_for_previous_kernels();
+    const Segments seg{a.offsets, a.tokens, a.segments};
+    for (uint32_t s = blockIdx.x / blocks; s < a.segments; s += gridDim.x / blocks) {
+        const uint64_t from = seg.edge(s), to = seg.edge(s + 1u);
+        const uint64_t n = from < to ? to - from : 0ull, b = from + n * rank / blocks, e = from + n * (rank + 1u) / blocks;
+        for (uint32_t i = tid; i < a.experts; i += kCountThreads) hist[i] = 0u;
+        if (tid == 0) tokens_in = 0u;
+        __syncthreads();
+        count_tokens(a, b, (uint32_t)(e - b), hist, &tokens_in);
+        cluster.sync();
+        for (uint32_t i = rank * kCountThreads + tid; i < a.experts; i += blocks * kCountThreads) {
+            uint32_t sum = 0u;
+            for (uint32_t o = 0; o < blocks; ++o) sum += *cluster.map_shared_rank(&hist[i], o);
+            a.counts[(uint64_t)s * a.experts + i] = sum;
+        }
+        if (rank == 0u && tid == 0) {
+            uint32_t sum = 0u;
+            for (uint32_t o = 0; o < blocks; ++o) sum += *cluster.map_shared_rank(&tokens_in, o);
+            a.counted[s] = sum;
+        }
+        cluster.sync();
+    }
+}
+
+// Many tokens: a block per run of them, a histogram per segment, added to the counts (cleared before) with integer atomics, whose order
+// changes nothing.
+__global__ void __launch_bounds__(kCountThreads) k_clear_counts(CountArgs a) {
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    const uint64_t n = (uint64_t)a.segments * a.experts, step = (uint64_t)gridDim.x * kCountThreads;
+    for (uint64_t i = (uint64_t)blockIdx.x * kCountThreads + threadIdx.x; i < n; i += step) a.counts[i] = 0u;
+    for (uint64_t i = (uint64_t)blockIdx.x * kCountThreads + threadIdx.x; i < a.segments; i += step) a.counted[i] = 0u;
+}
+__global__ void __launch_bounds__(kCountThreads) k_add_expert_counts(CountArgs a) {
     __shared__ uint32_t hist[kBalanceMaxExperts], tokens_in;
     const uint32_t tid = threadIdx.x;
     wait_for_previous_kernels();
@@ -59,38 +124,32 @@ __global__ void __launch_bounds__(kBalanceThreads) k_expert_counts(CountArgs a) 
         if (to > r1) to = r1;
         if (from >= to) continue;
         __syncthreads();
-        for (uint32_t e = tid; e < a.experts; e += kBalanceThreads) hist[e] = 0u;
+        for (uint32_t e = tid; e < a.experts; e += kCountThreads) hist[e] = 0u;
         if (tid == 0) tokens_in = 0u;
         __syncthreads();
-        const uint32_t n = (uint32_t)(to - from);
-        if (a.mask) {
-            uint32_t mine = 0u;
-            for (uint32_t t = tid; t < n; t += kBalanceThreads) mine += a.mask[from + t] != 0;
-            if (mine) atomicAdd(&tokens_in, mine);
-        } else if (tid == 0) tokens_in = n;
-        const int32_t* sel = a.selected + from * a.k;
-        for (uint32_t i = tid; i < n * a.k; i += kBalanceThreads) {
-            const int e = sel[i];
-            if (e >= 0 && (uint32_t)e < a.experts && (!a.mask || a.mask[from + i / a.k])) atomicAdd(&hist[e], 1u);
-        }
+        count_tokens(a, from, (uint32_t)(to - from), hist, &tokens_in);
         __syncthreads();
-        for (uint32_t e = tid; e < a.experts; e += kBalanceThreads) if (hist[e]) atomicAdd(&a.counts[(uint64_t)s * a.experts + e], hist[e]);
+        for (uint32_t e = tid; e < a.experts; e += kCountThreads) if (hist[e]) atomicAdd(&a.counts[(uint64_t)s * a.experts + e], hist[e]);
         if (tid == 0 && tokens_in) atomicAdd(&a.counted[s], tokens_in);
     }
 }
 
-// A block per run of tokens, a warp per token.  The sum of a block's part of segment s goes to partials[block + s]: of two
-// neighbours in the sequence of (block, segment) meetings one index grows, so that no two share a place.  The block that ends last
-// adds the parts of each segment in their order.
-template <class T, class TG>
+// A block per run of tokens; LANES lanes share a token, each with CHUNKS times eight neighbouring experts, whose f it keeps in
+// registers.  The sum of a block's part of segment s goes to partials[block + s]: of two neighbours in the sequence of (block, segment)
+// meetings one index grows, so that no two share a place.  The block that ends last adds the parts of each segment in their order.
+template <class T, class TG, int LANES, int CHUNKS>
 __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
-    __shared__ float f[kBalanceMaxExperts];
-    __shared__ unsigned long long whole[kBalanceWarps];
     __shared__ double part[kBalanceWarps];
     __shared__ uint32_t last;
-    constexpr int PER = kBalanceMaxExperts / 32;
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, E = a.experts;
+    constexpr uint32_t PER_WARP = 32 / LANES;              // tokens
+    constexpr int ROWS = CHUNKS > 1 ? 1 : 2;               // that a group of lanes has in flight
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, E = a.experts, group = lane / LANES, place = lane % LANES;
     constexpr float kLog2e = 1.4426950408889634f;
+    const T* xs = static_cast<const T*>(a.x);
+    TG* gs = static_cast<TG*>(a.grad);
+    auto width_of = [&](int c) { const uint32_t e = (c * LANES + place) * 8u; return e < E ? min(E - e, 8u) : 0u; };
+    const bool x_wide = ((reinterpret_cast<uintptr_t>(xs) | a.x_stride * sizeof(T)) & 15u) == 0u;
+    const bool g_wide = ((reinterpret_cast<uintptr_t>(gs) | a.grad_stride * sizeof(TG)) & 15u) == 0u;
     wait_for_previous_kernels();
     const uint64_t r0 = (uint64_t)blockIdx.x * a.rows_per_block, r1 = r0 + a.rows_per_block < a.tokens ? r0 + a.rows_per_block : a.tokens;
     const Segments seg{a.offsets, a.tokens, a.segments};
@@ -100,49 +159,88 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
         if (from < r0) from = r0;
         if (to > r1) to = r1;
         if (from >= to) continue;
-        __syncthreads();
-        unsigned long long mine = 0ull;
-        for (uint32_t e = tid; e < E; e += kBalanceThreads) mine += a.counts[(uint64_t)s * E + e];
-        const unsigned long long all = block_sum<kBalanceWarps>(mine, whole);
-        for (uint32_t e = tid; e < E; e += kBalanceThreads) f[e] = all ? (float)a.counts[(uint64_t)s * E + e] / (float)all : 0.f;
-        __syncthreads();
-        const uint32_t n = a.counted[s];
-        float scale = n ? a.coef * (float)E / (float)n : 0.f;
+        float f[CHUNKS][8];
+        {
+            uint32_t n[CHUNKS][8];
+            unsigned long long all = 0ull;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    n[c][i] = (uint32_t)i < width_of(c) ? a.counts[(uint64_t)s * E + (c * LANES + place) * 8u + i] : 0u;
+                    all += n[c][i];
+                }
+#pragma unroll
+            for (int o = LANES / 2; o; o >>= 1) all += __shfl_xor_sync(kFullMask, all, o);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = all ? (float)n[c][i] / (float)all : 0.f;
+        }
+        const uint32_t counted = a.counted[s];
+        float scale = counted ? a.coef * (float)E / (float)counted : 0.f;
         if (a.grad_loss) scale *= a.grad_loss[s];
         double sum = 0.0;
-        for (uint64_t t = from + warp; t < to; t += kBalanceWarps) {
-            const T* x = static_cast<const T*>(a.x) + t * a.x_stride;
-            TG* g = a.grad ? static_cast<TG*>(a.grad) + t * a.grad_stride : nullptr;
-            float v[PER], m = -INFINITY;
-            const bool counts = !a.mask || a.mask[t];
+        for (uint64_t t0 = from + (uint64_t)warp * (PER_WARP * ROWS); t0 < to; t0 += kBalanceWarps * PER_WARP * ROWS) {
+            float v[ROWS][CHUNKS][8];
+            bool there[ROWS], counts[ROWS];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t e = lane + 32u * i;
-                v[i] = counts && e < E ? to_float(x[e]) : -INFINITY;
-                m = fmaxf(m, v[i]);
+            for (int r = 0; r < ROWS; ++r) {
+                const uint64_t t = t0 + r * PER_WARP + group;
+                there[r] = t < to;
+                counts[r] = there[r] && (!a.mask || a.mask[t]);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, counts[r] ? width_of(c) : 0u, x_wide, -INFINITY, v[r][c]);
             }
-            m = fmaxf(warp_max(m), kLowest);               // (a token whose logits are all -inf: every p is 0)
-            float total = 0.f, dot = 0.f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t e = lane + 32u * i;
-                v[i] = exp2_fast((v[i] - m) * kLog2e);
-                total += v[i];
-                if (e < E) dot += v[i] * f[e];
-            }
-            total = warp_sum(total);
-            const float inv = total == 0.f ? 0.f : 1.f / total;
-            dot = warp_sum(dot) * inv;
-            if (g) {
+            for (int r = 0; r < ROWS; ++r) {
+                float m = kLowest;                         // (a token whose logits are all -inf: every p is 0)
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const uint32_t e = lane + 32u * i;
-                    if (e < E) g[e] = from_float<TG>(scale * (v[i] * inv) * (f[e] - dot));
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m = fmaxf(m, v[r][c][i]);
+#pragma unroll
+                for (int o = LANES / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFullMask, m, o));
+                const unsigned long long minus_m = pair_of(-m, -m), cc = pair_of(kLog2e, kLog2e);
+                unsigned long long totals = 0ull, dots = 0ull;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const float2 y = halves(mul_pairs(add_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), minus_m), cc));
+                        v[r][c][i] = exp2_fast(y.x); v[r][c][i + 1] = exp2_fast(y.y);
+                        const unsigned long long p = pair_of(v[r][c][i], v[r][c][i + 1]);
+                        totals = add_pairs(totals, p);
+                        dots = fma_pairs(p, pair_of(f[c][i], f[c][i + 1]), dots);
+                    }
+                const float2 tt = halves(totals), dd = halves(dots);
+                float total = tt.x + tt.y, dot = dd.x + dd.y;
+#pragma unroll
+                for (int o = LANES / 2; o; o >>= 1) { total += __shfl_xor_sync(kFullMask, total, o); dot += __shfl_xor_sync(kFullMask, dot, o); }
+                const float inv = total == 0.f ? 0.f : 1.f / total;
+                dot *= inv;
+                sum += (double)dot;
+                if (gs && there[r]) {
+                    const unsigned long long minus_dot = pair_of(-dot, -dot);
+                    const float by = counts[r] ? scale * inv : 0.f;
+                    const unsigned long long bb = pair_of(by, by);
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            const float2 y = halves(mul_pairs(mul_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), bb), add_pairs(pair_of(f[c][i], f[c][i + 1]), minus_dot)));
+                            v[r][c][i] = y.x; v[r][c][i + 1] = y.y;
+                        }
+                        store_eight(gs + (t0 + r * PER_WARP + group) * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_wide, v[r][c]);
+                    }
                 }
             }
-            sum += (double)dot;
         }
         if (a.loss) {
+            // every lane of a group has its tokens' sum: one lane of each
+            if (place) sum = 0.0;
+            sum = warp_sum(sum);
+            __syncthreads();
             if (lane == 0) part[warp] = sum;
             __syncthreads();
             if (tid == 0) {

@@ -65,12 +65,16 @@ template <int MODE> const void* distill_kernel(uint32_t z, uint32_t g) {
     if (z == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_distill<__nv_bfloat16, float, MODE> : (const void*)k_distill<__nv_bfloat16, __nv_bfloat16, MODE>;
     return g == FASTSGD_F32 ? (const void*)k_distill<__half, float, MODE> : (const void*)k_distill<__half, __half, MODE>;
 }
-const void* balance_kernel(uint32_t x, uint32_t g) {
-    if (x == FASTSGD_F32) return (const void*)k_balance<float, float>;
-    if (x == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_balance<__nv_bfloat16, float> : (const void*)k_balance<__nv_bfloat16, __nv_bfloat16>;
-    return g == FASTSGD_F32 ? (const void*)k_balance<__half, float> : (const void*)k_balance<__half, __half>;
+template <class T, class TG> const void* balance_kernel_of(uint32_t experts) {
+    return experts <= 8u ? (const void*)k_balance<T, TG, 1, 1> : experts <= 16u ? (const void*)k_balance<T, TG, 2, 1> : experts <= 32u ? (const void*)k_balance<T, TG, 4, 1>
+         : experts <= 64u ? (const void*)k_balance<T, TG, 8, 1> : experts <= 128u ? (const void*)k_balance<T, TG, 16, 1> : experts <= 256u ? (const void*)k_balance<T, TG, 32, 1>
+         : experts <= 512u ? (const void*)k_balance<T, TG, 32, 2> : (const void*)k_balance<T, TG, 32, 4>;
 }
-
+const void* balance_kernel(uint32_t x, uint32_t g, uint32_t experts) {
+    if (x == FASTSGD_F32) return balance_kernel_of<float, float>(experts);
+    if (x == FASTSGD_BF16) return g == FASTSGD_F32 ? balance_kernel_of<__nv_bfloat16, float>(experts) : balance_kernel_of<__nv_bfloat16, __nv_bfloat16>(experts);
+    return g == FASTSGD_F32 ? balance_kernel_of<__half, float>(experts) : balance_kernel_of<__half, __half>(experts);
+}
 template <uint32_t MOST> const void* top_kernel(uint32_t type) {
     return type == FASTSGD_F32 ? (const void*)k_top<float, MOST> : type == FASTSGD_BF16 ? (const void*)k_top<__nv_bfloat16, MOST> : (const void*)k_top<__half, MOST>;
 }
@@ -186,23 +190,30 @@ int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, 
     if (experts < 1u || experts > kBalanceMaxExperts || k < 1u || k > experts) return FASTSGD_E_BAD_PARAM;
     if (!counts || !counted || (tokens && !selected)) return FASTSGD_E_NULL;
     if (!aligned_to(selected, 4) || !aligned_to(counts, 4) || !aligned_to(counted, 4)) return FASTSGD_E_ALIGN;
-    if (tokens * k >= (1ull << 32)) return FASTSGD_E_BAD_N;
+    if (tokens * k >= (1ull << 31)) return FASTSGD_E_BAD_N;
     DeviceView dev;
     rc = device_view(&dev);
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (cudaMemsetAsync(counts, 0, 4ull * segments * experts, st) != cudaSuccess || cudaMemsetAsync(counted, 0, 4ull * segments, st) != cudaSuccess) {
-        cudaGetLastError();
-        return FASTSGD_E_CUDA;
-    }
-    if (!tokens) return FASTSGD_OK;
     CountArgs a{};
     a.selected = selected; a.mask = mask; a.offsets = offsets; a.counts = counts; a.counted = counted;
     a.tokens = tokens; a.k = k; a.experts = experts; a.segments = segments;
-    a.rows_per_block = rows_per_block(tokens, 64u, 4ull * (uint64_t)dev.sm_count);
     void* kargs[] = {&a};
+    // A cluster per segment; for many selections in few segments (one block of a cluster of eight would count more than 2^14 of them, if
+    // they are alike) two launches that spread over the GPU.
+    if (tokens * k <= (1ull << 17) * segments) {
+        unsigned blocks = 1u;
+        while (blocks < 8u && tokens * k > 2048ull * segments * blocks) blocks *= 2u;
+        uint64_t grid = (uint64_t)segments * blocks;
+        const uint64_t most = (uint64_t)dev.sm_count / 8u * 8u * 4u;
+        if (grid > most) grid = most;
+        return launched(launch_overlapped((const void*)k_expert_counts, (unsigned)grid, kCountThreads, 0, kargs, st, blocks));
+    }
+    a.rows_per_block = rows_per_block(tokens, 64u, (uint64_t)dev.sm_count);
     const unsigned grid = (unsigned)((tokens + a.rows_per_block - 1) / a.rows_per_block);
-    return launched(cudaLaunchKernel((const void*)k_expert_counts, dim3(grid), dim3(kBalanceThreads), kargs, 0, st));
+    const uint64_t cells = ((uint64_t)segments * experts + kCountThreads - 1) / kCountThreads;
+    rc = launched(launch_overlapped((const void*)k_clear_counts, (unsigned)(cells < 512u ? cells : 512u), kCountThreads, 0, kargs, st));
+    return rc ? rc : launched(launch_overlapped((const void*)k_add_expert_counts, grid, kCountThreads, 0, kargs, st));
 }
 
 int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, const uint64_t* offsets, uint32_t segments,
@@ -232,7 +243,7 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
     a.loss = loss; a.coef = coef;
     a.partials = reinterpret_cast<double*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset);
     a.done = loss ? &static_cast<Control*>(dev.ws)->loss_done : nullptr;
-    const void* fn = balance_kernel(logits->type, grad ? grad->type : logits->type);
+    const void* fn = balance_kernel(logits->type, grad ? grad->type : logits->type, a.experts);
     uint64_t blocks = 0;
     rc = resident_blocks(fn, kBalanceThreads, 0, dev, &blocks);
     if (rc) return rc;

@@ -140,6 +140,30 @@ template <class T, int N> __device__ __forceinline__ void store_values(T* p, con
     }
 }
 
+// Eight consecutive elements from p on, those behind the first n as `other`; wide: p lies on a 16-byte boundary.
+template <class T> __device__ __forceinline__ void load_eight(const T* p, uint32_t n, bool wide, float other, float (&f)[8]) {
+    constexpr int N = Vec<T>::N;
+    if (wide && n >= 8u) {
+#pragma unroll
+        for (int h = 0; h < 8; h += N) {
+            float x[N];
+            Vec<T>::unpack(load16(p + h), x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[h + i] = x[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (uint32_t)i < n ? to_float(p[i]) : other;
+    }
+}
+template <class T> __device__ __forceinline__ void store_eight(T* p, uint32_t n, bool wide, const float (&f)[8]) {
+    if (n >= 8u) store_values(p, f, wide);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if ((uint32_t)i < n) p[i] = from_float<T>(f[i]);
+    }
+}
+
 // A run of n elements from p on: `head` single elements up to a 16-byte boundary, `vecs` vectors, `tail` single elements.
 struct Span {
     uint32_t head, vecs, tail;
@@ -192,6 +216,12 @@ __device__ __forceinline__ unsigned long long add_pairs(unsigned long long a, un
 __device__ __forceinline__ unsigned long long mul_pairs(unsigned long long a, unsigned long long b) {
     unsigned long long r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ unsigned long long fma_pairs(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 
