@@ -39,10 +39,22 @@ struct Segments {
         const uint64_t v = offsets ? offsets[s] : (s ? tokens : 0ull);
         return v < tokens ? v : tokens;
     }
-    // the first segment that ends behind token t
+    // The first segment that ends behind token t.  A warp looks at 32 ends at a time (a search of two ends a step waits for memory
+    // three times as often).
     __device__ __forceinline__ uint32_t find(uint64_t t) const {
-        uint32_t lo = 0u, hi = count;
-        while (lo < hi) { const uint32_t mid = (lo + hi) >> 1; if (edge(mid + 1u) > t) hi = mid; else lo = mid + 1u; }
+        if (!offsets) return 0u;
+        const uint32_t lane = threadIdx.x & 31u;
+        uint32_t lo = 0u, hi = count;                      // it is among [lo, hi]
+        while (lo < hi) {
+            const uint32_t step = (hi - lo + 31u) / 32u, at = lo + step * lane;      // ends lo, lo + step, ...
+            const unsigned behind = __ballot_sync(kFullMask, at < hi && edge(at + 1u) > t);
+            const uint32_t first = behind ? (uint32_t)__ffs((int)behind) - 1u : 32u;
+            const uint32_t end = lo + step * first;        // the first of them behind t, or none
+            if (!first) return lo;
+            const uint32_t past = (hi - lo - 1u) / step;   // the last that was looked at
+            hi = behind ? end : hi;
+            lo = (behind ? end - step : lo + step * past) + 1u;
+        }
         return lo;
     }
 };
@@ -135,16 +147,20 @@ __global__ void __launch_bounds__(kCountThreads) k_add_expert_counts(CountArgs a
 }
 
 // A block per run of tokens; LANES lanes share a token, each with CHUNKS times eight neighbouring experts, whose f it keeps in
-// registers.  The sum of a block's part of segment s goes to partials[block + s]: of two neighbours in the sequence of (block, segment)
-// meetings one index grows, so that no two share a place.  The block that ends last adds the parts of each segment in their order.
+// registers.  The next tokens' logits are on their way while those at hand are worked on.
+// The sum of a block's part of segment s goes to partials[block + s]: of two
+// neighbours in the sequence of (block, segment) meetings one index grows, so that no two share a place.  The block that ends last
+// adds the parts of each segment in their order.
+template <int CHUNKS> constexpr int kBalanceRows = CHUNKS > 1 ? 1 : 2;      // tokens that a group of lanes works on at a time
 template <class T, class TG, int LANES, int CHUNKS>
-__global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
+__global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance(BalanceArgs a) {
     __shared__ double part[kBalanceWarps];
     __shared__ uint32_t last;
     constexpr uint32_t PER_WARP = 32 / LANES;              // tokens
-    constexpr int ROWS = CHUNKS > 1 ? 1 : 2;               // that a group of lanes has in flight
+    constexpr int ROWS = kBalanceRows<CHUNKS>;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, E = a.experts, group = lane / LANES, place = lane % LANES;
     constexpr float kLog2e = 1.4426950408889634f;
+    constexpr uint64_t kStep = kBalanceWarps * PER_WARP * ROWS;
     const T* xs = static_cast<const T*>(a.x);
     TG* gs = static_cast<TG*>(a.grad);
     auto width_of = [&](int c) { const uint32_t e = (c * LANES + place) * 8u; return e < E ? min(E - e, 8u) : 0u; };
@@ -159,6 +175,19 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
         if (from < r0) from = r0;
         if (to > r1) to = r1;
         if (from >= to) continue;
+        Eight<T> next[ROWS][CHUNKS];
+        bool next_counts[ROWS];
+        auto fetch = [&](uint64_t t0) {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const uint64_t t = t0 + r * PER_WARP + group;
+                next_counts[r] = t < to && (!a.mask || a.mask[t]);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) next[r][c] = load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, next_counts[r] ? width_of(c) : 0u, x_wide);
+            }
+        };
+        uint64_t t0 = from + (uint64_t)warp * (PER_WARP * ROWS);
+        fetch(t0);
         float f[CHUNKS][8];
         {
             uint32_t n[CHUNKS][8];
@@ -181,19 +210,19 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
         float scale = counted ? a.coef * (float)E / (float)counted : 0.f;
         if (a.grad_loss) scale *= a.grad_loss[s];
         double sum = 0.0;
-        for (uint64_t t0 = from + (uint64_t)warp * (PER_WARP * ROWS); t0 < to; t0 += kBalanceWarps * PER_WARP * ROWS) {
+        for (; t0 < to; t0 += kStep) {
             float v[ROWS][CHUNKS][8];
-            bool there[ROWS], counts[ROWS];
+            bool counts[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                counts[r] = next_counts[r];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) unpack_eight(next[r][c], v[r][c]);
+            }
+            if (t0 + kStep < to) fetch(t0 + kStep);
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 const uint64_t t = t0 + r * PER_WARP + group;
-                there[r] = t < to;
-                counts[r] = there[r] && (!a.mask || a.mask[t]);
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, counts[r] ? width_of(c) : 0u, x_wide, -INFINITY, v[r][c]);
-            }
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
                 float m = kLowest;                         // (a token whose logits are all -inf: every p is 0)
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
@@ -220,7 +249,7 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
                 const float inv = total == 0.f ? 0.f : 1.f / total;
                 dot *= inv;
                 sum += (double)dot;
-                if (gs && there[r]) {
+                if (gs && t < to) {
                     const unsigned long long minus_dot = pair_of(-dot, -dot);
                     const float by = counts[r] ? scale * inv : 0.f;
                     const unsigned long long bb = pair_of(by, by);
@@ -231,7 +260,7 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
                             const float2 y = halves(mul_pairs(mul_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), bb), add_pairs(pair_of(f[c][i], f[c][i + 1]), minus_dot)));
                             v[r][c][i] = y.x; v[r][c][i + 1] = y.y;
                         }
-                        store_eight(gs + (t0 + r * PER_WARP + group) * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_wide, v[r][c]);
+                        store_eight(gs + t * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_wide, v[r][c]);
                     }
                 }
             }
@@ -251,7 +280,6 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
         }
     }
     if (!a.loss) return;
-    __syncthreads();
     if (tid == 0) {
         __threadfence();                                   // (this thread wrote the block's parts)
         last = atomicAdd(a.done, 1u) == gridDim.x - 1u;
@@ -259,15 +287,30 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance(BalanceArgs a) {
     }
     __syncthreads();
     if (!last) return;
-    for (uint32_t s = warp; s < a.segments; s += kBalanceWarps) {
+    // Few segments: all threads for each; many: eight lanes for each.
+    auto parts_of = [&](uint32_t s, uint32_t first, uint32_t step) {
         const uint64_t from = seg.edge(s), to = seg.edge(s + 1u);
         double sum = 0.0;
         if (from < to) {
             const uint64_t b0 = from / a.rows_per_block, b1 = (to - 1u) / a.rows_per_block;
-            for (uint64_t b = b0 + lane; b <= b1; b += 32u) sum += __ldcg(a.partials + b + s);
+            for (uint64_t b = b0 + first; b <= b1; b += step) sum += __ldcg(a.partials + b + s);
         }
-        sum = warp_sum(sum);
-        if (lane == 0) { const uint32_t n = a.counted[s]; a.loss[s] = n ? (float)((double)a.coef * (double)E * sum / (double)n) : 0.f; }
+        return sum;
+    };
+    auto finish = [&](uint32_t s, double sum) { const uint32_t n = a.counted[s]; a.loss[s] = n ? (float)((double)a.coef * (double)E * sum / (double)n) : 0.f; };
+    if (a.segments < 8u) {
+        for (uint32_t s = 0; s < a.segments; ++s) {
+            const double sum = block_sum<kBalanceWarps>(parts_of(s, tid, kBalanceThreads), part);
+            if (tid == 0) finish(s, sum);
+        }
+    } else {
+        for (uint32_t s0 = 0; s0 < a.segments; s0 += kBalanceThreads / 8) {
+            const uint32_t s = s0 + tid / 8u;
+            double sum = s < a.segments ? parts_of(s, tid % 8u, 8u) : 0.0;
+#pragma unroll
+            for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
+            if (s < a.segments && tid % 8u == 0u) finish(s, sum);
+        }
     }
     if (tid == 0) *a.done = 0u;
 }

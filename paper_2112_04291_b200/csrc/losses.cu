@@ -248,7 +248,10 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
     rc = resident_blocks(fn, kBalanceThreads, 0, dev, &blocks);
     if (rc) return rc;
     if (blocks > kBalanceMaxBlocks) blocks = kBalanceMaxBlocks;
-    a.rows_per_block = rows_per_block(a.tokens, kBalanceWarps, blocks);
+    // whole steps of a block: every group of lanes as many tokens
+    const uint32_t lanes = a.experts <= 8u ? 1u : a.experts <= 16u ? 2u : a.experts <= 32u ? 4u : a.experts <= 64u ? 8u : a.experts <= 128u ? 16u : 32u;
+    const uint64_t step = (uint64_t)kBalanceWarps * (32u / lanes) * (a.experts <= 256u ? kBalanceRows<1> : kBalanceRows<2>);
+    a.rows_per_block = (uint32_t)((rows_per_block(a.tokens, 1u, blocks) + step - 1) / step * step);
     void* kargs[] = {&a};
     const unsigned grid = (unsigned)((a.tokens + a.rows_per_block - 1) / a.rows_per_block);
     return launched(launch_overlapped(fn, grid, kBalanceThreads, 0, kargs, st));

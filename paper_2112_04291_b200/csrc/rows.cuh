@@ -140,20 +140,31 @@ template <class T, int N> __device__ __forceinline__ void store_values(T* p, con
     }
 }
 
-// Eight consecutive elements from p on, those behind the first n as `other`; wide: p lies on a 16-byte boundary.
-template <class T> __device__ __forceinline__ void load_eight(const T* p, uint32_t n, bool wide, float other, float (&f)[8]) {
+// Eight consecutive elements from p on as they are, those behind the first n as -inf; wide: p lies on a 16-byte boundary.
+template <class T> struct Eight { uint4 raw[8 / Vec<T>::N]; };
+template <class T> __device__ __forceinline__ Eight<T> load_eight(const T* p, uint32_t n, bool wide) {
     constexpr int N = Vec<T>::N;
+    Eight<T> r;
     if (wide && n >= 8u) {
 #pragma unroll
-        for (int h = 0; h < 8; h += N) {
-            float x[N];
-            Vec<T>::unpack(load16(p + h), x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) f[h + i] = x[i];
-        }
+        for (int h = 0; h < 8 / N; ++h) r.raw[h] = load16(p + h * N);
     } else {
+        T x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (uint32_t)i < n ? to_float(p[i]) : other;
+        for (int i = 0; i < 8; ++i) x[i] = (uint32_t)i < n ? p[i] : from_float<T>(-INFINITY);
+#pragma unroll
+        for (int h = 0; h < 8 / N; ++h) r.raw[h] = *reinterpret_cast<const uint4*>(x + h * N);
+    }
+    return r;
+}
+template <class T> __device__ __forceinline__ void unpack_eight(const Eight<T>& r, float (&f)[8]) {
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int h = 0; h < 8 / N; ++h) {
+        float x[N];
+        Vec<T>::unpack(r.raw[h], x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[h * N + i] = x[i];
     }
 }
 template <class T> __device__ __forceinline__ void store_eight(T* p, uint32_t n, bool wide, const float (&f)[8]) {
