@@ -294,7 +294,7 @@ typedef struct fastsgd_matrix {
 
 /*
  * The k largest of each row as (key, value) pairs: the top logits of a teacher, the experts that a router selects.
- *   logits  rows x V
+ *   logits  rows x V, V <= 2^20 (else FASTSGD_E_NOT_IMPLEMENTED)
  *   k       1 .. min(V, 1024)
  *   keys    device, rows * k: column numbers in descending order of their values, equal values in ascending order of
  *           their columns (NaN above everything, -0 equal to +0)

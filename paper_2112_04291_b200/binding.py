@@ -286,105 +286,104 @@ def key_encode_paper(keys: torch.Tensor, flag_bits: int, out: torch.Tensor, stre
 
 
 # ---- losses on logits, and their data as key-value pairs ----------------------------------------
+# (Calls of a few microseconds: the checks ask tensors for numbers, not for objects.)
 
-def _matrix(t: torch.Tensor) -> Matrix:
+def _raw_stream(stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+
+
+def _matrix(t: torch.Tensor, dev: int) -> Matrix:
     """Rows of logits or of a gradient: unit stride along a row, any stride between rows."""
-    assert t.is_cuda and t.dim() == 2 and t.dtype in TYPES and (t.stride(1) == 1 or t.shape[1] == 1)
+    kind = TYPES.get(t.dtype)
+    assert t.get_device() == dev and kind is not None and t.dim() == 2
     rows, cols = t.shape
-    return Matrix(t.data_ptr() if rows else None, rows, cols, t.stride(0) if rows > 1 else cols, TYPES[t.dtype], 0)
+    step, unit = t.stride()
+    assert unit == 1 or cols == 1
+    return Matrix(t.data_ptr() if rows else None, rows, cols, step if rows > 1 else cols, kind, 0)
 
 
-def _beside(t, like: torch.Tensor, dtypes, shape):
-    """Address of a contiguous tensor of the given type(s) and shape on the device of `like` (None: 0)."""
+def _at(t, dev: int, dtype: torch.dtype, *shape):
+    """Address of a contiguous tensor of the given type and shape on the current device (None: 0)."""
     if t is None:
         return None
-    assert t.device == like.device and t.dtype in dtypes and t.is_contiguous() and t.shape == shape
+    assert t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous()
     return t.data_ptr()
 
 
-_F32, _I32 = (torch.float32,), (torch.int32,)
-
-
-def _here(t: torch.Tensor) -> None:
-    assert t.device.index == torch.cuda.current_device(), "tensors live on the current device"
+def _device_of(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    assert dev >= 0 and dev == torch.cuda.current_device(), "tensors live on the current device"
+    return dev
 
 
 def top_logits(logits: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, temperature: float = 1.0, lse: torch.Tensor = None,
                tail: torch.Tensor = None, stream=None) -> int:
     """fastsgd_top_logits: the k largest of each row as (key, value) pairs; keys and values are [rows, k]."""
-    m = _matrix(logits)
-    _here(logits)
+    dev = _device_of(logits)
+    m = _matrix(logits, dev)
     rows, k = keys.shape
     assert rows == m.rows
-    return lib().fastsgd_top_logits(C.byref(m), k, temperature, _beside(keys, logits, _I32, keys.shape),
-                                    _beside(values, logits, (logits.dtype,), keys.shape), _beside(lse, logits, _F32, (rows,)),
-                                    _beside(tail, logits, _F32, (rows,)), _stream_handle(stream))
+    return lib().fastsgd_top_logits(m, k, temperature, _at(keys, dev, torch.int32, rows, k), _at(values, dev, logits.dtype, rows, k),
+                                    _at(lse, dev, torch.float32, rows), _at(tail, dev, torch.float32, rows), _raw_stream(stream))
 
 
-def _teacher(student, keys, values, tail) -> Pairs:
-    rows, k = keys.shape
-    assert rows == student.shape[0]
-    return Pairs(_beside(keys, student, _I32, keys.shape), _beside(values, student, tuple(TYPES), keys.shape),
-                 _beside(tail, student, _F32, (rows,)), k, TYPES[values.dtype])
-
-
-def _gradient(grad, logits):
-    if grad is None:
-        return None
-    assert grad.device == logits.device
-    return C.byref(_matrix(grad))
+def _teacher(rows: int, keys, values, tail, dev: int) -> Pairs:
+    n, k = keys.shape
+    kind = TYPES.get(values.dtype)
+    assert n == rows and kind is not None
+    return Pairs(_at(keys, dev, torch.int32, rows, k), _at(values, dev, values.dtype, rows, k), _at(tail, dev, torch.float32, rows), k, kind)
 
 
 def distill_loss(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
                  temperature: float = 1.0, tail: torch.Tensor = None, weight: torch.Tensor = None, stats: torch.Tensor = None, stream=None) -> int:
     """fastsgd_distill_loss: loss [rows] of student logits against a teacher's pairs [rows, k], and its gradient."""
-    m, rows = _matrix(student), student.shape[0]
-    _here(student)
-    t = _teacher(student, keys, values, tail)
-    return lib().fastsgd_distill_loss(C.byref(m), C.byref(t), temperature, _beside(weight, student, _F32, (rows,)),
-                                      _beside(loss, student, _F32, (rows,)), _beside(stats, student, _F32, (rows, 2)),
-                                      _gradient(grad, student), _stream_handle(stream))
+    dev = _device_of(student)
+    m = _matrix(student, dev)
+    rows = m.rows
+    return lib().fastsgd_distill_loss(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, torch.float32, rows),
+                                      _at(loss, dev, torch.float32, rows), _at(stats, dev, torch.float32, rows, 2),
+                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream))
 
 
 def distill_loss_backward(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, stats: torch.Tensor, grad: torch.Tensor,
                           grad_loss: torch.Tensor = None, temperature: float = 1.0, tail: torch.Tensor = None, weight: torch.Tensor = None,
                           stream=None) -> int:
     """fastsgd_distill_loss_backward: the gradient from the stats [rows, 2] of a forward call, times grad_loss [rows]."""
-    m, rows = _matrix(student), student.shape[0]
-    _here(student)
-    t = _teacher(student, keys, values, tail)
-    return lib().fastsgd_distill_loss_backward(C.byref(m), C.byref(t), temperature, _beside(weight, student, _F32, (rows,)),
-                                               _beside(stats, student, _F32, (rows, 2)), _beside(grad_loss, student, _F32, (rows,)),
-                                               _gradient(grad, student), _stream_handle(stream))
+    dev = _device_of(student)
+    m = _matrix(student, dev)
+    rows = m.rows
+    return lib().fastsgd_distill_loss_backward(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, torch.float32, rows),
+                                               _at(stats, dev, torch.float32, rows, 2), _at(grad_loss, dev, torch.float32, rows),
+                                               _matrix(grad, dev), _raw_stream(stream))
 
 
-def _tokens(like, tokens, mask, offsets, segments):
-    assert offsets is not None or segments == 1
-    return (_beside(mask, like, (torch.bool, torch.uint8), (tokens,)), _beside(offsets, like, (torch.int64,), (segments + 1,)))
+def _mask(mask, dev: int, tokens: int):
+    return None if mask is None else _at(mask, dev, torch.uint8 if mask.dtype is torch.uint8 else torch.bool, tokens)
 
 
 def expert_counts(selected: torch.Tensor, counts: torch.Tensor, counted: torch.Tensor, mask: torch.Tensor = None, offsets: torch.Tensor = None,
                   stream=None) -> int:
     """fastsgd_expert_counts: selected [tokens, k] -> counts [segments, experts], counted [segments] (int32 tensors)."""
-    assert counts.is_cuda
-    _here(counts)
-    (tokens, k), (segments, experts) = selected.shape, counts.shape
-    at_mask, at_offsets = _tokens(counts, tokens, mask, offsets, segments)
-    return lib().fastsgd_expert_counts(_beside(selected, counts, _I32, (tokens, k)), tokens, k, experts, at_mask, at_offsets, segments,
-                                       _beside(counts, counts, _I32, (segments, experts)), _beside(counted, counts, _I32, (segments,)),
-                                       _stream_handle(stream))
+    dev = _device_of(counts)
+    tokens, k = selected.shape
+    segments, experts = counts.shape
+    assert offsets is not None or segments == 1
+    return lib().fastsgd_expert_counts(_at(selected, dev, torch.int32, tokens, k), tokens, k, experts, _mask(mask, dev, tokens),
+                                       _at(offsets, dev, torch.int64, segments + 1), segments, _at(counts, dev, torch.int32, segments, experts),
+                                       _at(counted, dev, torch.int32, segments), _raw_stream(stream))
 
 
 def balance_loss(logits: torch.Tensor, counts: torch.Tensor, counted: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
                  coef: float = 1.0, mask: torch.Tensor = None, offsets: torch.Tensor = None, grad_loss: torch.Tensor = None, stream=None) -> int:
     """fastsgd_balance_loss: loss [segments] of router logits [tokens, experts] for given counts, and its gradient."""
-    m = _matrix(logits)
-    _here(logits)
-    (tokens, experts), segments = logits.shape, counts.shape[0]
-    at_mask, at_offsets = _tokens(logits, tokens, mask, offsets, segments)
-    return lib().fastsgd_balance_loss(C.byref(m), at_mask, at_offsets, segments, _beside(counts, logits, _I32, (segments, experts)),
-                                      _beside(counted, logits, _I32, (segments,)), coef, _beside(grad_loss, logits, _F32, (segments,)),
-                                      _beside(loss, logits, _F32, (segments,)), _gradient(grad, logits), _stream_handle(stream))
+    dev = _device_of(logits)
+    m = _matrix(logits, dev)
+    tokens, experts, segments = m.rows, m.cols, counts.shape[0]
+    assert offsets is not None or segments == 1
+    return lib().fastsgd_balance_loss(m, _mask(mask, dev, tokens), _at(offsets, dev, torch.int64, segments + 1), segments,
+                                      _at(counts, dev, torch.int32, segments, experts), _at(counted, dev, torch.int32, segments), coef,
+                                      _at(grad_loss, dev, torch.float32, segments), _at(loss, dev, torch.float32, segments),
+                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream))
 
 
 def stream_info(stream_in: torch.Tensor, stream=None):

@@ -272,7 +272,7 @@ int device_view(DeviceView* out) {
     FSG_DEVICE_STATE();
     const int rc = ensure_device_setup();
     if (rc) return rc;
-    out->ws = g_state.ws; out->ws_bytes = g_state.ws_bytes; out->sm_count = g_state.sm_count;
+    out->ws = g_state.ws; out->ws_bytes = g_state.ws_bytes; out->sm_count = g_state.sm_count; out->device = (int)(&g_state - g_states);
     return FASTSGD_OK;
 }
 

@@ -10,6 +10,7 @@ struct DeviceView {
     void*    ws;          // the registered workspace, or nullptr
     uint64_t ws_bytes;
     int      sm_count;
+    int      device;
 };
 // The current device's; FASTSGD_OK or FASTSGD_E_CUDA.
 int device_view(DeviceView* out);

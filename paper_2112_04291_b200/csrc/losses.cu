@@ -3,6 +3,7 @@
 #include "../../include/fastsgd.h"
 
 #include <cmath>
+#include <mutex>
 
 #include "host.cuh"
 #include "top.cuh"
@@ -51,12 +52,28 @@ int launched(cudaError_t err, uint64_t launches = 1) {
     return FASTSGD_OK;
 }
 
-// Blocks of a kernel that stay on the GPU at once.
+// Blocks of a kernel that stay on the GPU at once (asked for once per device, kernel and size; asking costs as much as a small launch).
+struct Residency { int dev; const void* fn; size_t smem; uint64_t blocks; };
+constexpr int kResidencies = 64;
+std::mutex g_residency_mu;
+Residency g_residency[kResidencies];
+int g_residencies = 0;
 int resident_blocks(const void* fn, int threads, size_t smem, const DeviceView& dev, uint64_t* out) {
-    int per_sm = 0;
-    if (smem > 16u * 1024u && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
+    std::lock_guard<std::mutex> lock(g_residency_mu);
+    for (int i = 0; i < g_residencies; ++i) {
+        const Residency& r = g_residency[i];
+        if (r.fn == fn && r.smem == smem && r.dev == dev.device) { *out = r.blocks; return FASTSGD_OK; }
+    }
+    int per_sm = 0, most = 0;
+    cudaFuncAttributes at;
+    if (cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev.device) != cudaSuccess || cudaFuncGetAttributes(&at, fn) != cudaSuccess
+        || cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)at.sharedSizeBytes) != cudaSuccess) {
+        cudaGetLastError();
+        return FASTSGD_E_CUDA;
+    }
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, threads, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); return FASTSGD_E_CUDA; }
     *out = (uint64_t)per_sm * (uint64_t)dev.sm_count;
+    g_residency[g_residencies < kResidencies ? g_residencies++ : kResidencies - 1] = Residency{dev.device, fn, smem, *out};
     return FASTSGD_OK;
 }
 
@@ -110,7 +127,7 @@ int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teache
     const uint32_t gt = grad ? grad->type : student->type;
     const void* fn = mode == kLossOnly ? distill_kernel<kLossOnly>(student->type, gt)
                    : mode == kLossAndGrad ? distill_kernel<kLossAndGrad>(student->type, gt) : distill_kernel<kGradOnly>(student->type, gt);
-    const size_t smem = 4u * ((a.cols + 31u) / 32u + 1u);
+    const size_t smem = (4u * ((a.cols + 31u) / 32u + 1u) + 4095u) & ~(size_t)4095u;      // (whole pages: few different sizes)
     uint64_t grid = 0;
     rc = resident_blocks(fn, kDistillThreads, smem, dev, &grid);
     if (rc) return rc;
@@ -143,6 +160,7 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
     if (k < 1u || k > kTopMaxPairs || k > logits->cols || !is_temperature(temperature)) return FASTSGD_E_BAD_PARAM;
     if (logits->rows && (!keys || !values)) return FASTSGD_E_NULL;
     if (!aligned_to(keys, 4) || !aligned_to(values, size_of(logits->type)) || !aligned_to(lse, 4) || !aligned_to(tail, 4)) return FASTSGD_E_ALIGN;
+    if (logits->cols > kTopMaxCols) return FASTSGD_E_NOT_IMPLEMENTED;
     if (!logits->rows) return FASTSGD_OK;
     DeviceView dev;
     rc = device_view(&dev);

@@ -90,9 +90,9 @@ __global__ void __launch_bounds__(kTopRowsThreads) k_top_rows(TopArgs a) {
 
 // ---- many columns: a block or a cluster of blocks per row -----------------------------------------
 // One pass over the row in tiles.  A vector of 16 bytes whose maximum is below the bar cannot hold one of the k pairs: its
-// exponentials are summed and it is forgotten.  The others are listed, warp by warp; their elements above the bar become candidates,
-// and the rest of them joins the sum.  At the end the k-th largest candidate is found by histograms of eight bits, and the smaller
-// ones join the sum.
+// exponentials are summed and it is forgotten.  The others are listed, warp by warp, and at the end their elements above the bar
+// become candidates; the k-th largest of these is found by histograms of eight bits.  Then the listed vectors are gone through once
+// more for the exponentials of what is no pair, in the list's order: the order in which candidates were found changes no sum.
 //
 // The first tile is a sample of the row (its 512-byte pieces lie apart as many pieces as there are tiles), and the bar is the
 // maximum of one of its vectors: the one whose place from above the k-th of the row has among them, four standard deviations lower.
@@ -101,19 +101,22 @@ __global__ void __launch_bounds__(kTopRowsThreads) k_top_rows(TopArgs a) {
 // k-th largest maximum of the first tile, which rises to the k-th candidate whenever there are many.
 constexpr int kTopTile = 4;                                // vectors a thread takes per tile
 constexpr uint32_t kTopTileVecs = kTopTile * kTopThreads;
-constexpr uint32_t kTopList = 256u;                        // vectors a warp lists
-constexpr uint32_t kTopHead = 0xFFFFFFFEu, kTopTail = 0xFFFFFFFFu;
+constexpr uint32_t kTopList = 1024u;                       // vectors a warp lists
+constexpr uint32_t kTopHead = 0xFFFEu, kTopTail = 0xFFFFu;
+constexpr uint32_t kTopMaxCols = 1u << 20;                 // (a listed vector is its number among the warp's, in 16 bits: at most 511 tiles)
+static_assert(kTopMaxCols / 4u / kTopTileVecs < 511u, "fp32, four to a vector");
 constexpr uint32_t kTopBurst = 8u * kTopThreads + 16u;     // candidates that a step of the careful way can add
 constexpr uint32_t kTopByCount = 256u;                     // candidates that are sorted by counting the larger ones
 constexpr uint32_t kTopFewPairs = 128u;                    // k up to here: less shared memory
 
 // MOST: the largest k
 template <uint32_t MOST> struct TopShared {
-    static constexpr uint32_t kRoom = MOST + kTopBurst;
+    static constexpr uint32_t kRoom = MOST <= kTopFewPairs ? MOST + kTopBurst : 4u * MOST;
+    static_assert(kRoom >= MOST + kTopBurst, "a step of the careful way finds room");
     unsigned long long cand[kRoom];
     unsigned long long sorted[MOST < kTopByCount ? kTopByCount : MOST];
     uint4    ring[2][kTopTile][kTopThreads];               // the tile at hand and the next one
-    uint32_t list[kTopWarps][kTopList];                    // vectors by number; kTopHead, kTopTail: the elements around them
+    uint16_t list[kTopWarps][kTopList];                    // vectors as 32 (4 tile + u) + lane; kTopHead, kTopTail: the elements around them
     uint32_t hist[256];
     uint32_t cands, taken, bin, above, equal;              // (cands may count more than there is room for)
     float2   join[kTopWarps];
@@ -159,10 +162,10 @@ __device__ __forceinline__ bool select_step(S& s, W& word, uint32_t& need, int s
     return need == s.equal;
 }
 
-// The k largest of the n candidates (more than k of them, none below `floor`) stay; the others join the sum.  Returns a lower bound of
-// them all: the bar.  The histograms begin with the highest bit in which the candidates' distances from `floor` differ.
-template <class T, class S>
-__device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor, ExpSum* sum, float c, float slack) {
+// The k largest of the n candidates (more than k of them, none below `floor`) stay.  Returns a lower bound of them all: the bar.  The
+// histograms begin with the highest bit in which the candidates' distances from `floor` differ.
+template <class S>
+__device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor) {
     const uint32_t tid = threadIdx.x, base = (uint32_t)(floor >> 32);
     const unsigned long long low = (unsigned long long)base << 32;
     uint32_t most = 0u;
@@ -183,13 +186,10 @@ __device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint
     word += low;
     if (tid == 0) s.taken = 0u;
     __syncthreads();
-    ExpSum e = *sum;
     for (uint32_t i = tid; i < n; i += kTopThreads) {
         const unsigned long long w = s.cand[i];
         if (w >= word) s.sorted[atomicAdd(&s.taken, 1u)] = w;
-        else e.add(value_of_rank<T>((uint32_t)(w >> 32)), c, slack);
     }
-    *sum = e;
     __syncthreads();
     for (uint32_t i = tid; i < k; i += kTopThreads) s.cand[i] = s.sorted[i];
     if (tid == 0) s.cands = k;
@@ -197,44 +197,76 @@ __device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint
     return word;
 }
 
-// A warp's listed vectors: their elements above the bar become candidates (as far as there is room), the others join the sum.  Two
-// lanes a vector.
-template <class T, uint32_t MOST>
-__device__ __noinline__ void go_through(TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long cut, uint32_t first_key, uint32_t begin, uint32_t end,
-                                        ExpSum* sum, float c, float slack) {
-    constexpr int N = Vec<T>::N, H = N / 2;
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, part = lane & 1u;
-    ExpSum e = *sum;
+// The slice of a row as vectors: in pieces of 32, piece p in tile p % tiles.  A thread's vector u of tile t is number first + 32 t + step u.
+struct TopSlice { uint32_t head, tail, vecs, tiles, first, step; };
+template <class T> __device__ __forceinline__ TopSlice top_slice(const T* z, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const Span sp = span_of(z, n);
+    TopSlice q;
+    q.head = sp.head; q.tail = sp.tail; q.vecs = sp.vecs;
+    q.tiles = sp.vecs ? (sp.vecs + kTopTileVecs - 1u) / kTopTileVecs : 1u;
+    q.first = warp * q.tiles * 32u + lane; q.step = kTopWarps * q.tiles * 32u;
+    return q;
+}
+// of the four vectors of tile t, those that there are
+__device__ __forceinline__ uint32_t vectors_of(const TopSlice& q, uint32_t t) {
+    const uint32_t v = q.first + 32u * t;
+    return v + (kTopTile - 1u) * q.step < q.vecs ? kTopTile : v < q.vecs ? (q.vecs - 1u - v) / q.step + 1u : 0u;
+}
+
+// f(rank << 32 | ~key, value) for the elements of a warp's listed vectors, in the list's order.
+template <class T, uint32_t MOST, class F>
+__device__ __forceinline__ void each_listed(const TopShared<MOST>& s, const T* z, const TopSlice& q, uint32_t listed, uint32_t begin, uint32_t end, F f) {
+    constexpr int N = Vec<T>::N, U = 2;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, first_key = begin + q.head;
+    const uint4* body = reinterpret_cast<const uint4*>(z + first_key);
     __syncwarp();
-    for (uint32_t h = lane >> 1; h < listed; h += 16u) {
-        const uint32_t v = s.list[warp][h];
-        const uint32_t base = (v == kTopHead ? first_key - N : v == kTopTail ? end - (end - first_key) % N : first_key + v * N) + part * H;
-        T x[H];
-        if (v < kTopHead) *reinterpret_cast<unsigned long long*>(x) = *reinterpret_cast<const unsigned long long*>(z + base);
-        else {
+    for (uint32_t h = lane; h < listed; h += 32u * U) {
+        uint32_t base[U];
+        uint4 raw[U];
 #pragma unroll
-            for (int i = 0; i < H; ++i) x[i] = base + i - begin < end - begin ? z[base + i] : from_float<T>(0.f);
+        for (int u = 0; u < U; ++u) {
+            if (h + 32u * u >= listed) continue;
+            const uint32_t id = s.list[warp][h + 32u * u];
+            if (id < kTopHead) {
+                const uint32_t v = q.first - lane + (id & 31u) + 32u * (id >> 7) + q.step * (id >> 5 & 3u);
+                base[u] = first_key + v * N;
+                raw[u] = load16(body + v);
+            } else {
+                base[u] = id == kTopHead ? first_key - N : end - q.tail;
+                T x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = base[u] + i - begin < end - begin ? z[base[u] + i] : from_float<T>(0.f);
+                raw[u] = *reinterpret_cast<const uint4*>(x);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < H; ++i) {
-            if (base + i - begin >= end - begin) continue;
-            const float y = to_float(x[i]);
-            const unsigned long long w = candidate(rank_of<T>(y), base + i);
-            if (w >= cut) {
-                const uint32_t n = atomicAdd(&s.cands, 1u);
-                if (n < TopShared<MOST>::kRoom) s.cand[n] = w;
-            } else e.add(y, c, slack);
+        for (int u = 0; u < U; ++u) {
+            if (h + 32u * u >= listed) continue;
+            float x[N];
+            Vec<T>::unpack(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (base[u] + i - begin < end - begin) f(candidate(rank_of<T>(x[i]), base[u] + i), x[i]);
         }
     }
     __syncwarp();
-    *sum = e;
+}
+// Those above the bar become candidates, as far as there is room.
+template <class T, uint32_t MOST>
+__device__ __noinline__ void collect(TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long cut, uint32_t begin, uint32_t end) {
+    each_listed<T>(s, z, top_slice(z + begin, end - begin), listed, begin, end, [&](unsigned long long w, float) {
+        if (w < cut) return;
+        const uint32_t n = atomicAdd(&s.cands, 1u);
+        if (n < TopShared<MOST>::kRoom) s.cand[n] = w;
+    });
 }
 
-// The k largest of n candidates (all, if there are no more) in descending order to `sorted`; the others join the sum.
-template <class T, class S>
-__device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor, ExpSum* sum, float c, float slack) {
+// The k largest of n candidates (all, if there are no more) in descending order to `sorted`.
+template <class S>
+__device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor) {
     const uint32_t tid = threadIdx.x;
-    if (n > k + k / 2u + 32u || (n > kTopByCount && n > k)) { cut_candidates<T>(s, n, k, floor, sum, c, slack); n = k; }
+    if (n > k + k / 2u + 32u || (n > kTopByCount && n > k)) { cut_candidates(s, n, k, floor); n = k; }
     if (n <= kTopByCount) {                                // a candidate's place is the number of larger ones
         constexpr uint32_t kParts = 8u;                    // threads of a candidate, next to each other
         for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads / kParts) {
@@ -244,10 +276,7 @@ __device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, u
             for (uint32_t j = part; j < n; j += kParts) before += s.cand[j] > x;
 #pragma unroll
             for (uint32_t o = 1u; o < kParts; o <<= 1) before += __shfl_xor_sync(kFullMask, before, o);
-            if (i < n && part == 0u) {
-                if (before < k) s.sorted[before] = x;
-                else sum->add(value_of_rank<T>((uint32_t)(x >> 32)), c, slack);
-            }
+            if (i < n && part == 0u) s.sorted[before] = x;
         }
     } else {                                               // n <= k: a bitonic network
         uint32_t size2 = 2u * kTopByCount;
@@ -267,22 +296,6 @@ __device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, u
     return n < k ? n : k;
 }
 
-// The slice of a row as vectors: in pieces of 32, piece p in tile p % tiles.  A thread's vector u of tile t is number first + 32 t + step u.
-struct TopSlice { uint32_t head, tail, vecs, tiles, first, step; };
-template <class T> __device__ __forceinline__ TopSlice top_slice(const T* z, uint32_t n) {
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const Span sp = span_of(z, n);
-    TopSlice q;
-    q.head = sp.head; q.tail = sp.tail; q.vecs = sp.vecs;
-    q.tiles = sp.vecs ? (sp.vecs + kTopTileVecs - 1u) / kTopTileVecs : 1u;
-    q.first = warp * q.tiles * 32u + lane; q.step = kTopWarps * q.tiles * 32u;
-    return q;
-}
-// of the four vectors of tile t, those that there are
-__device__ __forceinline__ uint32_t vectors_of(const TopSlice& q, uint32_t t) {
-    const uint32_t v = q.first + 32u * t;
-    return v + (kTopTile - 1u) * q.step < q.vecs ? kTopTile : v < q.vecs ? (q.vecs - 1u - v) / q.step + 1u : 0u;
-}
 // a lower bound of the need-th largest rank among the maxima of the first tile's vectors (16 of its bits)
 template <class T, class S>
 __device__ __forceinline__ unsigned long long first_bar(S& s, uint32_t need, uint32_t mine, const float (&top)[kTopTile]) {
@@ -306,10 +319,11 @@ template <class T> __device__ __forceinline__ float bar_value(unsigned long long
     return lo > rank_of<T>(INFINITY) ? INFINITY : value_of_rank<T>(lo);      // (nothing is below NaN, the value of 0)
 }
 
-// The careful way through a slice.
+// The careful way through a slice: its candidates.  Returns the bar.
 template <class T, uint32_t MOST>
-__device__ __noinline__ unsigned long long top_carefully(TopShared<MOST>& s, const T* z, const TopSlice& q, uint32_t there, uint32_t k, uint32_t begin, uint32_t end, ExpSum* sum, float c, float slack) {
+__device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s, const T* z, uint32_t there, uint32_t k, uint32_t begin, uint32_t end) {
     constexpr int N = Vec<T>::N;
+    const TopSlice q = top_slice(z + begin, end - begin);
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, first_key = begin + q.head;
     const uint4* body = reinterpret_cast<const uint4*>(z + first_key);
     unsigned long long cut = 0ull;
@@ -332,28 +346,35 @@ __device__ __noinline__ unsigned long long top_carefully(TopShared<MOST>& s, con
             }
             bool hit = false;
             if (u < mine) {
-                const uint4 raw = load16(body + v + u * q.step);
-                const float top = Vec<T>::max_nan(raw);
+                const float top = Vec<T>::max_nan(load16(body + v + u * q.step));
                 hit = !(top < bar) && !(top == bar && first_key + (v + u * q.step) * N > ~(uint32_t)cut);
-                if (!hit) {
-                    float x[N];
-                    Vec<T>::unpack(raw, x);
-                    ExpSum e = *sum;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) e.add(x[i], c, slack);
-                    *sum = e;
-                }
             }
             const unsigned hits = __ballot_sync(kFullMask, hit);
-            if (hit) s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = v + u * q.step;
-            go_through<T>(s, z, listed + __popc(hits), cut, first_key, begin, end, sum, c, slack);
+            if (hit) s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = (uint16_t)(128u * t + 32u * u + lane);
+            collect<T>(s, z, listed + __popc(hits), cut, begin, end);
             __syncthreads();
             const uint32_t n = s.cands;
             __syncthreads();
-            if (n > MOST) cut = cut_candidates<T>(s, n, k, cut, sum, c, slack);
+            if (n > MOST) cut = cut_candidates(s, n, k, cut);
         }
     }
     return cut;
+}
+// The sum of what lies below the last pair, of the listed vectors ...
+template <class T, uint32_t MOST>
+__device__ __noinline__ ExpSum sum_listed(const TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long last, uint32_t begin, uint32_t end, ExpSum e, float c, float slack) {
+    each_listed<T>(s, z, top_slice(z + begin, end - begin), listed, begin, end, [&](unsigned long long w, float x) { if (w < last) e.add(x, c, slack); });
+    return e;
+}
+// ... or of the whole slice.
+template <class T>
+__device__ __noinline__ ExpSum sum_carefully(const T* z, unsigned long long last, uint32_t begin, uint32_t end, float c, float slack) {
+    ExpSum e;
+    for (uint32_t j = begin + threadIdx.x; j < end; j += kTopThreads) {
+        const float x = to_float(z[j]);
+        if (candidate(rank_of<T>(x), j) < last) e.add(x, c, slack);
+    }
+    return e;
 }
 
 template <class T, uint32_t MOST>
@@ -378,19 +399,15 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
     uint32_t slot = 0u;
     uint64_t row = blockIdx.x / blocks;
     const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
-    TopSlice q{};
-    if (row < a.rows) { q = top_slice(z + begin, end - begin); fetch(z, q, 0u, slot); }
+    if (row < a.rows) fetch(z, top_slice(z + begin, end - begin), 0u, slot);
     for (; row < a.rows; row += stride) {
-        const T* next_z = z + stride * a.z_stride;
-        TopSlice next{};
-        const uint32_t first_key = begin + q.head;
+        const TopSlice q = top_slice(z + begin, end - begin);
         // vectors in the first tile: of its pieces all but the row's last are whole
         const uint32_t pieces = (q.vecs + 31u) / 32u;
         const uint32_t there = pieces ? (pieces + q.tiles - 1u) / q.tiles * 32u - ((pieces - 1u) % q.tiles ? 0u : pieces * 32u - q.vecs) : 0u;
         const float expect = (float)k * (float)there / (float)max(q.vecs, 1u);
         const uint32_t guess = min(k, (uint32_t)(expect + 5.f * sqrtf(expect) + 5.f));
         ExpSums es;
-        ExpSum e;
         unsigned long long cut = 0ull;
         float bar = 0.f;
         uint32_t listed = 0u;
@@ -398,7 +415,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
         if (tid == 0) s.cands = 0u;
         for (uint32_t t = 0; t < q.tiles; ++t) {
             if (t + 1u < q.tiles) fetch(z, q, t + 1u, slot ^ 1u);
-            else if (row + stride < a.rows) { next = top_slice(next_z + begin, end - begin); fetch(next_z, next, 0u, slot ^ 1u); }
+            else if (row + stride < a.rows) { const T* next = z + stride * a.z_stride; fetch(next, top_slice(next + begin, end - begin), 0u, slot ^ 1u); }
             else copies_end_group();
             wait_copies<1>();
             uint4 raw[kTopTile];
@@ -406,7 +423,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
 #pragma unroll
             for (int u = 0; u < kTopTile; ++u) raw[u] = s.ring[slot][u][tid];
             slot ^= 1u;
-            const uint32_t v = q.first + 32u * t, mine = vectors_of(q, t);
+            const uint32_t mine = vectors_of(q, t);
             if (mine < kTopTile) {                         // (the last tiles may be short)
 #pragma unroll
                 for (int u = 0; u < kTopTile; ++u)
@@ -427,7 +444,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
                 const unsigned hits = __ballot_sync(kFullMask, hit);
                 if (hits) {
                     if (hit) {
-                        s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = v + u * q.step;
+                        s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = (uint16_t)(128u * t + 32u * u + lane);
                         raw[u] = make_uint4(Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf);      // (summed later)
                         top[u] = -INFINITY;
                     }
@@ -443,22 +460,27 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
                     es.add(x, a.c);
                 }
             }
-            if (listed > kTopList - 32u * kTopTile || t == q.tiles - 1u) {
-                go_through<T>(s, z, listed, cut, first_key, begin, end, &e, a.c, a.slack);
+            if (listed > kTopList - 32u * kTopTile && t + 1u < q.tiles) {      // no room for another tile's: the careful way
+                if (lane == 0) atomicAdd(&s.cands, TopShared<MOST>::kRoom + 1u);
                 listed = 0u;
             }
         }
-        const ExpSum streamed = es.whole();
-        e.join(streamed.m, streamed.s, a.c);
+        collect<T>(s, z, listed, cut, begin, end);
         __syncthreads();
         uint32_t n = s.cands;
-        if (n > TopShared<MOST>::kRoom || (n < k && cut)) {
+        const bool careful = n > TopShared<MOST>::kRoom || (n < k && cut);
+        if (careful) {
             __syncthreads();
-            e = ExpSum();
-            cut = top_carefully<T>(s, z, q, there, k, begin, end, &e, a.c, a.slack);
+            cut = collect_carefully<T>(s, z, there, k, begin, end);
             n = s.cands;
         }
-        const uint32_t have = sort_candidates<T>(s, n, k, cut, &e, a.c, a.slack);
+        const uint32_t have = sort_candidates(s, n, k, cut);
+        ExpSum e = es.whole();
+        if (sums) {
+            const unsigned long long least = have == k ? s.sorted[k - 1u] : 0ull;      // the last pair
+            if (careful) e = sum_carefully<T>(z, least, begin, end, a.c, a.slack);
+            else e = sum_listed<T>(s, z, listed, least, begin, end, e, a.c, a.slack);
+        }
 
         // ---- the pairs: a candidate's place is how many of the whole row's are larger -----------------
         if (tid == 0) s.count = have;
@@ -507,7 +529,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
             if (a.lse) a.lse[row] = none ? -INFINITY : top / a.temperature + logf(rest + inside);
             if (a.tail) a.tail[row] = none ? 0.f : rest / (rest + inside);
         }
-        z = next_z; q = next;
+        z += stride * a.z_stride;
     }
 }
 

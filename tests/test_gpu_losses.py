@@ -122,6 +122,20 @@ def test_top_logits_of_ties_infinities_nan_and_sorted_rows(dtype, cols, k):
     _check_top(z, _dev(z, TYPES[dtype]), k)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cols,k", [(50_001, 64), (50_001, 700), (200_003, 300)])
+def test_top_logits_sums_are_the_same_every_time(dtype, cols, k):
+    """Rows of the same values at places of the same alignment: the order in which a block finds its pairs must not show."""
+    row = _dev(_logits(np.random.default_rng(cols), 1, cols, dtype), TYPES[dtype])
+    row[0, 100:140] = row[0, 200:240]                                         # (ties)
+    z = torch.empty((200, cols + (-cols) % 8), dtype=TYPES[dtype], device="cuda")[:, :cols]
+    z.copy_(row.expand(200, cols))
+    first = _run_top(z, k, 1.0)
+    for got in (first, _run_top(z, k, 1.0)):
+        for a, b in zip(got, first):
+            assert _same(a, b[:1].expand_as(b).contiguous())
+
+
 def test_top_logits_optional_outputs_and_no_rows():
     z = torch.randn(3, 500, device="cuda")
     keys, values = torch.empty(3, 4, dtype=torch.int32, device="cuda"), torch.empty(3, 4, device="cuda")

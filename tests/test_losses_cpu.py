@@ -136,6 +136,8 @@ def test_top_logits_refusals(lib):
         assert call(m, 4, t, FAKE, FAKE, None, None, None) == binding.E_BAD_PARAM
     for args in ((FAKE + 1, FAKE, None, None), (FAKE, FAKE + 2, None, None), (FAKE, FAKE, FAKE + 1, None), (FAKE, FAKE, None, FAKE + 2)):
         assert call(m, 4, 1.0, *args, None) == binding.E_ALIGN
+    wide = C.byref(_matrix(cols=(1 << 20) + 1, row_stride=(1 << 20) + 1))
+    assert call(wide, 4, 1.0, FAKE, FAKE, None, None, None) == binding.E_NOT_IMPLEMENTED
     assert call(C.byref(_matrix(rows=0, data=None)), 4, 1.0, None, None, None, None, None) == binding.OK
 
 
