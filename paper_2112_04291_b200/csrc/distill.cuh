@@ -8,14 +8,19 @@
 // lose it where the student is sure), and the gradient of the others is their share of that sum times w T (rest - tail).
 #pragma once
 
+#include <cooperative_groups.h>
+
+#include "async.cuh"
 #include "rows.cuh"
 
 namespace fsg {
 
-constexpr int kDistillThreads = 512;
+constexpr int kDistillThreads = 256;                       // that go through the row
 constexpr int kDistillWarps   = kDistillThreads / 32;
+constexpr int kDistillBlock   = kDistillThreads + 32;      // and a warp for the pairs
 constexpr uint32_t kDistillMaxPairs = 1024u;
-constexpr uint32_t kDistillMaxCols  = 1u << 20;            // a bit per class in shared memory
+constexpr uint32_t kDistillMaxCols  = 1u << 20;
+constexpr uint32_t kDistillMaxBlocks = 8u;                 // of a cluster
 
 // what a launch computes
 constexpr int kLossOnly = 0, kLossAndGrad = 1, kGradOnly = 2;      // kGradOnly: from the sums that a forward launch kept
@@ -27,199 +32,454 @@ struct DistillArgs {
     float* loss; float* stats_out;
     uint64_t rows, z_stride, grad_stride;
     uint32_t cols, k, values_type;
+    uint32_t per, slots, kept;                             // vectors of a row that a block takes; of them a thread; in shared memory
+    uint32_t claims;                                       // there are more rows than blocks or clusters at a time
     float temperature, inv_t, c, slack;                    // c = log2(e) / T
 };
 
-struct DistillShared {
-    int   key[kDistillMaxPairs];                           // -1: absent
-    float z[kDistillMaxPairs], p[kDistillMaxPairs], lp[kDistillMaxPairs];
-    float2 join[kDistillWarps];
-    float  one[kDistillWarps];
-    double two[kDistillWarps];
+// What the pairs' warp finds out about a row ...
+struct DistillRow {
+    float zm, tsum, cross, ksum;                           // largest of the keys' logits; sums over the pairs, relative to the largest of their kind
+    float tail, scale, weight;                             // scale: of the gradient
+    float m, s;                                            // kGradOnly: what the forward launch kept
+    uint32_t flags, row;
+    // where the block's share of this row and of the next one is: its first vector, how many
+    const uint4* at; const uint4* next_at;
+    uint32_t count, next_count, head, tail_count;
 };
+constexpr uint32_t kRowCounts = 1u, kRowRepeats = 2u, kRowNone = 4u;      // there is a pair with a probability; a key of this block appears again; there are no more rows
+// ... and the others: the sum of exponentials, and that of the keys of all blocks.
+struct DistillSums { float m, s, ksum; };
 
-// bits j .. j + N - 1 of the map of keys (which has a word more than it needs)
-template <int N> __device__ __forceinline__ uint32_t key_bits(const uint32_t* map, uint32_t j) {
-    return __funnelshift_r(map[j >> 5], map[(j >> 5) + 1u], j & 31u) & ((1u << N) - 1u);
+struct DistillShared {
+    DistillRow  row[2];                                    // for even and odd rows, as everything below that two rows are at work on
+    DistillSums sums[2];
+    float2 join[kDistillWarps];
+    float4 peer[2][kDistillMaxBlocks];                     // m, sum and keys' sum of every block of the cluster
+    Claim  claim;                                          // of the first block: the cluster's next row
+    int    next[2];                                        // the others': what the first has been given
+    unsigned long long next_bar;
+};
+// dynamic: uint4 ring[kept][threads], then for each of two rows key, t (later e), z of every pair, then for each of two rows a byte per
+// vector of the slice, one for the elements before and one for those behind the vectors: which of the elements are keys of the row
+__host__ __device__ inline uint32_t distill_map_bytes(uint32_t per) { return (per + 2u + 3u) & ~3u; }
+__host__ __device__ inline size_t distill_smem(uint32_t kept, uint32_t k, uint32_t per) {
+    kept = (kept + 3u) & ~3u;                              // (four chunks)
+    return (size_t)kept * kDistillThreads * 16u + 24u * (size_t)k + 2u * distill_map_bytes(per);
 }
 
-// The sum of exponentials of a row's elements [0, n), without the keys of `map` where there is one.
+// the warps that go through the row wait for one another
+__device__ __forceinline__ void sync_readers() { asm volatile("bar.sync 1, %0;" ::"n"(kDistillThreads) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A block's share of a row: vectors [first, first + count) behind the row's head; the first block has the head, too, the last one the tail.
+struct DistillSlice {
+    uint32_t head, tail, vecs, first, count;
+};
+template <class T> __device__ __forceinline__ DistillSlice distill_slice(const T* z, uint32_t cols, uint32_t per, uint32_t rank) {
+    const Span sp = span_of(z, cols);
+    DistillSlice q;
+    q.head = sp.head; q.tail = sp.tail; q.vecs = sp.vecs;
+    q.first = min(rank * per, sp.vecs);
+    q.count = min(per, sp.vecs - q.first);
+    return q;
+}
+
+// The sum of exponentials of a block's share, without the keys of `map` where there is one: from global memory and with any
+// logits.
 template <class T>
-__device__ __forceinline__ ExpSum scan_row(const T* z, uint32_t n, const uint32_t* map, float c, float slack) {
-    constexpr int N = Vec<T>::N, U = 4;
-    const uint32_t tid = threadIdx.x;
-    const Span sp = span_of(z, n);
+__device__ __noinline__ ExpSum scan_far(const T* z, const uint8_t* map, uint32_t cols, uint32_t per, uint32_t rank, uint32_t blocks, float c, float slack) {
+    constexpr int N = Vec<T>::N;
+    const DistillSlice q = distill_slice(z, cols, per, rank);
     ExpSum e;
-    auto single = [&](uint32_t j) { if (!map || !(map[j >> 5] >> (j & 31u) & 1u)) e.add(to_float(z[j]), c, slack); };
-    if (tid < sp.head) single(tid);
-    if (tid < sp.tail) single(n - sp.tail + tid);
-    const T* body = z + sp.head;
-    for (uint32_t v0 = tid; v0 < sp.vecs; v0 += U * kDistillThreads) {
-        uint4 raw[U];
+    for (uint32_t i = threadIdx.x; i < q.count; i += kDistillThreads) {
+        float x[N];
+        Vec<T>::unpack(load16(z + q.head + (uint64_t)(q.first + i) * N), x);
+        const uint32_t keys = map ? map[i] : 0u;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kDistillThreads < sp.vecs) raw[u] = load16(body + (uint64_t)(v0 + u * kDistillThreads) * N);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t v = v0 + u * kDistillThreads;
-            if (v >= sp.vecs) break;
-            float f[N];
-            Vec<T>::unpack(raw[u], f);
-            float top = Vec<T>::max(raw[u]);
-            if (map) {
-                const uint32_t b = key_bits<N>(map, sp.head + v * N);
-                if (b) {
-                    top = kLowest;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) { if (b >> i & 1u) f[i] = -INFINITY; top = fmaxf(top, f[i]); }
-                }
-            }
-            e.raise(top, c, slack);
-#pragma unroll
-            for (int i = 0; i < N; ++i) e.s += exp2_fast((f[i] - e.m) * c);
-        }
+        for (int j = 0; j < N; ++j) if (!(keys >> j & 1u)) e.add(x[j], c, slack);
     }
+    if (rank == 0u && threadIdx.x < q.head && !(map && map[per] >> threadIdx.x & 1u)) e.add(to_float(z[threadIdx.x]), c, slack);
+    if (rank == blocks - 1u && threadIdx.x < q.tail && !(map && map[per + 1u] >> threadIdx.x & 1u)) e.add(to_float(z[cols - q.tail + threadIdx.x]), c, slack);
     return e;
 }
 
-// grad[j] = a 2^((z_j - m) c) for the elements [0, n) of a row (a = 0: zero).
+// grad = by 2^((z - m) c) of a block's share, from global memory and with any logits (by = 0: zero).
 template <class TZ, class TG>
-__device__ __forceinline__ void write_row(const TZ* z, TG* g, uint32_t n, float a, float m, float c) {
-    constexpr int N = Vec<TZ>::N, U = 4;
-    const uint32_t tid = threadIdx.x;
-    const Span sp = span_of(z, n);
-    const bool wide = (reinterpret_cast<uintptr_t>(g + sp.head) & 15u) == 0u;
-    auto single = [&](uint32_t j) { g[j] = from_float<TG>(exp2_fast((to_float(z[j]) - m) * c) * a); };
-    if (tid < sp.head) single(tid);
-    if (tid < sp.tail) single(n - sp.tail + tid);
-    const TZ* body = z + sp.head;
-    TG* out = g + sp.head;
-    for (uint32_t v0 = tid; v0 < sp.vecs; v0 += U * kDistillThreads) {
-        uint4 raw[U];
+__device__ __noinline__ void write_far(const TZ* z, TG* g, uint32_t cols, uint32_t per, uint32_t rank, uint32_t blocks, float by, float m, float c) {
+    constexpr int N = Vec<TZ>::N;
+    const DistillSlice q = distill_slice(z, cols, per, rank);
+    const bool wide = (reinterpret_cast<uintptr_t>(g + q.head) & 15u) == 0u;
+    for (uint32_t i = threadIdx.x; i < q.count; i += kDistillThreads) {
+        const uint64_t j = q.head + (uint64_t)(q.first + i) * N;
+        float x[N];
+        if (by != 0.f) Vec<TZ>::unpack(load16(z + j), x);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kDistillThreads < sp.vecs) raw[u] = load16(body + (uint64_t)(v0 + u * kDistillThreads) * N);
+        for (int n = 0; n < N; ++n) x[n] = by != 0.f ? exp2_fast((x[n] - m) * c) * by : 0.f;
+        store_values(g + j, x, wide);
+    }
+    auto single = [&](uint32_t j) { g[j] = from_float<TG>(by != 0.f ? exp2_fast((to_float(z[j]) - m) * c) * by : 0.f); };
+    if (rank == 0u && threadIdx.x < q.head) single(threadIdx.x);
+    if (rank == blocks - 1u && threadIdx.x < q.tail) single(cols - q.tail + threadIdx.x);
+}
+
+// The place of key j in the map of a block's share, in bits, or -1 if another block has it.
+template <class T>
+__device__ __forceinline__ int key_bit(const DistillSlice& q, uint32_t j, uint32_t per, uint32_t rank, uint32_t blocks) {
+    constexpr uint32_t N = Vec<T>::N;
+    if (j < q.head) return rank == 0u ? (int)(per * 8u + j) : -1;
+    const uint32_t v = (j - q.head) / N;
+    if (v >= q.vecs) return rank == blocks - 1u ? (int)((per + 1u) * 8u + j - q.head - q.vecs * N) : -1;
+    return v - q.first < q.count ? (int)((v - q.first) * 8u + (j - q.head) % N) : -1;
+}
+
+// The pairs' warp: what it finds out about a row, one row ahead of the others.
+template <class TZ, int MODE>
+__device__ __forceinline__ void prepare_pairs(const DistillArgs& a, uint64_t row, uint32_t rank, uint32_t blocks, DistillRow& out, int* s_key, float* s_t, float* s_z, uint8_t* map) {
+    constexpr uint32_t U = 4u;
+    const uint32_t lane = threadIdx.x & 31u, k = a.k;
+    const bool mapped = MODE != kLossOnly || a.tail;
+    const TZ* z = static_cast<const TZ*>(a.z) + row * a.z_stride;
+    const DistillSlice q = distill_slice(z, a.cols, a.per, rank);
+    DistillRow r;
+    r.weight = a.weight ? a.weight[row] : 1.f;
+    r.tail = a.tail ? a.tail[row] : 0.f;
+    r.scale = a.temperature * (MODE != kLossOnly && a.grad_loss ? a.grad_loss[row] : 1.f);
+    r.m = MODE == kGradOnly ? a.stats_in[2 * row] : 0.f;
+    r.s = MODE == kGradOnly ? a.stats_in[2 * row + 1] : 0.f;
+    float tm = -INFINITY, zm = kLowest;
+    bool again = false;
+    if (r.weight != 0.f) {
+        for (uint32_t i0 = lane; i0 < k; i0 += 32u * U) {
+            int key[U];
+            float t[U], zk[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t v = v0 + u * kDistillThreads;
-            if (v >= sp.vecs) break;
-            float f[N];
-            Vec<TZ>::unpack(raw[u], f);
+            for (uint32_t u = 0; u < U; ++u) {
+                const uint32_t i = i0 + 32u * u;
+                key[u] = -1; t[u] = -INFINITY;
+                if (i < k) { key[u] = a.keys[row * k + i]; t[u] = load_typed(a.values, row * k + i, a.values_type); }
+            }
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = exp2_fast((f[i] - m) * c) * a;
-            store_values(out + (uint64_t)v * N, f, wide);
+            for (uint32_t u = 0; u < U; ++u) {
+                if (key[u] < 0 || (uint32_t)key[u] >= a.cols) { key[u] = -1; t[u] = -INFINITY; }
+                zk[u] = key[u] >= 0 ? to_float(z[key[u]]) : -INFINITY;
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) {
+                const uint32_t i = i0 + 32u * u;
+                if (i >= k) continue;
+                s_key[i] = key[u]; s_t[i] = t[u]; s_z[i] = zk[u];
+                tm = fmaxf(tm, t[u]); zm = fmaxf(zm, zk[u]);
+                if (mapped && key[u] >= 0) {
+                    const int b = key_bit<TZ>(q, (uint32_t)key[u], a.per, rank, blocks);
+                    if (b >= 0) again |= atomicOr(reinterpret_cast<uint32_t*>(map) + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1u;
+                }
+            }
         }
     }
-}
-template <class TG>
-__device__ __forceinline__ void zero_row(TG* g, uint32_t n) {
-    constexpr int N = Vec<TG>::N;
-    const Span sp = span_of(g, n);
-    if (threadIdx.x < sp.head) g[threadIdx.x] = from_float<TG>(0.f);
-    if (threadIdx.x < sp.tail) g[n - sp.tail + threadIdx.x] = from_float<TG>(0.f);
-    for (uint32_t v = threadIdx.x; v < sp.vecs; v += kDistillThreads) store16(g + sp.head + (uint64_t)v * N, make_uint4(0u, 0u, 0u, 0u));
+    tm = warp_max(tm); zm = warp_max(zm);
+    again = __any_sync(kFullMask, again);
+    const bool counts = tm > -INFINITY;                    // weight 0, or no pair with any probability: the row counts for nothing
+    __syncwarp();
+    float tsum = 0.f, cross = 0.f, ksum = 0.f;
+    if (counts) {
+        for (uint32_t i = lane; i < k; i += 32u) {
+            const float d = s_t[i] - tm, e = exp2_fast(d * a.c), y = s_z[i] - zm;
+            tsum += e;
+            if (e != 0.f) cross += e * (d - y);
+            s_t[i] = e;
+            // a key that appears several times counts once for the student
+            bool first = mapped && s_key[i] >= 0 && key_bit<TZ>(q, (uint32_t)s_key[i], a.per, rank, blocks) >= 0;
+            if (again) for (uint32_t j = 0; j < i; ++j) first &= s_key[j] != s_key[i];
+            if (first) ksum += exp2_fast(y * a.c);
+        }
+    }
+    r.tsum = warp_sum(tsum); r.cross = warp_sum(cross); r.ksum = warp_sum(ksum); r.zm = zm;
+    r.scale *= r.weight;
+    r.flags = (counts ? kRowCounts : 0u) | (again ? kRowRepeats : 0u);
+    r.at = reinterpret_cast<const uint4*>(z + q.head) + q.first; r.count = q.count; r.head = q.head; r.tail_count = q.tail;
+    r.row = (uint32_t)row; r.next_at = nullptr; r.next_count = 0u;
+    if (lane == 0) out = r;
 }
 
-// A block per row: the pairs, one pass over the row for the sum of exponentials, one more for the gradient (from the L2).
+// What both kinds of warps conclude from the sums.
+struct DistillTotals { float top, rest, total; bool none; };
+__device__ __forceinline__ DistillTotals totals_of(const DistillRow& r, const DistillSums& e, float c) {
+    DistillTotals t;
+    const bool tailed = r.tail != 0.f;
+    t.top = tailed ? fmaxf(e.m, r.zm) : e.m;
+    t.rest = e.s * exp2_fast((e.m - t.top) * c);
+    t.total = tailed ? t.rest + e.ksum * exp2_fast((r.zm - t.top) * c) : e.s;
+    t.none = !(r.flags & kRowCounts) || t.total == 0.f;    // (every logit of the row is -inf: it counts for nothing, too)
+    return t;
+}
+
+// The pairs' warp: the loss, and the gradient of the keys, once the others have written theirs; the row's part of the map is clear again.
 template <class TZ, class TG, int MODE>
-__global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
-    extern __shared__ uint32_t map[];                      // a bit per class: it is a key of this row
-    __shared__ DistillShared s;
-    const uint32_t tid = threadIdx.x, k = a.k;
-    const uint32_t words = (a.cols + 31u) / 32u + 1u;
-    const bool mapped = MODE != kLossOnly || a.tail;
-    wait_for_previous_kernels();
-    if (mapped) for (uint32_t i = tid; i < words; i += kDistillThreads) map[i] = 0u;
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const TZ* z = static_cast<const TZ*>(a.z) + row * a.z_stride;
-        TG* g = MODE == kLossOnly ? nullptr : static_cast<TG*>(a.grad) + row * a.grad_stride;
-        const float w = a.weight ? a.weight[row] : 1.f;
-        __syncthreads();                                   // (the last row's pairs are no longer in use)
+__device__ __forceinline__ void finish_pairs(const DistillArgs& a, uint64_t row, uint32_t rank, uint32_t blocks, const DistillRow& r, const DistillSums& e,
+                                             const int* s_key, const float* s_t, const float* s_z, uint8_t* map) {
+    const uint32_t lane = threadIdx.x & 31u, k = a.k;
+    const TZ* z = static_cast<const TZ*>(a.z) + row * a.z_stride;
+    const DistillSlice q = distill_slice(z, a.cols, a.per, rank);
+    const DistillTotals t = totals_of(r, e, a.c);
+    if (MODE != kGradOnly && rank == 0u && lane == 0) {
+        float loss = 0.f;
+        if (!t.none) {
+            // sum p_i (log p_i - log q_i): both logarithms relative to the largest of their kind
+            const float log_total = logf(t.total), share = 1.f - r.tail;
+            if (share != 0.f) loss = share * (r.cross / r.tsum * a.inv_t + logf(share / r.tsum) + ((t.top - r.zm) * a.inv_t + log_total));
+            if (r.tail != 0.f) loss += r.tail * (logf(r.tail / e.s) - (e.m - t.top) * a.inv_t + log_total);
+            loss *= r.weight * a.temperature * a.temperature;
+        }
+        if (a.loss) a.loss[row] = loss;
+        if (a.stats_out) { a.stats_out[2 * row] = t.none ? 0.f : e.m; a.stats_out[2 * row + 1] = t.none ? 0.f : e.s; }
+    }
+    if (!(MODE != kLossOnly || a.tail) || r.weight == 0.f) return;
+    const float share = (1.f - r.tail) / r.tsum;
+    TG* g = MODE == kLossOnly ? nullptr : static_cast<TG*>(a.grad) + row * a.grad_stride;
+    for (uint32_t i = lane; i < k; i += 32u) {
+        const int key = s_key[i];
+        const int b = key >= 0 ? key_bit<TZ>(q, (uint32_t)key, a.per, rank, blocks) : -1;
+        if (b < 0) continue;
+        map[b >> 3] = 0u;
+        if (MODE == kLossOnly || t.none) continue;
+        // all probability of a key that appears several times goes to its first pair
+        float p = s_t[i];
+        bool first = true;
+        if (r.flags & kRowRepeats) {
+            p = 0.f;
+            for (uint32_t j = 0; j < k; ++j) if (s_key[j] == key) { p += s_t[j]; first &= j >= i; }
+        }
+        if (first) g[key] = from_float<TG>(r.scale * (exp2_fast((s_z[i] - t.top) * a.c) / t.total - p * share));
+    }
+}
 
-        // ---- the pairs -----------------------------------------------------------------------
-        float tm = -INFINITY, zm = kLowest;
-        bool again = false;
-        if (w != 0.f) {
-            for (uint32_t i = tid; i < k; i += kDistillThreads) {
-                const int key = a.keys[row * k + i];
-                const bool here = key >= 0 && (uint32_t)key < a.cols;
-                const float t = here ? load_typed(a.values, row * k + i, a.values_type) : -INFINITY;
-                const float zk = here ? to_float(z[key]) : -INFINITY;
-                s.key[i] = here ? key : -1; s.lp[i] = t; s.z[i] = zk;
-                tm = fmaxf(tm, t); zm = fmaxf(zm, zk);
-                if (here && mapped) again |= atomicOr(&map[key >> 5], 1u << (key & 31)) >> (key & 31) & 1u;
-            }
+// A block or a cluster of blocks per row.  A block's share of the row stays in shared memory between the two passes, each thread's
+// vectors in places of its own: the thread that has used a vector for the last time asks for the next row's vector in its place, so that
+// reads go on while gradients are written, and no barrier stands between a copy and its use.  (Vectors beyond the shared memory, of
+// rows above half a megabyte, are read twice.)  The ninth warp has the pairs: those of the next row while the others go through this
+// one, and the keys' gradients of the row before.
+template <class TZ, class TG, int MODE>
+__global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
+    extern __shared__ __align__(16) unsigned char distill_smem_bytes[];
+    __shared__ DistillShared s;
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    constexpr int N = Vec<TZ>::N;
+    constexpr int G = 4;                                   // groups of copies of a row
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, k = a.k, blocks = cluster.num_blocks(), rank = cluster.block_rank();
+    int* s_key = reinterpret_cast<int*>(distill_smem_bytes + (size_t)((a.kept + 3u) & ~3u) * kDistillThreads * 16u);      // two rows' each
+    float* s_t = reinterpret_cast<float*>(s_key + 2u * k);
+    float* s_z = s_t + 2u * k;
+    uint8_t* maps = reinterpret_cast<uint8_t*>(s_z + 2u * k);
+    const uint32_t map_bytes = distill_map_bytes(a.per);
+    wait_for_previous_kernels();
+    const uint32_t first = blockIdx.x / blocks;
+
+    if (warp == (uint32_t)kDistillWarps) {
+        for (uint32_t i = lane; i < map_bytes / 2u; i += 32u) reinterpret_cast<uint32_t*>(maps)[i] = 0u;
+        if (lane == 0) {
+            claim_init(s.claim);
+            mbar_init(&s.next_bar, 1u);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-        tm = block_max<kDistillWarps>(tm, s.one);
-        if (!(tm > -INFINITY)) {                           // weight 0, or no pair with any probability: the row counts for nothing
-            if (mapped && w != 0.f) for (uint32_t i = tid; i < k; i += kDistillThreads) if (s.key[i] >= 0) map[s.key[i] >> 5] = 0u;
-            if (MODE != kLossOnly) zero_row(g, a.cols);
-            if (tid == 0) {
-                if (MODE != kGradOnly && a.loss) a.loss[row] = 0.f;
-                if (MODE != kGradOnly && a.stats_out) { a.stats_out[2 * row] = 0.f; a.stats_out[2 * row + 1] = 0.f; }
-            }
-            continue;
+        __syncwarp();
+        if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (every block of the cluster has begun)
+        if (a.claims && rank == 0u && lane == 0) claim_ask(s.claim);
+        int row = (int)first, before = -1, last = -1;      // of this turn, the one before and the one before that
+        // turn i, before the others begin with the i-th row: the row before the last one is finished, the i-th is prepared
+        for (uint32_t i = 0;; ++i) {
+            const uint32_t b = i & 1u;
+            int next = -1;
+            __syncwarp();
+            if (last >= 0) finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[b], s.sums[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
+            __syncwarp();
+            if (row >= 0) {
+                prepare_pairs<TZ, MODE>(a, (uint64_t)row, rank, blocks, s.row[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
+                // the cluster's next row: the first block has asked for it a turn ago, and tells the others
+                if (a.claims && lane == 0) {
+                    if (rank == 0u) {
+                        next = claim_answer(s.claim, i);
+                        if (next >= 0) { next /= (int)blocks; claim_ask(s.claim); }
+                        for (uint32_t o = 1u; o < blocks; ++o) {
+                            *cluster.map_shared_rank(&s.next[b], o) = next;
+                            const uint32_t bar = smem_u32(&s.next_bar);
+                            asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(bar), "r"(o) : "memory");
+                        }
+                    } else if (mbar_wait_cluster(&s.next_bar, b)) next = s.next[b];
+                }
+                next = __shfl_sync(kFullMask, next, 0);
+                if (next >= 0 && lane == 0) {
+                    const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)next * a.z_stride;
+                    const DistillSlice n = distill_slice(z, a.cols, a.per, rank);
+                    s.row[b].next_at = reinterpret_cast<const uint4*>(z + n.head) + n.first; s.row[b].next_count = n.count;
+                }
+            } else if (lane == 0) s.row[b].flags = kRowNone;
+            if (blocks > 1u && i) cluster_wait();
+            __syncthreads();
+            last = before; before = row;
+            if (row < 0) break;
+            if (blocks > 1u) cluster_arrive();
+            row = next;
         }
-        zm = block_max<kDistillWarps>(zm, s.one);
-        again = __syncthreads_or(again);
-        float tsum = 0.f;
-        for (uint32_t i = tid; i < k; i += kDistillThreads) tsum += s.p[i] = exp2_fast((s.lp[i] - tm) * a.c);
-        tsum = block_sum<kDistillWarps>(tsum, s.one);
-        const float tail = a.tail ? a.tail[row] : 0.f;
-        const bool tailed = tail != 0.f;
-        const float share = (1.f - tail) / tsum, log_share = logf(1.f - tail) - logf(tsum);
-        for (uint32_t i = tid; i < k; i += kDistillThreads) { s.p[i] *= share; s.lp[i] = (s.lp[i] - tm) * a.inv_t + log_share; }
+        // (before is -1 now: the last row is the one before it)
+        {
+            const uint32_t b = s.row[0].flags & kRowNone ? 1u : 0u;
+            finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[b], s.sums[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
+        }
+        if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (no block leaves while another may write to its shared memory)
+        return;
+    }
+
+    uint4* ring = reinterpret_cast<uint4*>(distill_smem_bytes) + tid;
+    // One pass (the loss or the gradient alone): a row in chunks of `group` vectors a thread, four chunks ahead, whatever the row's length.  Two
+    // passes: four chunks that stay, and the rest of the row without.
+    constexpr bool kOnePass = MODE != kLossAndGrad;
+    const uint32_t group = (a.kept + G - 1u) / G, chunks = kOnePass ? max((a.slots + group - 1u) / group, (uint32_t)G) : (uint32_t)G;
+    auto mine_of = [&](uint32_t count) { return (count + kDistillThreads - 1u - tid) / kDistillThreads; };      // (this thread's of so many vectors)
+    // chunk n of a row to the chunk's place `to` in the shared memory
+    auto fetch = [&](const uint4* at, uint32_t mine, uint32_t n, uint32_t to) {
+        const uint32_t from = n * group, end = min(min(from + group, kOnePass ? a.slots : a.kept), mine);
+        at += tid;
+        uint4* place = ring + to * group * kDistillThreads;
+#pragma unroll 4
+        for (uint32_t i = from; i < end; ++i, place += kDistillThreads) copy16_async(place, at + i * kDistillThreads);
+        copies_end_group();
+    };
+    uint32_t turn = 0u;                                    // one pass: the place of the chunk at hand
+    auto fetch_ahead = [&](const DistillRow& r, uint32_t mine, uint32_t next_mine, uint32_t n) {
+        if (n + G < chunks) fetch(r.at, mine, n + G, turn); else fetch(r.next_at, next_mine, n + G - chunks, turn);
+        turn = (turn + 1u) % G;
+    };
+    {
+        const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)first * a.z_stride;
+        const DistillSlice q = distill_slice(z, a.cols, a.per, rank);
+#pragma unroll 1
+        for (uint32_t n = 0; n < (uint32_t)G; ++n) fetch(reinterpret_cast<const uint4*>(z + q.head) + q.first, mine_of(q.count), n, n);
+    }
+    if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
+    for (uint32_t b = 0u;; b ^= 1u) {
+        __syncthreads();
+        const DistillRow& r = s.row[b];
+        if (r.flags & kRowNone) break;
+        const uint64_t row = r.row;
+        const TZ* z = static_cast<const TZ*>(a.z) + row * a.z_stride;
+        const uint32_t mine = mine_of(r.count), next_mine = mine_of(r.next_count);
+        const bool counts = r.flags & kRowCounts, tailed = r.tail != 0.f;
 
         // ---- the sum of exponentials, of all classes or (with a tail) of those that are no key ----
         ExpSum e;
-        if (MODE == kGradOnly) { e.m = a.stats_in[2 * row]; e.s = a.stats_in[2 * row + 1]; }
-        else e = block_join<kDistillWarps>(scan_row(z, a.cols, tailed ? map : nullptr, a.c, a.slack), s.join, a.c);
-        __syncthreads();
-        // A key that appears several times counts once for the student, and all its pairs' probability goes to its first pair.
-        float ksum = 0.f, top = e.m, total = e.s, lead[(kDistillMaxPairs + kDistillThreads - 1) / kDistillThreads];
-        if (tailed) top = fmaxf(e.m, zm);
-#pragma unroll
-        for (int n = 0; n < (int)(sizeof(lead) / sizeof(float)); ++n) {
-            const uint32_t i = tid + n * kDistillThreads;
-            lead[n] = -1.f;                                // no gradient of its own
-            if (i >= k || s.key[i] < 0) continue;
-            float p = s.p[i];
-            bool first = true;
-            if (again) {
-                p = 0.f;
-                for (uint32_t j = 0; j < k; ++j) if (s.key[j] == s.key[i]) { p += s.p[j]; first &= j >= i; }
-            }
-            if (first) { lead[n] = p; if (tailed) ksum += exp2_fast((s.z[i] - top) * a.c); }
-        }
-        const float rest = e.s * exp2_fast((e.m - top) * a.c);
-        if (tailed) total = block_sum<kDistillWarps>(ksum, s.one) + rest;
-        const bool none = total == 0.f;                    // every logit of the row is -inf: it counts for nothing, too
+        const uint8_t* skip = tailed ? maps + b * map_bytes : nullptr;
         if (MODE != kGradOnly) {
-            double sum = 0.0;
-            const float log_total = logf(total);
-            for (uint32_t i = tid; i < k; i += kDistillThreads)
-                if (s.key[i] >= 0 && s.p[i] != 0.f) sum += (double)(s.p[i] * (s.lp[i] - (s.z[i] - top) * a.inv_t + log_total));
-            sum = block_sum<kDistillWarps>(sum, s.two);
-            if (tid == 0) {
-                if (tailed) sum += (double)(tail * (logf(tail) - (e.m - top) * a.inv_t - logf(e.s) + log_total));
-                if (a.loss) a.loss[row] = none ? 0.f : w * a.temperature * a.temperature * (float)sum;
-                if (a.stats_out) { a.stats_out[2 * row] = e.m; a.stats_out[2 * row + 1] = e.s; }
-            }
-        }
-        // ---- the gradient ----------------------------------------------------------------------
-        if (MODE != kLossOnly) {
-            const float scale = none ? 0.f : w * a.temperature * (a.grad_loss ? a.grad_loss[row] : 1.f);
-            if (none) zero_row(g, a.cols);
-            else write_row(z, g, a.cols, e.s == 0.f ? 0.f : scale * (tailed ? rest / total - tail : 1.f) / e.s, e.m, a.c);
-            __syncthreads();
+            FusedExpSums es;
+#pragma unroll 1
+            for (uint32_t n = 0; n < chunks + (kOnePass ? 0u : 1u); ++n) {
+                if (kOnePass) wait_copies<G - 1>();
+                else if (n == 0u) wait_copies<3>();
+                else if (n == 1u) wait_copies<2>();
+                else if (n == 2u) wait_copies<1>();
+                else wait_copies<0>();
+                // (two passes, the last round: what does not fit into the shared memory)
+                const bool rest = !kOnePass && n == chunks;
+                const uint32_t from = rest ? a.kept : n * group, to = counts ? rest ? mine : min(min(from + group, kOnePass ? a.slots : a.kept), mine) : 0u;
+                const uint4* place = ring + (kOnePass ? turn : n) * group * kDistillThreads;
+#pragma unroll 2
+                for (uint32_t i = from; i < to; ++i, place += kDistillThreads) {
+                    const uint4 raw = rest ? load16(r.at + i * kDistillThreads + tid) : *place;
+                    float x[N];
+                    Vec<TZ>::unpack(raw, x);
+                    float top = Vec<TZ>::max(raw);
+                    const uint32_t keys = skip ? skip[i * kDistillThreads + tid] : 0u;
+                    if (keys) {
+                        top = kLowest;
 #pragma unroll
-            for (int n = 0; n < (int)(sizeof(lead) / sizeof(float)); ++n) {
-                const uint32_t i = tid + n * kDistillThreads;
-                if (i < k && s.key[i] >= 0 && !none && !(lead[n] < 0.f)) g[s.key[i]] = from_float<TG>(scale * (exp2_fast((s.z[i] - top) * a.c) / total - lead[n]));
+                        for (int j = 0; j < N; ++j) { if (keys >> j & 1u) x[j] = -INFINITY; top = fmaxf(top, x[j]); }
+                    }
+                    es.raise(top, a.c, a.slack);
+                    es.add(x, a.c);
+                }
+                if (kOnePass) fetch_ahead(r, mine, next_mine, n);
+            }
+            if (counts) {
+                e = es.whole(a.c);
+                if (rank == 0u && tid < r.head && !(skip && skip[a.per] >> tid & 1u)) e.add(to_float(z[tid]), a.c, a.slack);
+                if (rank == blocks - 1u && tid < r.tail_count && !(skip && skip[a.per + 1u] >> tid & 1u)) e.add(to_float(z[a.cols - r.tail_count + tid]), a.c, a.slack);
+            }
+#pragma unroll 1
+            for (bool far = false;; far = true) {
+                e = warp_join(e, a.c);
+                if (lane == 0) s.join[warp] = make_float2(e.m, e.s);
+                sync_readers();
+                const float2 p = s.join[lane % kDistillWarps];
+                e.m = warp_max(p.x);
+                e.s = p.y * exp2_fast((p.x - e.m) * a.c);
+#pragma unroll
+                for (int o = kDistillWarps / 2; o; o >>= 1) e.s += __shfl_xor_sync(kFullMask, e.s, o);
+                if (far || !counts || !(e.s == 0.f || is_far(e.m, a.c))) break;
+                sync_readers();
+                e = scan_far(z, skip, a.cols, a.per, rank, blocks, a.c, a.slack);
             }
         }
-        if (mapped) for (uint32_t i = tid; i < k; i += kDistillThreads) if (s.key[i] >= 0) map[s.key[i] >> 5] = 0u;
+        DistillSums sums{e.m, e.s, r.ksum};
+        if (blocks > 1u) {
+            if (tid < blocks) cluster.map_shared_rank(&s, tid)->peer[b][rank] = make_float4(e.m, e.s, r.ksum, 0.f);
+            cluster_arrive();
+            cluster_wait();
+            // (eight places, of which the cluster has one, two, four or all)
+            const float4 p = s.peer[b][lane % blocks];
+            sums.m = warp_max(p.x);
+            sums.s = p.y * exp2_fast((p.x - sums.m) * a.c);
+            sums.ksum = p.z;
+            for (uint32_t o = blocks / 2u; o; o >>= 1) {
+                sums.s += __shfl_xor_sync(kFullMask, sums.s, o);
+                sums.ksum += __shfl_xor_sync(kFullMask, sums.ksum, o);
+            }
+        }
+        if (MODE == kGradOnly) { sums.m = r.m; sums.s = r.s; }
+        if (tid == 0) s.sums[b] = sums;
+
+        // ---- the gradient of the classes that are no key (the pairs' warp overwrites the keys') -----------
+        if (MODE != kLossOnly) {
+            const DistillTotals t = totals_of(r, sums, a.c);
+            TG* g = static_cast<TG*>(a.grad) + row * a.grad_stride;
+            const float ref = sums.m * a.c;
+            float by = t.none || sums.s == 0.f ? 0.f : r.scale * (tailed ? t.rest / t.total - r.tail : 1.f) / sums.s;
+            const bool near = by != 0.f && !is_far(sums.m, a.c);
+            if (!near) write_far(z, g, a.cols, a.per, rank, blocks, by, sums.m, a.c);
+            by *= exp2_fast(-__fmaf_rn(sums.m, a.c, -ref));
+            const unsigned long long cc = pair_of(a.c, a.c), bb = pair_of(by, by), minus_r = pair_of(-ref, -ref);
+            const bool wide = (reinterpret_cast<uintptr_t>(g + r.head) & 15u) == 0u;
+            TG* out = g + (reinterpret_cast<const TZ*>(r.at + tid) - z);
+            if (near) {
+                auto put_one = [&](uint32_t j) { g[j] = from_float<TG>(exp2_fast(__fmaf_rn(to_float(z[j]), a.c, -ref)) * by); };
+                if (rank == 0u && tid < r.head) put_one(tid);
+                if (rank == blocks - 1u && tid < r.tail_count) put_one(a.cols - r.tail_count + tid);
+            }
+#pragma unroll 1
+            for (uint32_t n = 0; n < chunks + (kOnePass ? 0u : 1u); ++n) {
+                if (kOnePass) wait_copies<G - 1>();
+                const bool rest = !kOnePass && n == chunks;
+                const uint32_t from = rest ? a.kept : n * group, to = near ? rest ? mine : min(min(from + group, kOnePass ? a.slots : a.kept), mine) : 0u;
+                const uint4* place = ring + (kOnePass ? turn : n) * group * kDistillThreads;
+#pragma unroll 2
+                for (uint32_t i = from; i < to; ++i, place += kDistillThreads) {
+                    float x[N];
+                    Vec<TZ>::unpack(rest ? load16(r.at + i * kDistillThreads + tid) : *place, x);
+#pragma unroll
+                    for (int j = 0; j < N; j += 2) {
+                        float2 y = halves(fma_pairs(pair_of(x[j], x[j + 1]), cc, minus_r));
+                        y = halves(mul_pairs(pair_of(exp2_fast(y.x), exp2_fast(y.y)), bb));
+                        x[j] = y.x; x[j + 1] = y.y;
+                    }
+                    store_values(out + (uint64_t)(i * kDistillThreads) * N, x, wide);
+                }
+                if (kOnePass) fetch_ahead(r, mine, next_mine, n);
+                else if (!rest) fetch(r.next_at, next_mine, n, n);
+            }
+        }
     }
+    if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
 }
 
 }  // namespace fsg

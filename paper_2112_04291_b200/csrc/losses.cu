@@ -127,13 +127,28 @@ int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teache
     const uint32_t gt = grad ? grad->type : student->type;
     const void* fn = mode == kLossOnly ? distill_kernel<kLossOnly>(student->type, gt)
                    : mode == kLossAndGrad ? distill_kernel<kLossAndGrad>(student->type, gt) : distill_kernel<kGradOnly>(student->type, gt);
-    const size_t smem = (4u * ((a.cols + 31u) / 32u + 1u) + 4095u) & ~(size_t)4095u;      // (whole pages: few different sizes)
-    uint64_t grid = 0;
-    rc = resident_blocks(fn, kDistillThreads, smem, dev, &grid);
+    // Both passes: a row in the shared memory of as many blocks as hold it at 64 KB each (three blocks on an SM), of eight at most (above
+    // half a megabyte: two blocks on an SM, and what does not fit is read twice).  One pass: a block, with 32 KB of copies ahead, as long as
+    // three find room with their maps of keys.  Few rows: more blocks each, as long as a block has a vector for every thread.
+    const uint32_t vecs = a.cols * size_of(student->type) / 16u;
+    const bool one_pass = mode != kLossAndGrad;
+    auto share = [&](unsigned blocks) { return (vecs + blocks - 1u) / blocks; };
+    unsigned blocks = 1u;
+    while (blocks < kDistillMaxBlocks && ((one_pass ? distill_smem(8u, a.k, share(blocks)) > 74u * 1024u : share(blocks) > 4096u) || (a.rows * blocks * 2u <= 2u * (uint64_t)dev.sm_count && share(blocks) > kDistillThreads))) blocks *= 2u;
+    a.per = share(blocks);
+    a.slots = (a.per + kDistillThreads - 1u) / kDistillThreads;
+    if (!a.slots) a.slots = 1u;
+    a.kept = one_pass && a.slots > 8u ? 8u : a.slots;
+    while (a.kept > 4u && distill_smem(a.kept, a.k, a.per) > (a.slots <= 16u ? 100u : 108u) * 1024u) --a.kept;
+    const size_t smem = (distill_smem(a.kept, a.k, a.per) + 1023u) & ~(size_t)1023u;      // (few different sizes)
+    uint64_t resident = 0;                                 // (asked for so that the kernel may use as much shared memory)
+    rc = resident_blocks(fn, kDistillBlock, smem, dev, &resident);
     if (rc) return rc;
-    if (grid > a.rows) grid = a.rows;
+    a.claims = a.rows * blocks > resident / 2u;
+    // a cluster per row: one that has finished its row takes over the next that has not begun
+    if (a.rows * blocks >= 1ull << 31) return FASTSGD_E_BAD_N;
     void* kargs[] = {&a};
-    return launched(launch_overlapped(fn, (unsigned)grid, kDistillThreads, smem, kargs, static_cast<cudaStream_t>(stream)));
+    return launched(launch_overlapped(fn, (unsigned)(a.rows * blocks), kDistillBlock, smem, kargs, static_cast<cudaStream_t>(stream), blocks));
 }
 
 // tokens a block of the router's kernels takes, and the blocks

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "async.cuh"
 #include "sum.cuh"
 #include "bits.cuh"
 
@@ -12,36 +13,6 @@ constexpr int      kBlockThreads = 512;                       // the block size 
 constexpr int      kBlockWarps   = kBlockThreads / 32;
 constexpr uint32_t kWaitLimit    = 1u << 22;                  // polls before a wait on another block gives up
 
-// ---- mbarrier / bulk-copy primitives (sm_90+ PTX) -------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// Bounded wait: the hardware suspends the thread for up to about the hinted time per try, so a
-// wait costs a handful of instructions; false when every try ran out.
-constexpr uint32_t kTryHintNs = 10000u;
-constexpr uint32_t kTryLimit  = 1u << 18;
-__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity, uint32_t tries = kTryLimit) {
-    const uint32_t addr = smem_u32(bar);
-    for (uint32_t t = 0; t < tries; ++t) {
-        uint32_t ok;
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(ok) : "r"(addr), "r"(parity), "r"(kTryHintNs) : "memory");
-        if (ok) return true;
-    }
-    return false;
-}
-__device__ __forceinline__ void bulk_load(void* dst_smem, const void* src_global, uint32_t bytes, unsigned long long* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst_smem)), "l"(__cvta_generic_to_global(src_global)), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
 // Words that carry their whole payload: relaxed accesses are enough.
 __device__ __forceinline__ unsigned long long ld_relaxed_u64(const unsigned long long* p) {
     unsigned long long v;

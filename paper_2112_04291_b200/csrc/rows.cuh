@@ -263,13 +263,49 @@ struct ExpSums {
         return e;
     }
 };
+// |m| c of 2^26 and more: m c rounded to fp32 would be off by 2 and more.
+__device__ __forceinline__ bool is_far(float m, float c) { return !(fabsf(m) * c < 67108864.f); }
+
+// The same with one fused operation for the argument: 2^(x c - r), r = m c rounded, which whole() makes up for.  Where m is far the
+// sum is 0 instead: next to a largest value that is not far, what it would hold is 0 indeed; where the row's largest value is far, or
+// its sum 0, the caller takes the sum the other way.
+struct FusedExpSums {
+    float m, r;
+    unsigned long long s[2];
+    __device__ __forceinline__ FusedExpSums() : m(kLowest), r(kLowest), s{0ull, 0ull} {}
+    __device__ __forceinline__ void raise(float top, float c, float slack) {
+        if (top > m + slack) {
+            const float now = top * c, f = exp2_fast(r - now);
+            const bool far = is_far(m, c);                 // (the sum may be anything)
+            s[0] = far ? 0ull : mul_pairs(s[0], pair_of(f, f)); s[1] = far ? 0ull : mul_pairs(s[1], pair_of(f, f));
+            m = top; r = now;
+        }
+    }
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float c) {
+        const unsigned long long minus_r = pair_of(-r, -r), cc = pair_of(c, c);
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = halves(fma_pairs(pair_of(x[i], x[i + 1]), cc, minus_r));
+            s[i / 2 & 1] = add_pairs(s[i / 2 & 1], pair_of(exp2_fast(y.x), exp2_fast(y.y)));
+        }
+    }
+    __device__ __forceinline__ ExpSum whole(float c) const {
+        const float2 p = halves(add_pairs(s[0], s[1]));
+        ExpSum e;
+        e.m = m;
+        e.s = is_far(m, c) ? 0.f : (p.x + p.y) * exp2_fast(-__fmaf_rn(m, c, -r));
+        return e;
+    }
+};
+
 // 40 powers of two, in logits (bounded: m + slack has to stay below any value when m is the lowest)
 __host__ __device__ __forceinline__ float exp_slack(float c) { return fminf(40.f / c, 1e30f); }
 
+// (as integers that ascend with the values; NaN must not be among them)
 __device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFullMask, v, o));
-    return v;
+    int b = __float_as_int(v);
+    b = __reduce_max_sync(kFullMask, b ^ (b >> 31 & 0x7FFFFFFF));
+    return __int_as_float(b ^ (b >> 31 & 0x7FFFFFFF));
 }
 template <class F> __device__ __forceinline__ F warp_sum(F v) {
 #pragma unroll
@@ -277,11 +313,9 @@ template <class F> __device__ __forceinline__ F warp_sum(F v) {
     return v;
 }
 __device__ __forceinline__ ExpSum warp_join(ExpSum e, float c) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float m2 = __shfl_xor_sync(kFullMask, e.m, o), s2 = __shfl_xor_sync(kFullMask, e.s, o);
-        e.join(m2, s2, c);
-    }
+    const float top = warp_max(e.m);
+    e.s = warp_sum(e.s * exp2_fast((e.m - top) * c));
+    e.m = top;
     return e;
 }
 
