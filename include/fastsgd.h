@@ -337,7 +337,8 @@ typedef struct fastsgd_pairs {
  * At least one of loss, stats and grad is wanted.
  * A row of weight 0, without a pair that is there, whose pairs all have value -inf, or whose logits are all -inf counts for
  * nothing: loss 0, gradient 0.  Where the student rules out (-inf) what the teacher gives probability to, the loss is +inf.
- * Pairs may come in any order, and keys may repeat.  One launch; the sums' order depends on the sizes and alignment alone.
+ * Pairs may come in any order, and keys may repeat.  One launch; the sums' order depends on the sizes, the alignment and on
+ * whether there is a gradient to write, and on nothing else.
  */
 int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,
                          float* loss, float* stats, const fastsgd_matrix* grad, void* stream);

@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     // One pass (the loss or the gradient alone): a row in chunks of `group` vectors a thread, four chunks ahead, whatever the row's length.  Two
     // passes: four chunks that stay, and the rest of the row without.
     constexpr bool kOnePass = MODE != kLossAndGrad;
+    constexpr uint32_t U = kOnePass ? 2u : 4u;
     const uint32_t group = (a.kept + G - 1u) / G, chunks = kOnePass ? max((a.slots + group - 1u) / group, (uint32_t)G) : (uint32_t)G;
     auto mine_of = [&](uint32_t count) { return (count + kDistillThreads - 1u - tid) / kDistillThreads; };      // (this thread's of so many vectors)
     // chunk n of a row to the chunk's place `to` in the shared memory
@@ -373,6 +374,15 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         const uint8_t* skip = tailed ? maps + b * map_bytes : nullptr;
         if (MODE != kGradOnly) {
             FusedExpSums es;
+            // a vector without the elements that are keys
+            auto without = [](uint4 raw, uint32_t keys) {
+                if (keys) {
+                    TZ* x = reinterpret_cast<TZ*>(&raw);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) if (keys >> j & 1u) x[j] = from_float<TZ>(-INFINITY);
+                }
+                return raw;
+            };
 #pragma unroll 1
             for (uint32_t n = 0; n < chunks + (kOnePass ? 0u : 1u); ++n) {
                 if (kOnePass) wait_copies<G - 1>();
@@ -384,19 +394,44 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 const bool rest = !kOnePass && n == chunks;
                 const uint32_t from = rest ? a.kept : n * group, to = counts ? rest ? mine : min(min(from + group, kOnePass ? a.slots : a.kept), mine) : 0u;
                 const uint4* place = ring + (kOnePass ? turn : n) * group * kDistillThreads;
-#pragma unroll 2
-                for (uint32_t i = from; i < to; ++i, place += kDistillThreads) {
-                    const uint4 raw = rest ? load16(r.at + i * kDistillThreads + tid) : *place;
+                uint32_t i = from;
+                // U vectors at a time: one look at their keys, one at their largest
+                if (!rest) {
+#pragma unroll 1
+                    for (; i + U <= to; i += U, place += U * kDistillThreads) {
+                        uint4 raw[U];
+                        float top[U];
+#pragma unroll
+                        for (int u = 0; u < (int)U; ++u) raw[u] = place[u * kDistillThreads];
+#pragma unroll
+                        for (int u = 0; u < (int)U; ++u) top[u] = Vec<TZ>::max(raw[u]);
+                        if (skip) {
+                            uint32_t keys = 0u;
+#pragma unroll
+                            for (int u = 0; u < (int)U; ++u) keys |= (uint32_t)skip[(i + u) * kDistillThreads + tid] << (8 * u);
+                            if (keys) {
+#pragma unroll
+                                for (int u = 0; u < (int)U; ++u) { raw[u] = without(raw[u], keys >> (8 * u) & 255u); top[u] = Vec<TZ>::max(raw[u]); }
+                            }
+                        }
+                        float most = top[0];
+#pragma unroll
+                        for (int u = 1; u < (int)U; ++u) most = fmaxf(most, top[u]);
+                        es.raise(most, a.c, a.slack);
+#pragma unroll
+                        for (int u = 0; u < (int)U; ++u) {
+                            float x[N];
+                            Vec<TZ>::unpack(raw[u], x);
+                            es.add(x, a.c);
+                        }
+                    }
+                }
+#pragma unroll 1
+                for (; i < to; ++i, place += kDistillThreads) {
+                    const uint4 raw = without(rest ? load16(r.at + i * kDistillThreads + tid) : *place, skip ? skip[i * kDistillThreads + tid] : 0u);
                     float x[N];
                     Vec<TZ>::unpack(raw, x);
-                    float top = Vec<TZ>::max(raw);
-                    const uint32_t keys = skip ? skip[i * kDistillThreads + tid] : 0u;
-                    if (keys) {
-                        top = kLowest;
-#pragma unroll
-                        for (int j = 0; j < N; ++j) { if (keys >> j & 1u) x[j] = -INFINITY; top = fmaxf(top, x[j]); }
-                    }
-                    es.raise(top, a.c, a.slack);
+                    es.raise(Vec<TZ>::max(raw), a.c, a.slack);
                     es.add(x, a.c);
                 }
                 if (kOnePass) fetch_ahead(r, mine, next_mine, n);
@@ -451,6 +486,17 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             const unsigned long long cc = pair_of(a.c, a.c), bb = pair_of(by, by), minus_r = pair_of(-ref, -ref);
             const bool wide = (reinterpret_cast<uintptr_t>(g + r.head) & 15u) == 0u;
             TG* out = g + (reinterpret_cast<const TZ*>(r.at + tid) - z);
+            auto put = [&](const uint4& raw, uint32_t i) {
+                float x[N];
+                Vec<TZ>::unpack(raw, x);
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    float2 y = halves(fma_pairs(pair_of(x[j], x[j + 1]), cc, minus_r));
+                    y = halves(mul_pairs(pair_of(exp2_fast(y.x), exp2_fast(y.y)), bb));
+                    x[j] = y.x; x[j + 1] = y.y;
+                }
+                store_values(out + (uint64_t)(i * kDistillThreads) * N, x, wide);
+            };
             if (near) {
                 auto put_one = [&](uint32_t j) { g[j] = from_float<TG>(exp2_fast(__fmaf_rn(to_float(z[j]), a.c, -ref)) * by); };
                 if (rank == 0u && tid < r.head) put_one(tid);
@@ -462,18 +508,19 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 const bool rest = !kOnePass && n == chunks;
                 const uint32_t from = rest ? a.kept : n * group, to = near ? rest ? mine : min(min(from + group, kOnePass ? a.slots : a.kept), mine) : 0u;
                 const uint4* place = ring + (kOnePass ? turn : n) * group * kDistillThreads;
-#pragma unroll 2
-                for (uint32_t i = from; i < to; ++i, place += kDistillThreads) {
-                    float x[N];
-                    Vec<TZ>::unpack(rest ? load16(r.at + i * kDistillThreads + tid) : *place, x);
+                uint32_t i = from;
+                if (!rest) {
+#pragma unroll 1
+                    for (; i + U <= to; i += U, place += U * kDistillThreads) {
+                        uint4 raw[U];
 #pragma unroll
-                    for (int j = 0; j < N; j += 2) {
-                        float2 y = halves(fma_pairs(pair_of(x[j], x[j + 1]), cc, minus_r));
-                        y = halves(mul_pairs(pair_of(exp2_fast(y.x), exp2_fast(y.y)), bb));
-                        x[j] = y.x; x[j + 1] = y.y;
+                        for (int u = 0; u < (int)U; ++u) raw[u] = place[u * kDistillThreads];
+#pragma unroll
+                        for (int u = 0; u < (int)U; ++u) put(raw[u], i + u);
                     }
-                    store_values(out + (uint64_t)(i * kDistillThreads) * N, x, wide);
                 }
+#pragma unroll 1
+                for (; i < to; ++i, place += kDistillThreads) put(rest ? load16(r.at + i * kDistillThreads + tid) : *place, i);
                 if (kOnePass) fetch_ahead(r, mine, next_mine, n);
                 else if (!rest) fetch(r.next_at, next_mine, n, n);
             }

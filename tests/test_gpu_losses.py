@@ -204,12 +204,12 @@ def _check_distill(z, dtype, keys, values, temperature=1.0, tail=None, weight=No
     up = np.random.default_rng(rows).normal(0, 1, rows).astype(np.float32)
     for kind in grad_types or dict.fromkeys([dtype, "fp32"]):
         loss2, grad, stats2 = _run_distill(view, k_, v_, temperature, t_, w_, kind)
-        assert _same(loss, loss2) and _same(stats, stats2)
+        check_loss(loss2)                                  # (the sums have another order than without a gradient)
         check_grad(grad, kind)
         back = torch.full_like(grad, MARK)
         assert binding.distill_loss_backward(view, k_, v_, stats, back, temperature=temperature, tail=t_, weight=w_) == 0
         check_grad(back, kind)
-        assert binding.distill_loss_backward(view, k_, v_, stats, back, grad_loss=_dev(up), temperature=temperature, tail=t_, weight=w_) == 0
+        assert binding.distill_loss_backward(view, k_, v_, stats2, back, grad_loss=_dev(up), temperature=temperature, tail=t_, weight=w_) == 0
         check_grad(back, kind, up.astype(np.float64))
         if kind == dtype:
             if view.is_contiguous() and view.data_ptr() % 16 == 0:      # (elsewhere the sums have another order than in the copy)
