@@ -31,6 +31,10 @@ __device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t pari
     }
     return false;
 }
+// One more arrival on a barrier of another block of the cluster; what this thread has written before is visible to whoever waits there.
+__device__ __forceinline__ void mbar_arrive_at(unsigned long long* bar, uint32_t block) {
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
+}
 // The same for a barrier that another block of the cluster arrives on, whose writes before are then visible.
 __device__ __forceinline__ bool mbar_wait_cluster(unsigned long long* bar, uint32_t parity, uint32_t tries = kTryLimit) {
     const uint32_t addr = smem_u32(bar);

@@ -54,8 +54,9 @@ struct DistillSums { float m, s, ksum; };
 struct DistillShared {
     DistillRow  row[2];                                    // for even and odd rows, as everything below that two rows are at work on
     DistillSums sums[2];
-    float2 join[kDistillWarps];
+    float2 join[2][kDistillWarps];
     float4 peer[2][kDistillMaxBlocks];                     // m, sum and keys' sum of every block of the cluster
+    unsigned long long ready[2], done[2], met[2];          // the row's pairs are known; its gradient is written; every block's sums are there
     Claim  claim;                                          // of the first block: the cluster's next row
     int    next[2];                                        // the others': what the first has been given
     unsigned long long next_bar;
@@ -280,21 +281,19 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     if (warp == (uint32_t)kDistillWarps) {
         for (uint32_t i = lane; i < map_bytes / 2u; i += 32u) reinterpret_cast<uint32_t*>(maps)[i] = 0u;
         if (lane == 0) {
+            for (int b = 0; b < 2; ++b) { mbar_init(&s.ready[b], 1u); mbar_init(&s.done[b], kDistillWarps); mbar_init(&s.met[b], blocks); }
             claim_init(s.claim);
             mbar_init(&s.next_bar, 1u);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-        __syncwarp();
+        __syncthreads();
         if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (every block of the cluster has begun)
         if (a.claims && rank == 0u && lane == 0) claim_ask(s.claim);
-        int row = (int)first, before = -1, last = -1;      // of this turn, the one before and the one before that
-        // turn i, before the others begin with the i-th row: the row before the last one is finished, the i-th is prepared
+        // turn i: the i-th row's pairs; then, once its gradient is written, the row before is finished
+        int row = (int)first, last = -1;
         for (uint32_t i = 0;; ++i) {
-            const uint32_t b = i & 1u;
+            const uint32_t b = i & 1u, o = b ^ 1u;
             int next = -1;
-            __syncwarp();
-            if (last >= 0) finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[b], s.sums[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
-            __syncwarp();
             if (row >= 0) {
                 prepare_pairs<TZ, MODE>(a, (uint64_t)row, rank, blocks, s.row[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
                 // the cluster's next row: the first block has asked for it a turn ago, and tells the others
@@ -302,11 +301,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                     if (rank == 0u) {
                         next = claim_answer(s.claim, i);
                         if (next >= 0) { next /= (int)blocks; claim_ask(s.claim); }
-                        for (uint32_t o = 1u; o < blocks; ++o) {
-                            *cluster.map_shared_rank(&s.next[b], o) = next;
-                            const uint32_t bar = smem_u32(&s.next_bar);
-                            asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(bar), "r"(o) : "memory");
-                        }
+                        for (uint32_t to = 1u; to < blocks; ++to) { *cluster.map_shared_rank(&s.next[b], to) = next; mbar_arrive_at(&s.next_bar, to); }
                     } else if (mbar_wait_cluster(&s.next_bar, b)) next = s.next[b];
                 }
                 next = __shfl_sync(kFullMask, next, 0);
@@ -316,17 +311,15 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                     s.row[b].next_at = reinterpret_cast<const uint4*>(z + n.head) + n.first; s.row[b].next_count = n.count;
                 }
             } else if (lane == 0) s.row[b].flags = kRowNone;
-            if (blocks > 1u && i) cluster_wait();
-            __syncthreads();
-            last = before; before = row;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.ready[b]);
+            if (last >= 0) {
+                mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u);
+                finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[o], s.sums[o], s_key + o * k, s_t + o * k, s_z + o * k, maps + o * map_bytes);
+                __syncwarp();
+            }
             if (row < 0) break;
-            if (blocks > 1u) cluster_arrive();
-            row = next;
-        }
-        // (before is -1 now: the last row is the one before it)
-        {
-            const uint32_t b = s.row[0].flags & kRowNone ? 1u : 0u;
-            finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[b], s.sums[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
+            last = row; row = next;
         }
         if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (no block leaves while another may write to its shared memory)
         return;
@@ -359,9 +352,11 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
 #pragma unroll 1
         for (uint32_t n = 0; n < (uint32_t)G; ++n) fetch(reinterpret_cast<const uint4*>(z + q.head) + q.first, mine_of(q.count), n, n);
     }
+    __syncthreads();
     if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
-    for (uint32_t b = 0u;; b ^= 1u) {
-        __syncthreads();
+    for (uint32_t i = 0u;; ++i) {
+        const uint32_t b = i & 1u, parity = i >> 1 & 1u;
+        mbar_wait(&s.ready[b], parity);
         const DistillRow& r = s.row[b];
         if (r.flags & kRowNone) break;
         const uint64_t row = r.row;
@@ -444,9 +439,9 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
 #pragma unroll 1
             for (bool far = false;; far = true) {
                 e = warp_join(e, a.c);
-                if (lane == 0) s.join[warp] = make_float2(e.m, e.s);
+                if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);
                 sync_readers();
-                const float2 p = s.join[lane % kDistillWarps];
+                const float2 p = s.join[b][lane % kDistillWarps];
                 e.m = warp_max(p.x);
                 e.s = p.y * exp2_fast((p.x - e.m) * a.c);
 #pragma unroll
@@ -458,9 +453,12 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         }
         DistillSums sums{e.m, e.s, r.ksum};
         if (blocks > 1u) {
-            if (tid < blocks) cluster.map_shared_rank(&s, tid)->peer[b][rank] = make_float4(e.m, e.s, r.ksum, 0.f);
-            cluster_arrive();
-            cluster_wait();
+            if (MODE == kGradOnly) sync_readers();         // (all have met for the row before: the barrier is free)
+            if (tid < blocks) {
+                cluster.map_shared_rank(&s, tid)->peer[b][rank] = make_float4(e.m, e.s, r.ksum, 0.f);
+                mbar_arrive_at(&s.met[b], tid);
+            }
+            mbar_wait_cluster(&s.met[b], parity);
             // (eight places, of which the cluster has one, two, four or all)
             const float4 p = s.peer[b][lane % blocks];
             sums.m = warp_max(p.x);
@@ -525,6 +523,8 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 else if (!rest) fetch(r.next_at, next_mine, n, n);
             }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.done[b]);
     }
     if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
 }

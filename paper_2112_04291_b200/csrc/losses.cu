@@ -139,7 +139,7 @@ int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teache
     a.slots = (a.per + kDistillThreads - 1u) / kDistillThreads;
     if (!a.slots) a.slots = 1u;
     a.kept = one_pass && a.slots > 8u ? 8u : a.slots;
-    while (a.kept > 4u && distill_smem(a.kept, a.k, a.per) > (a.slots <= 16u ? 100u : 108u) * 1024u) --a.kept;
+    while (!one_pass && a.kept > 4u && distill_smem(a.kept, a.k, a.per) > (a.slots <= 16u ? 100u : 108u) * 1024u) --a.kept;
     const size_t smem = (distill_smem(a.kept, a.k, a.per) + 1023u) & ~(size_t)1023u;      // (few different sizes)
     uint64_t resident = 0;                                 // (asked for so that the kernel may use as much shared memory)
     rc = resident_blocks(fn, kDistillBlock, smem, dev, &resident);
