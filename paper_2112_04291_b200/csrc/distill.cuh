@@ -88,21 +88,32 @@ template <class T> __device__ __forceinline__ DistillSlice distill_slice(const T
 }
 
 // The sum of exponentials of a block's share, without the keys of `map` where there is one: from global memory and with any
-// logits.
+// logits; thread tid's part of `threads`.
 template <class T>
-__device__ __noinline__ ExpSum scan_far(const T* z, const uint8_t* map, uint32_t cols, uint32_t per, uint32_t rank, uint32_t blocks, float c, float slack) {
+__device__ __noinline__ ExpSum scan_far(const T* z, const uint8_t* map, uint32_t cols, uint32_t per, uint32_t rank, uint32_t blocks, float c, float slack, uint32_t tid, uint32_t threads) {
     constexpr int N = Vec<T>::N;
     const DistillSlice q = distill_slice(z, cols, per, rank);
     ExpSum e;
-    for (uint32_t i = threadIdx.x; i < q.count; i += kDistillThreads) {
+    for (uint32_t i = tid; i < q.count; i += threads) {
         float x[N];
         Vec<T>::unpack(load16(z + q.head + (uint64_t)(q.first + i) * N), x);
         const uint32_t keys = map ? map[i] : 0u;
 #pragma unroll
         for (int j = 0; j < N; ++j) if (!(keys >> j & 1u)) e.add(x[j], c, slack);
     }
-    if (rank == 0u && threadIdx.x < q.head && !(map && map[per] >> threadIdx.x & 1u)) e.add(to_float(z[threadIdx.x]), c, slack);
-    if (rank == blocks - 1u && threadIdx.x < q.tail && !(map && map[per + 1u] >> threadIdx.x & 1u)) e.add(to_float(z[cols - q.tail + threadIdx.x]), c, slack);
+    if (rank == 0u && tid < q.head && !(map && map[per] >> tid & 1u)) e.add(to_float(z[tid]), c, slack);
+    if (rank == blocks - 1u && tid < q.tail && !(map && map[per + 1u] >> tid & 1u)) e.add(to_float(z[cols - q.tail + tid]), c, slack);
+    return e;
+}
+
+// The warps' sums in one, the same in every lane.
+__device__ __forceinline__ ExpSum join_warps(const float2* join, float c) {
+    const float2 p = join[(threadIdx.x & 31u) % kDistillWarps];
+    ExpSum e;
+    e.m = warp_max(p.x);
+    e.s = p.y * exp2_fast((p.x - e.m) * c);
+#pragma unroll
+    for (int o = kDistillWarps / 2; o; o >>= 1) e.s += __shfl_xor_sync(kFullMask, e.s, o);
     return e;
 }
 
@@ -268,7 +279,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     constexpr int N = Vec<TZ>::N;
-    constexpr int G = 4;                                   // groups of copies of a row
+    constexpr int G = MODE != kLossAndGrad ? 2 : 4;        // groups of copies of a row
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, k = a.k, blocks = cluster.num_blocks(), rank = cluster.block_rank();
     int* s_key = reinterpret_cast<int*>(distill_smem_bytes + (size_t)((a.kept + 3u) & ~3u) * kDistillThreads * 16u);      // two rows' each
     float* s_t = reinterpret_cast<float*>(s_key + 2u * k);
@@ -315,6 +326,14 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             if (lane == 0) mbar_arrive(&s.ready[b]);
             if (last >= 0) {
                 mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u);
+                if (MODE == kLossOnly && blocks == 1u) {
+                    const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)last * a.z_stride;
+                    ExpSum e = join_warps(s.join[o], a.c);
+                    if ((s.row[o].flags & kRowCounts) && (e.s == 0.f || is_far(e.m, a.c)))
+                        e = warp_join(scan_far(z, s.row[o].tail != 0.f ? maps + o * map_bytes : nullptr, a.cols, a.per, rank, blocks, a.c, a.slack, lane, 32u), a.c);
+                    if (lane == 0) s.sums[o] = DistillSums{e.m, e.s, s.row[o].ksum};
+                    __syncwarp();
+                }
                 finish_pairs<TZ, TG, MODE>(a, (uint64_t)last, rank, blocks, s.row[o], s.sums[o], s_key + o * k, s_t + o * k, s_z + o * k, maps + o * map_bytes);
                 __syncwarp();
             }
@@ -326,10 +345,10 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     }
 
     uint4* ring = reinterpret_cast<uint4*>(distill_smem_bytes) + tid;
-    // One pass (the loss or the gradient alone): a row in chunks of `group` vectors a thread, four chunks ahead, whatever the row's length.  Two
+    // One pass (the loss or the gradient alone): a row in chunks of `group` vectors a thread, two chunks ahead, whatever the row's length.  Two
     // passes: four chunks that stay, and the rest of the row without.
     constexpr bool kOnePass = MODE != kLossAndGrad;
-    constexpr uint32_t U = kOnePass ? 2u : 4u;
+    constexpr uint32_t U = 4u;                             // vectors between two looks at keys and largest
     const uint32_t group = (a.kept + G - 1u) / G, chunks = kOnePass ? max((a.slots + group - 1u) / group, (uint32_t)G) : (uint32_t)G;
     auto mine_of = [&](uint32_t count) { return (count + kDistillThreads - 1u - tid) / kDistillThreads; };      // (this thread's of so many vectors)
     // chunk n of a row to the chunk's place `to` in the shared memory
@@ -436,19 +455,21 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 if (rank == 0u && tid < r.head && !(skip && skip[a.per] >> tid & 1u)) e.add(to_float(z[tid]), a.c, a.slack);
                 if (rank == blocks - 1u && tid < r.tail_count && !(skip && skip[a.per + 1u] >> tid & 1u)) e.add(to_float(z[a.cols - r.tail_count + tid]), a.c, a.slack);
             }
-#pragma unroll 1
-            for (bool far = false;; far = true) {
-                e = warp_join(e, a.c);
+            e = warp_join(e, a.c);
+            if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);
+            if (MODE == kLossOnly && blocks == 1u) {       // (the pairs' warp joins them: nobody waits for anybody here)
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.done[b]);
+                continue;
+            }
+            sync_readers();
+            e = join_warps(s.join[b], a.c);
+            if (counts && (e.s == 0.f || is_far(e.m, a.c))) {
+                sync_readers();
+                e = warp_join(scan_far(z, skip, a.cols, a.per, rank, blocks, a.c, a.slack, tid, kDistillThreads), a.c);
                 if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);
                 sync_readers();
-                const float2 p = s.join[b][lane % kDistillWarps];
-                e.m = warp_max(p.x);
-                e.s = p.y * exp2_fast((p.x - e.m) * a.c);
-#pragma unroll
-                for (int o = kDistillWarps / 2; o; o >>= 1) e.s += __shfl_xor_sync(kFullMask, e.s, o);
-                if (far || !counts || !(e.s == 0.f || is_far(e.m, a.c))) break;
-                sync_readers();
-                e = scan_far(z, skip, a.cols, a.per, rank, blocks, a.c, a.slack);
+                e = join_warps(s.join[b], a.c);
             }
         }
         DistillSums sums{e.m, e.s, r.ksum};
