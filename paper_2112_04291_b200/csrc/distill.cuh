@@ -63,7 +63,13 @@ struct DistillShared {
 };
 // dynamic: uint4 ring[kept][threads], then for each of two rows key, t (later e), z of every pair, then for each of two rows a byte per
 // vector of the slice, one for the elements before and one for those behind the vectors: which of the elements are keys of the row
-__host__ __device__ inline uint32_t distill_map_bytes(uint32_t per) { return (per + 2u + 3u) & ~3u; }
+// (a thread's vectors i = 4 n .. 4 n + 3 in one word: vector i of thread t has byte (i / 4) 4 threads + 4 t + i % 4)
+__host__ __device__ inline uint32_t distill_map_vectors(uint32_t per) { return (per + 4u * kDistillThreads - 1u) / (4u * kDistillThreads) * (4u * kDistillThreads); }
+__host__ __device__ inline uint32_t distill_map_bytes(uint32_t per) { return distill_map_vectors(per) + 4u; }
+__device__ __forceinline__ uint32_t map_byte(uint32_t v) {
+    const uint32_t i = v / kDistillThreads, t = v % kDistillThreads;
+    return i / 4u * (4u * kDistillThreads) + 4u * t + i % 4u;
+}
 __host__ __device__ inline size_t distill_smem(uint32_t kept, uint32_t k, uint32_t per) {
     kept = (kept + 3u) & ~3u;                              // (four chunks)
     return (size_t)kept * kDistillThreads * 16u + 24u * (size_t)k + 2u * distill_map_bytes(per);
@@ -97,12 +103,12 @@ __device__ __noinline__ ExpSum scan_far(const T* z, const uint8_t* map, uint32_t
     for (uint32_t i = tid; i < q.count; i += threads) {
         float x[N];
         Vec<T>::unpack(load16(z + q.head + (uint64_t)(q.first + i) * N), x);
-        const uint32_t keys = map ? map[i] : 0u;
+        const uint32_t keys = map ? map[map_byte(i)] : 0u;
 #pragma unroll
         for (int j = 0; j < N; ++j) if (!(keys >> j & 1u)) e.add(x[j], c, slack);
     }
-    if (rank == 0u && tid < q.head && !(map && map[per] >> tid & 1u)) e.add(to_float(z[tid]), c, slack);
-    if (rank == blocks - 1u && tid < q.tail && !(map && map[per + 1u] >> tid & 1u)) e.add(to_float(z[cols - q.tail + tid]), c, slack);
+    if (rank == 0u && tid < q.head && !(map && map[distill_map_vectors(per)] >> tid & 1u)) e.add(to_float(z[tid]), c, slack);
+    if (rank == blocks - 1u && tid < q.tail && !(map && map[distill_map_vectors(per) + 1u] >> tid & 1u)) e.add(to_float(z[cols - q.tail + tid]), c, slack);
     return e;
 }
 
@@ -140,10 +146,11 @@ __device__ __noinline__ void write_far(const TZ* z, TG* g, uint32_t cols, uint32
 template <class T>
 __device__ __forceinline__ int key_bit(const DistillSlice& q, uint32_t j, uint32_t per, uint32_t rank, uint32_t blocks) {
     constexpr uint32_t N = Vec<T>::N;
-    if (j < q.head) return rank == 0u ? (int)(per * 8u + j) : -1;
+    const uint32_t edges = distill_map_vectors(per);
+    if (j < q.head) return rank == 0u ? (int)(edges * 8u + j) : -1;
     const uint32_t v = (j - q.head) / N;
-    if (v >= q.vecs) return rank == blocks - 1u ? (int)((per + 1u) * 8u + j - q.head - q.vecs * N) : -1;
-    return v - q.first < q.count ? (int)((v - q.first) * 8u + (j - q.head) % N) : -1;
+    if (v >= q.vecs) return rank == blocks - 1u ? (int)((edges + 1u) * 8u + j - q.head - q.vecs * N) : -1;
+    return v - q.first < q.count ? (int)(map_byte(v - q.first) * 8u + (j - q.head) % N) : -1;
 }
 
 // The pairs' warp: what it finds out about a row, one row ahead of the others.
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     // passes: four chunks that stay, and the rest of the row without.
     constexpr bool kOnePass = MODE != kLossAndGrad;
     constexpr uint32_t U = 4u;                             // vectors between two looks at keys and largest
-    const uint32_t group = (a.kept + G - 1u) / G, chunks = kOnePass ? max((a.slots + group - 1u) / group, (uint32_t)G) : (uint32_t)G;
+    const uint32_t group = ((a.kept + G - 1u) / G + U - 1u) / U * U, chunks = kOnePass ? max((a.slots + group - 1u) / group, (uint32_t)G) : (uint32_t)G;
     auto mine_of = [&](uint32_t count) { return (count + kDistillThreads - 1u - tid) / kDistillThreads; };      // (this thread's of so many vectors)
     // chunk n of a row to the chunk's place `to` in the shared memory
     auto fetch = [&](const uint4* at, uint32_t mine, uint32_t n, uint32_t to) {
@@ -420,9 +427,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
 #pragma unroll
                         for (int u = 0; u < (int)U; ++u) top[u] = Vec<TZ>::max(raw[u]);
                         if (skip) {
-                            uint32_t keys = 0u;
-#pragma unroll
-                            for (int u = 0; u < (int)U; ++u) keys |= (uint32_t)skip[(i + u) * kDistillThreads + tid] << (8 * u);
+                            const uint32_t keys = reinterpret_cast<const uint32_t*>(skip)[i / 4u * kDistillThreads + tid];      // (i is a multiple of four)
                             if (keys) {
 #pragma unroll
                                 for (int u = 0; u < (int)U; ++u) { raw[u] = without(raw[u], keys >> (8 * u) & 255u); top[u] = Vec<TZ>::max(raw[u]); }
@@ -442,7 +447,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 }
 #pragma unroll 1
                 for (; i < to; ++i, place += kDistillThreads) {
-                    const uint4 raw = without(rest ? load16(r.at + i * kDistillThreads + tid) : *place, skip ? skip[i * kDistillThreads + tid] : 0u);
+                    const uint4 raw = without(rest ? load16(r.at + i * kDistillThreads + tid) : *place, skip ? skip[map_byte(i * kDistillThreads + tid)] : 0u);
                     float x[N];
                     Vec<TZ>::unpack(raw, x);
                     es.raise(Vec<TZ>::max(raw), a.c, a.slack);
@@ -452,8 +457,8 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             }
             if (counts) {
                 e = es.whole(a.c);
-                if (rank == 0u && tid < r.head && !(skip && skip[a.per] >> tid & 1u)) e.add(to_float(z[tid]), a.c, a.slack);
-                if (rank == blocks - 1u && tid < r.tail_count && !(skip && skip[a.per + 1u] >> tid & 1u)) e.add(to_float(z[a.cols - r.tail_count + tid]), a.c, a.slack);
+                if (rank == 0u && tid < r.head && !(skip && skip[distill_map_vectors(a.per)] >> tid & 1u)) e.add(to_float(z[tid]), a.c, a.slack);
+                if (rank == blocks - 1u && tid < r.tail_count && !(skip && skip[distill_map_vectors(a.per) + 1u] >> tid & 1u)) e.add(to_float(z[a.cols - r.tail_count + tid]), a.c, a.slack);
             }
             e = warp_join(e, a.c);
             if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);
