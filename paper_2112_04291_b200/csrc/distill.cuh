@@ -430,7 +430,8 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                             const uint32_t keys = reinterpret_cast<const uint32_t*>(skip)[i / 4u * kDistillThreads + tid];      // (i is a multiple of four)
                             if (keys) {
 #pragma unroll
-                                for (int u = 0; u < (int)U; ++u) { raw[u] = without(raw[u], keys >> (8 * u) & 255u); top[u] = Vec<TZ>::max(raw[u]); }
+                                for (int u = 0; u < (int)U; ++u)
+                                    if (keys >> (8 * u) & 255u) { raw[u] = without(raw[u], keys >> (8 * u) & 255u); top[u] = Vec<TZ>::max(raw[u]); }
                             }
                         }
                         float most = top[0];
