@@ -199,8 +199,9 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
     unsigned blocks = 1u;
     while (blocks < 8u && a.rows * blocks * 2u <= resident && a.cols / (2u * blocks) >= 8192u) blocks *= 2u;
     a.slice = ((a.cols + blocks - 1u) / blocks + 63u) & ~63u;
-    uint64_t grid = a.rows * blocks < resident ? a.rows * blocks : resident / blocks * blocks;
-    return launched(launch_overlapped(fn, (unsigned)grid, kTopThreads, smem, kargs, st, blocks));
+    // (with clusters every row has its own; otherwise a block that has finished its row takes over the next that has not begun)
+    a.claims = blocks == 1u && a.rows > resident / 2u;
+    return launched(launch_overlapped(fn, (unsigned)(a.rows * blocks), kTopThreads, smem, kargs, st, blocks));
 }
 
 int fastsgd_distill_loss(const fastsgd_matrix* student, const fastsgd_pairs* teacher, float temperature, const float* weight,

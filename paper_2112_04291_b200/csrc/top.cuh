@@ -7,6 +7,7 @@
 
 #include <cooperative_groups.h>
 
+#include "async.cuh"
 #include "rows.cuh"
 
 namespace fsg {
@@ -19,6 +20,7 @@ struct TopArgs {
     const void* z; int32_t* keys; void* values; float* lse; float* tail;
     uint64_t rows, z_stride;
     uint32_t cols, k, slice;                               // columns of a row that a block takes (a cluster takes the row)
+    uint32_t claims;                                       // there are more rows than blocks at a time (no clusters then)
     float temperature, c, slack;                           // c = log2(e) / T
 };
 
@@ -91,8 +93,8 @@ __global__ void __launch_bounds__(kTopRowsThreads) k_top_rows(TopArgs a) {
 // ---- many columns: a block or a cluster of blocks per row -----------------------------------------
 // One pass over the row in tiles.  A vector of 16 bytes whose maximum is below the bar cannot hold one of the k pairs: its
 // exponentials are summed and it is forgotten.  The others are listed, warp by warp, and at the end their elements above the bar
-// become candidates; the k-th largest of these is found by histograms of eight bits.  Then the listed vectors are gone through once
-// more for the exponentials of what is no pair, in the list's order: the order in which candidates were found changes no sum.
+// become candidates, while the others join the sum; the k-th largest candidate is found by histograms of eight bits.  The order in which
+// candidates are found changes no sum: those that turn out to be no pairs are added as integers.
 //
 // The first tile is a sample of the row (its 512-byte pieces lie apart as many pieces as there are tiles), and the bar is the
 // maximum of one of its vectors: the one whose place from above the k-th of the row has among them, four standard deviations lower.
@@ -114,85 +116,92 @@ template <uint32_t MOST> struct TopShared {
     static constexpr uint32_t kRoom = MOST <= kTopFewPairs ? MOST + kTopBurst : 4u * MOST;
     static_assert(kRoom >= MOST + kTopBurst, "a step of the careful way finds room");
     unsigned long long cand[kRoom];
-    unsigned long long sorted[MOST < kTopByCount ? kTopByCount : MOST];
+    unsigned long long some[MOST < kTopByCount ? kTopByCount : MOST];
     uint4    ring[2][kTopTile][kTopThreads];               // the tile at hand and the next one
     uint16_t list[kTopWarps][kTopList];                    // vectors as 32 (4 tile + u) + lane; kTopHead, kTopTail: the elements around them
-    uint32_t hist[256];
-    uint32_t cands, taken, bin, above, equal;              // (cands may count more than there is room for)
+    uint32_t hist[3][256];                                 // of three steps in turn; zero when their turn comes
+    uint32_t cands, taken;                                 // (cands may count more than there is room for)
+    uint32_t most[kTopWarps];
+    uint32_t dropped_most;                                 // the candidates that are no pairs: their largest rank, the sum relative to it
+    unsigned long long dropped;
     float2   join[kTopWarps];
     float4   cluster[8];                                   // in the first block: m, rest and in of every block
     uint32_t count;                                        // for the neighbours: entries of `sorted`
+    Claim    claim;                                        // the block's next row
 };
 
-// The bin that holds the `need`-th entry counted from the last bin down, how many lie in later bins and in it.  One warp; there are
-// at least `need`.
-template <class S>
-__device__ __forceinline__ void find_bin(S& s, uint32_t need) {
+// One step of a selection: the histogram of the eight bits at `shift` of the words whose `fixed` bits are those of `word` (they may
+// overlap those eight).  Afterwards the need-th largest word begins with `word`, and `equal` words do.  One barrier: every warp looks
+// the bin up for itself, and the histogram of the step before is cleared for the step after the next.
+template <class S, class W, class EACH>
+__device__ __forceinline__ void select_step(S& s, uint32_t& step, W& word, uint32_t& need, uint32_t& equal, int shift, W fixed, EACH each) {
+    static_assert(kTopThreads == 256, "a bin a thread");
+    uint32_t* hist = s.hist[step % 3u];
+    each([&](W w) { if ((w & fixed) == word) atomicAdd(&hist[(uint32_t)(w >> shift) & 255u], 1u); });
+    __syncthreads();
     const int lane = threadIdx.x & 31;
     uint32_t h[8], sum = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += h[i] = s.hist[255 - (8 * lane + i)];
+    for (int i = 0; i < 8; ++i) sum += h[i] = hist[255 - (8 * lane + i)];
     uint32_t upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(kFullMask, upto, o); if (lane >= o) upto += y; }
-    uint32_t at = upto - sum;
-    if (at < need && need <= upto) {                       // one lane
+    uint32_t at = upto - sum, bin = 0u, above = 0u, in = 0u;
+    const bool here = at < need && need <= upto;           // one lane
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (at < need && need <= at + h[i]) { s.bin = 255u - (uint32_t)(8 * lane + i); s.above = at; s.equal = h[i]; }
-            at += h[i];
-        }
+    for (int i = 0; i < 8; ++i) {
+        if (at < need && need <= at + h[i]) { bin = 255u - (uint32_t)(8 * lane + i); above = at; in = h[i]; }
+        at += h[i];
     }
+    const int who = __ffs((int)__ballot_sync(kFullMask, here)) - 1;
+    word |= (W)__shfl_sync(kFullMask, bin, who) << shift;
+    need -= __shfl_sync(kFullMask, above, who);
+    equal = __shfl_sync(kFullMask, in, who);
+    s.hist[(step + 2u) % 3u][threadIdx.x] = 0u;
+    ++step;
 }
 
-// One step of a selection: the histogram of the eight bits at `shift` of the words whose `fixed` bits are those of `word` (they may
-// overlap those eight).  Afterwards the need-th largest word begins with `word`; true when as many begin with it as are still needed.
-template <class S, class W, class EACH>
-__device__ __forceinline__ bool select_step(S& s, W& word, uint32_t& need, int shift, W fixed, EACH each) {
-    __syncthreads();
-    s.hist[threadIdx.x] = 0u;
-    static_assert(kTopThreads == 256, "a bin a thread");
-    __syncthreads();
-    each([&](W w) { if ((w & fixed) == word) atomicAdd(&s.hist[(uint32_t)(w >> shift) & 255u], 1u); });
-    __syncthreads();
-    if (threadIdx.x < 32u) find_bin(s, need);
-    __syncthreads();
-    word |= (W)s.bin << shift;
-    need -= s.above;
-    return need == s.equal;
-}
-
-// The k largest of the n candidates (more than k of them, none below `floor`) stay.  Returns a lower bound of them all: the bar.  The
+// A lower bound of at least k and at most `enough` of the n candidates (more than k, none below `floor`): k of them if enough = k.  The
 // histograms begin with the highest bit in which the candidates' distances from `floor` differ.
 template <class S>
-__device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor) {
+__device__ __forceinline__ unsigned long long cut_of(S& s, uint32_t& step, uint32_t n, uint32_t k, uint32_t enough, unsigned long long floor) {
     const uint32_t tid = threadIdx.x, base = (uint32_t)(floor >> 32);
     const unsigned long long low = (unsigned long long)base << 32;
     uint32_t most = 0u;
     for (uint32_t i = tid; i < n; i += kTopThreads) most = max(most, (uint32_t)(s.cand[i] >> 32) - base);
     most = __reduce_max_sync(kFullMask, most);
+    if ((tid & 31u) == 0u) s.most[tid >> 5] = most;
     __syncthreads();
-    if ((tid & 31u) == 0u) s.hist[tid >> 5] = most;
-    __syncthreads();
-    for (int w = 0; w < kTopWarps; ++w) most = max(most, s.hist[w]);
+#pragma unroll
+    for (int w = 0; w < kTopWarps; ++w) most = max(most, s.most[w]);
     unsigned long long word = 0ull, fixed = 0ull;
-    uint32_t need = k;
+    uint32_t need = k, equal = 0u;
     int shift = 64 - __clz((int)most) - 8;                 // (0 or more: without a difference in rank, the keys' upper bits)
     shift = shift < 24 ? 24 : shift;
-    while (!select_step(s, word, need, shift, fixed, [&](auto put) { for (uint32_t i = tid; i < n; i += kTopThreads) put(s.cand[i] - low); }) && shift) {
+    for (;;) {
+        select_step(s, step, word, need, equal, shift, fixed, [&](auto put) { for (uint32_t i = tid; i < n; i += kTopThreads) put(s.cand[i] - low); });
+        if (k - need + equal <= enough || !shift) break;
         fixed = ~0ull << shift;
         shift = shift > 8 ? shift - 8 : 0;
     }
-    word += low;
+    return word + low;
+}
+
+// The k largest of the n candidates (more than k of them, none below `floor`) stay.  Returns a lower bound of them all: the bar.
+template <class S>
+__device__ __noinline__ unsigned long long cut_candidates(S& s, uint32_t step, uint32_t n, uint32_t k, unsigned long long floor) {
+    const uint32_t tid = threadIdx.x;
+    const unsigned long long word = cut_of(s, step, n, k, k, floor);
     if (tid == 0) s.taken = 0u;
     __syncthreads();
     for (uint32_t i = tid; i < n; i += kTopThreads) {
         const unsigned long long w = s.cand[i];
-        if (w >= word) s.sorted[atomicAdd(&s.taken, 1u)] = w;
+        if (w >= word) s.some[atomicAdd(&s.taken, 1u)] = w;
     }
     __syncthreads();
-    for (uint32_t i = tid; i < k; i += kTopThreads) s.cand[i] = s.sorted[i];
+    for (uint32_t i = tid; i < k; i += kTopThreads) s.cand[i] = s.some[i];
     if (tid == 0) s.cands = k;
+    for (int h = 0; h < 3; ++h) s.hist[h][tid] = 0u;       // (the caller's count of steps goes on from anywhere)
     __syncthreads();
     return word;
 }
@@ -252,64 +261,97 @@ __device__ __forceinline__ void each_listed(const TopShared<MOST>& s, const T* z
     }
     __syncwarp();
 }
-// Those above the bar become candidates, as far as there is room.
+// Those above the bar become candidates, as far as there is room; the others join the sum.
 template <class T, uint32_t MOST>
-__device__ __noinline__ void collect(TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long cut, uint32_t begin, uint32_t end) {
-    each_listed<T>(s, z, top_slice(z + begin, end - begin), listed, begin, end, [&](unsigned long long w, float) {
-        if (w < cut) return;
+__device__ __noinline__ ExpSum collect(TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long cut, uint32_t begin, uint32_t end, ExpSum e, float c, float slack) {
+    each_listed<T>(s, z, top_slice(z + begin, end - begin), listed, begin, end, [&](unsigned long long w, float x) {
+        if (w < cut) { e.add(x, c, slack); return; }
         const uint32_t n = atomicAdd(&s.cands, 1u);
         if (n < TopShared<MOST>::kRoom) s.cand[n] = w;
     });
+    return e;
 }
 
-// The k largest of n candidates (all, if there are no more) in descending order to `sorted`.
-template <class S>
-__device__ __noinline__ uint32_t sort_candidates(S& s, uint32_t n, uint32_t k, unsigned long long floor) {
+// The k largest of n candidates (all, if there are no more) in descending order to cand[0 ...).  Returns this thread's part of the others'
+// sum, which does not depend on their order.
+template <class T, class S>
+__device__ __noinline__ ExpSum sort_candidates(S& s, uint32_t step, uint32_t n, uint32_t k, unsigned long long floor, float c, float slack) {
     const uint32_t tid = threadIdx.x;
-    if (n > k + k / 2u + 32u || (n > kTopByCount && n > k)) { cut_candidates(s, n, k, floor); n = k; }
-    if (n <= kTopByCount) {                                // a candidate's place is the number of larger ones
+    ExpSum e;
+    uint32_t some = n;                                     // those that are sorted
+    if (tid == 0) { s.taken = 0u; s.dropped_most = 0u; s.dropped = 0ull; }
+    if (n > k && (n > kTopByCount || n > k + k / 2u + 32u)) {
+        // (up to 256 are sorted by counting: a few more than k do no harm)
+        const unsigned long long word = cut_of(s, step, n, k, k <= kTopByCount - 32u ? k + 32u : k, floor);
+        uint32_t most = 0u;
+        for (uint32_t i = tid; i < n; i += kTopThreads) {
+            const unsigned long long w = s.cand[i];
+            if (w >= word) s.some[atomicAdd(&s.taken, 1u)] = w; else most = max(most, (uint32_t)(w >> 32));
+        }
+        most = __reduce_max_sync(kFullMask, most);
+        if ((tid & 31u) == 0u) atomicMax(&s.dropped_most, most);
+        __syncthreads();
+        some = s.taken;
+        // relative to the largest of them, in units of 2^-40
+        const float m = value_of_rank<T>(s.dropped_most);
+        unsigned long long sum = 0ull;
+        for (uint32_t i = tid; i < n; i += kTopThreads) {
+            const unsigned long long w = s.cand[i];
+            if (w < word) sum += (unsigned long long)(exp2_fast((value_of_rank<T>((uint32_t)(w >> 32)) - m) * c) * 1099511627776.f);
+        }
+        sum = warp_sum(sum);
+        if ((tid & 31u) == 0u) atomicAdd(&s.dropped, sum);
+        __syncthreads();
+        if (tid == 0) { e.m = fmaxf(m, kLowest); e.s = (float)s.dropped * (1.f / 1099511627776.f); }
+    } else {
+        for (uint32_t i = tid; i < n; i += kTopThreads) s.some[i] = s.cand[i];
+        __syncthreads();
+    }
+    if (some <= kTopByCount) {                             // a candidate's place is the number of larger ones
         constexpr uint32_t kParts = 8u;                    // threads of a candidate, next to each other
-        for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads / kParts) {
+        for (uint32_t i0 = 0; i0 < some; i0 += kTopThreads / kParts) {
             const uint32_t i = i0 + tid / kParts, part = tid % kParts;
-            const unsigned long long x = i < n ? s.cand[i] : 0ull;
+            const unsigned long long x = i < some ? s.some[i] : 0ull;
             uint32_t before = 0u;
-            for (uint32_t j = part; j < n; j += kParts) before += s.cand[j] > x;
+            for (uint32_t j = part; j < some; j += kParts) before += s.some[j] > x;
 #pragma unroll
             for (uint32_t o = 1u; o < kParts; o <<= 1) before += __shfl_xor_sync(kFullMask, before, o);
-            if (i < n && part == 0u) s.sorted[before] = x;
+            if (i < some && part == 0u) s.cand[before] = x;
         }
-    } else {                                               // n <= k: a bitonic network
+        __syncthreads();
+        for (uint32_t i = k + tid; i < some; i += kTopThreads) e.add(value_of_rank<T>((uint32_t)(s.cand[i] >> 32)), c, slack);
+    } else {                                               // k of them: a bitonic network
         uint32_t size2 = 2u * kTopByCount;
-        while (size2 < n) size2 <<= 1;
-        for (uint32_t i = tid; i < size2; i += kTopThreads) s.sorted[i] = i < n ? s.cand[i] : 0ull;
+        while (size2 < some) size2 <<= 1;
+        for (uint32_t i = some + tid; i < size2; i += kTopThreads) s.some[i] = 0ull;
         for (uint32_t size = 2u; size <= size2; size <<= 1)
-            for (uint32_t step = size >> 1; step; step >>= 1) {
+            for (uint32_t step2 = size >> 1; step2; step2 >>= 1) {
                 __syncthreads();
                 for (uint32_t i = tid; i < size2 / 2u; i += kTopThreads) {
-                    const uint32_t p = 2u * i - (i & (step - 1u)), q = p + step;
-                    const unsigned long long x = s.sorted[p], y = s.sorted[q];
-                    if ((x < y) == ((p & size) == 0u)) { s.sorted[p] = y; s.sorted[q] = x; }
+                    const uint32_t p = 2u * i - (i & (step2 - 1u)), q = p + step2;
+                    const unsigned long long x = s.some[p], y = s.some[q];
+                    if ((x < y) == ((p & size) == 0u)) { s.some[p] = y; s.some[q] = x; }
                 }
             }
+        __syncthreads();
+        for (uint32_t i = tid; i < some; i += kTopThreads) s.cand[i] = s.some[i];
+        __syncthreads();
     }
-    __syncthreads();
-    return n < k ? n : k;
+    for (int h = 0; h < 3; ++h) s.hist[h][tid] = 0u;       // (the caller's count of steps goes on from anywhere)
+    return e;
 }
 
 // a lower bound of the need-th largest rank among the maxima of the first tile's vectors (16 of its bits)
 template <class T, class S>
-__device__ __forceinline__ unsigned long long first_bar(S& s, uint32_t need, uint32_t mine, const float (&top)[kTopTile]) {
-    constexpr int kTopBit = 8 * ((Rank<T>::kBits - 1) / 8);
-    uint32_t word = 0u;
+__device__ __forceinline__ unsigned long long first_bar(S& s, uint32_t& step, uint32_t need, uint32_t mine, const float (&top)[kTopTile]) {
+    constexpr int kTopBit = Rank<T>::kBits - 8;
+    uint32_t word = 0u, equal = 0u;
     auto each = [&](auto put) {
 #pragma unroll
         for (int u = 0; u < kTopTile; ++u) if ((uint32_t)u < mine) put(rank_of<T>(top[u]));
     };
-    if (!select_step(s, word, need, kTopBit, 0u, each)) {
-        const bool done = select_step(s, word, need, kTopBit - 8, ~0u << kTopBit, each);
-        // (of 19 bits the first eight are three: the last step, too)
-        if (kTopBit == 16 && !done) select_step(s, word, need, 0, ~0u << 8, each);
-    }
+    select_step(s, step, word, need, equal, kTopBit, 0u, each);
+    select_step(s, step, word, need, equal, kTopBit - 8, ~0u << kTopBit, each);
     return (unsigned long long)word << 32;
 }
 
@@ -321,7 +363,7 @@ template <class T> __device__ __forceinline__ float bar_value(unsigned long long
 
 // The careful way through a slice: its candidates.  Returns the bar.
 template <class T, uint32_t MOST>
-__device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s, const T* z, uint32_t there, uint32_t k, uint32_t begin, uint32_t end) {
+__device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s, uint32_t step, const T* z, uint32_t there, uint32_t k, uint32_t begin, uint32_t end) {
     constexpr int N = Vec<T>::N;
     const TopSlice q = top_slice(z + begin, end - begin);
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, first_key = begin + q.head;
@@ -334,7 +376,7 @@ __device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s,
             float top[kTopTile];
 #pragma unroll
             for (int u = 0; u < kTopTile; ++u) top[u] = (uint32_t)u < mine ? Vec<T>::max_nan(load16(body + v + u * q.step)) : 0.f;
-            if (k <= there) cut = first_bar<T>(s, k, mine, top);
+            if (k <= there) cut = first_bar<T>(s, step, k, mine, top);
         }
         __syncthreads();
         for (uint32_t u = 0; u < (uint32_t)kTopTile; ++u) {
@@ -351,22 +393,16 @@ __device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s,
             }
             const unsigned hits = __ballot_sync(kFullMask, hit);
             if (hit) s.list[warp][listed + __popc(hits & ((1u << lane) - 1u))] = (uint16_t)(128u * t + 32u * u + lane);
-            collect<T>(s, z, listed + __popc(hits), cut, begin, end);
+            collect<T>(s, z, listed + __popc(hits), cut, begin, end, ExpSum(), 0.f, 0.f);
             __syncthreads();
             const uint32_t n = s.cands;
             __syncthreads();
-            if (n > MOST) cut = cut_candidates(s, n, k, cut);
+            if (n > MOST) cut = cut_candidates(s, step, n, k, cut);
         }
     }
     return cut;
 }
-// The sum of what lies below the last pair, of the listed vectors ...
-template <class T, uint32_t MOST>
-__device__ __noinline__ ExpSum sum_listed(const TopShared<MOST>& s, const T* z, uint32_t listed, unsigned long long last, uint32_t begin, uint32_t end, ExpSum e, float c, float slack) {
-    each_listed<T>(s, z, top_slice(z + begin, end - begin), listed, begin, end, [&](unsigned long long w, float x) { if (w < last) e.add(x, c, slack); });
-    return e;
-}
-// ... or of the whole slice.
+// ... and the sum of what lies below its last pair, whatever the logits.
 template <class T>
 __device__ __noinline__ ExpSum sum_carefully(const T* z, unsigned long long last, uint32_t begin, uint32_t end, float c, float slack) {
     ExpSum e;
@@ -387,7 +423,6 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, k = a.k, blocks = cluster.num_blocks(), rank = cluster.block_rank();
     const bool sums = a.lse || a.tail;
     const uint32_t begin = rank * a.slice < a.cols ? rank * a.slice : a.cols, end = begin + a.slice < a.cols ? begin + a.slice : a.cols;
-    const uint64_t stride = gridDim.x / blocks;
     auto fetch = [&](const T* z, const TopSlice& q, uint32_t t, uint32_t slot) {
         const uint4* body = reinterpret_cast<const uint4*>(z + begin + q.head);
         uint32_t v = q.first + 32u * t;
@@ -395,19 +430,27 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
         for (int u = 0; u < kTopTile; ++u, v += q.step) if (v < q.vecs) copy16_async(&s.ring[slot][u][tid], body + v);
         copies_end_group();
     };
+    if (tid == 0) claim_init(s.claim);
+    for (int h = 0; h < 3; ++h) s.hist[h][tid] = 0u;
+    uint32_t step = 0u;
     wait_for_previous_kernels();
     uint32_t slot = 0u;
     uint64_t row = blockIdx.x / blocks;
-    const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
-    if (row < a.rows) fetch(z, top_slice(z + begin, end - begin), 0u, slot);
-    for (; row < a.rows; row += stride) {
+    {
+        const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
+        fetch(z, top_slice(z + begin, end - begin), 0u, slot);
+    }
+    if (tid == 0 && a.claims) claim_ask(s.claim);
+    for (uint32_t turn = 0u;; ++turn) {
+        const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
+        int next_row = -1;
         const TopSlice q = top_slice(z + begin, end - begin);
         // vectors in the first tile: of its pieces all but the row's last are whole
         const uint32_t pieces = (q.vecs + 31u) / 32u;
         const uint32_t there = pieces ? (pieces + q.tiles - 1u) / q.tiles * 32u - ((pieces - 1u) % q.tiles ? 0u : pieces * 32u - q.vecs) : 0u;
         const float expect = (float)k * (float)there / (float)max(q.vecs, 1u);
         const uint32_t guess = min(k, (uint32_t)(expect + 5.f * sqrtf(expect) + 5.f));
-        ExpSums es;
+        FusedExpSums es;
         unsigned long long cut = 0ull;
         float bar = 0.f;
         uint32_t listed = 0u;
@@ -415,8 +458,11 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
         if (tid == 0) s.cands = 0u;
         for (uint32_t t = 0; t < q.tiles; ++t) {
             if (t + 1u < q.tiles) fetch(z, q, t + 1u, slot ^ 1u);
-            else if (row + stride < a.rows) { const T* next = z + stride * a.z_stride; fetch(next, top_slice(next + begin, end - begin), 0u, slot ^ 1u); }
-            else copies_end_group();
+            else {
+                if (a.claims) next_row = claim_answer(s.claim, turn);
+                if (next_row >= 0) { const T* next = static_cast<const T*>(a.z) + (uint64_t)next_row * a.z_stride; fetch(next, top_slice(next + begin, end - begin), 0u, slot ^ 1u); }
+                else copies_end_group();
+            }
             wait_copies<1>();
             uint4 raw[kTopTile];
             float top[kTopTile];
@@ -432,7 +478,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
 #pragma unroll
             for (int u = 0; u < kTopTile; ++u) top[u] = Vec<T>::max_nan(raw[u]);
             if (t == 0u) {
-                if (guess <= there) cut = first_bar<T>(s, guess, mine, top);
+                if (guess <= there) cut = first_bar<T>(s, step, guess, mine, top);
                 else __syncthreads();
                 bar = bar_value<T>(cut);
                 if (warp == 0u && q.head) { if (lane == 0) s.list[0][listed] = kTopHead; ++listed; }
@@ -465,44 +511,53 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
                 listed = 0u;
             }
         }
-        collect<T>(s, z, listed, cut, begin, end);
+        ExpSum e = collect<T>(s, z, listed, cut, begin, end, ExpSum(), a.c, a.slack);
         __syncthreads();
+        if (tid == 0 && next_row >= 0) claim_ask(s.claim);      // (all have read the last answer)
         uint32_t n = s.cands;
         const bool careful = n > TopShared<MOST>::kRoom || (n < k && cut);
         if (careful) {
             __syncthreads();
-            cut = collect_carefully<T>(s, z, there, k, begin, end);
+            cut = collect_carefully<T>(s, step, z, there, k, begin, end);
             n = s.cands;
         }
-        const uint32_t have = sort_candidates(s, n, k, cut);
-        ExpSum e = es.whole();
+        const ExpSum dropped = sort_candidates<T>(s, step, n, k, cut, a.c, a.slack);
+        const uint32_t have = min(n, k);
+        // (of all that this block has seen, the first is the largest)
+        const float m = have ? fmaxf(value_of_rank<T>((uint32_t)(s.cand[0] >> 32)), kLowest) : kLowest;
         if (sums) {
-            const unsigned long long least = have == k ? s.sorted[k - 1u] : 0ull;      // the last pair
-            if (careful) e = sum_carefully<T>(z, least, begin, end, a.c, a.slack);
-            else e = sum_listed<T>(s, z, listed, least, begin, end, e, a.c, a.slack);
+            if (careful || is_far(m, a.c)) e = sum_carefully<T>(z, have == k ? s.cand[k - 1u] : 0ull, begin, end, a.c, a.slack);
+            else {
+                const ExpSum streamed = es.whole(a.c);
+                e.join(streamed.m, streamed.s, a.c);
+                e.join(dropped.m, dropped.s, a.c);
+            }
         }
 
         // ---- the pairs: a candidate's place is how many of the whole row's are larger -----------------
-        if (tid == 0) s.count = have;
-        if (blocks > 1u) cluster.sync();
-        // (of all that this block has seen, the first is the largest)
-        const float m = have ? fmaxf(value_of_rank<T>((uint32_t)(s.sorted[0] >> 32)), kLowest) : kLowest;
+        uint32_t* places = reinterpret_cast<uint32_t*>(s.list);
+        if (blocks > 1u) {
+            if (tid == 0) s.count = have;
+            for (uint32_t i = tid; i < have; i += kTopThreads) places[i] = i;
+            cluster.sync();
+            for (uint32_t j = tid; j < have * (blocks - 1u); j += kTopThreads) {
+                const uint32_t i = j / (blocks - 1u), b = j % (blocks - 1u);
+                const TopShared<MOST>& o = *cluster.map_shared_rank(&s, b + (b >= rank));
+                const unsigned long long w = s.cand[i];
+                uint32_t l = 0u, h = o.count;
+                while (l < h) { const uint32_t mid = (l + h) >> 1; if (o.cand[mid] > w) l = mid + 1u; else h = mid; }
+                atomicAdd(&places[i], l);
+            }
+            __syncthreads();
+        }
         float in = 0.f;
         for (uint32_t i = tid; i < have; i += kTopThreads) {
-            const unsigned long long w = s.sorted[i];
-            uint32_t place = i;
-            for (uint32_t b = 0; b < blocks; ++b) {
-                if (b == rank) continue;
-                const TopShared<MOST>& o = *cluster.map_shared_rank(&s, b);
-                uint32_t l = 0u, h = o.count;
-                while (l < h) { const uint32_t mid = (l + h) >> 1; if (o.sorted[mid] > w) l = mid + 1u; else h = mid; }
-                place += l;
-            }
+            const unsigned long long w = s.cand[i];
+            const uint32_t place = blocks > 1u ? places[i] : i;
             const float x = value_of_rank<T>((uint32_t)(w >> 32));
             if (place < k) {
-                const uint32_t key = ~(uint32_t)w;
-                a.keys[row * k + place] = (int32_t)key;
-                static_cast<T*>(a.values)[row * k + place] = z[key];
+                a.keys[row * k + place] = (int32_t)~(uint32_t)w;
+                static_cast<T*>(a.values)[row * k + place] = from_float<T>(x);
                 in += exp2_fast((x - m) * a.c);
             } else e.add(x, a.c, a.slack);
         }
@@ -529,7 +584,8 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
             if (a.lse) a.lse[row] = none ? -INFINITY : top / a.temperature + logf(rest + inside);
             if (a.tail) a.tail[row] = none ? 0.f : rest / (rest + inside);
         }
-        z += stride * a.z_stride;
+        if (next_row < 0) break;
+        row = (uint64_t)next_row;
     }
 }
 
