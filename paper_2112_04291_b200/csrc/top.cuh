@@ -217,6 +217,11 @@ template <class T> __device__ __forceinline__ TopSlice top_slice(const T* z, uin
     q.first = warp * q.tiles * 32u + lane; q.step = kTopWarps * q.tiles * 32u;
     return q;
 }
+// vectors in the first tile: of its pieces all but the row's last are whole
+__device__ __forceinline__ uint32_t first_tile_of(const TopSlice& q) {
+    const uint32_t pieces = (q.vecs + 31u) / 32u;
+    return pieces ? (pieces + q.tiles - 1u) / q.tiles * 32u - ((pieces - 1u) % q.tiles ? 0u : pieces * 32u - q.vecs) : 0u;
+}
 // of the four vectors of tile t, those that there are
 __device__ __forceinline__ uint32_t vectors_of(const TopSlice& q, uint32_t t) {
     const uint32_t v = q.first + 32u * t;
@@ -363,7 +368,7 @@ template <class T> __device__ __forceinline__ float bar_value(unsigned long long
 
 // The careful way through a slice: its candidates.  Returns the bar.
 template <class T, uint32_t MOST>
-__device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s, uint32_t step, const T* z, uint32_t there, uint32_t k, uint32_t begin, uint32_t end) {
+__device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s, uint32_t step, const T* z, uint32_t k, uint32_t begin, uint32_t end) {
     constexpr int N = Vec<T>::N;
     const TopSlice q = top_slice(z + begin, end - begin);
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, first_key = begin + q.head;
@@ -376,7 +381,7 @@ __device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s,
             float top[kTopTile];
 #pragma unroll
             for (int u = 0; u < kTopTile; ++u) top[u] = (uint32_t)u < mine ? Vec<T>::max_nan(load16(body + v + u * q.step)) : 0.f;
-            if (k <= there) cut = first_bar<T>(s, step, k, mine, top);
+            if (k <= first_tile_of(q)) cut = first_bar<T>(s, step, k, mine, top);
         }
         __syncthreads();
         for (uint32_t u = 0; u < (uint32_t)kTopTile; ++u) {
@@ -414,7 +419,7 @@ __device__ __noinline__ ExpSum sum_carefully(const T* z, unsigned long long last
 }
 
 template <class T, uint32_t MOST>
-__global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
+__global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_top(TopArgs a) {
     extern __shared__ __align__(16) unsigned char top_smem[];
     TopShared<MOST>& s = *reinterpret_cast<TopShared<MOST>*>(top_smem);
     namespace cg = cooperative_groups;
@@ -445,9 +450,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
         const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
         int next_row = -1;
         const TopSlice q = top_slice(z + begin, end - begin);
-        // vectors in the first tile: of its pieces all but the row's last are whole
-        const uint32_t pieces = (q.vecs + 31u) / 32u;
-        const uint32_t there = pieces ? (pieces + q.tiles - 1u) / q.tiles * 32u - ((pieces - 1u) % q.tiles ? 0u : pieces * 32u - q.vecs) : 0u;
+        const uint32_t there = first_tile_of(q);
         const float expect = (float)k * (float)there / (float)max(q.vecs, 1u);
         const uint32_t guess = min(k, (uint32_t)(expect + 5.f * sqrtf(expect) + 5.f));
         FusedExpSums es;
@@ -511,14 +514,14 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
                 listed = 0u;
             }
         }
-        ExpSum e = collect<T>(s, z, listed, cut, begin, end, ExpSum(), a.c, a.slack);
+        ExpSum e = collect<T>(s, z, listed, cut, begin, end, es.whole(a.c), a.c, a.slack);
         __syncthreads();
         if (tid == 0 && next_row >= 0) claim_ask(s.claim);      // (all have read the last answer)
         uint32_t n = s.cands;
         const bool careful = n > TopShared<MOST>::kRoom || (n < k && cut);
         if (careful) {
             __syncthreads();
-            cut = collect_carefully<T>(s, step, z, there, k, begin, end);
+            cut = collect_carefully<T>(s, step, z, k, begin, end);
             n = s.cands;
         }
         const ExpSum dropped = sort_candidates<T>(s, step, n, k, cut, a.c, a.slack);
@@ -527,11 +530,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) k_top(TopArgs a) {
         const float m = have ? fmaxf(value_of_rank<T>((uint32_t)(s.cand[0] >> 32)), kLowest) : kLowest;
         if (sums) {
             if (careful || is_far(m, a.c)) e = sum_carefully<T>(z, have == k ? s.cand[k - 1u] : 0ull, begin, end, a.c, a.slack);
-            else {
-                const ExpSum streamed = es.whole(a.c);
-                e.join(streamed.m, streamed.s, a.c);
-                e.join(dropped.m, dropped.s, a.c);
-            }
+            else e.join(dropped.m, dropped.s, a.c);
         }
 
         // ---- the pairs: a candidate's place is how many of the whole row's are larger -----------------
