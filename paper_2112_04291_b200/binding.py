@@ -288,8 +288,8 @@ def key_encode_paper(keys: torch.Tensor, flag_bits: int, out: torch.Tensor, stre
 # ---- losses on logits, and their data as key-value pairs ----------------------------------------
 # (Calls of a few microseconds: the checks ask tensors for numbers, not for objects.)
 
-def _raw_stream(stream) -> int:
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+def _raw_stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _matrix(t: torch.Tensor, dev: int) -> Matrix:
@@ -310,9 +310,12 @@ def _at(t, dev: int, dtype: torch.dtype, *shape):
     return t.data_ptr()
 
 
+_float32, _int32, _int64 = torch.float32, torch.int32, torch.int64
+
+
 def _device_of(t: torch.Tensor) -> int:
     dev = t.get_device()
-    assert dev >= 0 and dev == torch.cuda.current_device(), "tensors live on the current device"
+    assert dev >= 0 and dev == torch._C._cuda_getDevice(), "tensors live on the current device"
     return dev
 
 
@@ -323,15 +326,15 @@ def top_logits(logits: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, t
     m = _matrix(logits, dev)
     rows, k = keys.shape
     assert rows == m.rows
-    return lib().fastsgd_top_logits(m, k, temperature, _at(keys, dev, torch.int32, rows, k), _at(values, dev, logits.dtype, rows, k),
-                                    _at(lse, dev, torch.float32, rows), _at(tail, dev, torch.float32, rows), _raw_stream(stream))
+    return lib().fastsgd_top_logits(m, k, temperature, _at(keys, dev, _int32, rows, k), _at(values, dev, logits.dtype, rows, k),
+                                    _at(lse, dev, _float32, rows), _at(tail, dev, _float32, rows), _raw_stream(stream, dev))
 
 
 def _teacher(rows: int, keys, values, tail, dev: int) -> Pairs:
     n, k = keys.shape
     kind = TYPES.get(values.dtype)
     assert n == rows and kind is not None
-    return Pairs(_at(keys, dev, torch.int32, rows, k), _at(values, dev, values.dtype, rows, k), _at(tail, dev, torch.float32, rows), k, kind)
+    return Pairs(_at(keys, dev, _int32, rows, k), _at(values, dev, values.dtype, rows, k), _at(tail, dev, _float32, rows), k, kind)
 
 
 def distill_loss(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
@@ -340,9 +343,9 @@ def distill_loss(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor
     dev = _device_of(student)
     m = _matrix(student, dev)
     rows = m.rows
-    return lib().fastsgd_distill_loss(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, torch.float32, rows),
-                                      _at(loss, dev, torch.float32, rows), _at(stats, dev, torch.float32, rows, 2),
-                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream))
+    return lib().fastsgd_distill_loss(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, _float32, rows),
+                                      _at(loss, dev, _float32, rows), _at(stats, dev, _float32, rows, 2),
+                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream, dev))
 
 
 def distill_loss_backward(student: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, stats: torch.Tensor, grad: torch.Tensor,
@@ -352,9 +355,9 @@ def distill_loss_backward(student: torch.Tensor, keys: torch.Tensor, values: tor
     dev = _device_of(student)
     m = _matrix(student, dev)
     rows = m.rows
-    return lib().fastsgd_distill_loss_backward(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, torch.float32, rows),
-                                               _at(stats, dev, torch.float32, rows, 2), _at(grad_loss, dev, torch.float32, rows),
-                                               _matrix(grad, dev), _raw_stream(stream))
+    return lib().fastsgd_distill_loss_backward(m, _teacher(rows, keys, values, tail, dev), temperature, _at(weight, dev, _float32, rows),
+                                               _at(stats, dev, _float32, rows, 2), _at(grad_loss, dev, _float32, rows),
+                                               _matrix(grad, dev), _raw_stream(stream, dev))
 
 
 def _mask(mask, dev: int, tokens: int):
@@ -368,9 +371,9 @@ def expert_counts(selected: torch.Tensor, counts: torch.Tensor, counted: torch.T
     tokens, k = selected.shape
     segments, experts = counts.shape
     assert offsets is not None or segments == 1
-    return lib().fastsgd_expert_counts(_at(selected, dev, torch.int32, tokens, k), tokens, k, experts, _mask(mask, dev, tokens),
-                                       _at(offsets, dev, torch.int64, segments + 1), segments, _at(counts, dev, torch.int32, segments, experts),
-                                       _at(counted, dev, torch.int32, segments), _raw_stream(stream))
+    return lib().fastsgd_expert_counts(_at(selected, dev, _int32, tokens, k), tokens, k, experts, _mask(mask, dev, tokens),
+                                       _at(offsets, dev, _int64, segments + 1), segments, _at(counts, dev, _int32, segments, experts),
+                                       _at(counted, dev, _int32, segments), _raw_stream(stream, dev))
 
 
 def balance_loss(logits: torch.Tensor, counts: torch.Tensor, counted: torch.Tensor, loss: torch.Tensor = None, grad: torch.Tensor = None,
@@ -380,10 +383,10 @@ def balance_loss(logits: torch.Tensor, counts: torch.Tensor, counted: torch.Tens
     m = _matrix(logits, dev)
     tokens, experts, segments = m.rows, m.cols, counts.shape[0]
     assert offsets is not None or segments == 1
-    return lib().fastsgd_balance_loss(m, _mask(mask, dev, tokens), _at(offsets, dev, torch.int64, segments + 1), segments,
-                                      _at(counts, dev, torch.int32, segments, experts), _at(counted, dev, torch.int32, segments), coef,
-                                      _at(grad_loss, dev, torch.float32, segments), _at(loss, dev, torch.float32, segments),
-                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream))
+    return lib().fastsgd_balance_loss(m, _mask(mask, dev, tokens), _at(offsets, dev, _int64, segments + 1), segments,
+                                      _at(counts, dev, _int32, segments, experts), _at(counted, dev, _int32, segments), coef,
+                                      _at(grad_loss, dev, _float32, segments), _at(loss, dev, _float32, segments),
+                                      None if grad is None else _matrix(grad, dev), _raw_stream(stream, dev))
 
 
 def stream_info(stream_in: torch.Tensor, stream=None):

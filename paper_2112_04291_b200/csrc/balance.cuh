@@ -164,8 +164,7 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
     const T* xs = static_cast<const T*>(a.x);
     TG* gs = static_cast<TG*>(a.grad);
     auto width_of = [&](int c) { const uint32_t e = (c * LANES + place) * 8u; return e < E ? min(E - e, 8u) : 0u; };
-    const bool x_wide = ((reinterpret_cast<uintptr_t>(xs) | a.x_stride * sizeof(T)) & 15u) == 0u;
-    const bool g_wide = ((reinterpret_cast<uintptr_t>(gs) | a.grad_stride * sizeof(TG)) & 15u) == 0u;
+    const uint32_t x_unit = row_unit(xs, a.x_stride), g_unit = row_unit(gs, a.grad_stride);
     wait_for_previous_kernels();
     const uint64_t r0 = (uint64_t)blockIdx.x * a.rows_per_block, r1 = r0 + a.rows_per_block < a.tokens ? r0 + a.rows_per_block : a.tokens;
     const Segments seg{a.offsets, a.tokens, a.segments};
@@ -183,7 +182,7 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 const uint64_t t = t0 + r * PER_WARP + group;
                 next_counts[r] = t < to && (!a.mask || a.mask[t]);
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) next[r][c] = load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, next_counts[r] ? width_of(c) : 0u, x_wide);
+                for (int c = 0; c < CHUNKS; ++c) next[r][c] = load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, next_counts[r] ? width_of(c) : 0u, x_unit);
             }
         };
         uint64_t t0 = from + (uint64_t)warp * (PER_WARP * ROWS);
@@ -211,6 +210,7 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
         if (a.grad_loss) scale *= a.grad_loss[s];
         double sum = 0.0;
         for (; t0 < to; t0 += kStep) {
+            float dots_of_step = 0.f;
             float v[ROWS][CHUNKS][8];
             bool counts[ROWS];
 #pragma unroll
@@ -228,8 +228,11 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) m = fmaxf(m, v[r][c][i]);
+                if (LANES == 32) m = warp_max(m);
+                else {
 #pragma unroll
-                for (int o = LANES / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFullMask, m, o));
+                    for (int o = LANES / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFullMask, m, o));
+                }
                 const unsigned long long minus_m = pair_of(-m, -m), cc = pair_of(kLog2e, kLog2e);
                 unsigned long long totals = 0ull, dots = 0ull;
 #pragma unroll
@@ -248,7 +251,7 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 for (int o = LANES / 2; o; o >>= 1) { total += __shfl_xor_sync(kFullMask, total, o); dot += __shfl_xor_sync(kFullMask, dot, o); }
                 const float inv = total == 0.f ? 0.f : 1.f / total;
                 dot *= inv;
-                sum += (double)dot;
+                dots_of_step += dot;
                 if (gs && t < to) {
                     const unsigned long long minus_dot = pair_of(-dot, -dot);
                     const float by = counts[r] ? scale * inv : 0.f;
@@ -260,10 +263,11 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                             const float2 y = halves(mul_pairs(mul_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), bb), add_pairs(pair_of(f[c][i], f[c][i + 1]), minus_dot)));
                             v[r][c][i] = y.x; v[r][c][i + 1] = y.y;
                         }
-                        store_eight(gs + t * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_wide, v[r][c]);
+                        store_eight(gs + t * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_unit, v[r][c]);
                     }
                 }
             }
+            sum += (double)dots_of_step;
         }
         if (a.loss) {
             // every lane of a group has its tokens' sum: one lane of each
@@ -297,19 +301,21 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
         }
         return sum;
     };
-    auto finish = [&](uint32_t s, double sum) { const uint32_t n = a.counted[s]; a.loss[s] = n ? (float)((double)a.coef * (double)E * sum / (double)n) : 0.f; };
+    auto finish = [&](uint32_t s, uint32_t n, double sum) { a.loss[s] = n ? (float)((double)a.coef * (double)E * sum / (double)n) : 0.f; };
     if (a.segments < 8u) {
         for (uint32_t s = 0; s < a.segments; ++s) {
+            const uint32_t n = a.counted[s];
             const double sum = block_sum<kBalanceWarps>(parts_of(s, tid, kBalanceThreads), part);
-            if (tid == 0) finish(s, sum);
+            if (tid == 0) finish(s, n, sum);
         }
     } else {
         for (uint32_t s0 = 0; s0 < a.segments; s0 += kBalanceThreads / 8) {
             const uint32_t s = s0 + tid / 8u;
+            const uint32_t n = s < a.segments ? a.counted[s] : 0u;
             double sum = s < a.segments ? parts_of(s, tid % 8u, 8u) : 0.0;
 #pragma unroll
             for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
-            if (s < a.segments && tid % 8u == 0u) finish(s, sum);
+            if (s < a.segments && tid % 8u == 0u) finish(s, n, sum);
         }
     }
     if (tid == 0) *a.done = 0u;

@@ -140,18 +140,25 @@ template <class T, int N> __device__ __forceinline__ void store_values(T* p, con
     }
 }
 
-// Eight consecutive elements from p on as they are, those behind the first n as -inf; wide: p lies on a 16-byte boundary.
+// Eight consecutive elements from p on as they are, those behind the first n as -inf.  unit: 16 or 8 where p lies on a boundary of so
+// many bytes, otherwise less.
 template <class T> struct Eight { uint4 raw[8 / Vec<T>::N]; };
-template <class T> __device__ __forceinline__ Eight<T> load_eight(const T* p, uint32_t n, bool wide) {
-    constexpr int N = Vec<T>::N;
+template <class T> __device__ __forceinline__ Eight<T> load_eight(const T* p, uint32_t n, uint32_t unit) {
+    constexpr int N = Vec<T>::N, H = N / 2;                // elements of 16 and of 8 bytes
     Eight<T> r;
-    if (wide && n >= 8u) {
+    if (unit == 16u && n >= 8u) {
 #pragma unroll
         for (int h = 0; h < 8 / N; ++h) r.raw[h] = load16(p + h * N);
     } else {
         T x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (uint32_t)i < n ? p[i] : from_float<T>(-INFINITY);
+        for (int h = 0; h < 8; h += H) {
+            if (unit >= 8u && n >= (uint32_t)(h + H)) *reinterpret_cast<uint2*>(x + h) = *reinterpret_cast<const uint2*>(p + h);
+            else {
+#pragma unroll
+                for (int i = h; i < h + H; ++i) x[i] = (uint32_t)i < n ? p[i] : from_float<T>(-INFINITY);
+            }
+        }
 #pragma unroll
         for (int h = 0; h < 8 / N; ++h) r.raw[h] = *reinterpret_cast<const uint4*>(x + h * N);
     }
@@ -167,12 +174,27 @@ template <class T> __device__ __forceinline__ void unpack_eight(const Eight<T>& 
         for (int i = 0; i < N; ++i) f[h * N + i] = x[i];
     }
 }
-template <class T> __device__ __forceinline__ void store_eight(T* p, uint32_t n, bool wide, const float (&f)[8]) {
-    if (n >= 8u) store_values(p, f, wide);
+template <class T> __device__ __forceinline__ void store_eight(T* p, uint32_t n, uint32_t unit, const float (&f)[8]) {
+    constexpr int H = Vec<T>::N / 2;
+    if (unit == 16u && n >= 8u) store_values(p, f, true);
     else {
+        T x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if ((uint32_t)i < n) p[i] = from_float<T>(f[i]);
+        for (int i = 0; i < 8; ++i) x[i] = from_float<T>(f[i]);
+#pragma unroll
+        for (int h = 0; h < 8; h += H) {
+            if (unit >= 8u && n >= (uint32_t)(h + H)) *reinterpret_cast<uint2*>(p + h) = *reinterpret_cast<const uint2*>(x + h);
+            else {
+#pragma unroll
+                for (int i = h; i < h + H; ++i) if ((uint32_t)i < n) p[i] = x[i];
+            }
+        }
     }
+}
+// 16, 8 or 0: the boundary on which every row of so many elements apart begins
+template <class T> __device__ __forceinline__ uint32_t row_unit(const T* p, uint64_t stride) {
+    const uint64_t at = reinterpret_cast<uintptr_t>(p) | stride * sizeof(T);
+    return at & 7u ? 0u : at & 15u ? 8u : 16u;
 }
 
 // A run of n elements from p on: `head` single elements up to a 16-byte boundary, `vecs` vectors, `tail` single elements.
