@@ -147,20 +147,22 @@ __global__ void __launch_bounds__(kCountThreads) k_add_expert_counts(CountArgs a
 }
 
 // A block per run of tokens; LANES lanes share a token, each with CHUNKS times eight neighbouring experts, whose f it keeps in
-// registers.  The next tokens' logits are on their way while those at hand are worked on.
+// registers.  The logits of the next few tokens are on their way while those at hand are worked on (of one step ahead alone, 24 warps an
+// SM had 24 KB in flight, half of what the memory's latency takes).
 // The sum of a block's part of segment s goes to partials[block + s]: of two
 // neighbours in the sequence of (block, segment) meetings one index grows, so that no two share a place.  The block that ends last
 // adds the parts of each segment in their order.
-template <int CHUNKS> constexpr int kBalanceRows = CHUNKS > 1 ? 1 : 2;      // tokens that a group of lanes works on at a time
+template <class T, int CHUNKS> constexpr int kBalanceAhead = CHUNKS > 1 ? 1 : sizeof(T) == 2 ? 4 : 2;      // tokens that a group of lanes has in flight
 template <class T, class TG, int LANES, int CHUNKS>
 __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance(BalanceArgs a) {
     __shared__ double part[kBalanceWarps];
     __shared__ uint32_t last;
     constexpr uint32_t PER_WARP = 32 / LANES;              // tokens
-    constexpr int ROWS = kBalanceRows<CHUNKS>;
+    constexpr int AHEAD = kBalanceAhead<T, CHUNKS>;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, E = a.experts, group = lane / LANES, place = lane % LANES;
     constexpr float kLog2e = 1.4426950408889634f;
-    constexpr uint64_t kStep = kBalanceWarps * PER_WARP * ROWS;
+    constexpr uint32_t kStep = kBalanceWarps * PER_WARP;
+    const uint64_t x_step = kStep * a.x_stride, g_step = kStep * a.grad_stride;
     const T* xs = static_cast<const T*>(a.x);
     TG* gs = static_cast<TG*>(a.grad);
     auto width_of = [&](int c) { const uint32_t e = (c * LANES + place) * 8u; return e < E ? min(E - e, 8u) : 0u; };
@@ -174,19 +176,22 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
         if (from < r0) from = r0;
         if (to > r1) to = r1;
         if (from >= to) continue;
-        Eight<T> next[ROWS][CHUNKS];
-        bool next_counts[ROWS];
-        auto fetch = [&](uint64_t t0) {
+        // (32-bit numbers of the tokens behind `from`, pointers that walk)
+        const uint32_t n_tokens = (uint32_t)(to - from), mine = warp * PER_WARP + group;
+        Eight<T> next[AHEAD][CHUNKS];
+        bool next_counts[AHEAD];
+        uint32_t ahead = mine;
+        const T* x_at = xs + (from + mine) * a.x_stride + place * 8u;
+        const uint8_t* mask_at = a.mask ? a.mask + from + mine : nullptr;
+        auto fetch = [&](int d) {
+            next_counts[d] = ahead < n_tokens && (!mask_at || *mask_at);
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const uint64_t t = t0 + r * PER_WARP + group;
-                next_counts[r] = t < to && (!a.mask || a.mask[t]);
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) next[r][c] = load_eight(xs + t * a.x_stride + (c * LANES + place) * 8u, next_counts[r] ? width_of(c) : 0u, x_unit);
-            }
+            for (int c = 0; c < CHUNKS; ++c) next[d][c] = load_eight(x_at + c * (LANES * 8), next_counts[d] ? width_of(c) : 0u, x_unit);
+            ahead += kStep; x_at += x_step;
+            if (mask_at) mask_at += kStep;
         };
-        uint64_t t0 = from + (uint64_t)warp * (PER_WARP * ROWS);
-        fetch(t0);
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) fetch(d);
         float f[CHUNKS][8];
         {
             uint32_t n[CHUNKS][8];
@@ -200,34 +205,32 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 }
 #pragma unroll
             for (int o = LANES / 2; o; o >>= 1) all += __shfl_xor_sync(kFullMask, all, o);
+            const float share = all ? 1.f / (float)all : 0.f;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[c][i] = all ? (float)n[c][i] / (float)all : 0.f;
+                for (int i = 0; i < 8; ++i) f[c][i] = (float)n[c][i] * share;
         }
         const uint32_t counted = a.counted[s];
         float scale = counted ? a.coef * (float)E / (float)counted : 0.f;
         if (a.grad_loss) scale *= a.grad_loss[s];
         double sum = 0.0;
-        for (; t0 < to; t0 += kStep) {
-            float dots_of_step = 0.f;
-            float v[ROWS][CHUNKS][8];
-            bool counts[ROWS];
+        TG* g_at = gs + (from + mine) * a.grad_stride + place * 8u;
+        for (uint32_t i0 = warp * PER_WARP; i0 < n_tokens;) {
+            float dots_of_steps = 0.f;
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                counts[r] = next_counts[r];
+            for (int d = 0; d < AHEAD; ++d, i0 += kStep, g_at += g_step) {
+                if (i0 >= n_tokens) break;
+                float v[CHUNKS][8];
+                const bool counts = next_counts[d];
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) unpack_eight(next[r][c], v[r][c]);
-            }
-            if (t0 + kStep < to) fetch(t0 + kStep);
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const uint64_t t = t0 + r * PER_WARP + group;
+                for (int c = 0; c < CHUNKS; ++c) unpack_eight(next[d][c], v[c]);
+                fetch(d);
                 float m = kLowest;                         // (a token whose logits are all -inf: every p is 0)
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) m = fmaxf(m, v[r][c][i]);
+                    for (int i = 0; i < 8; ++i) m = fmaxf(m, v[c][i]);
                 if (LANES == 32) m = warp_max(m);
                 else {
 #pragma unroll
@@ -239,9 +242,9 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
-                        const float2 y = halves(mul_pairs(add_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), minus_m), cc));
-                        v[r][c][i] = exp2_fast(y.x); v[r][c][i + 1] = exp2_fast(y.y);
-                        const unsigned long long p = pair_of(v[r][c][i], v[r][c][i + 1]);
+                        const float2 y = halves(mul_pairs(add_pairs(pair_of(v[c][i], v[c][i + 1]), minus_m), cc));
+                        v[c][i] = exp2_fast(y.x); v[c][i + 1] = exp2_fast(y.y);
+                        const unsigned long long p = pair_of(v[c][i], v[c][i + 1]);
                         totals = add_pairs(totals, p);
                         dots = fma_pairs(p, pair_of(f[c][i], f[c][i + 1]), dots);
                     }
@@ -251,23 +254,23 @@ __global__ void __launch_bounds__(kBalanceThreads, CHUNKS > 1 ? 2 : 3) k_balance
                 for (int o = LANES / 2; o; o >>= 1) { total += __shfl_xor_sync(kFullMask, total, o); dot += __shfl_xor_sync(kFullMask, dot, o); }
                 const float inv = total == 0.f ? 0.f : 1.f / total;
                 dot *= inv;
-                dots_of_step += dot;
-                if (gs && t < to) {
+                dots_of_steps += dot;
+                if (gs && i0 + group < n_tokens) {
                     const unsigned long long minus_dot = pair_of(-dot, -dot);
-                    const float by = counts[r] ? scale * inv : 0.f;
+                    const float by = counts ? scale * inv : 0.f;
                     const unsigned long long bb = pair_of(by, by);
 #pragma unroll
                     for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
                         for (int i = 0; i < 8; i += 2) {
-                            const float2 y = halves(mul_pairs(mul_pairs(pair_of(v[r][c][i], v[r][c][i + 1]), bb), add_pairs(pair_of(f[c][i], f[c][i + 1]), minus_dot)));
-                            v[r][c][i] = y.x; v[r][c][i + 1] = y.y;
+                            const float2 y = halves(mul_pairs(mul_pairs(pair_of(v[c][i], v[c][i + 1]), bb), add_pairs(pair_of(f[c][i], f[c][i + 1]), minus_dot)));
+                            v[c][i] = y.x; v[c][i + 1] = y.y;
                         }
-                        store_eight(gs + t * a.grad_stride + (c * LANES + place) * 8u, width_of(c), g_unit, v[r][c]);
+                        store_eight(g_at + c * (LANES * 8), width_of(c), g_unit, v[c]);
                     }
                 }
             }
-            sum += (double)dots_of_step;
+            sum += (double)dots_of_steps;
         }
         if (a.loss) {
             // every lane of a group has its tokens' sum: one lane of each

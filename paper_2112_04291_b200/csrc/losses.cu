@@ -284,7 +284,7 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
     if (blocks > kBalanceMaxBlocks) blocks = kBalanceMaxBlocks;
     // whole steps of a block: every group of lanes as many tokens
     const uint32_t lanes = a.experts <= 8u ? 1u : a.experts <= 16u ? 2u : a.experts <= 32u ? 4u : a.experts <= 64u ? 8u : a.experts <= 128u ? 16u : 32u;
-    const uint64_t step = (uint64_t)kBalanceWarps * (32u / lanes) * (a.experts <= 256u ? kBalanceRows<1> : kBalanceRows<2>);
+    const uint64_t step = (uint64_t)kBalanceWarps * (32u / lanes);
     a.rows_per_block = (uint32_t)((rows_per_block(a.tokens, 1u, blocks) + step - 1) / step * step);
     void* kargs[] = {&a};
     const unsigned grid = (unsigned)((a.tokens + a.rows_per_block - 1) / a.rows_per_block);
