@@ -59,7 +59,7 @@ struct DistillShared {
     unsigned long long ready[2], done[2], met[2];          // the row's pairs are known; its gradient is written; every block's sums are there
     Claim  claim;                                          // of the first block: the cluster's next row
     int    next[2];                                        // the others': what the first has been given
-    unsigned long long next_bar;
+    unsigned long long told[2];                            // (two: the first block may be a turn ahead of another's pairs' warp)
 };
 // dynamic: uint4 ring[kept][threads], then for each of two rows key, t (later e), z of every pair, then for each of two rows a byte per
 // vector of the slice, one for the elements before and one for those behind the vectors: which of the elements are keys of the row
@@ -76,9 +76,9 @@ __host__ __device__ inline size_t distill_smem(uint32_t kept, uint32_t k, uint32
 }
 
 // the warps that go through the row wait for one another
-__device__ __forceinline__ void sync_readers() { asm volatile("bar.sync 1, %0;" ::"n"(kDistillThreads) : "memory"); }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void sync_readers() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(kDistillThreads) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { __syncwarp(); asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // A block's share of a row: vectors [first, first + count) behind the row's head; the first block has the head, too, the last one the tail.
 struct DistillSlice {
@@ -279,6 +279,8 @@ __device__ __forceinline__ void finish_pairs(const DistillArgs& a, uint64_t row,
 // reads go on while gradients are written, and no barrier stands between a copy and its use.  (Vectors beyond the shared memory, of
 // rows above half a megabyte, are read twice.)  The ninth warp has the pairs: those of the next row while the others go through this
 // one, and the keys' gradients of the row before.
+// Every wait has a limit.  What a warp may overwrite is what others have told it that they are done with: where such a wait runs out the
+// pairs' warp leaves its rows as they are and ends, and then those that wait for it do; sums that never came make the row's loss NaN.
 template <class TZ, class TG, int MODE>
 __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     extern __shared__ __align__(16) unsigned char distill_smem_bytes[];
@@ -299,9 +301,8 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     if (warp == (uint32_t)kDistillWarps) {
         for (uint32_t i = lane; i < map_bytes / 2u; i += 32u) reinterpret_cast<uint32_t*>(maps)[i] = 0u;
         if (lane == 0) {
-            for (int b = 0; b < 2; ++b) { mbar_init(&s.ready[b], 1u); mbar_init(&s.done[b], kDistillWarps); mbar_init(&s.met[b], blocks); }
+            for (int b = 0; b < 2; ++b) { mbar_init(&s.ready[b], 1u); mbar_init(&s.done[b], kDistillWarps); mbar_init(&s.met[b], blocks); mbar_init(&s.told[b], 1u); }
             claim_init(s.claim);
-            mbar_init(&s.next_bar, 1u);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -319,8 +320,10 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                     if (rank == 0u) {
                         next = claim_answer(s.claim, i);
                         if (next >= 0) { next /= (int)blocks; claim_ask(s.claim); }
-                        for (uint32_t to = 1u; to < blocks; ++to) { *cluster.map_shared_rank(&s.next[b], to) = next; mbar_arrive_at(&s.next_bar, to); }
-                    } else if (mbar_wait_cluster(&s.next_bar, b)) next = s.next[b];
+                        // (it is here once row i - 2's gradient is written, to which every block has contributed after it had read
+                        // what it was told then: that place and its barrier are free)
+                        for (uint32_t to = 1u; to < blocks; ++to) { *cluster.map_shared_rank(&s.next[b], to) = next; mbar_arrive_at(&s.told[b], to); }
+                    } else if (mbar_wait_cluster(&s.told[b], i >> 1 & 1u)) next = s.next[b];
                 }
                 next = __shfl_sync(kFullMask, next, 0);
                 if (next >= 0 && lane == 0) {
@@ -332,7 +335,11 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.ready[b]);
             if (last >= 0) {
-                mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u);
+                if (!__all_sync(kFullMask, mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u))) {
+                    // (given up: what the others still read stays as it is)
+                    if (a.claims && rank == 0u && lane == 0 && next >= 0) claim_answer(s.claim, i + 1u);
+                    break;
+                }
                 if (MODE == kLossOnly && blocks == 1u) {
                     const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)last * a.z_stride;
                     ExpSum e = join_warps(s.join[o], a.c);
@@ -382,7 +389,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
     for (uint32_t i = 0u;; ++i) {
         const uint32_t b = i & 1u, parity = i >> 1 & 1u;
-        mbar_wait(&s.ready[b], parity);
+        if (!__all_sync(kFullMask, mbar_wait(&s.ready[b], parity))) break;
         const DistillRow& r = s.row[b];
         if (r.flags & kRowNone) break;
         const uint64_t row = r.row;
@@ -485,7 +492,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 cluster.map_shared_rank(&s, tid)->peer[b][rank] = make_float4(e.m, e.s, r.ksum, 0.f);
                 mbar_arrive_at(&s.met[b], tid);
             }
-            mbar_wait_cluster(&s.met[b], parity);
+            const bool met = __all_sync(kFullMask, mbar_wait_cluster(&s.met[b], parity));
             // (eight places, of which the cluster has one, two, four or all)
             const float4 p = s.peer[b][lane % blocks];
             sums.m = warp_max(p.x);
@@ -495,6 +502,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 sums.s += __shfl_xor_sync(kFullMask, sums.s, o);
                 sums.ksum += __shfl_xor_sync(kFullMask, sums.ksum, o);
             }
+            if (!met) sums.s = NAN;
         }
         if (MODE == kGradOnly) { sums.m = r.m; sums.s = r.s; }
         if (tid == 0) s.sums[b] = sums;
@@ -553,6 +561,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.done[b]);
     }
+    wait_copies<0>();
     if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
 }
 

@@ -381,6 +381,41 @@ def test_distillation_is_the_same_every_time_and_on_another_stream():
     assert _same(loss, alone)
 
 
+@pytest.mark.parametrize("cols", [60_001, 128_000])
+def test_many_rows_of_several_blocks_beside_other_work(cols):
+    """Rows that two and more blocks share, handed out as blocks become free: what runs beside them delays some blocks and not others."""
+    rows, k = 3_001, 64
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    z = torch.randn((rows, cols), generator=gen, device="cuda").to(torch.bfloat16)
+    keys = torch.randint(0, cols, (rows, k), generator=gen, device="cuda", dtype=torch.int32)
+    values = torch.randn((rows, k), generator=gen, device="cuda")
+    tail = torch.rand(rows, generator=gen, device="cuda") * 0.9
+    side, other = torch.cuda.Stream(), torch.randn(3_000_000, device="cuda")
+    first = None
+    for turn in range(12):
+        loss, grad = torch.full((rows,), MARK, device="cuda"), torch.empty_like(z)
+        torch.cuda.synchronize()
+        for _ in range(turn):
+            with torch.cuda.stream(side):
+                for n in (300, 3_000_000, 60_000):
+                    other[:n] = other[:n] * 0.5 + 1.0
+        assert binding.distill_loss(z, keys, values, loss=loss, grad=grad, tail=tail) == 0
+        for _ in range(4 * turn):
+            with torch.cuda.stream(side):
+                for n in (60_000, 300, 3_000_000):
+                    other[:n] = other[:n] * 0.5 + 1.0
+        torch.cuda.synchronize()
+        if first is None:
+            first = loss, grad
+        assert _same(loss, first[0]) and _same(grad, first[1])
+    for r in (0, 1_500, rows - 1):
+        want_loss, want_grad, grad_err, loss_err = ref.distill(z[r:r + 1].double().cpu().numpy(), keys[r:r + 1].cpu().numpy(), values[r:r + 1].double().cpu().numpy(), 1.0,
+                                                               tail[r:r + 1].double().cpu().numpy())
+        assert abs(loss[r].item() - want_loss[0]) <= loss_err[0]
+        off = np.abs(grad[r].double().cpu().numpy() - want_grad[0])
+        assert np.all(off <= grad_err[0] + ref.HALF_STEP["bf16"] * (np.abs(want_grad[0]) + grad_err[0]) + 2.0 ** -120)
+
+
 def test_rows_beyond_two_to_the_31_elements():
     """Offsets of the last rows pass 32 bits: 2.2 G elements of bf16, gradient in place."""
     rows, cols, k = 17_200, 128_003, 5
