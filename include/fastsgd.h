@@ -274,7 +274,8 @@ int fastsgd_key_encode_paper(const uint32_t* keys, uint64_t d, uint32_t flag_bit
 
 /* ---- where a worker's gradient begins: losses on logits, and their data as key-value pairs ----------
  * (No counterpart in the paper, whose models end in a logistic or linear loss: these are the losses of
- * models whose gradients are compressed today.)  All of them only enqueue kernels on `stream`.
+ * models whose gradients are compressed today.)  All of them only enqueue kernels on `stream`.  Those without a
+ * workspace may run on several streams at once.
  */
 
 /* element types of logits and of their gradients */
@@ -285,7 +286,7 @@ int fastsgd_key_encode_paper(const uint32_t* keys, uint64_t d, uint32_t flag_bit
 /* rows of logits, or of their gradient (host struct, device data) */
 typedef struct fastsgd_matrix {
     void*    data;        /* aligned to its type; rows may begin at any element               */
-    uint64_t rows;        /* 0 .. 2^31 - 1; no row: the call checks its arguments and does nothing else */
+    uint64_t rows;        /* 0 .. 2^31 - 1; 0: nothing is read (a balance loss is then 0)  */
     uint64_t cols;        /* 1 .. 2^31 - 1                                                    */
     uint64_t row_stride;  /* elements from one row to the next, cols .. 2^31 - 1; what lies between is not touched */
     uint32_t type;        /* FASTSGD_F32, FASTSGD_BF16 or FASTSGD_F16                          */
@@ -298,7 +299,7 @@ typedef struct fastsgd_matrix {
  *   k       1 .. min(V, 1024)
  *   keys    device, rows * k: column numbers in descending order of their values, equal values in ascending order of
  *           their columns (NaN above everything, -0 equal to +0)
- *   values  device, rows * k, the logits' type: their values
+ *   values  device, rows * k, the logits' type: their values (-0 as +0, any NaN as the same one)
  *   lse     device, rows floats, or NULL: log sum_j exp(z_j / temperature) of the row
  *   tail    device, rows floats, or NULL: the share of that sum outside the k pairs (formed from them alone: no
  *           difference of nearly equal numbers)
@@ -325,7 +326,8 @@ typedef struct fastsgd_pairs {
  *   grad[r, j] = d loss[r] / d z[r, j] = weight[r] T ( q_j - sum of p_i over the pairs with key_i = j )  for a key j
  *                                        weight[r] T q_j (1 - tail / rest)                               else
  * Without a tail the teacher's probability is that of the pairs alone, and the loss is the divergence from them to q.
- *   student  rows x V, V <= 2^20 (else FASTSGD_E_NOT_IMPLEMENTED)
+ *   student  rows x V, V <= 2^20 (else FASTSGD_E_NOT_IMPLEMENTED); a row takes 1, 2, 4 or 8 blocks, and rows times blocks
+ *            stay below 2^31 (else FASTSGD_E_BAD_N)
  *   temperature  T, 2^-20 .. 2^20
  *   weight   device, rows floats, or NULL (1): 1 / rows for the mean; a row of weight 0 (padding) is not read
  *   loss     device, rows floats, or NULL
@@ -337,6 +339,9 @@ typedef struct fastsgd_pairs {
  * At least one of loss, stats and grad is wanted.
  * A row of weight 0, without a pair that is there, whose pairs all have value -inf, or whose logits are all -inf counts for
  * nothing: loss 0, gradient 0.  Where the student rules out (-inf) what the teacher gives probability to, the loss is +inf.
+ * The sums run in fp32 from the largest logit down; the logits' types are widened exactly, and a gradient of 16 bits is
+ * rounded once.  The kernel's waits within a row have a limit of some seconds, as the other launches' have; where one ran
+ * out the row's loss is NaN.
  * Pairs may come in any order, and keys may repeat.  One launch; the sums' order depends on the sizes, the alignment and on
  * whether there is a gradient to write, and on nothing else.
  */
@@ -376,7 +381,8 @@ int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, 
  *   logits     cols = experts, 1 .. 1024
  *   mask, offsets, segments (1 .. 2^24), counts, counted   as for fastsgd_expert_counts
  *   grad_loss  device, segments floats, or NULL (1)
- *   loss       device, segments floats, or NULL; needs a workspace of 2 MiB + 8 (2048 + segments) bytes, whatever the tokens
+ *   loss       device, segments floats, or NULL; needs a workspace of 2 MiB + 8 (2048 + segments) bytes, whatever the tokens,
+ *              and is serialised with the other calls that use it; without a loss the call uses none
  *   grad       tokens x experts, or NULL: type and place as for fastsgd_distill_loss.  Zero for tokens that do not count; rows
  *              of tokens that belong to no segment are left as they are.
  * A segment without counted tokens or without selections has loss 0 and gradient 0; so has a token whose logits are all -inf.

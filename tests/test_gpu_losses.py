@@ -136,6 +136,53 @@ def test_top_logits_sums_are_the_same_every_time(dtype, cols, k):
             assert _same(a, b[:1].expand_as(b).contiguous())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cols,k", [(40, 6), (5_000, 6), (70_000, 200)])
+def test_top_logits_have_one_zero_and_one_nan(dtype, cols, k):
+    z = torch.full((2, cols), -1.0, device="cuda").to(TYPES[dtype])
+    words = z.view(torch.int32 if dtype == "fp32" else torch.int16)
+    words[:, 5] = -2 ** 31 if dtype == "fp32" else -2 ** 15                    # -0
+    z[:, 9] = 0.0
+    words[1, 7], words[1, 11] = (-3, 0x7FC00123) if dtype == "fp32" else (-3, 0x7FFD)      # NaN, of either sign
+    keys, values, lse, tail = _run_top(z, k, 1.0)
+    assert keys[0, :2].tolist() == [5, 9] and keys[1, :4].tolist() == [7, 11, 5, 9]
+    bits = values.view(words.dtype)
+    assert bits[0, :2].tolist() == [0, 0] and bits[1, 2:4].tolist() == [0, 0]
+    assert bool(values[1, :2].isnan().all()) and bits[1, 0] == bits[1, 1]
+    assert bool((values[:, 4:] == -1.0).all()) and bool(lse[1].isnan()) and bool(tail[1].isnan())
+
+
+def test_calls_on_two_streams_at_once():
+    """They share nothing: neither a workspace nor anything the library keeps."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    z = [torch.randn((700, 50_001), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    x = [torch.randn((5_000, 60), generator=gen, device="cuda") for _ in range(2)]
+
+    def all_calls(i):
+        keys, values = torch.empty((700, 64), dtype=torch.int32, device="cuda"), torch.empty((700, 64), dtype=torch.bfloat16, device="cuda")
+        lse, tail, loss, grad = torch.empty(700, device="cuda"), torch.empty(700, device="cuda"), torch.empty(700, device="cuda"), torch.empty_like(z[i])
+        chosen, weights = torch.empty((5_000, 6), dtype=torch.int32, device="cuda"), torch.empty((5_000, 6), device="cuda")
+        counts, counted, slope = torch.empty((1, 60), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda"), torch.empty_like(x[i])
+        assert binding.top_logits(z[i], keys, values, lse=lse, tail=tail) == 0
+        assert binding.distill_loss(z[1 - i], keys, values, loss=loss, grad=grad, tail=tail) == 0
+        assert binding.top_logits(x[i], chosen, weights) == 0
+        assert binding.expert_counts(chosen, counts, counted) == 0
+        assert binding.balance_loss(x[i], counts, counted, grad=slope) == 0
+        return keys, values, lse, tail, loss, grad, chosen, weights, counts, counted, slope
+
+    alone = [all_calls(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        both = []
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                both.append(all_calls(i))
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(_same(a, b) for a, b in zip(alone[i], both[i]))
+
+
 def test_top_logits_optional_outputs_and_no_rows():
     z = torch.randn(3, 500, device="cuda")
     keys, values = torch.empty(3, 4, dtype=torch.int32, device="cuda"), torch.empty(3, 4, device="cuda")
