@@ -99,6 +99,12 @@ template <class T> const void* top_rows_kernel_of(uint32_t cols) {
     return cols <= 32u ? (const void*)k_top_rows<T, 1> : cols <= 64u ? (const void*)k_top_rows<T, 2> : cols <= 128u ? (const void*)k_top_rows<T, 4>
          : cols <= 256u ? (const void*)k_top_rows<T, 8> : cols <= 512u ? (const void*)k_top_rows<T, 16> : (const void*)k_top_rows<T, 32>;
 }
+template <class T> const void* top_lanes_kernel_of(uint32_t width) {
+    return width == 8u ? (const void*)k_top_lanes<T, 8> : width == 16u ? (const void*)k_top_lanes<T, 16> : (const void*)k_top_lanes<T, 32>;
+}
+const void* top_lanes_kernel(uint32_t type, uint32_t width) {
+    return type == FASTSGD_F32 ? top_lanes_kernel_of<float>(width) : type == FASTSGD_BF16 ? top_lanes_kernel_of<__nv_bfloat16>(width) : top_lanes_kernel_of<__half>(width);
+}
 const void* top_rows_kernel(uint32_t type, uint32_t cols) {
     return type == FASTSGD_F32 ? top_rows_kernel_of<float>(cols) : type == FASTSGD_BF16 ? top_rows_kernel_of<__nv_bfloat16>(cols) : top_rows_kernel_of<__half>(cols);
 }
@@ -187,6 +193,19 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
     void* kargs[] = {&a};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a.cols <= kTopRowsMaxCols && k <= kTopRowsMaxPairs) {
+        // A lane per row takes as long for 32 rows of a warp as for one: worth it from 1024 rows a column that it has registers for
+        // (us, a warp against a lane per row: 2048 x 8, k = 2: 1.8, 2.0; 8192 x 8: 2.9, 2.0; 8192 x 16: 2.9, 3.4; 32768 x 16: 7.9, 3.6;
+        // 8192 x 32: 2.9, 5.4; 32768 x 32, k = 1, 8, 16: 7.4, 10.6, 14.5 and 5.0, 10.4, 16.5; 65536 x 32, k = 8: 19.8, 12.2; 65536 x 64, k = 8:
+        // 24.9, 30.6 with 64 registers of ranks).
+        const uint32_t width = a.cols <= 8u ? 8u : a.cols <= 16u ? 16u : 32u;
+        if (a.cols <= width && a.rows >= 1024u * width) {
+            const unsigned grid = (unsigned)((a.rows + kTopLanesThreads - 1) / kTopLanesThreads);
+            return launched(launch_overlapped(top_lanes_kernel(logits->type, width), grid, kTopLanesThreads, 0, kargs, st));
+        }
+        // One by one each pair costs five instructions a value of a lane (four or eight and more of them); by the bar it is one, after some
+        // 150, and above 16 pairs more than 32 candidates become likely (us, one by one against the bar, 65536 x 128, k = 4, 6, 16: 26.1, 31.0, 55.9
+        // and 26.6, 29.7, 44.1; 65536 x 256, k = 2, 4, 8, 16, 32: 32.4, 41.7, 61.2, 101.7, 183 and 34.3, 36.8, 42.6, 55.3, 214).
+        a.by_bar = k <= 16u && (a.cols > 128u ? k >= 4u : a.cols > 64u && k >= 6u);
         const unsigned grid = (unsigned)((a.rows + kTopRowsThreads / 32 - 1) / (kTopRowsThreads / 32));
         return launched(launch_overlapped(top_rows_kernel(logits->type, a.cols), grid, kTopRowsThreads, 0, kargs, st));
     }

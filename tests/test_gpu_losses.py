@@ -137,6 +137,33 @@ def test_top_logits_sums_are_the_same_every_time(dtype, cols, k):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols,k,gap,shift", [(8_192, 1, 1, 0, 0), (8_300, 7, 3, 2, 5), (8_191, 8, 2, 0, 0), (8_192, 8, 8, 0, 8), (16_390, 16, 2, 0, 0), (16_401, 13, 13, 0, 1),
+                                                   (32_800, 32, 4, 0, 4), (32_769, 27, 9, 5, 3)])
+def test_top_logits_of_many_short_rows(dtype, rows, cols, k, gap, shift):
+    z = _logits(np.random.default_rng([rows, cols, k]), rows, cols, dtype)
+    z[::7, cols // 2:] = z[::7, :1]                        # equal values
+    z[3::11, :cols // 2] = -np.inf
+    z[5], z[rows - 1, 0], z[rows - 2, cols - 1] = -np.inf, np.nan, np.inf
+    store, view = _strided(z, dtype, gap, shift)
+    _check_top(z, view, k, 0.8)
+    assert _untouched(store, view)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cols,k", [(65, 6), (100, 16), (128, 16), (129, 4), (256, 16), (257, 5), (777, 16), (1024, 9)])
+def test_top_logits_of_few_columns_with_few_different_values(dtype, cols, k):
+    """From all different to all alike: few and many values as large as the k-th."""
+    rng = np.random.default_rng([cols, k])
+    z = _logits(rng, 60, cols, dtype)
+    for r in range(60):
+        levels = _logits(rng, 1, 1 + r // 2, dtype)[0]
+        if r % 2 == 0:
+            z[r] = levels[rng.integers(0, len(levels), cols)]
+    z[1, 3:], z[3, 1::2], z[7, 32:] = -np.inf, -np.inf, -np.inf
+    _check_top(z, _strided(z, dtype)[1], k)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("cols,k", [(40, 6), (5_000, 6), (70_000, 200)])
 def test_top_logits_have_one_zero_and_one_nan(dtype, cols, k):
     z = torch.full((2, cols), -1.0, device="cuda").to(TYPES[dtype])
