@@ -258,37 +258,11 @@ __device__ __forceinline__ unsigned long long fma_pairs(unsigned long long a, un
     return r;
 }
 
-// The same sum, of vectors: four partial sums, two operations at a time.  raise() before add(), with the maximum of what is added.
-struct ExpSums {
-    float m;
-    unsigned long long s[2];
-    __device__ __forceinline__ ExpSums() : m(kLowest), s{0ull, 0ull} {}
-    __device__ __forceinline__ void raise(float top, float c, float slack) {
-        if (top > m + slack) {
-            const float f = exp2_fast((m - top) * c);
-            s[0] = mul_pairs(s[0], pair_of(f, f)); s[1] = mul_pairs(s[1], pair_of(f, f));
-            m = top;
-        }
-    }
-    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float c) {
-        const unsigned long long minus_m = pair_of(-m, -m), cc = pair_of(c, c);
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 y = halves(mul_pairs(add_pairs(pair_of(x[i], x[i + 1]), minus_m), cc));
-            s[i / 2 & 1] = add_pairs(s[i / 2 & 1], pair_of(exp2_fast(y.x), exp2_fast(y.y)));
-        }
-    }
-    __device__ __forceinline__ ExpSum whole() const {
-        const float2 p = halves(add_pairs(s[0], s[1]));
-        ExpSum e;
-        e.m = m; e.s = p.x + p.y;
-        return e;
-    }
-};
 // |m| c of 2^26 and more: m c rounded to fp32 would be off by 2 and more.
 __device__ __forceinline__ bool is_far(float m, float c) { return !(fabsf(m) * c < 67108864.f); }
 
-// The same with one fused operation for the argument: 2^(x c - r), r = m c rounded, which whole() makes up for.  Where m is far the
+// The same sum, of vectors: four partial sums, two operations at a time; raise() before add(), with the maximum of what is added.  The
+// argument takes one fused operation: 2^(x c - r), r = m c rounded, which whole() makes up for.  Where m is far the
 // sum is 0 instead: next to a largest value that is not far, what it would hold is 0 indeed; where the row's largest value is far, or
 // its sum 0, the caller takes the sum the other way.
 struct FusedExpSums {

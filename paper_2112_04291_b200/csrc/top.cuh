@@ -189,9 +189,9 @@ __global__ void __launch_bounds__(kTopLanesThreads) k_top_lanes(TopArgs a) {
 // exponentials are summed and it is forgotten.  The others are listed, warp by warp, and at the end their elements above the bar
 // become candidates, while the others join the sum; the k-th largest candidate is found by histograms of eight bits.  The order in which
 // candidates are found changes no sum: those that turn out to be no pairs are added as integers.
-// Top 64 of 2048 x 128000 bf16 with lse and tail: 170 us, 3.1 TB/s (525 MB; a copy's time 80).  Bound by instructions: the largest of a
-// vector costs it five, each element three for its exponential, and the selection at the end some 10 us a row of which other blocks of
-// the SM hide a part.  Every value against a list: 2655; a bar that rises from nothing in place of the sample: 284; all candidates kept
+// Top 64 of 2048 x 128000 bf16 with lse and tail: 170 us, 3.1 TB/s (525 MB; a copy's time 80).  Neither DRAM (33 %) nor the issue slots
+// (47 %, 13 instructions an element and lane) are full: 24 warps an SM wait for their tiles, and for one another in the selection at a row's
+// end, of which the other blocks of the SM hide a part.  Every value against a list: 2655; a bar that rises from nothing in place of the sample: 284; all candidates kept
 // in one place, a barrier a tile: 245.  One row of 128000 over a cluster of eight blocks: 10.3 us (one block: 91, one barrier fewer a step
 // of the selection than before: 16).
 //
