@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(kCountThreads) k_add_expert_counts(CountArgs a
     }
 }
 
-// 65536 x 256 bf16 with its gradient and the counts of 8 experts a token: 26 us in three launches (67 MB and 2 MB; a copy's time 10.6): the
-// launches 6, k_balance about 15, issue-bound: some 150 instructions a warp and token for two exponentials' worth of memory.  A warp
-// per token whatever the width: 81; the next tokens' logits not ahead: 34.  30001 x 60 fp16 in 37 ragged segments: 20.6 us.
+// 65536 x 256 bf16 with its gradient: 16 us, 4.2 TB/s (67 MB; a copy's time 10.2), with the counts of 8 experts a token 23 us in three launches.
+// Bound by issue slots (57 %) and latency: 16 warps an SM.  A warp per token whatever the width: 81 with the counts; the next tokens' logits not
+// ahead: 34; eight experts a lane: 26 (the reductions over lanes, and all that a token costs once, are then spread over half as many values).
 // A block per run of tokens; LANES lanes share a token, each with CHUNKS times eight neighbouring experts, whose f it keeps in
 // registers.  The logits of the next few tokens are on their way while those at hand are worked on (of one step ahead alone, 24 warps an
 // SM had 24 KB in flight, half of what the memory's latency takes).

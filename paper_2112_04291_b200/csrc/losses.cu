@@ -82,9 +82,19 @@ template <int MODE> const void* distill_kernel(uint32_t z, uint32_t g) {
     if (z == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_distill<__nv_bfloat16, float, MODE> : (const void*)k_distill<__nv_bfloat16, __nv_bfloat16, MODE>;
     return g == FASTSGD_F32 ? (const void*)k_distill<__half, float, MODE> : (const void*)k_distill<__half, __half, MODE>;
 }
+// Lanes that share a token: with 16 of its experts each, where that is quicker than 8 (us for 65536 tokens with 8, with 16: bf16 x 16: 6.5, 6.0, x 64:
+// 10.1, 7.9, x 256: 21.0, 16.1; fp32 x 16: 6.6, 7.0, x 32: 7.7, 8.0, x 64: 10.4, 9.7, x 256: 26.7, 23.0).
+uint32_t balance_lanes(uint32_t type, uint32_t experts) {
+    const uint32_t each = experts > 8u && (type != FASTSGD_F32 || experts > 32u) ? 16u : 8u;
+    uint32_t lanes = 1u;
+    while (lanes < 32u && lanes * each < experts) lanes *= 2u;
+    return lanes;
+}
 template <class T, class TG> const void* balance_kernel_of(uint32_t experts) {
-    return experts <= 8u ? (const void*)k_balance<T, TG, 1, 1> : experts <= 16u ? (const void*)k_balance<T, TG, 2, 1> : experts <= 32u ? (const void*)k_balance<T, TG, 4, 1>
-         : experts <= 64u ? (const void*)k_balance<T, TG, 8, 1> : experts <= 128u ? (const void*)k_balance<T, TG, 16, 1> : experts <= 256u ? (const void*)k_balance<T, TG, 32, 1>
+    if (experts <= 8u) return (const void*)k_balance<T, TG, 1, 1>;
+    if (sizeof(T) == 4 && experts <= 32u) return experts <= 16u ? (const void*)k_balance<T, TG, 2, 1> : (const void*)k_balance<T, TG, 4, 1>;
+    return experts <= 16u ? (const void*)k_balance<T, TG, 1, 2> : experts <= 32u ? (const void*)k_balance<T, TG, 2, 2> : experts <= 64u ? (const void*)k_balance<T, TG, 4, 2>
+         : experts <= 128u ? (const void*)k_balance<T, TG, 8, 2> : experts <= 256u ? (const void*)k_balance<T, TG, 16, 2>
          : experts <= 512u ? (const void*)k_balance<T, TG, 32, 2> : (const void*)k_balance<T, TG, 32, 4>;
 }
 const void* balance_kernel(uint32_t x, uint32_t g, uint32_t experts) {
@@ -302,7 +312,7 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
     if (rc) return rc;
     if (blocks > kBalanceMaxBlocks) blocks = kBalanceMaxBlocks;
     // whole steps of a block: every group of lanes as many tokens
-    const uint32_t lanes = a.experts <= 8u ? 1u : a.experts <= 16u ? 2u : a.experts <= 32u ? 4u : a.experts <= 64u ? 8u : a.experts <= 128u ? 16u : 32u;
+    const uint32_t lanes = balance_lanes(logits->type, a.experts);
     const uint64_t step = (uint64_t)kBalanceWarps * (32u / lanes);
     a.rows_per_block = (uint32_t)((rows_per_block(a.tokens, 1u, blocks) + step - 1) / step * step);
     void* kargs[] = {&a};
