@@ -305,6 +305,7 @@ typedef struct fastsgd_matrix {
  *           difference of nearly equal numbers)
  *   temperature  2^-20 .. 2^20; bears on lse and tail only
  * A row of -inf has lse = -inf and tail = 0; NaN or +inf in a row makes both NaN.
+ * One launch; the sums' order depends on the sizes (the number of rows among them), the type and the alignment alone.
  */
 int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperature, int32_t* keys, void* values,
                        float* lse, float* tail, void* stream);
@@ -386,7 +387,7 @@ int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, 
  *   grad       tokens x experts, or NULL: type and place as for fastsgd_distill_loss.  Zero for tokens that do not count; rows
  *              of tokens that belong to no segment are left as they are.
  * A segment without counted tokens or without selections has loss 0 and gradient 0; so has a token whose logits are all -inf.
- * One launch; the order of the sums depends on the sizes and offsets alone.
+ * One launch; the order of the sums depends on the sizes, the type and the offsets alone.
  */
 int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, const uint64_t* offsets, uint32_t segments,
                          const uint32_t* counts, const uint32_t* counted, float coef, const float* grad_loss,
