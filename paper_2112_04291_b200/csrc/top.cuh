@@ -504,6 +504,8 @@ __device__ __noinline__ unsigned long long collect_carefully(TopShared<MOST>& s,
             if (n > MOST) cut = cut_candidates(s, step, n, k, cut);
         }
     }
+    for (int h = 0; h < 3; ++h) s.hist[h][tid] = 0u;       // (the bar's steps have left some; the caller's count of steps goes on from anywhere)
+    __syncthreads();
     return cut;
 }
 // ... and the sum of what lies below its last pair, whatever the logits.

@@ -1,0 +1,41 @@
+"""Top logits, the distillation loss and the router's counts where their quick ways end: values that mislead the sample of a row, NaN that comes
+before any finite value, logits at the border of what the fused exponential takes, segments that no single cluster counts."""
+import numpy as np
+import pytest
+import torch
+
+import loss_ref as ref
+from paper_2112_04291_b200 import binding
+from test_gpu_losses import MARK, TYPES, _check_distill, _dev, _logits, _run_top, _same
+
+pytestmark = pytest.mark.gpu
+
+
+def _check_repeated_top(rows, repeats, k, dtype, temperature=1.0):
+    """Each of `rows` many times over, in a mixed order: every copy has the pairs, the sum and the tail of the definition."""
+    which = np.random.default_rng(k).permutation(np.repeat(np.arange(rows.shape[0]), repeats))
+    keys, values, lse, tail = _run_top(_dev(rows, TYPES[dtype])[torch.from_numpy(which).cuda()].contiguous(), k, temperature)
+    want_keys, want_values, want_lse, want_tail = ref.top(rows, k, temperature)
+    assert np.array_equal(keys.cpu().numpy(), want_keys[which])
+    assert np.array_equal(values.double().cpu().numpy(), want_values[which])
+    # an exponential is off by EX2 + 3 U |d|, a sum by (cols / 512 + 40) U; m / T, a logarithm and their sum by half a step each
+    d = np.minimum((rows.max(1) - rows.min(1)) / temperature, 104.0)
+    unit = (ref.EX2 + (3.0 * d + rows.shape[1] / 512.0 + 40.0) * ref.U)[which]
+    size = (np.abs(rows.max(1)) / temperature + np.log(rows.shape[1]) + np.abs(want_lse))[which]
+    assert np.all(np.abs(lse.double().cpu().numpy() - want_lse[which]) <= unit + 4.0 * ref.U * size)
+    assert np.all(np.abs(tail.double().cpu().numpy() - want_tail[which]) <= 2.0 * unit * want_tail[which] + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("tiles,k", [(2, 300), (2, 700), (3, 300), (4, 60), (6, 40), (4, 300), (4, 1000)])
+def test_top_logits_whose_largest_lie_in_the_sample(dtype, tiles, k):
+    """Fewer than k values reach the bar that the sample of a row suggests (pieces of 512 bytes, every tiles-th one): the row is gone through again."""
+    n = 16 // TYPES[dtype].itemsize
+    cols, rng = tiles * 1024 * n, np.random.default_rng([tiles, k])
+    vectors = np.arange(tiles * 1024)
+    vectors = vectors[vectors // 32 % tiles == 0]
+    z = _logits(rng, 12, cols, dtype)
+    for r, count in enumerate(np.linspace(k // 5, k - 1, 12).astype(int)):
+        chosen = rng.choice(vectors, min(count, len(vectors)), replace=False)
+        z[r, chosen * n + rng.integers(0, n, len(chosen))] += 40.0
+    _check_repeated_top(torch.from_numpy(z).to(TYPES[dtype]).double().numpy(), 50, k, dtype)
