@@ -264,16 +264,21 @@ __device__ __forceinline__ bool is_far(float m, float c) { return !(fabsf(m) * c
 // The same sum, of vectors: four partial sums, two operations at a time; raise() before add(), with the maximum of what is added.  The
 // argument takes one fused operation: 2^(x c - r), r = m c rounded, which whole() makes up for.  Where m is far the
 // sum is 0 instead: next to a largest value that is not far, what it would hold is 0 indeed; where the row's largest value is far, or
-// its sum 0, the caller takes the sum the other way.
+// its sum 0, the caller takes the sum the other way.  A NaN that was added stays: r is finite, so that no other value gives one.
 struct FusedExpSums {
     float m, r;
     unsigned long long s[2];
     __device__ __forceinline__ FusedExpSums() : m(kLowest), r(kLowest), s{0ull, 0ull} {}
+    static __device__ __forceinline__ float nan_or_zero(float x) { return x != x ? x : 0.f; }
     __device__ __forceinline__ void raise(float top, float c, float slack) {
         if (top > m + slack) {
-            const float now = top * c, f = exp2_fast(r - now);
+            const float now = fminf(fmaxf(top * c, kLowest), -kLowest), f = exp2_fast(r - now);
             const bool far = is_far(m, c);                 // (the sum may be anything)
-            s[0] = far ? 0ull : mul_pairs(s[0], pair_of(f, f)); s[1] = far ? 0ull : mul_pairs(s[1], pair_of(f, f));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 p = halves(s[i]);
+                s[i] = far ? pair_of(nan_or_zero(p.x), nan_or_zero(p.y)) : mul_pairs(s[i], pair_of(f, f));
+            }
             m = top; r = now;
         }
     }
@@ -289,7 +294,7 @@ struct FusedExpSums {
         const float2 p = halves(add_pairs(s[0], s[1]));
         ExpSum e;
         e.m = m;
-        e.s = is_far(m, c) ? 0.f : (p.x + p.y) * exp2_fast(-__fmaf_rn(m, c, -r));
+        e.s = is_far(m, c) ? nan_or_zero(p.x + p.y) : (p.x + p.y) * exp2_fast(-__fmaf_rn(m, c, -r));
         return e;
     }
 };

@@ -39,3 +39,30 @@ def test_top_logits_whose_largest_lie_in_the_sample(dtype, tiles, k):
         chosen = rng.choice(vectors, min(count, len(vectors)), replace=False)
         z[r, chosen * n + rng.integers(0, n, len(chosen))] += 40.0
     _check_repeated_top(torch.from_numpy(z).to(TYPES[dtype]).double().numpy(), 50, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("tailed", [False, True])
+@pytest.mark.parametrize("cols,repeats", [(1_000, 40), (5_000, 40), (5_000, 1), (40_000, 40), (128_000, 1)])
+def test_no_nan_of_the_students_is_lost(dtype, tailed, cols, repeats):
+    """NaN that a thread meets before any finite value, beside -inf or alone; rows without NaN in between."""
+    rng = np.random.default_rng(cols)
+    n = 16 // TYPES[dtype].itemsize
+    z = _logits(rng, 7, cols, dtype)
+    z[0, :n - 1], z[0, n - 1] = -np.inf, np.nan                               # the first vector of a thread
+    z[1, :n] = np.nan
+    z[2, cols - n:] = np.nan                                                  # ... the last
+    front = min(4 * 256 * n, cols // 2)
+    z[3, :front] = -np.inf                                                    # all of a block's first vectors
+    z[3, front // 2 + 3] = np.nan
+    z[5, ::n] = np.nan
+    z[5, 1:] = np.where(rng.random(cols - 1) < 0.5, -np.inf, z[5, 1:])
+    z = np.tile(z, (repeats, 1))
+    rows = z.shape[0]
+    keys = np.stack([rng.choice(cols, 9, replace=False) for _ in range(rows)]).astype(np.int32)
+    values = rng.normal(0, 2, (rows, 9)).astype(np.float32)
+    # (keys with finite logits: those that the student rules out have their own test)
+    for r in range(rows):
+        fine = np.flatnonzero(np.isfinite(z[r]))
+        keys[r] = rng.choice(fine, 9, replace=False)
+    _check_distill(z, dtype, keys, values, 1.0, rng.uniform(0.05, 0.5, rows).astype(np.float32) if tailed else None)
