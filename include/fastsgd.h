@@ -340,7 +340,8 @@ typedef struct fastsgd_pairs {
  * At least one of loss, stats and grad is wanted.
  * A row of weight 0, without a pair that is there, whose pairs all have value -inf, or whose logits are all -inf counts for
  * nothing: loss 0, gradient 0.  Where the student rules out (-inf) what the teacher gives probability to, the loss is +inf.
- * NaN or +inf among the logits of any other row makes its loss and its gradient NaN.
+ * NaN or +inf among the logits of any other row makes its loss and its gradient NaN; among the values of its pairs that are there, its
+ * loss and the gradient of its keys.
  * The sums run in fp32 from the largest logit down; the logits' types are widened exactly, and a gradient of 16 bits is
  * rounded once.  The kernel's waits within a row have a limit of some seconds, as the other launches' have; where one ran
  * out the row's loss is NaN.

@@ -168,7 +168,7 @@ __device__ __forceinline__ void prepare_pairs(const DistillArgs& a, uint64_t row
     r.m = MODE == kGradOnly ? a.stats_in[2 * row] : 0.f;
     r.s = MODE == kGradOnly ? a.stats_in[2 * row + 1] : 0.f;
     float tm = -INFINITY, zm = kLowest;
-    bool again = false;
+    bool again = false, no_number = false;
     if (r.weight != 0.f) {
         for (uint32_t i0 = lane; i0 < k; i0 += 32u * U) {
             int key[U];
@@ -189,7 +189,7 @@ __device__ __forceinline__ void prepare_pairs(const DistillArgs& a, uint64_t row
                 const uint32_t i = i0 + 32u * u;
                 if (i >= k) continue;
                 s_key[i] = key[u]; s_t[i] = t[u]; s_z[i] = zk[u];
-                tm = fmaxf(tm, t[u]); zm = fmaxf(zm, zk[u]);
+                tm = fmaxf(tm, t[u]); zm = fmaxf(zm, zk[u]); no_number |= t[u] != t[u];
                 if (mapped && key[u] >= 0) {
                     const int b = key_bit<TZ>(q, (uint32_t)key[u], a.per, rank, blocks);
                     if (b >= 0) again |= atomicOr(reinterpret_cast<uint32_t*>(map) + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1u;
@@ -199,7 +199,8 @@ __device__ __forceinline__ void prepare_pairs(const DistillArgs& a, uint64_t row
     }
     tm = warp_max(tm); zm = warp_max(zm);
     again = __any_sync(kFullMask, again);
-    const bool counts = tm > -INFINITY;                    // weight 0, or no pair with any probability: the row counts for nothing
+    // weight 0, or no pair with any probability: the row counts for nothing (the largest does not show a NaN, which makes the row's sums NaN)
+    const bool counts = tm > -INFINITY || __any_sync(kFullMask, no_number);
     __syncwarp();
     float tsum = 0.f, cross = 0.f, ksum = 0.f;
     if (counts) {
@@ -247,7 +248,7 @@ __device__ __forceinline__ void finish_pairs(const DistillArgs& a, uint64_t row,
         if (!t.none) {
             // sum p_i (log p_i - log q_i): both logarithms relative to the largest of their kind
             const float log_total = logf(t.total), share = 1.f - r.tail;
-            if (share != 0.f) loss = share * (r.cross / r.tsum * a.inv_t + logf(share / r.tsum) + ((t.top - r.zm) * a.inv_t + log_total));
+            if (share != 0.f || r.tsum != r.tsum) loss = share * (r.cross / r.tsum * a.inv_t + logf(share / r.tsum) + ((t.top - r.zm) * a.inv_t + log_total));
             if (r.tail != 0.f) loss += r.tail * (logf(r.tail / e.s) - (e.m - t.top) * a.inv_t + log_total);
             loss *= r.weight * a.temperature * a.temperature;
         }

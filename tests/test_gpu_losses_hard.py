@@ -66,3 +66,23 @@ def test_no_nan_of_the_students_is_lost(dtype, tailed, cols, repeats):
         fine = np.flatnonzero(np.isfinite(z[r]))
         keys[r] = rng.choice(fine, 9, replace=False)
     _check_distill(z, dtype, keys, values, 1.0, rng.uniform(0.05, 0.5, rows).astype(np.float32) if tailed else None)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("tailed", [False, True])
+@pytest.mark.parametrize("k", [1, 2, 40])
+def test_a_teacher_of_nan_alone_is_no_row_that_counts_for_nothing(dtype, tailed, k):
+    rng = np.random.default_rng(k)
+    rows, cols = 6, 3_000
+    z = _logits(rng, rows, cols, dtype)
+    keys = np.stack([rng.choice(cols, k, replace=False) for _ in range(rows)]).astype(np.int32)
+    values = rng.normal(0, 2, (rows, k)).astype(np.float32)
+    values[0] = np.nan
+    values[1, 0], values[1, 1:] = np.nan, -np.inf
+    values[2], keys[2] = np.nan, -1                                           # (pairs that are not there may hold anything)
+    values[3] = -np.inf
+    values[4, -1] = np.nan
+    tail = rng.uniform(0.05, 0.5, rows).astype(np.float32) if tailed else None
+    if tailed:
+        tail[0] = 1.0
+    _check_distill(z, dtype, keys, values, 1.0, tail)
