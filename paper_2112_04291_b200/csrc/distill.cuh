@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 if (MODE == kLossOnly && blocks == 1u) {
                     const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)last * a.z_stride;
                     ExpSum e = join_warps(s.join[o], a.c);
-                    if ((s.row[o].flags & kRowCounts) && (e.s == 0.f || is_far(e.m, a.c)))
+                    if ((s.row[o].flags & kRowCounts) && (e.s == 0.f || may_miss_far(e.m, a.c)))
                         e = warp_join(scan_far(z, s.row[o].tail != 0.f ? maps + o * map_bytes : nullptr, a.cols, a.per, rank, blocks, a.c, a.slack, lane, 32u), a.c);
                     if (lane == 0) s.sums[o] = DistillSums{e.m, e.s, s.row[o].ksum};
                     __syncwarp();
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             }
             sync_readers();
             e = join_warps(s.join[b], a.c);
-            if (counts && (e.s == 0.f || is_far(e.m, a.c))) {
+            if (counts && (e.s == 0.f || may_miss_far(e.m, a.c))) {
                 sync_readers();
                 e = warp_join(scan_far(z, skip, a.cols, a.per, rank, blocks, a.c, a.slack, tid, kDistillThreads), a.c);
                 if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);

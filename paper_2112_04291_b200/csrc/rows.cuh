@@ -260,11 +260,14 @@ __device__ __forceinline__ unsigned long long fma_pairs(unsigned long long a, un
 
 // |m| c of 2^26 and more: m c rounded to fp32 would be off by 2 and more.
 __device__ __forceinline__ bool is_far(float m, float c) { return !(fabsf(m) * c < 67108864.f); }
+// ... of 2^25 and more: there may be something left next to m of a sum whose own largest value is far (neighbours of fp32 are 2^4 to 2^8 apart
+// there, and the value that a sum is relative to may be 2^40 below its largest).
+__device__ __forceinline__ bool may_miss_far(float m, float c) { return !(fabsf(m) * c < 33554432.f); }
 
 // The same sum, of vectors: four partial sums, two operations at a time; raise() before add(), with the maximum of what is added.  The
 // argument takes one fused operation: 2^(x c - r), r = m c rounded, which whole() makes up for.  Where m is far the
-// sum is 0 instead: next to a largest value that is not far, what it would hold is 0 indeed; where the row's largest value is far, or
-// its sum 0, the caller takes the sum the other way.  A NaN that was added stays: r is finite, so that no other value gives one.
+// sum is 0 instead: next to a largest value well below that border, what it would hold is 0 indeed; where the row's largest value may miss
+// something, or its sum is 0, the caller takes the sum the other way.  A NaN that was added stays: r is finite, so that no other value gives one.
 struct FusedExpSums {
     float m, r;
     unsigned long long s[2];

@@ -630,7 +630,7 @@ __global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_t
         // (of all that this block has seen, the first is the largest)
         const float m = have ? fmaxf(value_of_rank<T>((uint32_t)(s.cand[0] >> 32)), kLowest) : kLowest;
         if (sums) {
-            if (careful || is_far(m, a.c)) e = sum_carefully<T>(z, have == k ? s.cand[k - 1u] : 0ull, begin, end, a.c, a.slack);
+            if (careful || may_miss_far(m, a.c)) e = sum_carefully<T>(z, have == k ? s.cand[k - 1u] : 0ull, begin, end, a.c, a.slack);
             else e.join(dropped.m, dropped.s, a.c);
         }
 

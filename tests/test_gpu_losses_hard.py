@@ -86,3 +86,31 @@ def test_a_teacher_of_nan_alone_is_no_row_that_counts_for_nothing(dtype, tailed,
     if tailed:
         tail[0] = 1.0
     _check_distill(z, dtype, keys, values, 1.0, tail)
+
+
+@pytest.mark.parametrize("temperature", [1.0, 2.0 ** -20])
+@pytest.mark.parametrize("tailed", [False, True])
+@pytest.mark.parametrize("rows", [4, 200])
+def test_distillation_where_logits_become_far(temperature, tailed, rows):
+    """|z| log2(e) / T of 2^26, from where on a fused exponential is not trusted: neighbours of fp32 are 2^5.8 apart there."""
+    rng = np.random.default_rng(rows)
+    cols = 8_192
+    slot, thread = np.arange(cols) // 4 // 256, np.arange(cols) // 4 % 256
+    z = np.where(thread < 128, np.where(slot < 4, -46_516_320.0, -46_516_300.0), -46_516_308.0)
+    z = np.stack([z, z[::-1], np.where(thread < 128, -46_516_324.0, -46_516_316.0), rng.choice([-46_516_324.0, -46_516_320.0, -46_516_316.0, -46_516_312.0], cols)])
+    z = np.tile(z, (rows // 4, 1)) * temperature
+    keys = np.stack([rng.choice(cols, 5, replace=False) for _ in range(rows)]).astype(np.int32)
+    values = (rng.normal(0, 2, (rows, 5)) * temperature).astype(np.float32)
+    _check_distill(z, "fp32", keys, values, temperature, rng.uniform(0.05, 0.5, rows).astype(np.float32) if tailed else None)
+
+
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -20])
+def test_top_logits_where_logits_become_far(scale):
+    """... on the two sides of a bar, which is a value of 16 bits: the pairs are not far, what is below the bar is."""
+    rng = np.random.default_rng(1)
+    cols, temperature = 8_192, float(np.float32(46_923_774.0 / (2.0 ** 26 / np.log2(np.e)) * scale))
+    z = np.full((3, cols), -46_923_776.0)
+    z[1, ::3], z[2, ::2] = -46_923_780.0, -46_923_784.0
+    for r in range(3):
+        z[r, rng.choice(cols, 200, replace=False)] = -46_923_772.0
+    _check_repeated_top(z * scale, 100, 64, "fp32", temperature)
