@@ -305,7 +305,8 @@ typedef struct fastsgd_matrix {
  *           difference of nearly equal numbers)
  *   temperature  2^-20 .. 2^20; bears on lse and tail only
  * A row of -inf has lse = -inf and tail = 0; NaN or +inf in a row makes both NaN.
- * One launch; the sums' order depends on the sizes (the number of rows among them), the type and the alignment alone.
+ * One launch; the sums' order depends on the sizes (the number of rows among them), the type and the alignment alone.  A block's wait to
+ * be told of its next row has a limit of some seconds: where it ran out that row has keys of -1, and NaN for values, lse and tail.
  */
 int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperature, int32_t* keys, void* values,
                        float* lse, float* tail, void* stream);
@@ -344,7 +345,7 @@ typedef struct fastsgd_pairs {
  * loss and the gradient of its keys.
  * The sums run in fp32 from the largest logit down; the logits' types are widened exactly, and a gradient of 16 bits is
  * rounded once.  The kernel's waits within a row have a limit of some seconds, as the other launches' have; where one ran
- * out the row's loss is NaN.
+ * out, loss, stats and gradient of the rows that its blocks had at hand are NaN throughout, and all other rows are as ever.
  * Pairs may come in any order, and keys may repeat.  One launch; the sums' order depends on the sizes, the alignment and on
  * whether there is a gradient to write, and on nothing else.
  */

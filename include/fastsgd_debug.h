@@ -28,12 +28,13 @@ uint64_t fastsgd_launch_count(void);
 
 /* Iteration limits of the kernels' bounded waits, for the launches that follow:
  *   block_polls  polls of a flag, descriptor or prefix another thread block writes
- *   copy_tries   tries (about 10 us each) of a wait on a bulk copy
+ *   copy_tries   tries (about 10 us each) of a wait on a bulk copy, and of the waits of fastsgd_top_logits and fastsgd_distill_loss(_backward)
+ *                (0xFFFFFFFF: these do not wait at all, bulk copies as by default)
  *   queue_polls  polls of the decoder's queue of large groups (0xFFFFFFFF: give
  *                up at the first poll that finds the slot empty)
  * 0 restores a default.  Tests shorten them so that a wait that cannot complete
- * (a counter they have set beyond reach) ends in FASTSGD_ST_TIMEOUT within
- * milliseconds; production code never calls this. */
+ * (a counter they have set beyond reach) ends in FASTSGD_ST_TIMEOUT, or a loss on
+ * logits in rows of NaN, within milliseconds; production code never calls this. */
 int fastsgd_debug_set_wait_limits(uint32_t block_polls, uint32_t copy_tries, uint32_t queue_polls);
 
 /* Caps the number of thread blocks of the encoders' launches (fastsgd_compress,

@@ -44,6 +44,7 @@ struct Tunables {
     uint32_t   grid_override = 0;          // blocks of the encoders' launches (0: as many as are resident); tests only
     uint32_t   wait_limit = kWaitLimit;    // bounded waits of the kernels (shortened only by fastsgd_debug_set_wait_limits)
     uint32_t   try_limit = kTryLimit;
+    uint32_t   loss_tries = kTryLimit;     // the same for the losses on logits, which may be told not to wait at all
     uint32_t   dec_spin_limit = kDecSpinLimit;
 };
 constexpr int kMaxDevices = 64;
@@ -272,7 +273,7 @@ int device_view(DeviceView* out) {
     FSG_DEVICE_STATE();
     const int rc = ensure_device_setup();
     if (rc) return rc;
-    out->ws = g_state.ws; out->ws_bytes = g_state.ws_bytes; out->sm_count = g_state.sm_count; out->device = (int)(&g_state - g_states);
+    out->ws = g_state.ws; out->ws_bytes = g_state.ws_bytes; out->sm_count = g_state.sm_count; out->tries = g_tun.loss_tries; out->device = (int)(&g_state - g_states);
     return FASTSGD_OK;
 }
 
@@ -323,7 +324,8 @@ uint64_t fastsgd_launch_count(void) { return g_launches.load(std::memory_order_r
 int fastsgd_debug_set_wait_limits(uint32_t block_polls, uint32_t copy_tries, uint32_t queue_polls) {
     std::lock_guard<std::mutex> lock(g_mu);
     g_tun.wait_limit = block_polls ? block_polls : kWaitLimit;
-    g_tun.try_limit = copy_tries ? copy_tries : kTryLimit;
+    g_tun.try_limit = copy_tries && copy_tries != 0xFFFFFFFFu ? copy_tries : kTryLimit;
+    g_tun.loss_tries = copy_tries == 0xFFFFFFFFu ? 0u : copy_tries ? copy_tries : kTryLimit;
     g_tun.dec_spin_limit = queue_polls == 0xFFFFFFFFu ? 0u : (queue_polls ? queue_polls : kDecSpinLimit);
     return FASTSGD_OK;
 }

@@ -68,9 +68,11 @@ __device__ __forceinline__ void claim_ask(Claim& c) {
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
                  ::"r"(smem_u32(&c.answer)), "r"(smem_u32(&c.bar)) : "memory");
 }
-// The answer to the n-th question (n counts from 0): the first block of the work that is now ours, or -1.
-__device__ __forceinline__ int claim_answer(Claim& c, uint32_t n) {
-    if (!mbar_wait(&c.bar, n & 1u)) return -1;
+// The answer to the n-th question (n counts from 0): the first block of the work that is now ours, or -1; kNoAnswer where the wait has
+// run out.  What was granted then is ours all the same, and the answer still comes: a block asks for it once more before it leaves.
+constexpr int kNoAnswer = -2;
+__device__ __forceinline__ int claim_answer(Claim& c, uint32_t n, uint32_t tries = kTryLimit) {
+    if (!mbar_wait(&c.bar, n & 1u, tries)) return kNoAnswer;
     uint32_t granted, x;
     asm volatile("{\n .reg .pred p;\n .reg .b128 r;\n ld.shared.b128 r, [%2];\n clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
                  " selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"

@@ -34,6 +34,7 @@ struct DistillArgs {
     uint32_t cols, k, values_type;
     uint32_t per, slots, kept;                             // vectors of a row that a block takes; of them a thread; in shared memory
     uint32_t claims;                                       // there are more rows than blocks or clusters at a time
+    uint32_t tries;                                        // of every wait
     float temperature, inv_t, c, slack;                    // c = log2(e) / T
 };
 
@@ -57,6 +58,7 @@ struct DistillShared {
     float2 join[2][kDistillWarps];
     float4 peer[2][kDistillMaxBlocks];                     // m, sum and keys' sum of every block of the cluster
     unsigned long long ready[2], done[2], met[2];          // the row's pairs are known; its gradient is written; every block's sums are there
+    unsigned long long level;                              // the warps that go through the row have all come so far
     Claim  claim;                                          // of the first block: the cluster's next row
     int    next[2];                                        // the others': what the first has been given
     unsigned long long told[2];                            // (one would not do: the first block may be a turn ahead of another's pairs' warp)
@@ -75,8 +77,13 @@ __host__ __device__ inline size_t distill_smem(uint32_t kept, uint32_t k, uint32
     return (size_t)kept * kDistillThreads * 16u + 24u * (size_t)k + 2u * distill_map_bytes(per);
 }
 
-// the warps that go through the row wait for one another
-__device__ __forceinline__ void sync_readers() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(kDistillThreads) : "memory"); }
+// The warps that go through the row wait for one another, for the n-th time; false where that has run out.  (Not bar.sync, which waits
+// without a limit for a warp whose own wait has run out.)
+__device__ __forceinline__ bool readers_level(DistillShared& s, uint32_t& n, uint32_t tries) {
+    __syncwarp();
+    if ((threadIdx.x & 31u) == 0u) mbar_arrive(&s.level);
+    return __all_sync(kFullMask, mbar_wait(&s.level, n++ & 1u, tries));
+}
 __device__ __forceinline__ void cluster_arrive() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { __syncwarp(); asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -275,6 +282,15 @@ __device__ __forceinline__ void finish_pairs(const DistillArgs& a, uint64_t row,
     }
 }
 
+// A row that has been given up: nothing of it is a number.  One warp.
+template <class TG>
+__device__ __noinline__ void give_up_row(TG* g, uint32_t cols, float* loss, float* stats) {
+    const uint32_t lane = threadIdx.x & 31u;
+    if (g) for (uint32_t j = lane; j < cols; j += 32u) g[j] = from_float<TG>(NAN);
+    if (lane == 0 && loss) *loss = NAN;
+    if (lane < 2u && stats) stats[lane] = NAN;
+}
+
 // A block or a cluster of blocks per row.  A block's share of the row stays in shared memory between the two passes, each thread's
 // vectors in places of its own: the thread that has used a vector for the last time asks for the next row's vector in its place, so that
 // reads go on while gradients are written, and no barrier stands between a copy and its use.  (Vectors beyond the shared memory, of
@@ -286,8 +302,9 @@ __device__ __forceinline__ void finish_pairs(const DistillArgs& a, uint64_t row,
 // slowest block twice a row, and what it waits with is 3 x 64 KB an SM.
 // 1023 x 50257 fp32, loss alone: 47 us, 4.4 TB/s (a copy's time 31.5); one pass has 32 KB of copies ahead in place of the row: 55 -> 47.
 // The backward pass of 2048 x 32000 fp16: 47.5 to 51 us, 5.1 to 5.5 TB/s (40).
-// Every wait has a limit.  What a warp may overwrite is what others have told it that they are done with: where such a wait runs out the
-// pairs' warp leaves its rows as they are and ends, and then those that wait for it do; sums that never came make the row's loss NaN.
+// Every wait has a limit.  What a warp may overwrite is what others have told it that they are done with, and what it reads is what it has
+// been told is there: a warp whose wait runs out goes to the kernel's end, and then those that wait for it do.  There, once the whole cluster
+// has come, the pairs' warp of a block that has not finished its rows, or has been granted one that it never began, makes all of them NaN.
 template <class TZ, class TG, int MODE>
 __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     extern __shared__ __align__(16) unsigned char distill_smem_bytes[];
@@ -309,6 +326,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         for (uint32_t i = lane; i < map_bytes / 2u; i += 32u) reinterpret_cast<uint32_t*>(maps)[i] = 0u;
         if (lane == 0) {
             for (int b = 0; b < 2; ++b) { mbar_init(&s.ready[b], 1u); mbar_init(&s.done[b], kDistillWarps); mbar_init(&s.met[b], blocks); mbar_init(&s.told[b], 1u); }
+            mbar_init(&s.level, kDistillWarps);
             claim_init(s.claim);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -316,23 +334,25 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (every block of the cluster has begun)
         if (a.claims && rank == 0u && lane == 0) claim_ask(s.claim);
         // turn i: the i-th row's pairs; then, once its gradient is written, the row before is finished
-        int row = (int)first, last = -1;
+        int row = (int)first, last = -1, next = -1, question = -1;      // (question: one without an answer when a wait ran out)
+        bool lost = false;
         for (uint32_t i = 0;; ++i) {
             const uint32_t b = i & 1u, o = b ^ 1u;
-            int next = -1;
+            next = -1;
             if (row >= 0) {
                 prepare_pairs<TZ, MODE>(a, (uint64_t)row, rank, blocks, s.row[b], s_key + b * k, s_t + b * k, s_z + b * k, maps + b * map_bytes);
                 // the cluster's next row: the first block has asked for it a turn ago, and tells the others
                 if (a.claims && lane == 0) {
                     if (rank == 0u) {
-                        next = claim_answer(s.claim, i);
+                        next = claim_answer(s.claim, i, a.tries);
                         if (next >= 0) { next /= (int)blocks; claim_ask(s.claim); }
                         // (it is here once row i - 2's gradient is written, to which every block has contributed after it had read
                         // what it was told then: that place and its barrier are free)
-                        for (uint32_t to = 1u; to < blocks; ++to) { *cluster.map_shared_rank(&s.next[b], to) = next; mbar_arrive_at(&s.told[b], to); }
-                    } else if (mbar_wait_cluster(&s.told[b], i >> 1 & 1u)) next = s.next[b];
+                        if (next != kNoAnswer) for (uint32_t to = 1u; to < blocks; ++to) { *cluster.map_shared_rank(&s.next[b], to) = next; mbar_arrive_at(&s.told[b], to); }
+                    } else next = mbar_wait_cluster(&s.told[b], i >> 1 & 1u, a.tries) ? s.next[b] : kNoAnswer;
                 }
                 next = __shfl_sync(kFullMask, next, 0);
+                if (next == kNoAnswer) { lost = true; question = (int)i; break; }
                 if (next >= 0 && lane == 0) {
                     const TZ* z = static_cast<const TZ*>(a.z) + (uint64_t)next * a.z_stride;
                     const DistillSlice n = distill_slice(z, a.cols, a.per, rank);
@@ -342,9 +362,9 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.ready[b]);
             if (last >= 0) {
-                if (!__all_sync(kFullMask, mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u))) {
-                    // (given up: what the others still read stays as it is)
-                    if (a.claims && rank == 0u && lane == 0 && next >= 0) claim_answer(s.claim, i + 1u);
+                if (!__all_sync(kFullMask, mbar_wait(&s.done[o], ((i - 1u) >> 1) & 1u, a.tries))) {
+                    lost = true;
+                    if (next >= 0) question = (int)i + 1;
                     break;
                 }
                 if (MODE == kLossOnly && blocks == 1u) {
@@ -361,7 +381,16 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
             if (row < 0) break;
             last = row; row = next;
         }
-        if (blocks > 1u) { cluster_arrive(); cluster_wait(); }      // (no block leaves while another may write to its shared memory)
+        cluster_arrive(); cluster_wait();                  // (no block leaves while another may write to its shared memory)
+        if (lost) {
+            int granted = -1;
+            if (rank == 0u && lane == 0 && a.claims && question >= 0) granted = claim_answer(s.claim, (uint32_t)question);
+            granted = __shfl_sync(kFullMask, granted, 0);
+            for (int n = 0; n < 4; ++n) {
+                const int r = n == 0 ? last : n == 1 ? row : n == 2 ? next : granted < 0 ? -1 : granted / (int)blocks;
+                if (r >= 0) give_up_row(MODE == kLossOnly ? nullptr : static_cast<TG*>(a.grad) + (uint64_t)r * a.grad_stride, a.cols, a.loss ? a.loss + r : nullptr, a.stats_out ? a.stats_out + 2 * (uint64_t)r : nullptr);
+            }
+        }
         return;
     }
 
@@ -394,9 +423,10 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
     }
     __syncthreads();
     if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
+    uint32_t meetings = 0u;
     for (uint32_t i = 0u;; ++i) {
         const uint32_t b = i & 1u, parity = i >> 1 & 1u;
-        if (!__all_sync(kFullMask, mbar_wait(&s.ready[b], parity))) break;
+        if (!__all_sync(kFullMask, mbar_wait(&s.ready[b], parity, a.tries))) break;
         const DistillRow& r = s.row[b];
         if (r.flags & kRowNone) break;
         const uint64_t row = r.row;
@@ -482,24 +512,24 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 if (lane == 0) mbar_arrive(&s.done[b]);
                 continue;
             }
-            sync_readers();
+            if (!readers_level(s, meetings, a.tries)) break;
             e = join_warps(s.join[b], a.c);
             if (counts && (e.s == 0.f || may_miss_far(e.m, a.c))) {
-                sync_readers();
+                if (!readers_level(s, meetings, a.tries)) break;
                 e = warp_join(scan_far(z, skip, a.cols, a.per, rank, blocks, a.c, a.slack, tid, kDistillThreads), a.c);
                 if (lane == 0) s.join[b][warp] = make_float2(e.m, e.s);
-                sync_readers();
+                if (!readers_level(s, meetings, a.tries)) break;
                 e = join_warps(s.join[b], a.c);
             }
         }
         DistillSums sums{e.m, e.s, r.ksum};
         if (blocks > 1u) {
-            if (MODE == kGradOnly) sync_readers();         // (all have met for the row before: the barrier is free)
+            if (MODE == kGradOnly && !readers_level(s, meetings, a.tries)) break;      // (all have met for the row before: the barrier is free)
             if (tid < blocks) {
                 cluster.map_shared_rank(&s, tid)->peer[b][rank] = make_float4(e.m, e.s, r.ksum, 0.f);
                 mbar_arrive_at(&s.met[b], tid);
             }
-            const bool met = __all_sync(kFullMask, mbar_wait_cluster(&s.met[b], parity));
+            if (!__all_sync(kFullMask, mbar_wait_cluster(&s.met[b], parity, a.tries))) break;
             // (eight places, of which the cluster has one, two, four or all)
             const float4 p = s.peer[b][lane % blocks];
             sums.m = warp_max(p.x);
@@ -509,7 +539,6 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
                 sums.s += __shfl_xor_sync(kFullMask, sums.s, o);
                 sums.ksum += __shfl_xor_sync(kFullMask, sums.ksum, o);
             }
-            if (!met) sums.s = NAN;
         }
         if (MODE == kGradOnly) { sums.m = r.m; sums.s = r.s; }
         if (tid == 0) s.sums[b] = sums;
@@ -569,7 +598,7 @@ __global__ void __launch_bounds__(kDistillBlock, 3) k_distill(DistillArgs a) {
         if (lane == 0) mbar_arrive(&s.done[b]);
     }
     wait_copies<0>();
-    if (blocks > 1u) { cluster_arrive(); cluster_wait(); }
+    cluster_arrive(); cluster_wait();
 }
 
 }  // namespace fsg

@@ -10,6 +10,7 @@ struct DeviceView {
     void*    ws;          // the registered workspace, or nullptr
     uint64_t ws_bytes;
     int      sm_count;
+    uint32_t tries;       // of the waits of the losses on logits
     int      device;
 };
 // The current device's; FASTSGD_OK or FASTSGD_E_CUDA.

@@ -140,6 +140,7 @@ int distill(int mode, const fastsgd_matrix* student, const fastsgd_pairs* teache
     a.keys = teacher->keys; a.values = teacher->values; a.tail = teacher->tail; a.k = teacher->k; a.values_type = teacher->type;
     a.weight = weight; a.grad_loss = grad_loss; a.stats_in = stats_in; a.loss = loss; a.stats_out = stats_out;
     a.temperature = temperature; a.inv_t = 1.f / temperature; a.c = (float)(kLog2E / (double)temperature); a.slack = exp_slack(a.c);
+    a.tries = dev.tries;
     const uint32_t gt = grad ? grad->type : student->type;
     const void* fn = mode == kLossOnly ? distill_kernel<kLossOnly>(student->type, gt)
                    : mode == kLossAndGrad ? distill_kernel<kLossAndGrad>(student->type, gt) : distill_kernel<kGradOnly>(student->type, gt);
@@ -200,6 +201,7 @@ int fastsgd_top_logits(const fastsgd_matrix* logits, uint32_t k, float temperatu
     a.z = logits->data; a.rows = logits->rows; a.cols = (uint32_t)logits->cols; a.z_stride = logits->row_stride;
     a.keys = keys; a.values = values; a.lse = lse; a.tail = tail; a.k = k;
     a.temperature = temperature; a.c = (float)(kLog2E / (double)temperature); a.slack = exp_slack(a.c);
+    a.tries = dev.tries;
     void* kargs[] = {&a};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a.cols <= kTopRowsMaxCols && k <= kTopRowsMaxPairs) {

@@ -22,6 +22,7 @@ struct TopArgs {
     uint32_t cols, k, slice;                               // columns of a row that a block takes (a cluster takes the row)
     uint32_t claims;                                       // there are more rows than blocks at a time (no clusters then)
     uint32_t by_bar;                                       // few columns: the pairs by a bar, not one by one
+    uint32_t tries;                                        // of the wait for a claim's answer
     float temperature, c, slack;                           // c = log2(e) / T
 };
 
@@ -519,6 +520,14 @@ __device__ __noinline__ ExpSum sum_carefully(const T* z, unsigned long long last
     return e;
 }
 
+// A row that was never gone through.
+template <class T>
+__device__ __noinline__ void give_up_pairs(int32_t* keys, T* values, uint32_t k, float* lse, float* tail) {
+    for (uint32_t i = threadIdx.x; i < k; i += kTopThreads) { keys[i] = -1; values[i] = from_float<T>(NAN); }
+    if (threadIdx.x == 0 && lse) *lse = NAN;
+    if (threadIdx.x == 0 && tail) *tail = NAN;
+}
+
 template <class T, uint32_t MOST>
 __global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_top(TopArgs a) {
     extern __shared__ __align__(16) unsigned char top_smem[];
@@ -563,7 +572,7 @@ __global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_t
         for (uint32_t t = 0; t < q.tiles; ++t) {
             if (t + 1u < q.tiles) fetch(z, q, t + 1u, slot ^ 1u);
             else {
-                if (a.claims) next_row = claim_answer(s.claim, turn);
+                if (a.claims) next_row = claim_answer(s.claim, turn, a.tries);
                 if (next_row >= 0) { const T* next = static_cast<const T*>(a.z) + (uint64_t)next_row * a.z_stride; fetch(next, top_slice(next + begin, end - begin), 0u, slot ^ 1u); }
                 else copies_end_group();
             }
@@ -616,8 +625,9 @@ __global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_t
             }
         }
         ExpSum e = collect<T>(s, z, listed, cut, begin, end, es.whole(a.c), a.c, a.slack);
-        __syncthreads();
-        if (tid == 0 && next_row >= 0) claim_ask(s.claim);      // (all have read the last answer)
+        // (all have read the last answer; where one's wait for it has run out, it comes too late for all)
+        if (__syncthreads_or(next_row == kNoAnswer)) next_row = kNoAnswer;
+        if (tid == 0 && next_row >= 0) claim_ask(s.claim);
         uint32_t n = s.cands;
         const bool careful = n > TopShared<MOST>::kRoom || (n < k && cut);
         if (careful) {
@@ -683,6 +693,11 @@ __global__ void __launch_bounds__(kTopThreads, MOST <= kTopFewPairs ? 3 : 2) k_t
             const bool none = rest + inside == 0.f;        // every logit is -inf
             if (a.lse) a.lse[row] = none ? -INFINITY : top / a.temperature + logf(rest + inside);
             if (a.tail) a.tail[row] = none ? 0.f : rest / (rest + inside);
+        }
+        if (next_row == kNoAnswer) {                       // a row that this block was granted has no pairs
+            wait_copies<0>();
+            const int lost = claim_answer(s.claim, turn);
+            if (lost >= 0) give_up_pairs(a.keys + (uint64_t)lost * k, static_cast<T*>(a.values) + (uint64_t)lost * k, k, a.lse ? a.lse + lost : nullptr, a.tail ? a.tail + lost : nullptr);
         }
         if (next_row < 0) break;
         row = (uint64_t)next_row;

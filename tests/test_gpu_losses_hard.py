@@ -114,3 +114,73 @@ def test_top_logits_where_logits_become_far(scale):
     for r in range(3):
         z[r, rng.choice(cols, 200, replace=False)] = -46_923_772.0
     _check_repeated_top(z * scale, 100, 64, "fp32", temperature)
+
+
+NO_WAITS = 0xFFFFFFFF
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 2_001, 3_000), ("fp32", 9, 6_001), ("fp16", 700, 60_001), ("bf16", 301, 128_000), ("fp32", 3, 262_144), ("fp32", 230, 200_003)])
+def test_distillation_rows_whose_waits_run_out_are_nan(dtype, rows, cols):
+    """From no wait at all to waits of some tries: a row is what it is with waits of any length, or has no number in it; nothing else is written."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    kind, k = TYPES[dtype], 20
+    z = torch.randn((rows, cols), generator=gen, device="cuda").to(kind)
+    keys = torch.randint(0, cols, (rows, k), generator=gen, device="cuda", dtype=torch.int32)
+    values = torch.randn((rows, k), generator=gen, device="cuda")
+    tail, up = 0.5 * torch.rand(rows, generator=gen, device="cuda"), torch.randn(rows, generator=gen, device="cuda")
+    kept = torch.empty((rows, 2), device="cuda")
+    assert binding.distill_loss(z, keys, values, stats=kept, tail=tail) == 0
+
+    def loss_alone():
+        loss, stats = torch.full((rows,), MARK, device="cuda"), torch.full((rows, 2), MARK, device="cuda")
+        assert binding.distill_loss(z, keys, values, loss=loss, stats=stats, tail=tail) == 0
+        return torch.cat([loss[:, None], stats], 1)
+
+    def with_gradient():
+        loss, stats = torch.full((rows,), MARK, device="cuda"), torch.full((rows, 2), MARK, device="cuda")
+        mine = torch.full((rows + 2, cols), MARK, dtype=kind, device="cuda")
+        mine[1:-1] = z
+        assert binding.distill_loss(mine[1:-1], keys, values, loss=loss, grad=mine[1:-1], stats=stats, tail=tail) == 0
+        assert bool((mine[0] == MARK).all()) and bool((mine[-1] == MARK).all())
+        return torch.cat([loss[:, None], stats, mine[1:-1].float()], 1)
+
+    def backward():
+        grad = torch.full((rows + 2, cols), MARK, device="cuda")
+        assert binding.distill_loss_backward(z, keys, values, kept, grad[1:-1], grad_loss=up, tail=tail) == 0
+        assert bool((grad[0] == MARK).all()) and bool((grad[-1] == MARK).all())
+        return grad[1:-1]
+
+    for call in (loss_alone, with_gradient, backward):
+        want = call()
+        assert bool(want.isfinite().all())
+        for tries in (NO_WAITS, 1, 1, 1, 2, 4, 16):
+            try:
+                binding.debug_set_wait_limits(copy_tries=tries)
+                got = call()
+                torch.cuda.synchronize()
+            finally:
+                binding.debug_set_wait_limits()
+            lost = got.isnan()
+            assert torch.equal(lost, lost.all(1, keepdim=True).expand_as(lost))
+            assert bool((lost | (got == want)).all())
+            assert bool(lost.all()) or tries != NO_WAITS
+        assert torch.equal(call(), want)
+
+
+@pytest.mark.parametrize("rows,cols,k", [(1_000, 20_000, 64), (900, 9_000, 700), (448, 3_000, 40), (3, 200_000, 20)])
+def test_top_logits_rows_whose_claims_come_late_are_not_there(rows, cols, k):
+    z = torch.randn((rows, cols), generator=torch.Generator(device="cuda").manual_seed(k), device="cuda").to(torch.bfloat16)
+    want = _run_top(z, k, 1.0)
+    for tries in (NO_WAITS, 1, 2):
+        try:
+            binding.debug_set_wait_limits(copy_tries=tries)
+            keys, values, lse, tail = _run_top(z, k, 1.0)
+            torch.cuda.synchronize()
+        finally:
+            binding.debug_set_wait_limits()
+        lost = lse.isnan()
+        # (a row is lost with the block's wait for it: the blocks that there are at first have their own)
+        assert bool(lost.any()) or rows < 900 or tries != NO_WAITS
+        assert bool((keys[lost] == -1).all()) and bool(values[lost].isnan().all()) and bool(tail[lost].isnan().all())
+        assert all(_same(a[~lost].contiguous(), b[~lost].contiguous()) for a, b in zip((keys, values, lse, tail), want))
+    assert all(_same(a, b) for a, b in zip(_run_top(z, k, 1.0), want))
