@@ -150,7 +150,7 @@ template <class T> __device__ __forceinline__ Eight<T> load_eight(const T* p, ui
 #pragma unroll
         for (int h = 0; h < 8 / N; ++h) r.raw[h] = load16(p + h * N);
     } else {
-        T x[8];
+        alignas(16) T x[8];
 #pragma unroll
         for (int h = 0; h < 8; h += H) {
             if (unit >= 8u && n >= (uint32_t)(h + H)) *reinterpret_cast<uint2*>(x + h) = *reinterpret_cast<const uint2*>(p + h);
@@ -178,7 +178,7 @@ template <class T> __device__ __forceinline__ void store_eight(T* p, uint32_t n,
     constexpr int H = Vec<T>::N / 2;
     if (unit == 16u && n >= 8u) store_values(p, f, true);
     else {
-        T x[8];
+        alignas(16) T x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = from_float<T>(f[i]);
 #pragma unroll

@@ -348,7 +348,7 @@ __device__ __forceinline__ void each_listed(const TopShared<MOST>& s, const T* z
                 raw[u] = load16(body + v);
             } else {
                 base[u] = id == kTopHead ? first_key - N : end - q.tail;
-                T x[N];
+                alignas(16) T x[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) x[i] = base[u] + i - begin < end - begin ? z[base[u] + i] : from_float<T>(0.f);
                 raw[u] = *reinterpret_cast<const uint4*>(x);
