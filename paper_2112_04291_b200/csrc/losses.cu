@@ -77,10 +77,12 @@ int resident_blocks(const void* fn, int threads, size_t smem, const DeviceView& 
     return FASTSGD_OK;
 }
 
+template <class T, int MODE> const void* distill_kernel_of(uint32_t g) {
+    if constexpr (MODE != kLossOnly && sizeof(T) == 2) if (g == FASTSGD_F32) return (const void*)k_distill<T, float, MODE>;
+    return (const void*)k_distill<T, T, MODE>;
+}
 template <int MODE> const void* distill_kernel(uint32_t z, uint32_t g) {
-    if (z == FASTSGD_F32) return (const void*)k_distill<float, float, MODE>;
-    if (z == FASTSGD_BF16) return g == FASTSGD_F32 ? (const void*)k_distill<__nv_bfloat16, float, MODE> : (const void*)k_distill<__nv_bfloat16, __nv_bfloat16, MODE>;
-    return g == FASTSGD_F32 ? (const void*)k_distill<__half, float, MODE> : (const void*)k_distill<__half, __half, MODE>;
+    return z == FASTSGD_F32 ? distill_kernel_of<float, MODE>(g) : z == FASTSGD_BF16 ? distill_kernel_of<__nv_bfloat16, MODE>(g) : distill_kernel_of<__half, MODE>(g);
 }
 // Lanes that share a token: with 16 of its experts each, where that is quicker than 8 (us for 65536 tokens with 8, with 16: bf16 x 16: 6.5, 6.0, x 64:
 // 10.1, 7.9, x 256: 21.0, 16.1; fp32 x 16: 6.6, 7.0, x 32: 7.7, 8.0, x 64: 10.4, 9.7, x 256: 26.7, 23.0).
@@ -92,9 +94,9 @@ uint32_t balance_lanes(uint32_t type, uint32_t experts) {
 }
 template <class T, class TG> const void* balance_kernel_of(uint32_t experts) {
     if (experts <= 8u) return (const void*)k_balance<T, TG, 1, 1>;
-    if (sizeof(T) == 4 && experts <= 32u) return experts <= 16u ? (const void*)k_balance<T, TG, 2, 1> : (const void*)k_balance<T, TG, 4, 1>;
-    return experts <= 16u ? (const void*)k_balance<T, TG, 1, 2> : experts <= 32u ? (const void*)k_balance<T, TG, 2, 2> : experts <= 64u ? (const void*)k_balance<T, TG, 4, 2>
-         : experts <= 128u ? (const void*)k_balance<T, TG, 8, 2> : experts <= 256u ? (const void*)k_balance<T, TG, 16, 2>
+    constexpr int FEW = sizeof(T) == 4 ? 1 : 2;            // (up to 32 experts)
+    if (experts <= 32u) return experts <= 16u ? (const void*)k_balance<T, TG, 2 / FEW, FEW> : (const void*)k_balance<T, TG, 4 / FEW, FEW>;
+    return experts <= 64u ? (const void*)k_balance<T, TG, 4, 2> : experts <= 128u ? (const void*)k_balance<T, TG, 8, 2> : experts <= 256u ? (const void*)k_balance<T, TG, 16, 2>
          : experts <= 512u ? (const void*)k_balance<T, TG, 32, 2> : (const void*)k_balance<T, TG, 32, 4>;
 }
 const void* balance_kernel(uint32_t x, uint32_t g, uint32_t experts) {

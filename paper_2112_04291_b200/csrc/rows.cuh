@@ -324,14 +324,6 @@ __device__ __forceinline__ ExpSum warp_join(ExpSum e, float c) {
 }
 
 // Block-wide, the result in every thread; `s` holds a value per warp and is free again once the next barrier has passed.
-template <int WARPS> __device__ __forceinline__ float block_max(float v, float* s) {
-    v = warp_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return warp_max(lane < WARPS ? s[lane] : -INFINITY);
-}
 template <int WARPS, class F> __device__ __forceinline__ F block_sum(F v, F* s) {
     v = warp_sum(v);
     __syncthreads();
@@ -339,16 +331,6 @@ template <int WARPS, class F> __device__ __forceinline__ F block_sum(F v, F* s) 
     __syncthreads();
     const int lane = threadIdx.x & 31;
     return warp_sum(lane < WARPS ? s[lane] : (F)0);
-}
-template <int WARPS> __device__ __forceinline__ ExpSum block_join(ExpSum e, float2* s, float c) {
-    e = warp_join(e, c);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(e.m, e.s);
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    ExpSum r;
-    if (lane < WARPS) { r.m = s[lane].x; r.s = s[lane].y; }
-    return warp_join(r, c);
 }
 
 }  // namespace fsg
