@@ -184,3 +184,26 @@ def test_top_logits_rows_whose_claims_come_late_are_not_there(rows, cols, k):
         assert bool((keys[lost] == -1).all()) and bool(values[lost].isnan().all()) and bool(tail[lost].isnan().all())
         assert all(_same(a[~lost].contiguous(), b[~lost].contiguous()) for a, b in zip((keys, values, lse, tail), want))
     assert all(_same(a, b) for a, b in zip(_run_top(z, k, 1.0), want))
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("tokens,k,experts,segments", [
+    (200_003, 8, 60, [5, 5, 6, 70_000, 70_000, 70_001, 199_990]), (131_072, 4, 1024, [0, 65_536, 131_072]), (300_007, 1, 7, [0, 300_007]),
+    (90_001, 16, 256, [0, 0, 1_000, 1_000, 90_001, 90_001]),                                        # spread over the GPU
+    (100_003, 4, 33, [0] * 3 + [17] * 20 + [99_999] * 20), (100_003, 4, 33, list(range(0, 40)) + [100_003])])      # clusters, of which one has nearly all tokens
+def test_counts_of_long_segments(masked, tokens, k, experts, segments):
+    """Blocks that meet several segments, segments that several blocks share, empty ones, and tokens outside of all."""
+    rng = np.random.default_rng([tokens, k])
+    selected = rng.integers(-1, experts + 1, (tokens, k)).astype(np.int32)
+    mask = rng.random(tokens) < 0.6 if masked else None
+    offsets = np.asarray(segments, np.int64)
+    count = len(segments) - 1
+    want, want_tokens = np.zeros((count, experts), np.int64), np.zeros(count, np.int64)
+    for s in range(count):
+        part = slice(segments[s], segments[s + 1])
+        kept = selected[part] if mask is None else selected[part][mask[part]]
+        want[s], want_tokens[s] = np.bincount(kept[(kept >= 0) & (kept < experts)], minlength=experts), len(kept)
+    for _ in range(2):
+        counts, counted = torch.full((count, experts), -3, dtype=torch.int32, device="cuda"), torch.full((count,), -3, dtype=torch.int32, device="cuda")
+        assert binding.expert_counts(_dev(selected), counts, counted, mask=None if mask is None else _dev(mask), offsets=_dev(offsets)) == 0
+        assert np.array_equal(counts.cpu().numpy(), want) and np.array_equal(counted.cpu().numpy(), want_tokens)
