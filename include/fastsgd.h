@@ -272,9 +272,10 @@ uint64_t fastsgd_key_encode_paper_bound(uint64_t d, uint32_t flag_bits);
 int fastsgd_key_encode_paper(const uint32_t* keys, uint64_t d, uint32_t flag_bits,
                              void* out, uint64_t out_bytes, void* stream);
 
-/* ---- where a worker's gradient begins: losses on logits, and their data as key-value pairs ----------
- * (No counterpart in the paper, whose models end in a logistic or linear loss: these are the losses of
- * models whose gradients are compressed today.)  All of them only enqueue kernels on `stream`.  Those without a
+/* ---- where a worker's gradient begins: losses on logits, and top logits as key-value pairs ----------
+ * (No counterpart in the paper, whose models end in a logistic or linear loss.  The gradients are those of logits; what a
+ * worker compresses, the gradient of its weights, follows from them by the caller's own products.  The pairs are in descending order
+ * of their values: not the ascending keys that fastsgd_compress_kv takes.)  All of them only enqueue kernels on `stream`.  Those without a
  * workspace may run on several streams at once.
  */
 
@@ -331,12 +332,13 @@ typedef struct fastsgd_pairs {
  *   student  rows x V, V <= 2^20 (else FASTSGD_E_NOT_IMPLEMENTED); a row takes 1, 2, 4 or 8 blocks, and rows times blocks
  *            stay below 2^31 (else FASTSGD_E_BAD_N)
  *   temperature  T, 2^-20 .. 2^20
- *   weight   device, rows floats, or NULL (1): 1 / rows for the mean; a row of weight 0 (padding) is not read
+ *   weight   device, rows floats, or NULL (1): 1 / rows for the mean; a row of weight 0 (padding) may hold anything, but is
+ *            copied like the others: its logits have to be memory that can be read
  *   loss     device, rows floats, or NULL
  *   stats    device, 2 * rows floats, or NULL: what fastsgd_distill_loss_backward takes (of the logits that the sum runs over
  *            -- all, or with a tail > 0 those that are no key -- one that is near the largest, and the sum of
  *            exp((z - it) / T))
- *   grad     rows x V, or NULL: of the logits' type, or fp32, as fastsgd_compress takes it; it may be the logits' own
+ *   grad     rows x V, or NULL: of the logits' type, or fp32; it may be the logits' own
  *            place (same data, type and stride), otherwise apart from them
  * At least one of loss, stats and grad is wanted.
  * A row of weight 0, without a pair that is there, whose pairs all have value -inf, or whose logits are all -inf counts for

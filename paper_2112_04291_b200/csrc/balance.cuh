@@ -150,8 +150,8 @@ __global__ void __launch_bounds__(kCountThreads) k_add_expert_counts(CountArgs a
 // Bound by issue slots (57 %) and latency: 16 warps an SM.  A warp per token whatever the width: 81 with the counts; the next tokens' logits not
 // ahead: 34; eight experts a lane: 26 (the reductions over lanes, and all that a token costs once, are then spread over half as many values).
 // A block per run of tokens; LANES lanes share a token, each with CHUNKS times eight neighbouring experts, whose f it keeps in
-// registers.  The logits of the next few tokens are on their way while those at hand are worked on (of one step ahead alone, 24 warps an
-// SM had 24 KB in flight, half of what the memory's latency takes).
+// registers.  The logits of the next token (of the next few, with eight experts a lane: two in fp32, four in 16 bits) are on their way while those
+// at hand are worked on.  With sixteen 16-bit experts a lane that is 16 KB an SM, half of what the memory's latency takes.
 // The sum of a block's part of segment s goes to partials[block + s]: of two
 // neighbours in the sequence of (block, segment) meetings one index grows, so that no two share a place.  The block that ends last
 // adds the parts of each segment in their order.

@@ -296,12 +296,12 @@ __device__ __noinline__ void give_up_row(TG* g, uint32_t cols, float* loss, floa
 // reads go on while gradients are written, and no barrier stands between a copy and its use.  (Vectors beyond the shared memory, of
 // rows above half a megabyte, are read twice.)  The ninth warp has the pairs: those of the next row while the others go through this
 // one, and the keys' gradients of the row before.
-// 4096 x 128000 bf16 with a bf16 gradient: 432 to 471 us by the GPU, 4.5 to 4.9 TB/s (2.1 GB; a copy's time 320).  A row in one block that
+// 4096 x 128000 bf16 with a bf16 gradient: 432 to 492 us by the GPU, 4.3 to 4.9 TB/s (2.1 GB; a copy's time 320).  A row in one block that
 // reads it twice: 597; in the shared memory of a cluster, block-wide barriers: 488; several vectors between two looks at the largest: 467;
-// mbarriers in place of the block-wide barriers: 438.  Neither DRAM nor the instructions' issue (53 %) is full: a cluster of four waits for its
+// mbarriers in place of the block-wide barriers: 438; in place of the readers' own as well: 461 -> 444 on one GPU.  Neither DRAM nor the instructions' issue (53 %) is full: a cluster of four waits for its
 // slowest block twice a row, and what it waits with is 3 x 64 KB an SM.
 // 1023 x 50257 fp32, loss alone: 47 us, 4.4 TB/s (a copy's time 31.5); one pass has 32 KB of copies ahead in place of the row: 55 -> 47.
-// The backward pass of 2048 x 32000 fp16: 47.5 to 51 us, 5.1 to 5.5 TB/s (40).
+// The backward pass of 2048 x 32000 fp16: 47.5 to 53 us by the GPU, 5.0 to 5.5 TB/s (40).
 // Every wait has a limit.  What a warp may overwrite is what others have told it that they are done with, and what it reads is what it has
 // been told is there: a warp whose wait runs out goes to the kernel's end, and then those that wait for it do.  There, once the whole cluster
 // has come, the pairs' warp of a block that has not finished its rows, or has been granted one that it never began, makes all of them NaN.

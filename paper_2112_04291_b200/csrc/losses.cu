@@ -267,7 +267,8 @@ int fastsgd_expert_counts(const int32_t* selected, uint64_t tokens, uint32_t k, 
     a.tokens = tokens; a.k = k; a.experts = experts; a.segments = segments;
     void* kargs[] = {&a};
     // A cluster per segment; for many selections in few segments (one block of a cluster of eight would count more than 2^14 of them, if
-    // they are alike) two launches that spread over the GPU.
+    // they are alike) two launches that spread over the GPU.  (The offsets are not known here: where one of many segments has nearly all tokens its
+    // cluster counts them alone.  39 M selections in 300 equal segments: 86 us, all in one of the 300: 1760, in one segment: 112.)
     if (tokens * k <= (1ull << 17) * segments) {
         unsigned blocks = 1u;
         while (blocks < 8u && tokens * k > 2048ull * segments * blocks) blocks *= 2u;

@@ -190,14 +190,14 @@ __global__ void __launch_bounds__(kTopLanesThreads) k_top_lanes(TopArgs a) {
 // exponentials are summed and it is forgotten.  The others are listed, warp by warp, and at the end their elements above the bar
 // become candidates, while the others join the sum; the k-th largest candidate is found by histograms of eight bits.  The order in which
 // candidates are found changes no sum: those that turn out to be no pairs are added as integers.
-// Top 64 of 2048 x 128000 bf16 with lse and tail: 170 us, 3.1 TB/s (525 MB; a copy's time 80).  Neither DRAM (33 %) nor the issue slots
+// Top 64 of 2048 x 128000 bf16 with lse and tail: 165 to 173 us by the GPU, 3.0 to 3.2 TB/s (525 MB; a copy's time 80).  Neither DRAM (33 %) nor the issue slots
 // (47 %, 13 instructions an element and lane) are full: 24 warps an SM wait for their tiles, and for one another in the selection at a row's
 // end, of which the other blocks of the SM hide a part.  Every value against a list: 2655; a bar that rises from nothing in place of the sample: 284; all candidates kept
 // in one place, a barrier a tile: 245.  One row of 128000 over a cluster of eight blocks: 10.3 us (one block: 91, one barrier fewer a step
 // of the selection than before: 16).
 //
 // The first tile is a sample of the row (its 512-byte pieces lie apart as many pieces as there are tiles), and the bar is the
-// maximum of one of its vectors: the one whose place from above the k-th of the row has among them, four standard deviations lower.
+// maximum of one of its vectors: the one whose place from above the k-th of the row has among them (n in the mean), 5 sqrt(n) + 5 places lower.
 // With a bar that turns out too high (fewer than k candidates) or too low (no room for them: values in an order that the sample
 // does not meet, or many equal ones) the row is gone through again step by step: from a bar that is a lower bound for sure, the
 // k-th largest maximum of the first tile, which rises to the k-th candidate whenever there are many.
