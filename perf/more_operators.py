@@ -203,17 +203,17 @@ def _run_own(s):
         _done(binding.embedding(s["table"], s["ids"], s["rows"], scale=s["scale"]))
         return {"rows": s["rows"]}
     if s["kind"] == "gradient":
-        binding.ensure_rows_workspace(s["tokens"], s["vocab"])
+        binding.ensure_rows_workspace(s["tokens"], s["cols"])
         _done(binding.order_ids(s["ids"], s["order"], s["starts"]))
-        _done(binding.embedding_backward(s["grad"], s["order"], s["starts"], s["table_grad"], scale=s["scale"]))
+        _done(binding.embedding_backward(s["grad"], s["ids"], s["order"], s["starts"], s["table_grad"], scale=s["scale"]))
         return {"order": s["order"], "starts": s["starts"], "table_grad": s["table_grad"]}
     if s["kind"] == "pairs":
-        binding.ensure_rows_workspace(s["tokens"], s["vocab"])
+        binding.ensure_rows_workspace(s["tokens"], s["cols"])
         _done(binding.order_ids(s["ids"], s["order"], s["starts"], distinct=s["distinct"], number=s["number"]))
-        _done(binding.embedding_backward_pairs(s["grad"], s["order"], s["starts"], s["distinct"], s["number"], s["keys"], s["values"], scale=s["scale"]))
+        _done(binding.embedding_backward_pairs(s["grad"], s["ids"], s["order"], s["starts"], s["distinct"], s["number"], s["keys"], s["values"], scale=s["scale"]))
         return {"order": s["order"], "starts": s["starts"], "distinct": s["distinct"], "number": s["number"], "keys": s["keys"], "values": s["values"]}
     if s["kind"] == "forward":
-        binding.ensure_rows_workspace(s["tokens"] * s["chosen"], s["experts"])
+        binding.ensure_rows_workspace(s["tokens"] * s["chosen"])
         _done(binding.order_ids(s["selected"], s["order"], s["starts"]))
         _done(binding.expert_product(s["x"], s["w"], s["starts"], s["y"], order=s["order"], per_row=s["chosen"]))
         return {"order": s["order"], "starts": s["starts"], "y": s["y"]}
