@@ -398,6 +398,107 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
                          const uint32_t* counts, const uint32_t* counted, float coef, const float* grad_loss,
                          float* loss, const fastsgd_matrix* grad, void* stream);
 
+/* ---- rows that are chosen by an id: an embedding, and a router's experts -----------------------------
+ * (No counterpart in the paper.)  The sparse gradient that fastsgd_compress_kv takes begins as that of an embedding: the rows of the
+ * tokens that occur.  The experts whose selections fastsgd_expert_counts counts have products of their own.  Both work through
+ * rows in the order of an id (token, expert), which fastsgd_order_ids makes once for all of them.  All calls only enqueue kernels on `stream`;
+ * those that use the workspace say so and are serialised with the others that do, the rest may run on several streams at once.
+ */
+
+/*
+ * Ids in order.
+ *   ids       device, count < 2^31; one outside [0, range) was padded or dropped and is left out
+ *   range     1 .. 2^20 (above: FASTSGD_E_NOT_IMPLEMENTED)
+ *   order     device, room for count: the positions of the ids that are not left out, in ascending order of the ids, equal ids in
+ *             ascending order of their positions; what lies behind the last of them is not written
+ *   starts    device, range + 1: positions of id v are order[starts[v]] .. order[starts[v + 1] - 1]
+ *   distinct  device, room for min(count, range), or NULL: the ids that occur, ascending
+ *   number    device, one, or NULL: how many these are
+ * Up to 65536 ids: one launch, no workspace.  More: up to eleven launches and a workspace of fastsgd_rows_workspace_bytes(count, 1).
+ */
+int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32_t* order, uint32_t* starts,
+                      uint32_t* distinct, uint32_t* number, void* stream);
+
+/*
+ * An embedding's lookup: out[t, :] = scale * table[ids[t], :], zero where ids[t] is no row of the table.
+ *   table  rows x cols
+ *   ids    device, out->rows of them
+ *   out    cols as the table's; of the table's type, or one of the two fp32; apart from the table
+ * Formed in fp32 and rounded once.
+ */
+int fastsgd_embedding(const fastsgd_matrix* table, const int32_t* ids, float scale, const fastsgd_matrix* out, void* stream);
+
+/*
+ * The gradient of an embedding's table: table_grad[v, :] = scale * sum of grad[t, :] over the t with ids[t] = v.  Every row is written,
+ * with zeros where there is none.  (With the tokens of selected rows for ids and scale 1: the sum of each token's rows.)
+ *   grad           rows x cols, as many rows as ids
+ *   order, starts  as fastsgd_order_ids wrote them for these ids and range = table_grad->rows
+ *   table_grad     of grad's type, or one of the two fp32; apart from grad
+ * Sums run in fp32 in the order of the positions, by tiles of equal length whose parts are added in their order: the order depends on the
+ * sizes and the ids alone.  One or two launches; workspace: fastsgd_rows_workspace_bytes(rows, cols).
+ */
+int fastsgd_embedding_backward(const fastsgd_matrix* grad, const int32_t* ids, const uint32_t* order, const uint32_t* starts,
+                               float scale, const fastsgd_matrix* table_grad, void* stream);
+
+/*
+ * The same gradient as key-value pairs, the rows of the ids that occur alone: what fastsgd_compress_kv takes (count = *number * cols,
+ * n = range * cols).
+ *   distinct, number  as fastsgd_order_ids wrote them
+ *   range             of the ids; range * cols < 2^31
+ *   keys, values      device, room for most * cols each: row i holds the keys distinct[i] * cols + c and their values; rows from *number on
+ *                     are not written, rows from `most` on are not there.  Apart from each other and from grad
+ */
+int fastsgd_embedding_backward_pairs(const fastsgd_matrix* grad, const int32_t* ids, const uint32_t* order, const uint32_t* starts,
+                                     const uint32_t* distinct, const uint32_t* number, uint64_t range, float scale,
+                                     uint32_t* keys, float* values, uint64_t most, void* stream);
+
+/* the weights of several experts, or their gradients (host struct, device data): expert e's are outs x ins */
+typedef struct fastsgd_experts {
+    void*    data;           /* 16-byte aligned                                                    */
+    uint64_t experts;        /* 1 .. 1024                                                          */
+    uint64_t outs, ins;      /* multiples of 8                                                     */
+    uint64_t row_stride;     /* elements from one of an expert's rows to the next, a multiple of 8 */
+    uint64_t expert_stride;  /* elements from one expert to the next, a multiple of 8              */
+    uint32_t type;           /* FASTSGD_BF16 or FASTSGD_F16; a gradient's also FASTSGD_F32         */
+    uint32_t reserved;       /* must be 0                                                          */
+} fastsgd_experts;
+
+/*
+ * Products of rows sorted by expert with their expert's weights: y[r, :] = x[source(r), :] W_e^T for starts[e] <= r < starts[e + 1].
+ *   x        tokens x ins, of the weights' type
+ *   order    device: source(r) = order[r] / per_row, as fastsgd_order_ids made it of the per_row experts that each token selects
+ *            (y then has tokens * per_row rows); or NULL, per_row = 1: x is sorted already, source(r) = r
+ *   starts   device, experts + 1, ascending
+ *   y        rows x outs, of that type or fp32; rows that belong to no expert (dropped selections) are left as they are.  Apart from x and
+ *            the weights
+ * Matrices begin on 16 bytes; their columns and strides are multiples of 8 (else FASTSGD_E_ALIGN); x and the weights are of 16 bits (fp32:
+ * FASTSGD_E_NOT_IMPLEMENTED).  Products are summed in fp32 and rounded once.  One launch, no workspace.
+ * The kernel's waits have a limit of some seconds; where one ran out, what its block had not yet written is NaN.
+ */
+int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, const uint32_t* starts,
+                           const fastsgd_experts* weights, const fastsgd_matrix* y, void* stream);
+
+/*
+ * The gradient of the sorted rows: grad_x[r, :] = grad_y[r, :] W_e.  (A token's own gradient is the sum of its rows': fastsgd_embedding_backward
+ * with the tokens of the sorted rows for ids.)
+ *   grad_y  rows x outs, of the weights' type; what rows that belong to no expert hold has no influence
+ *   grad_x  rows x ins, of that type or fp32; otherwise as y above
+ */
+int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const uint32_t* starts, const fastsgd_experts* weights,
+                                          const fastsgd_matrix* grad_x, void* stream);
+
+/*
+ * The gradient of the weights: grad_W_e = sum of grad_y[r, :]^T x[source(r), :] over the expert's rows, zero where it has none: every expert's
+ * is written.
+ *   grad_weights  of x's type or fp32; apart from grad_y and x
+ * Other arguments as above.
+ */
+int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row,
+                                            const uint32_t* starts, const fastsgd_experts* grad_weights, void* stream);
+
+/* bytes of workspace for these calls on `count` ids or rows of `cols` columns; 0 for invalid arguments */
+uint64_t fastsgd_rows_workspace_bytes(uint64_t count, uint64_t cols);
+
 /* ---- helpers, not on the timed path (no counterpart in the paper) ---------- */
 
 /* worst-case stream size in bytes (every entry kept, every delta at the widest

@@ -31,6 +31,8 @@ EXPORTS = [
     "fastsgd_sparse_adam_update_batch", "fastsgd_sparse_adam_update_packed_batch", "fastsgd_key_encode_paper", "fastsgd_key_encode_paper_bound",
     "fastsgd_compress_kv",
     "fastsgd_top_logits", "fastsgd_distill_loss", "fastsgd_distill_loss_backward", "fastsgd_expert_counts", "fastsgd_balance_loss",
+    "fastsgd_order_ids", "fastsgd_embedding", "fastsgd_embedding_backward", "fastsgd_embedding_backward_pairs",
+    "fastsgd_expert_product", "fastsgd_expert_product_backward_input", "fastsgd_expert_product_backward_weights", "fastsgd_rows_workspace_bytes",
     "fastsgd_debug_set_wait_limits", "fastsgd_debug_layout", "fastsgd_debug_set_grid",
     "fastsgd_debug_decoder_route",
 ]
@@ -52,6 +54,11 @@ class Matrix(C.Structure):
 
 class Pairs(C.Structure):
     _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p), ("tail", C.c_void_p), ("k", C.c_uint32), ("type", C.c_uint32)]
+
+
+class Experts(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("experts", C.c_uint64), ("outs", C.c_uint64), ("ins", C.c_uint64), ("row_stride", C.c_uint64),
+                ("expert_stride", C.c_uint64), ("type", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 F32, BF16, F16 = 0, 1, 2
@@ -111,6 +118,23 @@ def lib():
         L.fastsgd_expert_counts.argtypes = [vp, u64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp, vp]
         L.fastsgd_balance_loss.restype = C.c_int
         L.fastsgd_balance_loss.argtypes = [MP, vp, vp, C.c_uint32, vp, vp, C.c_float, vp, vp, MP, vp]
+        EP, u32 = C.POINTER(Experts), C.c_uint32
+        L.fastsgd_order_ids.restype = C.c_int
+        L.fastsgd_order_ids.argtypes = [vp, u64, u64, vp, vp, vp, vp, vp]
+        L.fastsgd_embedding.restype = C.c_int
+        L.fastsgd_embedding.argtypes = [MP, vp, C.c_float, MP, vp]
+        L.fastsgd_embedding_backward.restype = C.c_int
+        L.fastsgd_embedding_backward.argtypes = [MP, vp, vp, vp, C.c_float, MP, vp]
+        L.fastsgd_embedding_backward_pairs.restype = C.c_int
+        L.fastsgd_embedding_backward_pairs.argtypes = [MP, vp, vp, vp, vp, vp, u64, C.c_float, vp, vp, u64, vp]
+        L.fastsgd_expert_product.restype = C.c_int
+        L.fastsgd_expert_product.argtypes = [MP, vp, u32, vp, EP, MP, vp]
+        L.fastsgd_expert_product_backward_input.restype = C.c_int
+        L.fastsgd_expert_product_backward_input.argtypes = [MP, vp, EP, MP, vp]
+        L.fastsgd_expert_product_backward_weights.restype = C.c_int
+        L.fastsgd_expert_product_backward_weights.argtypes = [MP, MP, vp, u32, vp, EP, vp]
+        L.fastsgd_rows_workspace_bytes.restype = u64
+        L.fastsgd_rows_workspace_bytes.argtypes = [u64, u64]
         L.fastsgd_compress_bound.restype = u64
         L.fastsgd_compress_bound.argtypes = [u64, PP]
         L.fastsgd_workspace_bytes.restype = u64
@@ -188,7 +212,10 @@ def set_workspace(ws: torch.Tensor, stream=None) -> None:
 
 def ensure_workspace(n: int, p: Params, device="cuda") -> torch.Tensor:
     """Allocates (torch) and registers a workspace large enough for n entries, if needed."""
-    need = workspace_bytes(n, p)
+    return _ensure(workspace_bytes(n, p), device)
+
+
+def _ensure(need: int, device) -> torch.Tensor:
     ws = _workspace_keepalive
     dev = torch.device(device)
     if dev.index is None:
@@ -387,6 +414,90 @@ def balance_loss(logits: torch.Tensor, counts: torch.Tensor, counted: torch.Tens
                                       _at(counts, dev, _int32, segments, experts), _at(counted, dev, _int32, segments), coef,
                                       _at(grad_loss, dev, _float32, segments), _at(loss, dev, _float32, segments),
                                       None if grad is None else _matrix(grad, dev), _raw_stream(stream, dev))
+
+
+# ---- rows that are chosen by an id: an embedding, and a router's experts ------------------------
+
+def rows_workspace_bytes(count: int, cols: int = 1) -> int:
+    return int(lib().fastsgd_rows_workspace_bytes(count, cols))
+
+
+def ensure_rows_workspace(count: int, cols: int = 1, device="cuda") -> torch.Tensor:
+    """Allocates (torch) and registers a workspace large enough for these calls on `count` ids or rows of `cols` columns, if needed."""
+    return _ensure(rows_workspace_bytes(count, cols), device)
+
+
+def order_ids(ids: torch.Tensor, order: torch.Tensor, starts: torch.Tensor, distinct: torch.Tensor = None, number: torch.Tensor = None, stream=None) -> int:
+    """fastsgd_order_ids: ids (int32, any shape) -> order [count], starts [range + 1], distinct [min(count, range)], number [1] (int32 tensors)."""
+    dev = _device_of(starts)
+    count, span = ids.numel(), starts.numel() - 1
+    return lib().fastsgd_order_ids(_at(ids, dev, _int32, *ids.shape), count, span, _at(order, dev, _int32, count), _at(starts, dev, _int32, span + 1),
+                                   _at(distinct, dev, _int32, min(count, span)), _at(number, dev, _int32, 1), _raw_stream(stream, dev))
+
+
+def embedding(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None) -> int:
+    """fastsgd_embedding: out [tokens, cols] = scale * table[ids]."""
+    dev = _device_of(table)
+    m = _matrix(out, dev)
+    return lib().fastsgd_embedding(_matrix(table, dev), _at(ids, dev, _int32, m.rows), scale, m, _raw_stream(stream, dev))
+
+
+def embedding_backward(grad: torch.Tensor, ids: torch.Tensor, order: torch.Tensor, starts: torch.Tensor, table_grad: torch.Tensor, scale: float = 1.0,
+                       stream=None) -> int:
+    """fastsgd_embedding_backward: grad [tokens, cols] added up by token into table_grad [range, cols]."""
+    dev = _device_of(grad)
+    g, t = _matrix(grad, dev), _matrix(table_grad, dev)
+    return lib().fastsgd_embedding_backward(g, _at(ids, dev, _int32, g.rows), _at(order, dev, _int32, g.rows), _at(starts, dev, _int32, t.rows + 1), scale, t,
+                                            _raw_stream(stream, dev))
+
+
+def embedding_backward_pairs(grad: torch.Tensor, ids: torch.Tensor, order: torch.Tensor, starts: torch.Tensor, distinct: torch.Tensor, number: torch.Tensor,
+                             keys: torch.Tensor, values: torch.Tensor, scale: float = 1.0, stream=None) -> int:
+    """fastsgd_embedding_backward_pairs: the rows that occur as ascending keys (int32) and values (fp32), [most, cols] each."""
+    dev = _device_of(grad)
+    g = _matrix(grad, dev)
+    span, most = starts.numel() - 1, keys.shape[0]
+    return lib().fastsgd_embedding_backward_pairs(g, _at(ids, dev, _int32, g.rows), _at(order, dev, _int32, g.rows), _at(starts, dev, _int32, span + 1),
+                                                  _at(distinct, dev, _int32, min(g.rows, span)), _at(number, dev, _int32, 1), span, scale,
+                                                  _at(keys, dev, _int32, most, g.cols), _at(values, dev, _float32, most, g.cols), most, _raw_stream(stream, dev))
+
+
+def _experts(w: torch.Tensor, dev: int) -> Experts:
+    """Weights [experts, outs, ins]: unit stride along the ins, any other strides."""
+    kind = TYPES.get(w.dtype)
+    assert w.get_device() == dev and kind is not None and w.dim() == 3
+    experts, outs, ins = w.shape
+    apart, step, unit = w.stride()
+    assert unit == 1 or ins == 1
+    step = step if outs > 1 else ins
+    return Experts(w.data_ptr(), experts, outs, ins, step, apart if experts > 1 else outs * step, kind, 0)
+
+
+def _order(order, dev: int, rows: int):
+    return None if order is None else _at(order, dev, _int32, rows)
+
+
+def expert_product(x: torch.Tensor, weights: torch.Tensor, starts: torch.Tensor, y: torch.Tensor, order: torch.Tensor = None, per_row: int = 1, stream=None) -> int:
+    """fastsgd_expert_product: y [rows, outs] = rows of x (by order // per_row) times their expert's weights [experts, outs, ins]."""
+    dev = _device_of(x)
+    w, m = _experts(weights, dev), _matrix(y, dev)
+    return lib().fastsgd_expert_product(_matrix(x, dev), _order(order, dev, m.rows), per_row, _at(starts, dev, _int32, w.experts + 1), w, m, _raw_stream(stream, dev))
+
+
+def expert_product_backward_input(grad_y: torch.Tensor, weights: torch.Tensor, starts: torch.Tensor, grad_x: torch.Tensor, stream=None) -> int:
+    """fastsgd_expert_product_backward_input: grad_x [rows, ins] of the sorted rows."""
+    dev = _device_of(grad_y)
+    w = _experts(weights, dev)
+    return lib().fastsgd_expert_product_backward_input(_matrix(grad_y, dev), _at(starts, dev, _int32, w.experts + 1), w, _matrix(grad_x, dev), _raw_stream(stream, dev))
+
+
+def expert_product_backward_weights(grad_y: torch.Tensor, x: torch.Tensor, starts: torch.Tensor, grad_weights: torch.Tensor, order: torch.Tensor = None,
+                                    per_row: int = 1, stream=None) -> int:
+    """fastsgd_expert_product_backward_weights: grad_weights [experts, outs, ins]."""
+    dev = _device_of(grad_y)
+    g, w = _matrix(grad_y, dev), _experts(grad_weights, dev)
+    return lib().fastsgd_expert_product_backward_weights(g, _matrix(x, dev), _order(order, dev, g.rows), per_row, _at(starts, dev, _int32, w.experts + 1), w,
+                                                         _raw_stream(stream, dev))
 
 
 def stream_info(stream_in: torch.Tensor, stream=None):

@@ -3,7 +3,6 @@
 #include "../../include/fastsgd.h"
 
 #include <cmath>
-#include <mutex>
 
 #include "host.cuh"
 #include "top.cuh"
@@ -17,22 +16,7 @@ using namespace fsg;
 constexpr double kLog2E = 1.4426950408889634;
 constexpr float  kLeastTemperature = 1.f / 1048576.f, kMostTemperature = 1048576.f;
 
-uint32_t size_of(uint32_t type) { return type == FASTSGD_F32 ? 4u : 2u; }
-bool is_type(uint32_t type) { return type == FASTSGD_F32 || type == FASTSGD_BF16 || type == FASTSGD_F16; }
-bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool is_temperature(float t) { return t >= kLeastTemperature && t <= kMostTemperature; }
-
-int check_matrix(const fastsgd_matrix* m) {
-    if (!m) return FASTSGD_E_NULL;
-    if (!is_type(m->type) || m->reserved) return FASTSGD_E_BAD_PARAM;
-    if (m->rows >= (1ull << 31) || m->cols == 0 || m->cols >= (1ull << 31)) return FASTSGD_E_BAD_N;
-    if (m->row_stride < m->cols || m->row_stride >= (1ull << 31)) return FASTSGD_E_BAD_PARAM;
-    if (m->rows && !m->data) return FASTSGD_E_NULL;
-    if (!aligned_to(m->data, size_of(m->type))) return FASTSGD_E_ALIGN;
-    return FASTSGD_OK;
-}
-
-uint64_t span_bytes(const fastsgd_matrix* m) { return m->rows ? ((m->rows - 1) * m->row_stride + m->cols) * size_of(m->type) : 0; }
 
 // A gradient: of the logits' shape, in their type or fp32; the logits' own place, element for element, or apart from them.
 int check_grad(const fastsgd_matrix* grad, const fastsgd_matrix* logits) {
@@ -43,37 +27,6 @@ int check_grad(const fastsgd_matrix* grad, const fastsgd_matrix* logits) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(grad->data), b = reinterpret_cast<uintptr_t>(logits->data);
     const bool same = a == b && grad->type == logits->type && grad->row_stride == logits->row_stride;
     if (!same && a < b + span_bytes(logits) && b < a + span_bytes(grad)) return FASTSGD_E_BAD_PARAM;
-    return FASTSGD_OK;
-}
-
-int launched(cudaError_t err, uint64_t launches = 1) {
-    if (err != cudaSuccess) { cudaGetLastError(); return FASTSGD_E_CUDA; }
-    count_launches(launches);
-    return FASTSGD_OK;
-}
-
-// Blocks of a kernel that stay on the GPU at once (asked for once per device, kernel and size; asking costs as much as a small launch).
-struct Residency { int dev; const void* fn; size_t smem; uint64_t blocks; };
-constexpr int kResidencies = 64;
-std::mutex g_residency_mu;
-Residency g_residency[kResidencies];
-int g_residencies = 0;
-int resident_blocks(const void* fn, int threads, size_t smem, const DeviceView& dev, uint64_t* out) {
-    std::lock_guard<std::mutex> lock(g_residency_mu);
-    for (int i = 0; i < g_residencies; ++i) {
-        const Residency& r = g_residency[i];
-        if (r.fn == fn && r.smem == smem && r.dev == dev.device) { *out = r.blocks; return FASTSGD_OK; }
-    }
-    int per_sm = 0, most = 0;
-    cudaFuncAttributes at;
-    if (cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev.device) != cudaSuccess || cudaFuncGetAttributes(&at, fn) != cudaSuccess
-        || cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)at.sharedSizeBytes) != cudaSuccess) {
-        cudaGetLastError();
-        return FASTSGD_E_CUDA;
-    }
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, threads, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); return FASTSGD_E_CUDA; }
-    *out = (uint64_t)per_sm * (uint64_t)dev.sm_count;
-    g_residency[g_residencies < kResidencies ? g_residencies++ : kResidencies - 1] = Residency{dev.device, fn, smem, *out};
     return FASTSGD_OK;
 }
 

@@ -1,0 +1,352 @@
+// Ids put in order: positions by (id, position), where each id's begin, and the ids that occur.  What the gradient of an embedding
+// and a router's experts are both worked by.
+//
+// A stable sort by digits, lowest first, of 10 bits at most: one digit for a router's experts, two for a vocabulary.  Ids outside the
+// range become the range itself, the largest key, and are sorted like the others but not written.  Within a warp equal digits find one
+// another by match; each warp counts its digits in shared memory, so that an element's place is the sum of four numbers: elements of lower
+// digits, of its digit in earlier blocks, in earlier warps, and before it in its warp.  No place depends on the order in which threads run.
+//
+// Up to 2^16 ids are sorted by one cluster of eight blocks in its shared memory (k_order): no launch between digits and no
+// workspace.  More take three launches a digit (k_order_count, k_order_offsets, k_order_place), with keys and positions in the workspace.
+#pragma once
+
+#include "common.cuh"
+
+namespace fsg {
+
+constexpr int      kOrderThreads  = 1024;
+constexpr int      kOrderWarps    = kOrderThreads / 32;
+constexpr uint32_t kOrderBlocks   = 8u;                   // of the cluster
+constexpr uint32_t kOrderMaxBins  = 1024u;
+constexpr uint32_t kOrderRounds   = 8u;                   // elements of a thread
+constexpr uint32_t kOrderTile     = kOrderThreads * kOrderRounds;
+constexpr uint32_t kOrderMaxFew   = kOrderTile * kOrderBlocks;      // ids that the cluster takes
+constexpr uint32_t kOrderMaxRange = 1u << 20;
+
+struct OrderArgs {
+    const int32_t* ids;
+    uint32_t  count, range;
+    uint32_t* order;
+    uint32_t* starts;                                     // range + 1
+    uint32_t* distinct;                                   // or nullptr
+    uint32_t* number;                                     // or nullptr
+    uint32_t  passes, bits;                               // digits and their width
+    uint32_t  pass;                                       // (many ids) this launch's
+    uint32_t  blocks;                                     // (many ids) tiles
+    uint32_t* keys[2];                                    // (many ids) between passes
+    uint32_t* places[2];
+    uint32_t* table;                                      // (many ids) bins x blocks: counts, then elements of that digit in earlier tiles
+    uint32_t* totals;                                     // (many ids) bins
+};
+
+__device__ __forceinline__ uint32_t order_key(const OrderArgs& a, uint32_t i) {
+    const uint32_t id = (uint32_t)a.ids[i];
+    return id < a.range ? id : a.range;
+}
+__device__ __forceinline__ uint32_t digit_of(const OrderArgs& a, uint32_t key, uint32_t pass) { return (key >> (pass * a.bits)) & ((1u << a.bits) - 1u); }
+
+// The exclusive sum of one value a thread over the block, and the sum of all; every thread calls it.
+__device__ __forceinline__ uint32_t order_scan(uint32_t x, uint32_t* warp_sums, uint32_t* total) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    uint32_t y = x;
+#pragma unroll
+    for (uint32_t d = 1; d < 32u; d *= 2u) {
+        const uint32_t up = __shfl_up_sync(kFullMask, y, d);
+        if (lane >= d) y += up;
+    }
+    if (lane == 31u) warp_sums[warp] = y;
+    __syncthreads();
+    if (warp == 0u) {
+        uint32_t w = warp_sums[lane];
+#pragma unroll
+        for (uint32_t d = 1; d < 32u; d *= 2u) {
+            const uint32_t up = __shfl_up_sync(kFullMask, w, d);
+            if (lane >= d) w += up;
+        }
+        warp_sums[lane] = w;
+    }
+    __syncthreads();
+    const uint32_t before = warp ? warp_sums[warp - 1u] : 0u;
+    *total = warp_sums[31];
+    __syncthreads();
+    return before + y - x;
+}
+
+// Each warp's elements of a tile lie next to each other.  Counts the warp's digits in `mine` (bins, zero before) and gives each element the
+// number of those of its digit before it in the warp.  `have` elements of this warp; digits beyond are of no account.
+template <class Key> __device__ __forceinline__ void order_rank(uint16_t* mine, uint32_t have, Key key_at, uint32_t (&digit)[kOrderRounds], uint32_t (&rank)[kOrderRounds]) {
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll
+    for (uint32_t j = 0; j < kOrderRounds; ++j) {
+        digit[j] = ~0u;
+        if (32u * j >= have) continue;
+        const bool in = 32u * j + lane < have;
+        if (in) digit[j] = key_at(j);
+        const uint32_t same = __match_any_sync(kFullMask, digit[j]);
+        const uint32_t before = __popc(same & ((1u << lane) - 1u));
+        uint32_t old = 0;
+        if (in) old = mine[digit[j]];
+        __syncwarp();
+        if (in && before == 0u) mine[digit[j]] = (uint16_t)(old + __popc(same));
+        __syncwarp();
+        rank[j] = old + before;
+    }
+}
+
+// Over the block's warps: counts become the numbers of the same digit in earlier warps; sums[bin]: in all.
+__device__ __forceinline__ void order_over_warps(uint16_t* counts, uint32_t bins, uint32_t* sums) {
+    if (threadIdx.x < bins) {
+        uint32_t sum = 0;
+#pragma unroll 8
+        for (int w = 0; w < kOrderWarps; ++w) {
+            uint16_t* c = counts + (uint32_t)w * bins + threadIdx.x;
+            const uint32_t n = *c;
+            *c = (uint16_t)sum;
+            sum += n;
+        }
+        sums[threadIdx.x] = sum;
+    }
+}
+
+__device__ __forceinline__ uint32_t cluster_block() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+// Every thread of the cluster's blocks; what they wrote before, to shared or global memory, is visible behind it.
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t address_in(const void* p, uint32_t block) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(block));
+    return r;
+}
+__device__ __forceinline__ uint32_t load_from(uint32_t at) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory"); return v; }
+__device__ __forceinline__ void store_to(uint32_t at, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void store_to(uint32_t at, uint16_t v) { asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
+
+struct OrderShared {
+    uint32_t sums[kOrderMaxBins];                         // this block's, by digit
+    uint32_t base[kOrderMaxBins];                         // places of its first element of each digit
+    uint32_t warp_sums[32];
+    uint32_t of_block[2];                                 // occurrences and ids that occur in this block's part of the range
+    uint32_t pad[2];
+    uint32_t keys[2][kOrderTile];
+    uint16_t places[2][kOrderTile];
+    uint16_t counts[kOrderWarps * kOrderMaxBins];         // by warp and digit (as many digits as there are)
+};
+
+// Where each id's positions begin, from its number of occurrences in starts (one cluster; `slice` ids a block), and the ids that occur.
+__device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, OrderShared& s, uint32_t block) {
+    const uint32_t slice = ((a.range + kOrderBlocks) / kOrderBlocks + 3u) & ~3u;      // (of range + 1 entries)
+    const uint32_t lo = block * slice, hi = min(lo + slice, a.range + 1u);
+    uint32_t sum = 0, occur = 0;
+    for (uint32_t v = lo + threadIdx.x; v < hi; v += kOrderThreads) {
+        const uint32_t n = v < a.range ? __ldcg(a.starts + v) : 0u;
+        sum += n;
+        occur += n != 0u;
+    }
+    uint32_t total = 0, total_occur = 0;
+    order_scan(sum, s.warp_sums, &total);
+    order_scan(occur, s.warp_sums, &total_occur);
+    if (threadIdx.x == 0) { s.of_block[0] = total; s.of_block[1] = total_occur; }
+    cluster_meet();
+    uint32_t at = 0, at_occur = 0, all_occur = 0;
+    for (uint32_t b = 0; b < kOrderBlocks; ++b) {
+        const uint32_t from = address_in(s.of_block, b), n = load_from(from), o = load_from(from + 4u);
+        if (b < block) { at += n; at_occur += o; }
+        all_occur += o;
+    }
+    for (uint32_t v0 = lo; v0 < hi; v0 += kOrderThreads) {
+        const uint32_t v = v0 + threadIdx.x;
+        const uint32_t n = v < hi && v < a.range ? __ldcg(a.starts + v) : 0u;
+        const uint32_t before = order_scan(n, s.warp_sums, &total);
+        if (v < hi) a.starts[v] = at + before;
+        at += total;
+        if (a.distinct) {
+            const uint32_t rank = order_scan(n != 0u, s.warp_sums, &total_occur);
+            if (n) a.distinct[at_occur + rank] = v;
+            at_occur += total_occur;
+        }
+    }
+    if (a.number && block == 0u && threadIdx.x == 0) *a.number = all_occur;
+}
+
+// One cluster: everything.
+__global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constant__ OrderArgs a) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    OrderShared& s = *reinterpret_cast<OrderShared*>(raw);
+    const uint32_t block = cluster_block(), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t bins = 1u << a.bits;
+    // slices of a power of two of elements, from 32 a warp on
+    uint32_t per_log = 5;                                 // log2 of a warp's
+    while ((kOrderBlocks * kOrderWarps << per_log) < a.count) ++per_log;
+    const uint32_t slice_log = per_log + 5u, slice = 1u << slice_log;
+    const uint32_t begin = min(a.count, block << slice_log), end = min(a.count, begin + slice);
+    const uint32_t first = begin + (warp << per_log);
+    const uint32_t have = first < end ? min(end - first, 1u << per_log) : 0u;
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    for (uint32_t v = block * kOrderThreads + threadIdx.x; v < a.range; v += kOrderBlocks * kOrderThreads) a.starts[v] = 0u;
+    for (uint32_t i = threadIdx.x; i < end - begin; i += kOrderThreads) s.keys[0][i] = order_key(a, begin + i);
+    cluster_meet();
+    for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
+        const uint32_t i = i0 + threadIdx.x;
+        const uint32_t key = i < end - begin ? s.keys[0][i] : a.range;
+        const uint32_t same = __match_any_sync(kFullMask, key);
+        if (key < a.range && lane == (uint32_t)__ffs((int)same) - 1u) atomicAdd(a.starts + key, (uint32_t)__popc(same));
+    }
+    uint32_t from = 0;
+    for (uint32_t pass = 0; pass < a.passes; ++pass) {
+        for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
+        __syncthreads();
+        uint16_t* mine = s.counts + warp * bins;
+        uint32_t digit[kOrderRounds], rank[kOrderRounds];
+        const uint32_t local = warp << per_log;
+        order_rank(mine, have, [&](uint32_t j) { return digit_of(a, s.keys[from][local + 32u * j + lane], pass); }, digit, rank);
+        __syncthreads();
+        order_over_warps(s.counts, bins, s.sums);
+        cluster_meet();
+        uint32_t all = 0, before = 0, total = 0;
+        if (threadIdx.x < bins)
+            for (uint32_t b = 0; b < kOrderBlocks; ++b) {
+                const uint32_t n = load_from(address_in(s.sums + threadIdx.x, b));
+                all += n;
+                if (b < block) before += n;
+            }
+        const uint32_t lower = order_scan(all, s.warp_sums, &total);
+        if (threadIdx.x < bins) s.base[threadIdx.x] = lower + before;
+        __syncthreads();
+        const bool last = pass + 1u == a.passes;
+#pragma unroll
+        for (uint32_t j = 0; j < kOrderRounds; ++j) {
+            if (digit[j] == ~0u) continue;
+            const uint32_t i = local + 32u * j + lane;
+            const uint32_t key = s.keys[from][i];
+            const uint32_t place = pass ? s.places[from][i] : begin + i;
+            const uint32_t to = s.base[digit[j]] + mine[digit[j]] + rank[j];
+            if (last) {
+                if (key < a.range) a.order[to] = place;
+            } else {
+                const uint32_t there = to >> slice_log, at = to & (slice - 1u);
+                store_to(address_in(&s.keys[from ^ 1u][at], there), key);
+                store_to(address_in(&s.places[from ^ 1u][at], there), (uint16_t)place);
+            }
+        }
+        from ^= 1u;
+        cluster_meet();                                   // (also: the sums have been read before they are formed anew, or their block ends)
+    }
+    order_starts_from_counts(a, s, block);
+    cluster_meet();                                       // (no block ends while others read its shared memory)
+}
+
+struct OrderTileShared {
+    uint32_t sums[kOrderMaxBins];
+    uint32_t warp_sums[32];
+    uint16_t counts[kOrderWarps * kOrderMaxBins];
+};
+
+__device__ __forceinline__ uint32_t many_key(const OrderArgs& a, uint32_t i) { return a.pass ? a.keys[a.pass & 1u][i] : order_key(a, i); }
+
+// Counts of a tile's digits (MODE 0), or its elements to their places (MODE 1).
+template <int PLACE> __global__ void __launch_bounds__(kOrderThreads, 1) k_order_tile(const __grid_constant__ OrderArgs a) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    OrderTileShared& s = *reinterpret_cast<OrderTileShared*>(raw);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, bins = 1u << a.bits;
+    const uint32_t first = blockIdx.x * kOrderTile + warp * 32u * kOrderRounds;
+    const uint32_t have = first < a.count ? min(a.count - first, 32u * kOrderRounds) : 0u;
+    for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    __syncthreads();
+    uint16_t* mine = s.counts + warp * bins;
+    uint32_t digit[kOrderRounds], rank[kOrderRounds], key[kOrderRounds];
+    order_rank(mine, have, [&](uint32_t j) { key[j] = many_key(a, first + 32u * j + lane); return digit_of(a, key[j], a.pass); }, digit, rank);
+    __syncthreads();
+    order_over_warps(s.counts, bins, s.sums);
+    if constexpr (PLACE == 0) {
+        if (threadIdx.x < bins) a.table[(uint64_t)threadIdx.x * a.blocks + blockIdx.x] = s.sums[threadIdx.x];
+        return;
+    }
+    uint32_t total = 0;
+    const uint32_t lower = order_scan(threadIdx.x < bins ? __ldcg(a.totals + threadIdx.x) : 0u, s.warp_sums, &total);
+    if (threadIdx.x < bins) s.sums[threadIdx.x] = lower + __ldcg(a.table + (uint64_t)threadIdx.x * a.blocks + blockIdx.x);
+    __syncthreads();
+    const bool last = a.pass + 1u == a.passes;
+    const uint32_t to_buffer = (a.pass + 1u) & 1u;
+#pragma unroll
+    for (uint32_t j = 0; j < kOrderRounds; ++j) {
+        if (digit[j] == ~0u) continue;
+        const uint32_t i = first + 32u * j + lane;
+        const uint32_t place = a.pass ? a.places[a.pass & 1u][i] : i;
+        const uint32_t to = s.sums[digit[j]] + mine[digit[j]] + rank[j];
+        a.keys[to_buffer][to] = key[j];
+        if (!last) a.places[to_buffer][to] = place;
+        else if (key[j] < a.range) a.order[to] = place;
+    }
+}
+
+// A warp a digit: counts of its tiles become the numbers in earlier tiles.
+__global__ void __launch_bounds__(256) k_order_offsets(const __grid_constant__ OrderArgs a) {
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    const uint32_t bin = blockIdx.x * 8u + (threadIdx.x >> 5), lane = threadIdx.x & 31u;
+    if (bin >= 1u << a.bits) return;
+    uint32_t* row = a.table + (uint64_t)bin * a.blocks;
+    uint32_t sum = 0;
+    for (uint32_t b0 = 0; b0 < a.blocks; b0 += 32u) {
+        const uint32_t b = b0 + lane, n = b < a.blocks ? row[b] : 0u;
+        uint32_t y = n;
+#pragma unroll
+        for (uint32_t d = 1; d < 32u; d *= 2u) {
+            const uint32_t up = __shfl_up_sync(kFullMask, y, d);
+            if (lane >= d) y += up;
+        }
+        if (b < a.blocks) row[b] = sum + y - n;
+        sum += __shfl_sync(kFullMask, y, 31);
+    }
+    if (lane == 0u) a.totals[bin] = sum;
+}
+
+// Where each id's positions begin: the first place whose key is not below it.
+__global__ void __launch_bounds__(256) k_order_starts(const __grid_constant__ OrderArgs a) {
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    const uint32_t* keys = a.keys[a.passes & 1u];
+    const uint32_t v = blockIdx.x * 256u + threadIdx.x;
+    if (v > a.range) return;
+    uint32_t lo = 0, hi = a.count;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        if (keys[mid] < v) lo = mid + 1u; else hi = mid;
+    }
+    a.starts[v] = lo;
+}
+
+// The ids that occur, from the starts (one cluster).
+__global__ void __launch_bounds__(kOrderThreads, 1) k_order_distinct(const __grid_constant__ OrderArgs a) {
+    __shared__ uint32_t warp_sums[32], of_block;
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    const uint32_t block = cluster_block(), slice = (a.range + kOrderBlocks - 1u) / kOrderBlocks;
+    const uint32_t lo = min(block * slice, a.range), hi = min(lo + slice, a.range);
+    uint32_t occur = 0, total = 0;
+    for (uint32_t v = lo + threadIdx.x; v < hi; v += kOrderThreads) occur += a.starts[v + 1u] != a.starts[v];
+    order_scan(occur, warp_sums, &total);
+    if (threadIdx.x == 0) of_block = total;
+    cluster_meet();
+    uint32_t at = 0, all = 0;
+    for (uint32_t b = 0; b < kOrderBlocks; ++b) {
+        const uint32_t n = load_from(address_in(&of_block, b));
+        if (b < block) at += n;
+        all += n;
+    }
+    for (uint32_t v0 = lo; v0 < hi; v0 += kOrderThreads) {
+        const uint32_t v = v0 + threadIdx.x;
+        const bool occurs = v < hi && a.starts[v + 1u] != a.starts[v];
+        const uint32_t rank = order_scan(occurs, warp_sums, &total);
+        if (occurs && a.distinct) a.distinct[at + rank] = v;
+        at += total;
+    }
+    if (a.number && block == 0u && threadIdx.x == 0) *a.number = all;
+    cluster_meet();
+}
+
+}  // namespace fsg

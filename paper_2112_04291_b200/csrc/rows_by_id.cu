@@ -1,0 +1,369 @@
+// C-ABI entries of the operators on rows that are chosen by an id: ids in order, an embedding's lookup and gradient, a router's
+// experts' products.  Argument checks and launches on the caller's stream, as in losses.cu.
+#include <atomic>
+
+#include "host.cuh"
+#include "order.cuh"
+#include "embed.cuh"
+#include "experts.cuh"
+
+namespace {
+
+using namespace fsg;
+
+bool apart(const void* p, uint64_t p_bytes, const void* q, uint64_t q_bytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return !p || !q || a + p_bytes <= b || b + q_bytes <= a;
+}
+bool apart(const fastsgd_matrix* p, const fastsgd_matrix* q) { return apart(p->data, span_bytes(p), q->data, span_bytes(q)); }
+
+// one of the two is of 32 bits, or they are alike
+bool types_go(uint32_t from, uint32_t to) { return from == to || from == FASTSGD_F32 || to == FASTSGD_F32; }
+bool rows_on_16(const fastsgd_matrix* m) { return aligned_to(m->data, 16) && (m->rows < 2 || m->row_stride * size_of(m->type) % 16u == 0); }
+
+uint64_t up_to(uint64_t x, uint64_t unit) { return (x + unit - 1) / unit * unit; }
+
+// ---- ids in order ---------------------------------------------------------------------------------
+
+uint64_t order_blocks(uint64_t count) { return (count + kOrderTile - 1) / kOrderTile; }
+uint64_t order_bytes(uint64_t count) {                     // behind the workspace's fixed part
+    return count <= kOrderMaxFew ? 0 : 4u * up_to(4u * count, 256) + up_to(4ull * kOrderMaxBins * order_blocks(count), 256) + 4u * kOrderMaxBins;
+}
+
+// ---- an embedding's gradient -------------------------------------------------------------------------
+
+// Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave 2^13 warps, a few rounds of
+// what the GPU holds at once.
+struct GradientShape { uint32_t lanes_log, chunks, tile_log, tiles; uint64_t part_stride; };
+GradientShape gradient_shape(uint64_t count, uint64_t cols) {
+    GradientShape g{};
+    while (g.lanes_log < 5u && (8ull << g.lanes_log) < cols) ++g.lanes_log;
+    const uint64_t chunks = (cols + (8ull << g.lanes_log) - 1) / (8ull << g.lanes_log);
+    g.chunks = (uint32_t)chunks;
+    g.tile_log = 4;
+    while ((((count + (1ull << g.tile_log) - 1) >> g.tile_log) * chunks << g.lanes_log) > (1ull << 13) * 32u && (1ull << g.tile_log) < count) ++g.tile_log;
+    g.tiles = (uint32_t)((count + (1ull << g.tile_log) - 1) >> g.tile_log);
+    g.part_stride = up_to(cols, 4);
+    return g;
+}
+uint64_t part_bytes(const GradientShape& g) { return 8ull * g.tiles * g.part_stride; }
+
+template <class T, bool WIDE, bool PAIRS> const void* sum_kernel_of(uint32_t to) {
+    if constexpr (PAIRS) return (const void*)k_embedding_sum<T, float, WIDE, true>;
+    else {
+        if (to == FASTSGD_F32) return (const void*)k_embedding_sum<T, float, WIDE, false>;
+        if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? (const void*)k_embedding_sum<T, __nv_bfloat16, WIDE, false> : (const void*)k_embedding_sum<T, __half, WIDE, false>;
+        else return (const void*)k_embedding_sum<T, T, WIDE, false>;
+    }
+}
+template <bool WIDE, bool PAIRS> const void* sum_kernel(uint32_t from, uint32_t to) {
+    return from == FASTSGD_F32 ? sum_kernel_of<float, WIDE, PAIRS>(to) : from == FASTSGD_BF16 ? sum_kernel_of<__nv_bfloat16, WIDE, PAIRS>(to) : sum_kernel_of<__half, WIDE, PAIRS>(to);
+}
+template <bool WIDE, bool PAIRS> const void* join_kernel(uint32_t to) {
+    if constexpr (PAIRS) return (const void*)k_embedding_join<float, WIDE, true>;
+    else return to == FASTSGD_F32 ? (const void*)k_embedding_join<float, WIDE, false> : to == FASTSGD_BF16 ? (const void*)k_embedding_join<__nv_bfloat16, WIDE, false>
+                                                                                       : (const void*)k_embedding_join<__half, WIDE, false>;
+}
+template <class T, bool WIDE> const void* lookup_kernel_of(uint32_t to) {
+    if (to == FASTSGD_F32) return (const void*)k_embedding<T, float, WIDE>;
+    if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? (const void*)k_embedding<T, __nv_bfloat16, WIDE> : (const void*)k_embedding<T, __half, WIDE>;
+    else return (const void*)k_embedding<T, T, WIDE>;
+}
+template <bool WIDE> const void* lookup_kernel(uint32_t from, uint32_t to) {
+    return from == FASTSGD_F32 ? lookup_kernel_of<float, WIDE>(to) : from == FASTSGD_BF16 ? lookup_kernel_of<__nv_bfloat16, WIDE>(to) : lookup_kernel_of<__half, WIDE>(to);
+}
+
+template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& g, bool wide, uint32_t from, uint32_t to, const DeviceView& dev, cudaStream_t st) {
+    if (part_bytes(g) && (!dev.ws || dev.ws_bytes < kPartialsOffset + part_bytes(g))) return FASTSGD_E_NO_WORKSPACE;
+    a.lanes_log = g.lanes_log; a.chunks = g.chunks; a.tile_log = g.tile_log; a.tiles = g.tiles; a.part_stride = g.part_stride;
+    a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset);
+    const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log;
+    a.sum_blocks = ((uint64_t)g.tiles * g.chunks + groups - 1) / groups;
+    uint64_t blocks = a.sum_blocks;
+    if (!PAIRS) {
+        const uint64_t all = ((uint64_t)a.vocab * g.chunks + groups - 1) / groups, some = 16ull * (uint64_t)dev.sm_count;
+        blocks += all < some ? all : some;
+    }
+    if (blocks >= 1ull << 31 || (uint64_t)g.tiles * g.chunks >= 1ull << 31) return FASTSGD_E_BAD_N;
+    void* kargs[] = {&a};
+    if (blocks) {
+        const int rc = launched(launch_overlapped(wide ? sum_kernel<true, PAIRS>(from, to) : sum_kernel<false, PAIRS>(from, to), (unsigned)blocks, kEmbedThreads, 0, kargs, st));
+        if (rc) return rc;
+    }
+    if (g.tiles < 2u) return FASTSGD_OK;
+    return launched(launch_overlapped(wide ? join_kernel<true, PAIRS>(to) : join_kernel<false, PAIRS>(to), g.tiles * g.chunks, kEmbedThreads, 0, kargs, st));
+}
+
+// ---- experts' products ----------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static std::atomic<EncodeTiled> known{nullptr};
+    EncodeTiled fn = known.load(std::memory_order_relaxed);
+    if (!fn) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) { cudaGetLastError(); return nullptr; }
+        fn = reinterpret_cast<EncodeTiled>(p);
+        known.store(fn, std::memory_order_relaxed);
+    }
+    return fn;
+}
+// A map of a matrix of 16-bit values (experts > 0: of so many of them) for boxes of 64 columns and box_rows rows.
+int map_rows(CUtensorMap* map, const void* data, uint32_t type, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows, uint64_t experts = 0, uint64_t expert_stride = 0) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return FASTSGD_E_CUDA;
+    const cuuint64_t dims[3] = {cols, rows, experts}, strides[2] = {stride * 2u, expert_stride * 2u};
+    const cuuint32_t box[3] = {64u, box_rows, 1u}, steps[3] = {1u, 1u, 1u};
+    const CUresult rc = encode(map, type == FASTSGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, experts ? 3u : 2u, const_cast<void*>(data), dims, strides, box, steps,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? FASTSGD_OK : FASTSGD_E_CUDA;
+}
+
+// Rows of a product: of 16 bits (an output: or of 32), on 16 bytes, in vectors of 8 values.
+int check_product_rows(const fastsgd_matrix* m, bool output) {
+    const int rc = check_matrix(m);
+    if (rc) return rc;
+    if (!output && m->type == FASTSGD_F32) return FASTSGD_E_NOT_IMPLEMENTED;
+    if (!aligned_to(m->data, 16) || m->cols % 8u || m->row_stride % 8u) return FASTSGD_E_ALIGN;
+    return FASTSGD_OK;
+}
+int check_experts(const fastsgd_experts* w, bool output) {
+    if (!w || !w->data) return FASTSGD_E_NULL;
+    if (!is_type(w->type) || w->reserved || w->experts < 1 || w->experts > kProductMaxExperts) return FASTSGD_E_BAD_PARAM;
+    if (!w->outs || !w->ins || w->outs >= 1ull << 31 || w->ins >= 1ull << 31) return FASTSGD_E_BAD_N;
+    if (w->row_stride < w->ins || w->row_stride >= 1ull << 31 || w->expert_stride / w->row_stride < w->outs || w->expert_stride >= 1ull << 38) return FASTSGD_E_BAD_PARAM;
+    if (!output && w->type == FASTSGD_F32) return FASTSGD_E_NOT_IMPLEMENTED;
+    if (!aligned_to(w->data, 16) || w->ins % 8u || w->outs % 8u || w->row_stride % 8u || w->expert_stride % 8u) return FASTSGD_E_ALIGN;
+    return FASTSGD_OK;
+}
+uint64_t span_bytes(const fastsgd_experts* w) { return ((w->experts - 1) * w->expert_stride + (w->outs - 1) * w->row_stride + w->ins) * size_of(w->type); }
+
+template <int MODE> const void* product_kernel(uint32_t to) {
+    return to == FASTSGD_F32 ? (const void*)k_product<float, MODE> : to == FASTSGD_BF16 ? (const void*)k_product<__nv_bfloat16, MODE> : (const void*)k_product<__half, MODE>;
+}
+
+// `tiles`: at most
+template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t to, const DeviceView& dev, cudaStream_t st) {
+    if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
+    a.tries = dev.tries;
+    a.stages = (uint32_t)((216u * 1024u) / product_stage_bytes(a.most_n));
+    if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
+    const void* fn = product_kernel<MODE>(to);
+    const size_t smem = (size_t)a.stages * product_stage_bytes(a.most_n) + 1024u;
+    uint64_t resident = 0;
+    const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);
+    if (rc) return rc;
+    const uint64_t blocks = tiles < resident ? tiles : resident;
+    void* kargs[] = {&a};
+    return launched(launch_overlapped(fn, (unsigned)blocks, kProductThreads, smem, kargs, st));
+}
+
+// Columns of a tile where the rows' side is ragged: enough for most experts' rows in one.
+uint32_t columns_for(uint64_t rows, uint64_t experts) {
+    uint32_t n = 32u;
+    while (n < 256u && n * experts < 2u * rows) n *= 2u;
+    return n;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t fastsgd_rows_workspace_bytes(uint64_t count, uint64_t cols) {
+    if (count >= (1ull << 31) || cols < 1 || cols >= (1ull << 31)) return 0;
+    const uint64_t order = order_bytes(count), parts = part_bytes(gradient_shape(count, cols));
+    return up_to(kPartialsOffset + (order > parts ? order : parts), 256);
+}
+
+int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32_t* order, uint32_t* starts, uint32_t* distinct, uint32_t* number, void* stream) {
+    if (count >= (1ull << 31)) return FASTSGD_E_BAD_N;
+    if (range < 1) return FASTSGD_E_BAD_PARAM;
+    if ((count && (!ids || !order)) || !starts) return FASTSGD_E_NULL;
+    if (!aligned_to(ids, 4) || !aligned_to(order, 4) || !aligned_to(starts, 4) || !aligned_to(distinct, 4) || !aligned_to(number, 4)) return FASTSGD_E_ALIGN;
+    if (range > kOrderMaxRange) return FASTSGD_E_NOT_IMPLEMENTED;
+    DeviceView dev;
+    int rc = device_view(&dev);
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    OrderArgs a{};
+    a.ids = ids; a.count = (uint32_t)count; a.range = (uint32_t)range; a.order = order; a.starts = starts; a.distinct = distinct; a.number = number;
+    uint32_t width = 1;                                    // of the keys, the range itself among them
+    while ((range >> width) != 0) ++width;
+    a.passes = (width + 9u) / 10u;
+    a.bits = (width + a.passes - 1u) / a.passes;
+    void* kargs[] = {&a};
+    uint64_t resident = 0;
+    if (count <= kOrderMaxFew) {
+        rc = resident_blocks((const void*)k_order, kOrderThreads, sizeof(OrderShared), dev, &resident);
+        return rc ? rc : launched(launch_overlapped((const void*)k_order, kOrderBlocks, kOrderThreads, sizeof(OrderShared), kargs, st, kOrderBlocks));
+    }
+    if (!dev.ws || dev.ws_bytes < kPartialsOffset + order_bytes(count)) return FASTSGD_E_NO_WORKSPACE;
+    a.blocks = (uint32_t)order_blocks(count);
+    unsigned char* at = static_cast<unsigned char*>(dev.ws) + kPartialsOffset;
+    for (uint32_t** p : {&a.keys[0], &a.keys[1], &a.places[0], &a.places[1]}) { *p = reinterpret_cast<uint32_t*>(at); at += up_to(4u * count, 256); }
+    a.table = reinterpret_cast<uint32_t*>(at);
+    a.totals = reinterpret_cast<uint32_t*>(at + up_to(4ull * kOrderMaxBins * a.blocks, 256));
+    for (const void* fn : {(const void*)k_order_tile<0>, (const void*)k_order_tile<1>}) {
+        rc = resident_blocks(fn, kOrderThreads, sizeof(OrderTileShared), dev, &resident);
+        if (rc) return rc;
+    }
+    for (a.pass = 0; a.pass < a.passes; ++a.pass) {
+        cudaError_t err = launch_overlapped((const void*)k_order_tile<0>, a.blocks, kOrderThreads, sizeof(OrderTileShared), kargs, st);
+        if (err == cudaSuccess) err = launch_overlapped((const void*)k_order_offsets, (1u << a.bits) / 8u + 1u, 256, 0, kargs, st);
+        if (err == cudaSuccess) err = launch_overlapped((const void*)k_order_tile<1>, a.blocks, kOrderThreads, sizeof(OrderTileShared), kargs, st);
+        rc = launched(err, 3);
+        if (rc) return rc;
+    }
+    rc = launched(launch_overlapped((const void*)k_order_starts, a.range / 256u + 1u, 256, 0, kargs, st));
+    if (rc || (!distinct && !number)) return rc;
+    return launched(launch_overlapped((const void*)k_order_distinct, kOrderBlocks, kOrderThreads, 0, kargs, st, kOrderBlocks));
+}
+
+int fastsgd_embedding(const fastsgd_matrix* table, const int32_t* ids, float scale, const fastsgd_matrix* out, void* stream) {
+    int rc = check_matrix(table);
+    if (rc) return rc;
+    rc = check_matrix(out);
+    if (rc) return rc;
+    if (table->cols != out->cols || !types_go(table->type, out->type) || !apart(table, out)) return FASTSGD_E_BAD_PARAM;
+    if (out->rows && !ids) return FASTSGD_E_NULL;
+    if (!aligned_to(ids, 4)) return FASTSGD_E_ALIGN;
+    if (!out->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    const GradientShape g = gradient_shape(1, table->cols);
+    LookupArgs a{};
+    a.table = table->data; a.table_stride = table->row_stride; a.ids = ids; a.count = (uint32_t)out->rows; a.vocab = (uint32_t)table->rows; a.cols = (uint32_t)table->cols;
+    a.lanes_log = g.lanes_log; a.chunks = g.chunks; a.scale = scale; a.out = out->data; a.out_stride = out->row_stride;
+    const bool wide = rows_on_16(table) && rows_on_16(out);
+    const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log, all = ((uint64_t)a.count * a.chunks + groups * kLookupAhead - 1) / (groups * kLookupAhead);
+    const uint64_t some = 64ull * (uint64_t)dev.sm_count;
+    void* kargs[] = {&a};
+    return launched(launch_overlapped(wide ? lookup_kernel<true>(table->type, out->type) : lookup_kernel<false>(table->type, out->type), (unsigned)(all < some ? all : some), kEmbedThreads, 0, kargs,
+                                      static_cast<cudaStream_t>(stream)));
+}
+
+int fastsgd_embedding_backward(const fastsgd_matrix* grad, const int32_t* ids, const uint32_t* order, const uint32_t* starts, float scale, const fastsgd_matrix* table_grad, void* stream) {
+    int rc = check_matrix(grad);
+    if (rc) return rc;
+    rc = check_matrix(table_grad);
+    if (rc) return rc;
+    if (grad->cols != table_grad->cols || !types_go(grad->type, table_grad->type) || !apart(grad, table_grad)) return FASTSGD_E_BAD_PARAM;
+    if ((grad->rows && (!ids || !order)) || !starts) return FASTSGD_E_NULL;
+    if (!aligned_to(ids, 4) || !aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!table_grad->rows) return FASTSGD_E_BAD_N;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    GradientArgs a{};
+    a.grad = grad->data; a.grad_stride = grad->row_stride; a.ids = ids; a.order = order; a.starts = starts;
+    a.count = (uint32_t)grad->rows; a.vocab = (uint32_t)table_grad->rows; a.cols = (uint32_t)grad->cols; a.scale = scale; a.out = table_grad->data; a.out_stride = table_grad->row_stride;
+    return launch_gradient<false>(a, gradient_shape(grad->rows, grad->cols), rows_on_16(grad) && rows_on_16(table_grad), grad->type, table_grad->type, dev, static_cast<cudaStream_t>(stream));
+}
+
+int fastsgd_embedding_backward_pairs(const fastsgd_matrix* grad, const int32_t* ids, const uint32_t* order, const uint32_t* starts, const uint32_t* distinct, const uint32_t* number,
+                                     uint64_t range, float scale, uint32_t* keys, float* values, uint64_t most, void* stream) {
+    int rc = check_matrix(grad);
+    if (rc) return rc;
+    if (range < 1 || range * grad->cols >= (1ull << 31) || range >= (1ull << 31) || most >= (1ull << 31)) return FASTSGD_E_BAD_N;
+    if (!starts || !number || (grad->rows && (!ids || !order || !distinct)) || (most && (!keys || !values))) return FASTSGD_E_NULL;
+    if (!aligned_to(ids, 4) || !aligned_to(order, 4) || !aligned_to(starts, 4) || !aligned_to(distinct, 4) || !aligned_to(number, 4) || !aligned_to(keys, 4) || !aligned_to(values, 4))
+        return FASTSGD_E_ALIGN;
+    const uint64_t bytes = 4u * most * grad->cols;
+    if (!apart(grad->data, span_bytes(grad), keys, bytes) || !apart(grad->data, span_bytes(grad), values, bytes) || !apart(keys, bytes, values, bytes)) return FASTSGD_E_BAD_PARAM;
+    if (!grad->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    GradientArgs a{};
+    a.grad = grad->data; a.grad_stride = grad->row_stride; a.ids = ids; a.order = order; a.starts = starts; a.distinct = distinct; a.number = number;
+    a.count = (uint32_t)grad->rows; a.vocab = (uint32_t)range; a.cols = (uint32_t)grad->cols; a.scale = scale; a.keys = keys; a.values = values; a.most = (uint32_t)most;
+    const bool wide = rows_on_16(grad) && aligned_to(keys, 16) && aligned_to(values, 16) && grad->cols % 4u == 0;
+    return launch_gradient<true>(a, gradient_shape(grad->rows, grad->cols), wide, grad->type, FASTSGD_F32, dev, static_cast<cudaStream_t>(stream));
+}
+
+int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, const uint32_t* starts, const fastsgd_experts* weights, const fastsgd_matrix* y, void* stream) {
+    int rc = check_product_rows(x, false);
+    if (!rc) rc = check_experts(weights, false);
+    if (!rc) rc = check_product_rows(y, true);
+    if (rc) return rc;
+    if (x->cols != weights->ins || y->cols != weights->outs || x->type != weights->type || (y->type != x->type && y->type != FASTSGD_F32)) return FASTSGD_E_BAD_PARAM;
+    if (per_row < 1u || (!order && per_row != 1u) || x->rows * per_row != y->rows) return FASTSGD_E_BAD_PARAM;
+    if (!apart(x, y) || !apart(weights->data, span_bytes(weights), y->data, span_bytes(y))) return FASTSGD_E_BAD_PARAM;
+    if (!starts) return FASTSGD_E_NULL;
+    if (!aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!y->rows || !x->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    ProductArgs a{};
+    a.most_n = columns_for(y->rows, weights->experts);
+    a.box = a.most_n < 128u ? a.most_n : 128u;
+    rc = map_rows(&a.a_map, weights->data, weights->type, weights->outs, weights->ins, weights->row_stride, kProductM, weights->experts, weights->expert_stride);
+    if (!rc) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, order ? 1u : a.box);
+    if (rc) return rc;
+    a.starts = starts; a.order = order; a.per_row = per_row; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)y->rows;
+    a.m = (uint32_t)weights->outs; a.k = (uint32_t)weights->ins; a.out = y->data; a.out_stride = y->row_stride;
+    a.kind = product_kind(x->type == FASTSGD_BF16, false, false);
+    return launch_product<kForward>(a, (y->rows / a.most_n + weights->experts) * ((weights->outs + kProductM - 1) / kProductM), y->type, dev, static_cast<cudaStream_t>(stream));
+}
+
+int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const uint32_t* starts, const fastsgd_experts* weights, const fastsgd_matrix* grad_x, void* stream) {
+    int rc = check_product_rows(grad_y, false);
+    if (!rc) rc = check_experts(weights, false);
+    if (!rc) rc = check_product_rows(grad_x, true);
+    if (rc) return rc;
+    if (grad_y->cols != weights->outs || grad_x->cols != weights->ins || grad_y->rows != grad_x->rows || grad_y->type != weights->type
+        || (grad_x->type != grad_y->type && grad_x->type != FASTSGD_F32)) return FASTSGD_E_BAD_PARAM;
+    if (!apart(grad_y, grad_x) || !apart(weights->data, span_bytes(weights), grad_x->data, span_bytes(grad_x))) return FASTSGD_E_BAD_PARAM;
+    if (!starts) return FASTSGD_E_NULL;
+    if (!aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!grad_y->rows) return FASTSGD_OK;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    ProductArgs a{};
+    a.most_n = columns_for(grad_y->rows, weights->experts);
+    a.box = a.most_n < 128u ? a.most_n : 128u;
+    rc = map_rows(&a.a_map, weights->data, weights->type, weights->outs, weights->ins, weights->row_stride, kProductK, weights->experts, weights->expert_stride);
+    if (!rc) rc = map_rows(&a.b_map, grad_y->data, grad_y->type, grad_y->rows, grad_y->cols, grad_y->row_stride, a.box);
+    if (rc) return rc;
+    a.starts = starts; a.per_row = 1u; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)grad_y->rows;
+    a.m = (uint32_t)weights->ins; a.k = (uint32_t)weights->outs; a.out = grad_x->data; a.out_stride = grad_x->row_stride;
+    a.kind = product_kind(grad_y->type == FASTSGD_BF16, true, false);
+    return launch_product<kInput>(a, (grad_y->rows / a.most_n + weights->experts) * ((weights->ins + kProductM - 1) / kProductM), grad_x->type, dev, static_cast<cudaStream_t>(stream));
+}
+
+int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, const uint32_t* starts, const fastsgd_experts* grad_weights,
+                                            void* stream) {
+    int rc = check_product_rows(grad_y, false);
+    if (!rc) rc = check_product_rows(x, false);
+    if (!rc) rc = check_experts(grad_weights, true);
+    if (rc) return rc;
+    if (grad_y->cols != grad_weights->outs || x->cols != grad_weights->ins || grad_y->type != x->type || (grad_weights->type != x->type && grad_weights->type != FASTSGD_F32)) return FASTSGD_E_BAD_PARAM;
+    if (per_row < 1u || (!order && per_row != 1u) || x->rows * per_row != grad_y->rows) return FASTSGD_E_BAD_PARAM;
+    if (!apart(grad_weights->data, span_bytes(grad_weights), grad_y->data, span_bytes(grad_y)) || !apart(grad_weights->data, span_bytes(grad_weights), x->data, span_bytes(x))) return FASTSGD_E_BAD_PARAM;
+    if (!starts) return FASTSGD_E_NULL;
+    if (!aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    DeviceView dev;
+    rc = device_view(&dev);
+    if (rc) return rc;
+    ProductArgs a{};
+    a.rows = x->rows ? (uint32_t)grad_y->rows : 0u;        // (none: the kernel writes zeros and uses no map)
+    a.most_n = grad_weights->ins <= 64 ? 64u : grad_weights->ins <= 128 ? 128u : 256u;
+    a.box = kProductK;
+    if (a.rows) {
+        rc = map_rows(&a.a_map, grad_y->data, grad_y->type, grad_y->rows, grad_y->cols, grad_y->row_stride, kProductK);
+        if (!rc) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, order ? 1u : kProductK);
+        if (rc) return rc;
+    }
+    a.starts = starts; a.order = order; a.per_row = per_row; a.experts = (uint32_t)grad_weights->experts;
+    a.m = (uint32_t)grad_weights->outs; a.n = (uint32_t)grad_weights->ins; a.out = grad_weights->data; a.out_stride = grad_weights->row_stride; a.out_expert = grad_weights->expert_stride;
+    a.kind = product_kind(x->type == FASTSGD_BF16, true, true);
+    return launch_product<kWeights>(a, grad_weights->experts * ((grad_weights->outs + kProductM - 1) / kProductM) * ((grad_weights->ins + a.most_n - 1) / a.most_n), grad_weights->type, dev,
+                                    static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
