@@ -52,6 +52,13 @@ __device__ __forceinline__ void bulk_load(void* dst_smem, const void* src_global
                  : "memory");
 }
 
+// ---- clusters ---------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_block() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+// Every thread of the cluster's blocks; what they wrote before, to shared or global memory, is visible behind it.
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // ---- dynamic rows -----------------------------------------------------------------------------
 // A grid has a block (or cluster) per piece of work.  One that is running asks for the launch of another to be cancelled and, when that
 // is granted, does its work: blocks that have a larger share of their SM take more, and what they set up they set up once.

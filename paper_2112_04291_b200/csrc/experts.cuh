@@ -4,9 +4,18 @@
 //   input    gx[r, :] = gy[r, :] W_e                                   over the outs
 //   weights  gW_e     = sum over the expert's rows of gy[r, :]^T x[source(r), :]     over the rows
 //
-// All three are A B^T of a tile of 128 of the weights' rows (A: the accumulator's lanes) and up to 256 of the ragged side (B: its columns):
-// the ragged side is the one whose tiles may have any multiple of 16, so that an expert with few rows costs few instructions, and the weights,
+// All three are A B^T of a tile of 256 of the weights' rows (A: the accumulator's lanes) and up to 256 of the ragged side (B: its columns):
+// the ragged side is the one whose tiles may have any multiple of 32, so that an expert with few rows costs few instructions, and the weights,
 // which bound the time where rows are few, fill whole tiles.
+//
+// A pair of blocks (two SMs) works on a tile: each copies half of A and half of B, so that an operand byte in shared memory serves twice as many
+// products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products, a third tells it what has
+// landed, and with the fourth fetches rows by the order; eight write results, while the next tile's products go into the other half of the
+// accumulators.
+//
+// The tensor cores cut off each addition to an accumulator where it exceeds 32 bits: over n values of the contraction the result loses about
+// n / 16 halves of its last bit, always towards zero (770 rows: 1.6e-6 of the result).  Where the result is wanted in 32 bits, accumulators
+// begin anew every 256 values, and the warps that write add them up in registers, rounding to nearest.
 #pragma once
 
 #include "rows.cuh"
@@ -15,18 +24,24 @@
 namespace fsg {
 
 constexpr uint32_t kProductMaxExperts = 1024u;
-constexpr int      kProductThreads    = 256;              // a warp that copies, one that multiplies, two at rest, four that write
-constexpr uint32_t kProductM          = 128u;             // of a tile
+constexpr int      kProductThreads    = 384;              // four warps that feed, eight that write
+constexpr uint32_t kProductM          = 256u;             // of a tile; half of it a block's
 constexpr uint32_t kProductK          = 64u;              // of a stage
-constexpr uint32_t kProductMaxStages  = 8u;
-constexpr uint32_t kProductBand       = 16u;              // tiles of weights that are gone through together
+constexpr uint32_t kProductMaxStages  = 12u;
+constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
+constexpr uint32_t kProductSum        = 4u;               // stages between two additions in registers (results of 32 bits)
+constexpr uint32_t kProductLag        = 3u;               // stages whose fetched rows may be on their way
+constexpr uint32_t kProductSources    = 512u;             // rows whose sources are looked up at a time
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
 struct alignas(64) ProductArgs {
     CUtensorMap a_map, b_map;
     const uint32_t* starts;
     const uint32_t* order;                                // or nullptr: source(r) = r
-    uint32_t  experts, rows, per_row, sources;            // rows: of the sorted side; sources: rows that order may name, times per_row
+    const void* x;                                        // (with an order) the rows that it names
+    uint32_t  x_stride;                                   // bytes
+    uint32_t  x_rows;
+    uint32_t  experts, rows, per_row;                     // rows: of the sorted side
     uint32_t  m, n, k;                                    // m: A's rows; n: B's (weights only); k: the contraction (forward, input)
     void*     out;
     uint64_t  out_stride, out_expert;
@@ -35,17 +50,33 @@ struct alignas(64) ProductArgs {
     uint32_t  tries;
 };
 
-__host__ __device__ constexpr uint32_t product_stage_bytes(uint32_t most_n) { return kProductM * 128u + most_n * 128u; }
+// of one block: half of A's rows and half of B's (weights: in strips of 64)
+template <int MODE> __host__ __device__ constexpr uint32_t product_stage_bytes(uint32_t most_n) {
+    return kProductM / 2u * 128u + (MODE == kWeights ? (most_n / 2u + 63u) / 64u * 8192u : most_n / 2u * 128u);
+}
 
 struct ProductShared {
-    unsigned long long full[kProductMaxStages], empty[kProductMaxStages], ready[2], taken[2], drained;
+    unsigned long long landed[kProductMaxStages];         // this block's copies
+    unsigned long long full[kProductMaxStages];           // (first block) both blocks' operands
+    unsigned long long empty[kProductMaxStages];          // the products that read them are done
+    unsigned long long ready[2];                          // an accumulator's products are done
+    unsigned long long taken[2];                          // (first block) ... and have been read, by both blocks
+    unsigned long long drained;
     uint32_t tmem, tiles;
+    uint32_t left[kProductMaxStages];                     // rows of the stage that count (weights)
+    uint32_t sources[kProductSources];
     uint32_t first_row[kProductMaxExperts + 1];
     uint32_t first_tile[kProductMaxExperts + 1];
 };
 
+// The stages in turn, and the parity of the round.
+struct ProductRing {
+    uint32_t stage = 0, round = 0;
+    __device__ __forceinline__ void next(uint32_t stages) { if (++stage == stages) { stage = 0; round ^= 1u; } }
+};
+
 struct ProductTile {
-    uint32_t expert, m0, n0, n, row, steps;               // n0: first row (weights: in); row, and steps of the contraction
+    uint32_t expert, m0, n0, n, half, row, end, steps;    // n0: first row (weights: in); half: columns of a block's B; rows row .. end; steps of the contraction
 };
 
 template <int MODE> __device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, const ProductShared& s, uint32_t t) {
@@ -59,7 +90,8 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
         p.n0 = i / mt * a.most_n;
         p.n = min(a.most_n, a.n - p.n0);
         p.row = s.first_row[p.expert];
-        p.steps = (s.first_row[p.expert + 1u] - p.row + kProductK - 1u) / kProductK;
+        p.end = s.first_row[p.expert + 1u];
+        p.steps = (p.end - p.row + kProductK - 1u) / kProductK;
     } else {
         uint32_t lo = 0, hi = a.experts;                  // the last expert whose tiles begin at t or before
         while (hi - lo > 1u) {
@@ -68,14 +100,17 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
         }
         p.expert = lo;
         const uint32_t i = t - s.first_tile[lo], rows = s.first_row[lo + 1u] - s.first_row[lo];
-        const uint32_t nt = (rows + a.most_n - 1u) / a.most_n, each = ((rows + nt - 1u) / nt + 15u) & ~15u;
+        // an expert's rows in tiles of equal length: no tile is empty, since all but one of the fewest tiles that hold them do not
+        const uint32_t nt = (rows + a.most_n - 1u) / a.most_n, each = ((rows + nt - 1u) / nt + 31u) & ~31u;
         const uint32_t band = i / (nt * kProductBand), j = i - band * nt * kProductBand, wide = min(kProductBand, mt - band * kProductBand);
         p.m0 = (band * kProductBand + j % wide) * kProductM;
         p.n0 = s.first_row[lo] + j / wide * each;
         p.n = min(each, s.first_row[lo + 1u] - p.n0);
         p.row = p.n0;
+        p.end = p.n0 + p.n;
         p.steps = (a.k + kProductK - 1u) / kProductK;
     }
+    p.half = ((p.n + 31u) & ~31u) / 2u;
     return p;
 }
 
@@ -115,179 +150,307 @@ template <int MODE> __device__ __forceinline__ void product_tables(const Product
     __syncthreads();
 }
 
-// Four sources of sorted rows r .. r + 3, those from `end` on that of the last.
-__device__ __forceinline__ int4 product_sources(const ProductArgs& a, uint32_t r, uint32_t end) {
-    int x[4];
-#pragma unroll
-    for (uint32_t i = 0; i < 4u; ++i) x[i] = (int)(a.order[min(r + i, end - 1u)] / a.per_row);
-    return make_int4(x[0], x[1], x[2], x[3]);
+// Sources of up to kProductSources rows from r on; rows from `end` on, and sources that are no row of x, are ~0.  Each of the two warps that
+// fetch rows looks up those that it fetches itself (four of every eight): neither waits for the other.
+__device__ __forceinline__ void product_sources(const ProductArgs& a, ProductShared& s, uint32_t r, uint32_t end) {
+    const uint32_t lane = threadIdx.x & 31u, mine = threadIdx.x >> 3 & 4u;
+    __syncwarp();                                         // (the last ones have been used)
+    for (uint32_t e = lane; e < kProductSources / 2u; e += 32u) {
+        const uint32_t i = (e & ~3u) * 2u + mine + (e & 3u);
+        const uint32_t source = r + i < end ? a.order[r + i] / a.per_row : ~0u;
+        s.sources[i] = source < a.x_rows ? source : ~0u;
+        if (r + i >= end + kProductK) break;              // (nor will anyone ask for those behind)
+    }
+    __syncwarp();
+}
+
+// Rows of a stage's strips from `left` on become zero: what lies behind an expert's last row counts nothing, whatever it holds.  One warp.
+__device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, uint32_t left) {
+    if (left >= kProductK) return;
+    for (uint32_t j = 0; j < strips; ++j)
+        for (uint32_t c = left * 8u + (threadIdx.x & 31u); c < kProductK * 8u; c += 32u)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(from + j * 8192u + c * 16u), "r"(0u) : "memory");
+    fence_async_reads();
+    __syncwarp();
 }
 
 template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads, 1) k_product(const __grid_constant__ ProductArgs a) {
     extern __shared__ unsigned char raw[];
     __shared__ ProductShared s;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    constexpr bool SUMS = sizeof(TO) == 4;                // accumulators are added up in registers
+    const uint32_t warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u, block = blockIdx.x & 1u;
+    const uint32_t first = blockIdx.x / 2u, step_tiles = gridDim.x / 2u;
     const uint32_t stage0 = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t stage_bytes = product_stage_bytes(a.most_n);
+    const uint32_t stage_bytes = product_stage_bytes<MODE>(a.most_n);
+    const bool fetch = MODE != kInput && a.order;
     uint32_t columns = 32u;
     while (columns < 2u * a.most_n) columns *= 2u;
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.full[i], 1u); mbar_init(&s.empty[i], 1u); }
-        for (uint32_t i = 0; i < 2u; ++i) { mbar_init(&s.ready[i], 1u); mbar_init(&s.taken[i], 4u); }
+        for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.landed[i], 1u); mbar_init(&s.full[i], fetch ? 4u : 2u); mbar_init(&s.empty[i], 1u); }
+        for (uint32_t i = 0; i < 2u; ++i) { mbar_init(&s.ready[i], 1u); mbar_init(&s.taken[i], 16u); }
         mbar_init(&s.drained, 1u);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncwarp();
     if (warp == 2u) tmem_alloc(&s.tmem, columns);
     tmem_before_barrier();
     __syncthreads();
+    cluster_meet();
     tmem_after_barrier();
     const uint32_t tmem = s.tmem;
     wait_for_previous_kernels();
     allow_next_kernel();
     product_tables<MODE>(a, s);
     const uint32_t tiles = s.tiles;
-
-    if (warp == 0u) {                                     // copies
-        uint32_t it = 0;
-        bool fine = true;
-        for (uint32_t t = blockIdx.x; t < tiles && fine; t += gridDim.x) {
-            const ProductTile p = product_tile<MODE>(a, s, t);
-            const uint32_t end = p.row + p.n, expert_end = s.first_row[p.expert + 1u];
-            const uint32_t groups = (p.n + 3u) / 4u;      // (forward, with an order)
-            int4 sources[2];
-            if (MODE == kForward && a.order) {
-#pragma unroll
-                for (uint32_t j = 0; j < 2u; ++j) if (lane + 32u * j < groups) sources[j] = product_sources(a, p.row + 4u * (lane + 32u * j), end);
-            }
-            const uint32_t boxes = (p.n + a.box - 1u) / a.box, strips = (p.n + 63u) / 64u;
-            const uint32_t bytes = kProductM * 128u + (MODE == kWeights ? strips * 8192u : MODE == kForward && a.order ? groups * 512u : boxes * a.box * 128u);
-            for (uint32_t step = 0; step < p.steps; ++step, ++it) {
-                const uint32_t stage = it % a.stages, round = it / a.stages;
-                int4 rows;
-                const uint32_t row = p.row + step * kProductK;
-                if (MODE == kWeights && a.order) rows = product_sources(a, row + 4u * (lane & 15u), expert_end);
-                fine = round == 0u || mbar_wait(&s.empty[stage], (round - 1u) & 1u, a.tries);
-                fine = __all_sync(kFullMask, fine);
-                if (!fine) break;
-                const uint32_t bar = smem_u32(&s.full[stage]), to_a = stage0 + stage * stage_bytes, to_b = to_a + kProductM * 128u;
-                const int at = (int)(step * kProductK);
-                if (lane == 0u) {
-                    mbar_expect_tx(&s.full[stage], bytes);
-                    if constexpr (MODE == kForward) tile_load_3d(to_a, &a.a_map, at, (int)p.m0, (int)p.expert, bar);
-                    else if constexpr (MODE == kInput) {
-                        tile_load_3d(to_a, &a.a_map, (int)p.m0, at, (int)p.expert, bar);
-                        tile_load_3d(to_a + 8192u, &a.a_map, (int)p.m0 + 64, at, (int)p.expert, bar);
-                    } else {
-                        tile_load_2d(to_a, &a.a_map, (int)p.m0, (int)row, bar);
-                        tile_load_2d(to_a + 8192u, &a.a_map, (int)p.m0 + 64, (int)row, bar);
-                    }
-                    if (MODE == kWeights && !a.order) for (uint32_t j = 0; j < strips; ++j) tile_load_2d(to_b + j * 8192u, &a.b_map, (int)(p.n0 + 64u * j), (int)row, bar);
-                    if (MODE == kInput || (MODE == kForward && !a.order))
-                        for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, (int)(p.row + j * a.box), bar);
-                }
-                __syncwarp();
-                if (MODE == kForward && a.order) {
-#pragma unroll
-                    for (uint32_t j = 0; j < 2u; ++j) if (lane + 32u * j < groups) rows_load(to_b + 512u * (lane + 32u * j), &a.b_map, at, sources[j], bar);
-                }
-                if (MODE == kWeights && a.order)
-                    for (uint32_t j = lane >> 4; j < strips; j += 2u) rows_load(to_b + j * 8192u + 512u * (lane & 15u), &a.b_map, (int)(p.n0 + 64u * j), rows, bar);
-            }
-        }
-        // what is still on its way lands before the block ends, whoever has given up
-        for (uint32_t i = it > a.stages ? it - a.stages : 0u; i < it; ++i) mbar_wait(&s.full[i % a.stages], i / a.stages & 1u);
-    } else if (warp == 1u) {                              // products
-        uint32_t it = 0, turn = 0;
-        bool fine = true;
-        for (uint32_t t = blockIdx.x; t < tiles && fine; t += gridDim.x) {
-            const ProductTile p = product_tile<MODE>(a, s, t);
-            if (!p.steps) continue;
-            const uint32_t buffer = turn & 1u, acc = tmem + buffer * a.most_n, shape = product_shape(a.kind, kProductM, (p.n + 15u) & ~15u);
-            if (turn >= 2u) fine = mbar_wait(&s.taken[buffer], (turn / 2u - 1u) & 1u, a.tries);
-            fine = __all_sync(kFullMask, fine);
-            if (!fine) break;
-            tmem_after_barrier();
-            const uint32_t end = s.first_row[p.expert + 1u];
-            for (uint32_t step = 0; step < p.steps; ++step, ++it) {
-                const uint32_t stage = it % a.stages;
-                fine = mbar_wait(&s.full[stage], it / a.stages & 1u, a.tries);
-                fine = __all_sync(kFullMask, fine);
-                if (!fine) break;
-                const uint32_t from_a = stage0 + stage * stage_bytes, from_b = from_a + kProductM * 128u;
-                if (MODE == kWeights && p.row + (step + 1u) * kProductK > end) {     // rows behind the expert's last count nothing, whatever they hold
-                    const uint32_t left = end - p.row - step * kProductK;
-                    const uint32_t strips = 2u + (p.n + 63u) / 64u;
-                    for (uint32_t j = 0; j < strips; ++j)
-                        for (uint32_t i = left * 8u + lane; i < 512u; i += 32u)
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(from_a + j * 8192u + i * 16u), "r"(0u) : "memory");
-                    fence_async_reads();
-                    __syncwarp();
-                }
-                tmem_after_barrier();
-                if (lane == 0u) {
-#pragma unroll
-                    for (uint32_t i = 0; i < kProductK / 16u; ++i) {
-                        const uint64_t da = MODE == kForward ? operand_at(from_a + 32u * i, 0u) : operand_at(from_a + 2048u * i, 8192u);
-                        const uint64_t db = MODE == kWeights ? operand_at(from_b + 2048u * i, 8192u) : operand_at(from_b + 32u * i, 0u);
-                        multiply(acc, da, db, shape, step || i);
-                    }
-                    products_arrive(&s.empty[stage]);
-                }
-                __syncwarp();
-            }
-            if (fine && lane == 0u) products_arrive(&s.ready[buffer]);
-            __syncwarp();
-            ++turn;
-        }
-        if (lane == 0u) products_arrive(&s.drained);      // no product is under way any more when the accumulators are given back
-        __syncwarp();
-        mbar_wait(&s.drained, 0u);
-    } else if (warp >= 4u) {                              // results
+    // (results of 32 bits: 168 registers a thread at launch are 96 x 128 + 200 x 256 of 168 x 384)
+    if (warp >= 4u) {                                     // results
+        if constexpr (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         uint32_t turn = 0;
         bool fine = true;
-        for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const uint32_t part = warp & 3u, side = (warp - 4u) >> 2;         // lanes; every other 32 columns
+        for (uint32_t t = first; t < tiles; t += step_tiles) {
             const ProductTile p = product_tile<MODE>(a, s, t);
-            const uint32_t buffer = turn & 1u, part = warp & 3u, feature = p.m0 + 32u * part + lane;
-            if (p.steps && fine) {
-                fine = __all_sync(kFullMask, mbar_wait(&s.ready[buffer], turn / 2u & 1u, a.tries));
-                tmem_after_barrier();
-            }
-            for (uint32_t c0 = 0; c0 < p.n; c0 += 32u) {
-                uint32_t r[32];
-                if (p.steps && fine) {
-                    tmem_load(tmem + (32u * part << 16) + buffer * a.most_n + c0, r);
-                    tmem_wait_loads();
-                } else {                                  // no rows: zero; a wait ran out: not a number
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) r[i] = fine ? 0u : 0x7FC00000u;
-                }
-                if (feature >= a.m) continue;
+            const uint32_t feature = p.m0 + block * kProductM / 2u + 32u * part + lane;
+            const uint32_t from = tmem + (32u * part << 16);
+            auto write = [&](const float (&f)[32], uint32_t c0) {
+                if (feature >= a.m) return;
                 if constexpr (MODE == kWeights) {
                     TO* to = static_cast<TO*>(a.out) + p.expert * a.out_expert + feature * a.out_stride + p.n0 + c0;
                     constexpr int V = Vec<TO>::N;
 #pragma unroll
                     for (int i = 0; i < 32; i += V) {
-                        float f[V];
+                        float g[V];
 #pragma unroll
-                        for (int j = 0; j < V; ++j) f[j] = __uint_as_float(r[i + j]);
-                        if (c0 + (uint32_t)i < p.n) store_values(to + i, f, true);
+                        for (int j = 0; j < V; ++j) g[j] = f[i + j];
+                        if (c0 + (uint32_t)i < p.n) store_values(to + i, g, true);
                     }
                 } else {
                     TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + feature;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) if (c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(__uint_as_float(r[i]));
+                    for (int i = 0; i < 32; ++i) if (c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
+                }
+            };
+            auto wait = [&]() {
+                if (fine) fine = __all_sync(kFullMask, mbar_wait(&s.ready[turn & 1u], turn / 2u & 1u, a.tries));
+                tmem_after_barrier();
+            };
+            auto give_back = [&]() {
+                tmem_before_barrier();
+                __syncwarp();
+                if (lane == 0u) mbar_tell(&s.taken[turn & 1u], 0u);
+                ++turn;
+            };
+            // (no rows: zero; a wait that ran out: not a number)
+            if constexpr (SUMS) {
+                float sum[4][32];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum[j][i] = 0.f;
+                }
+                for (uint32_t step = 0; step < p.steps; step += kProductSum) {
+                    wait();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t c0 = 64u * (uint32_t)j + 32u * side;
+                        if (c0 >= p.n) continue;
+#pragma unroll
+                        for (int h = 0; h < 32; h += 16) {
+                            uint32_t r[16];
+                            tmem_load(from + (turn & 1u) * a.most_n + c0 + (uint32_t)h, r);
+                            tmem_wait_loads();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum[j][h + i] += __uint_as_float(r[i]);
+                        }
+                    }
+                    give_back();
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t c0 = 64u * (uint32_t)j + 32u * side;
+                    if (!fine) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[j][i] = __uint_as_float(0x7FC00000u);
+                    }
+                    if (c0 < p.n) write(sum[j], c0);
+                }
+            } else {
+                if (p.steps) wait();
+                for (uint32_t c0 = 32u * side; c0 < p.n; c0 += 64u) {
+                    float f[32];
+                    uint32_t r[32];
+                    if (p.steps && fine) {
+                        tmem_load(from + (turn & 1u) * a.most_n + c0, r);
+                        tmem_wait_loads();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = !p.steps ? 0.f : fine ? __uint_as_float(r[i]) : __uint_as_float(0x7FC00000u);
+                    write(f, c0);
+                }
+                if (p.steps) give_back();
+            }
+        }
+    } else {
+    if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    if (warp == 0u) {                                     // copies of tiles
+        if (elect_one()) {
+            ProductRing ring;
+            uint32_t issued = 0;
+            bool fine = true;
+            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+                const ProductTile p = product_tile<MODE>(a, s, t);
+                const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
+                const uint32_t bytes = kProductM / 2u * 128u + (fetch ? 0u : MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
+                const int m0 = (int)(p.m0 + block * kProductM / 2u);
+                const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
+                int at = MODE == kWeights ? (int)p.row : 0;            // in the contraction
+                for (uint32_t step = 0; step < p.steps; ++step, at += (int)kProductK) {
+                    fine = mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
+                    if (!fine) break;
+                    const uint32_t bar = smem_u32(&s.landed[ring.stage]), to_a = stage0 + ring.stage * stage_bytes, to_b = to_a + kProductM / 2u * 128u;
+                    mbar_expect_tx(&s.landed[ring.stage], bytes);
+                    if constexpr (MODE == kForward) tile_load_3d(to_a, &a.a_map, at, m0, (int)p.expert, bar);
+                    else if constexpr (MODE == kInput) {
+                        tile_load_3d(to_a, &a.a_map, m0, at, (int)p.expert, bar);
+                        tile_load_3d(to_a + 8192u, &a.a_map, m0 + 64, at, (int)p.expert, bar);
+                    } else {
+                        tile_load_2d(to_a, &a.a_map, m0, at, bar);
+                        tile_load_2d(to_a + 8192u, &a.a_map, m0 + 64, at, bar);
+                    }
+                    if (!fetch) {
+                        if constexpr (MODE == kWeights) {
+                            tile_load_2d(to_b, &a.b_map, n0, at, bar);
+                            if (strips > 1u) tile_load_2d(to_b + 8192u, &a.b_map, n0 + 64, at, bar);
+                        } else for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, n0 + (int)(j * a.box), bar);
+                    }
+                    ring.next(a.stages);
+                    ++issued;
                 }
             }
-            if (!p.steps) continue;
-            tmem_before_barrier();
-            __syncwarp();
-            if (lane == 0u) mbar_arrive(&s.taken[buffer]);
-            ++turn;
+            // what is still on its way lands before the block ends, whoever has given up: the last round of each stage
+            for (uint32_t i = min(issued, a.stages); i > 0u; --i) {
+                const uint32_t back = ring.stage >= i ? ring.stage - i : ring.stage + a.stages - i;
+                mbar_wait(&s.landed[back], back < ring.stage ? ring.round : ring.round ^ 1u);
+            }
         }
+    } else if (warp == 1u && block == 0u) {               // products
+        if (elect_one()) {
+            ProductRing ring;
+            uint32_t turn = 0;
+            bool fine = true;
+            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+                const ProductTile p = product_tile<MODE>(a, s, t);
+                const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
+                uint32_t acc = 0;
+                for (uint32_t step = 0; step < p.steps; ++step) {
+                    const bool begins = SUMS ? step % kProductSum == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && (step + 1u) % kProductSum == 0u);
+                    if (begins) {
+                        fine = mbar_wait(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
+                        acc = tmem + (turn & 1u) * a.most_n;
+                    }
+                    fine = fine && mbar_wait(&s.full[ring.stage], ring.round, a.tries);
+                    if (!fine) break;
+                    tmem_after_barrier();
+                    const uint32_t from_a = stage0 + ring.stage * stage_bytes, from_b = from_a + kProductM / 2u * 128u;
+                    const uint32_t da = operand_at(from_a, MODE == kForward ? 0u : 8192u), db = operand_at(from_b, MODE == kWeights ? 8192u : 0u);
+                    constexpr uint32_t STEP_A = (MODE == kForward ? 32u : 2048u) >> 4, STEP_B = (MODE == kWeights ? 2048u : 32u) >> 4;
+#pragma unroll
+                    for (uint32_t i = 0; i < kProductK / 16u; ++i) multiply(acc, da + STEP_A * i, db + STEP_B * i, shape, !begins || i);
+                    products_arrive(&s.empty[ring.stage]);
+                    if (ends) { products_arrive(&s.ready[turn & 1u]); ++turn; }
+                    ring.next(a.stages);
+                }
+            }
+            products_arrive(&s.drained);                  // no product is under way any more when the accumulators are given back
+            mbar_wait(&s.drained, 0u);
+        }
+    } else if (warp == 1u) {
+        mbar_wait(&s.drained, 0u);                        // (every signal of the other block's products has come)
+    } else if (!fetch) {                                  // what has landed
+        if (warp == 2u) {
+            ProductRing ring;
+            bool fine = true;
+            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+                const ProductTile p = product_tile<MODE>(a, s, t);
+                for (uint32_t step = 0; step < p.steps; ++step) {
+                    fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
+                    if (!fine) break;
+                    if (MODE == kWeights && step + 1u == p.steps)
+                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
+                    if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
+                    ring.next(a.stages);
+                }
+            }
+        }
+    } else if constexpr (MODE != kInput) {                // the same, and rows by the order
+        const uint32_t thread = threadIdx.x - 64u, chunk = thread & 7u, group = thread >> 3;      // 16 bytes of every eighth row
+        const uint32_t stride = a.x_stride;
+        ProductRing ring, told;                           // what is fetched, and what of that has arrived: kProductLag stages later
+        uint32_t it = 0;
+        bool fine = true;
+        auto tell = [&]() {
+            if (warp == 2u) {
+                fine = __all_sync(kFullMask, mbar_wait(&s.landed[told.stage], told.round, a.tries));
+                if (!fine) return;
+                if (MODE == kWeights && s.left[told.stage] < kProductK) product_clear(stage0 + told.stage * stage_bytes, kProductM / 128u, s.left[told.stage]);
+            }
+            fence_async_reads();
+            __syncwarp();
+            if (lane == 0u) mbar_tell(&s.full[told.stage], 0u);
+            told.next(a.stages);
+        };
+        for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+            const ProductTile p = product_tile<MODE>(a, s, t);
+            const uint32_t from_n = block * p.half;       // this block's columns of the tile
+            const unsigned char* rows[kProductM / 16u];   // forward: this thread's
+            if constexpr (MODE == kForward) {
+#pragma unroll
+                for (uint32_t i = 0; i < kProductM / 16u; ++i) {      // (rows behind the tile's last are anyone's: their columns are not written)
+                    const uint32_t r = min(p.row + from_n + group + 8u * i, p.end - 1u);
+                    rows[i] = static_cast<const unsigned char*>(a.x) + (uint64_t)min(8u * i < p.half ? a.order[r] / a.per_row : 0u, a.x_rows - 1u) * stride + chunk * 16u;
+                }
+            }
+            for (uint32_t step = 0; step < p.steps; ++step, ++it) {
+                if (MODE == kWeights && step % (kProductSources / kProductK) == 0u) product_sources(a, s, p.row + step * kProductK, p.end);
+                fine = __all_sync(kFullMask, mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries));
+                if (!fine) break;
+                const uint32_t to_b = stage0 + ring.stage * stage_bytes + kProductM / 2u * 128u + group * 128u + ((chunk ^ group) << 4);
+                if constexpr (MODE == kForward) {
+                    const uint32_t at = step * kProductK * 2u;
+                    const bool there = step * kProductK + chunk * 8u < a.k;
+#pragma unroll
+                    for (uint32_t i = 0; i < kProductM / 16u; ++i) if (8u * i < p.half) copy16_or_zero(to_b + i * 1024u, rows[i] + at, there);
+                } else {
+                    const uint32_t c = p.n0 + from_n + chunk * 8u;
+                    const unsigned char* from = static_cast<const unsigned char*>(a.x) + c * 2ull;
+                    const bool there = c < a.n, there_too = c + 64u < a.n;
+                    const uint32_t* sources = s.sources + step % (kProductSources / kProductK) * kProductK + group;
+#pragma unroll
+                    for (uint32_t i = 0; i < kProductK / 8u; ++i) {
+                        const uint32_t source = sources[8u * i];
+                        const unsigned char* row = from + (uint64_t)min(source, a.x_rows - 1u) * stride;
+                        copy16_or_zero(to_b + i * 1024u, row, there && source != ~0u);
+                        if (p.half > 64u) copy16_or_zero(to_b + i * 1024u + 8192u, row + 128, there_too && source != ~0u);
+                    }
+                    if (warp == 2u && lane == 0u) s.left[ring.stage] = p.end - p.row - step * kProductK;
+                }
+                copies_end_group();
+                ring.next(a.stages);
+                if (it >= kProductLag) {
+                    wait_copies<(int)kProductLag>();
+                    tell();
+                    if (!fine) break;
+                }
+            }
+        }
+        wait_copies<0>();
+        for (uint32_t i = min(it, kProductLag); i > 0u && fine; --i) tell();
+    }
     }
     __syncwarp();
     tmem_before_barrier();
     __syncthreads();
+    cluster_meet();                                       // (neither block ends, or frees its accumulators, while the other's products or signals may need it)
     tmem_after_barrier();
     if (warp == 2u) tmem_free(tmem, columns);
 }

@@ -10,7 +10,7 @@
 // workspace.  More take three launches a digit (k_order_count, k_order_offsets, k_order_place), with keys and positions in the workspace.
 #pragma once
 
-#include "common.cuh"
+#include "async.cuh"
 
 namespace fsg {
 
@@ -108,11 +108,6 @@ __device__ __forceinline__ void order_over_warps(uint16_t* counts, uint32_t bins
     }
 }
 
-__device__ __forceinline__ uint32_t cluster_block() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-// Every thread of the cluster's blocks; what they wrote before, to shared or global memory, is visible behind it.
-__device__ __forceinline__ void cluster_meet() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ uint32_t address_in(const void* p, uint32_t block) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(block));

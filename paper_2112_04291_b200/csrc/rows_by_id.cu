@@ -148,16 +148,16 @@ template <int MODE> const void* product_kernel(uint32_t to) {
 template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t to, const DeviceView& dev, cudaStream_t st) {
     if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
     a.tries = dev.tries;
-    a.stages = (uint32_t)((216u * 1024u) / product_stage_bytes(a.most_n));
+    a.stages = (uint32_t)((215u * 1024u) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
     const void* fn = product_kernel<MODE>(to);
-    const size_t smem = (size_t)a.stages * product_stage_bytes(a.most_n) + 1024u;
+    const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + 1024u;
     uint64_t resident = 0;
     const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);
     if (rc) return rc;
-    const uint64_t blocks = tiles < resident ? tiles : resident;
+    const uint64_t pairs = tiles < resident / 2u ? tiles : resident / 2u;
     void* kargs[] = {&a};
-    return launched(launch_overlapped(fn, (unsigned)blocks, kProductThreads, smem, kargs, st));
+    return launched(launch_overlapped(fn, (unsigned)(2u * pairs), kProductThreads, smem, kargs, st, 2u));
 }
 
 // Columns of a tile where the rows' side is ragged: enough for most experts' rows in one.
@@ -300,11 +300,11 @@ int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint3
     if (rc) return rc;
     ProductArgs a{};
     a.most_n = columns_for(y->rows, weights->experts);
-    a.box = a.most_n < 128u ? a.most_n : 128u;
-    rc = map_rows(&a.a_map, weights->data, weights->type, weights->outs, weights->ins, weights->row_stride, kProductM, weights->experts, weights->expert_stride);
-    if (!rc) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, order ? 1u : a.box);
+    a.box = a.most_n < 128u ? a.most_n / 2u : 64u;
+    rc = map_rows(&a.a_map, weights->data, weights->type, weights->outs, weights->ins, weights->row_stride, kProductM / 2u, weights->experts, weights->expert_stride);
+    if (!rc && !order) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, a.box);
     if (rc) return rc;
-    a.starts = starts; a.order = order; a.per_row = per_row; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)y->rows;
+    a.starts = starts; a.order = order; a.per_row = per_row; a.x = x->data; a.x_stride = (uint32_t)(x->row_stride * 2u); a.x_rows = (uint32_t)x->rows; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)y->rows;
     a.m = (uint32_t)weights->outs; a.k = (uint32_t)weights->ins; a.out = y->data; a.out_stride = y->row_stride;
     a.kind = product_kind(x->type == FASTSGD_BF16, false, false);
     return launch_product<kForward>(a, (y->rows / a.most_n + weights->experts) * ((weights->outs + kProductM - 1) / kProductM), y->type, dev, static_cast<cudaStream_t>(stream));
@@ -326,7 +326,7 @@ int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const ui
     if (rc) return rc;
     ProductArgs a{};
     a.most_n = columns_for(grad_y->rows, weights->experts);
-    a.box = a.most_n < 128u ? a.most_n : 128u;
+    a.box = a.most_n < 128u ? a.most_n / 2u : 64u;
     rc = map_rows(&a.a_map, weights->data, weights->type, weights->outs, weights->ins, weights->row_stride, kProductK, weights->experts, weights->expert_stride);
     if (!rc) rc = map_rows(&a.b_map, grad_y->data, grad_y->type, grad_y->rows, grad_y->cols, grad_y->row_stride, a.box);
     if (rc) return rc;
@@ -356,10 +356,10 @@ int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const 
     a.box = kProductK;
     if (a.rows) {
         rc = map_rows(&a.a_map, grad_y->data, grad_y->type, grad_y->rows, grad_y->cols, grad_y->row_stride, kProductK);
-        if (!rc) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, order ? 1u : kProductK);
+        if (!rc && !order) rc = map_rows(&a.b_map, x->data, x->type, x->rows, x->cols, x->row_stride, kProductK);
         if (rc) return rc;
     }
-    a.starts = starts; a.order = order; a.per_row = per_row; a.experts = (uint32_t)grad_weights->experts;
+    a.starts = starts; a.order = order; a.per_row = per_row; a.x = x->data; a.x_stride = (uint32_t)(x->row_stride * 2u); a.x_rows = (uint32_t)x->rows; a.experts = (uint32_t)grad_weights->experts;
     a.m = (uint32_t)grad_weights->outs; a.n = (uint32_t)grad_weights->ins; a.out = grad_weights->data; a.out_stride = grad_weights->row_stride; a.out_expert = grad_weights->expert_stride;
     a.kind = product_kind(x->type == FASTSGD_BF16, true, true);
     return launch_product<kWeights>(a, grad_weights->experts * ((grad_weights->outs + kProductM - 1) / kProductM) * ((grad_weights->ins + a.most_n - 1) / a.most_n), grad_weights->type, dev,
