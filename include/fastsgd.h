@@ -472,7 +472,8 @@ typedef struct fastsgd_experts {
  *   y        rows x outs, of that type or fp32; rows that belong to no expert (dropped selections) are left as they are.  Apart from x and
  *            the weights
  * Matrices begin on 16 bytes; their columns and strides are multiples of 8 (else FASTSGD_E_ALIGN); x and the weights are of 16 bits (fp32:
- * FASTSGD_E_NOT_IMPLEMENTED).  Products are summed in fp32 and rounded once.  One launch, no workspace.
+ * FASTSGD_E_NOT_IMPLEMENTED).  Products are summed in fp32 and rounded once.  One launch and no workspace for sorted rows; with an order x's
+ * rows are sorted first: a launch more, and a workspace of fastsgd_products_workspace_bytes(y->rows, x->cols).
  * The kernel's waits have a limit of some seconds; where one ran out, what its block had not yet written is NaN.
  */
 int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, const uint32_t* starts,
@@ -496,8 +497,10 @@ int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const ui
 int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row,
                                             const uint32_t* starts, const fastsgd_experts* grad_weights, void* stream);
 
-/* bytes of workspace for these calls on `count` ids or rows of `cols` columns; 0 for invalid arguments */
+/* bytes of workspace for fastsgd_order_ids and fastsgd_embedding_backward(_pairs) of `count` ids or rows of `cols` columns, and for products of
+ * `rows` rows of `ins` columns by an order, which is made in it, too; 0 for invalid arguments */
 uint64_t fastsgd_rows_workspace_bytes(uint64_t count, uint64_t cols);
+uint64_t fastsgd_products_workspace_bytes(uint64_t rows, uint64_t ins);
 
 /* ---- helpers, not on the timed path (no counterpart in the paper) ---------- */
 

@@ -33,6 +33,7 @@ EXPORTS = [
     "fastsgd_top_logits", "fastsgd_distill_loss", "fastsgd_distill_loss_backward", "fastsgd_expert_counts", "fastsgd_balance_loss",
     "fastsgd_order_ids", "fastsgd_embedding", "fastsgd_embedding_backward", "fastsgd_embedding_backward_pairs",
     "fastsgd_expert_product", "fastsgd_expert_product_backward_input", "fastsgd_expert_product_backward_weights", "fastsgd_rows_workspace_bytes",
+    "fastsgd_products_workspace_bytes",
     "fastsgd_debug_set_wait_limits", "fastsgd_debug_layout", "fastsgd_debug_set_grid",
     "fastsgd_debug_decoder_route",
 ]
@@ -135,6 +136,8 @@ def lib():
         L.fastsgd_expert_product_backward_weights.argtypes = [MP, MP, vp, u32, vp, EP, vp]
         L.fastsgd_rows_workspace_bytes.restype = u64
         L.fastsgd_rows_workspace_bytes.argtypes = [u64, u64]
+        L.fastsgd_products_workspace_bytes.restype = u64
+        L.fastsgd_products_workspace_bytes.argtypes = [u64, u64]
         L.fastsgd_compress_bound.restype = u64
         L.fastsgd_compress_bound.argtypes = [u64, PP]
         L.fastsgd_workspace_bytes.restype = u64
@@ -423,8 +426,13 @@ def rows_workspace_bytes(count: int, cols: int = 1) -> int:
 
 
 def ensure_rows_workspace(count: int, cols: int = 1, device="cuda") -> torch.Tensor:
-    """Allocates (torch) and registers a workspace large enough for these calls on `count` ids or rows of `cols` columns, if needed."""
+    """Allocates (torch) and registers a workspace large enough for order_ids and embedding_backward(_pairs) of `count` ids or rows of `cols` columns, if needed."""
     return _ensure(rows_workspace_bytes(count, cols), device)
+
+
+def ensure_products_workspace(rows: int, ins: int, device="cuda") -> torch.Tensor:
+    """The same for an order of `rows` selections and products by it of rows of `ins` columns."""
+    return _ensure(int(lib().fastsgd_products_workspace_bytes(rows, ins)), device)
 
 
 def order_ids(ids: torch.Tensor, order: torch.Tensor, starts: torch.Tensor, distinct: torch.Tensor = None, number: torch.Tensor = None, stream=None) -> int:

@@ -71,6 +71,7 @@ struct LookupArgs {
     const void* table;
     uint64_t  table_stride;
     const int32_t* ids;
+    uint32_t  per_row;                                    // ids of each of the table's rows: row ids[t] / per_row
     uint32_t  count, vocab, cols;
     uint32_t  lanes_log;                                  // lanes that share a row's chunk of 8 lanes columns, 1 .. 32
     uint32_t  chunks;
@@ -93,7 +94,7 @@ template <class T, class TO, bool WIDE> __global__ void __launch_bounds__(kEmbed
         for (uint32_t j = 0; j < kLookupAhead; ++j) {
             const uint64_t u = u0 + groups * j;
             row[j] = (uint32_t)(u / a.chunks); chunk[j] = (uint32_t)(u - (uint64_t)row[j] * a.chunks);
-            id[j] = u < all ? (uint32_t)a.ids[row[j]] : ~0u;
+            id[j] = u < all ? (uint32_t)a.ids[row[j]] / a.per_row : ~0u;
         }
 #pragma unroll
         for (uint32_t j = 0; j < kLookupAhead; ++j)

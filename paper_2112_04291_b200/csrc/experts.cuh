@@ -1,8 +1,8 @@
 // Matrix products of a router's experts: rows sorted by expert, each expert's rows times its own weights, and the two gradients.
 //
-//   forward  y[r, :]  = x[source(r), :] W_e^T                          contraction over the ins
-//   input    gx[r, :] = gy[r, :] W_e                                   over the outs
-//   weights  gW_e     = sum over the expert's rows of gy[r, :]^T x[source(r), :]     over the rows
+//   forward  y[r, :]  = x[r, :] W_e^T                          contraction over the ins
+//   input    gx[r, :] = gy[r, :] W_e                           over the outs
+//   weights  gW_e     = sum over the expert's rows of gy[r, :]^T x[r, :]     over the rows
 //
 // All three are A B^T of a tile of 256 of the weights' rows (A: the accumulator's lanes) and up to 256 of the ragged side (B: its columns):
 // the ragged side is the one whose tiles may have any multiple of 32, so that an expert with few rows costs few instructions, and the weights,
@@ -10,7 +10,7 @@
 //
 // A pair of blocks (two SMs) works on a tile: each copies half of A and half of B, so that an operand byte in shared memory serves twice as many
 // products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products, a third tells it what has
-// landed, and with the fourth fetches rows by the order; eight write results, while the next tile's products go into the other half of the
+// landed; eight write results, while the next tile's products go into the other half of the
 // accumulators.
 //
 // The tensor cores cut off each addition to an accumulator where it exceeds 32 bits: over n values of the contraction the result loses about
@@ -30,18 +30,12 @@ constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 4u;               // stages between two additions in registers (results of 32 bits)
-constexpr uint32_t kProductLag        = 3u;               // stages whose fetched rows may be on their way
-constexpr uint32_t kProductSources    = 512u;             // rows whose sources are looked up at a time
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
 struct alignas(64) ProductArgs {
     CUtensorMap a_map, b_map;
     const uint32_t* starts;
-    const uint32_t* order;                                // or nullptr: source(r) = r
-    const void* x;                                        // (with an order) the rows that it names
-    uint32_t  x_stride;                                   // bytes
-    uint32_t  x_rows;
-    uint32_t  experts, rows, per_row;                     // rows: of the sorted side
+    uint32_t  experts, rows;                              // rows: of the sorted side
     uint32_t  m, n, k;                                    // m: A's rows; n: B's (weights only); k: the contraction (forward, input)
     void*     out;
     uint64_t  out_stride, out_expert;
@@ -63,8 +57,6 @@ struct ProductShared {
     unsigned long long taken[2];                          // (first block) ... and have been read, by both blocks
     unsigned long long drained;
     uint32_t tmem, tiles;
-    uint32_t left[kProductMaxStages];                     // rows of the stage that count (weights)
-    uint32_t sources[kProductSources];
     uint32_t first_row[kProductMaxExperts + 1];
     uint32_t first_tile[kProductMaxExperts + 1];
 };
@@ -150,20 +142,6 @@ template <int MODE> __device__ __forceinline__ void product_tables(const Product
     __syncthreads();
 }
 
-// Sources of up to kProductSources rows from r on; rows from `end` on, and sources that are no row of x, are ~0.  Each of the two warps that
-// fetch rows looks up those that it fetches itself (four of every eight): neither waits for the other.
-__device__ __forceinline__ void product_sources(const ProductArgs& a, ProductShared& s, uint32_t r, uint32_t end) {
-    const uint32_t lane = threadIdx.x & 31u, mine = threadIdx.x >> 3 & 4u;
-    __syncwarp();                                         // (the last ones have been used)
-    for (uint32_t e = lane; e < kProductSources / 2u; e += 32u) {
-        const uint32_t i = (e & ~3u) * 2u + mine + (e & 3u);
-        const uint32_t source = r + i < end ? a.order[r + i] / a.per_row : ~0u;
-        s.sources[i] = source < a.x_rows ? source : ~0u;
-        if (r + i >= end + kProductK) break;              // (nor will anyone ask for those behind)
-    }
-    __syncwarp();
-}
-
 // Rows of a stage's strips from `left` on become zero: what lies behind an expert's last row counts nothing, whatever it holds.  One warp.
 __device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, uint32_t left) {
     if (left >= kProductK) return;
@@ -182,17 +160,16 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     const uint32_t first = blockIdx.x / 2u, step_tiles = gridDim.x / 2u;
     const uint32_t stage0 = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t stage_bytes = product_stage_bytes<MODE>(a.most_n);
-    const bool fetch = MODE != kInput && a.order;
     uint32_t columns = 32u;
     while (columns < 2u * a.most_n) columns *= 2u;
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.landed[i], 1u); mbar_init(&s.full[i], fetch ? 4u : 2u); mbar_init(&s.empty[i], 1u); }
+        for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.landed[i], 1u); mbar_init(&s.full[i], 2u); mbar_init(&s.empty[i], 1u); }
         for (uint32_t i = 0; i < 2u; ++i) { mbar_init(&s.ready[i], 1u); mbar_init(&s.taken[i], 16u); }
         mbar_init(&s.drained, 1u);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    if (warp == 2u) tmem_alloc(&s.tmem, columns);
+    if (warp == 3u) tmem_alloc(&s.tmem, columns);
     tmem_before_barrier();
     __syncthreads();
     cluster_meet();
@@ -202,7 +179,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     allow_next_kernel();
     product_tables<MODE>(a, s);
     const uint32_t tiles = s.tiles;
-    // (results of 32 bits: 168 registers a thread at launch are 96 x 128 + 200 x 256 of 168 x 384)
+    // (results of 32 bits: of 168 registers a thread at launch 96 x 128 + 200 x 256 are less than 168 x 384)
     if (warp >= 4u) {                                     // results
         if constexpr (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         uint32_t turn = 0;
@@ -300,7 +277,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
             for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
                 const ProductTile p = product_tile<MODE>(a, s, t);
                 const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
-                const uint32_t bytes = kProductM / 2u * 128u + (fetch ? 0u : MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
+                const uint32_t bytes = kProductM / 2u * 128u + (MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
                 const int m0 = (int)(p.m0 + block * kProductM / 2u);
                 const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
                 int at = MODE == kWeights ? (int)p.row : 0;            // in the contraction
@@ -317,12 +294,10 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                         tile_load_2d(to_a, &a.a_map, m0, at, bar);
                         tile_load_2d(to_a + 8192u, &a.a_map, m0 + 64, at, bar);
                     }
-                    if (!fetch) {
-                        if constexpr (MODE == kWeights) {
-                            tile_load_2d(to_b, &a.b_map, n0, at, bar);
-                            if (strips > 1u) tile_load_2d(to_b + 8192u, &a.b_map, n0 + 64, at, bar);
-                        } else for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, n0 + (int)(j * a.box), bar);
-                    }
+                    if constexpr (MODE == kWeights) {
+                        tile_load_2d(to_b, &a.b_map, n0, at, bar);
+                        if (strips > 1u) tile_load_2d(to_b + 8192u, &a.b_map, n0 + 64, at, bar);
+                    } else for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, n0 + (int)(j * a.box), bar);
                     ring.next(a.stages);
                     ++issued;
                 }
@@ -366,85 +341,20 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
         }
     } else if (warp == 1u) {
         mbar_wait(&s.drained, 0u);                        // (every signal of the other block's products has come)
-    } else if (!fetch) {                                  // what has landed
-        if (warp == 2u) {
-            ProductRing ring;
-            bool fine = true;
-            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
-                const ProductTile p = product_tile<MODE>(a, s, t);
-                for (uint32_t step = 0; step < p.steps; ++step) {
-                    fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
-                    if (!fine) break;
-                    if (MODE == kWeights && step + 1u == p.steps)
-                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
-                    if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
-                    ring.next(a.stages);
-                }
-            }
-        }
-    } else if constexpr (MODE != kInput) {                // the same, and rows by the order
-        const uint32_t thread = threadIdx.x - 64u, chunk = thread & 7u, group = thread >> 3;      // 16 bytes of every eighth row
-        const uint32_t stride = a.x_stride;
-        ProductRing ring, told;                           // what is fetched, and what of that has arrived: kProductLag stages later
-        uint32_t it = 0;
+    } else if (warp == 2u) {                              // what has landed
+        ProductRing ring;
         bool fine = true;
-        auto tell = [&]() {
-            if (warp == 2u) {
-                fine = __all_sync(kFullMask, mbar_wait(&s.landed[told.stage], told.round, a.tries));
-                if (!fine) return;
-                if (MODE == kWeights && s.left[told.stage] < kProductK) product_clear(stage0 + told.stage * stage_bytes, kProductM / 128u, s.left[told.stage]);
-            }
-            fence_async_reads();
-            __syncwarp();
-            if (lane == 0u) mbar_tell(&s.full[told.stage], 0u);
-            told.next(a.stages);
-        };
         for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
             const ProductTile p = product_tile<MODE>(a, s, t);
-            const uint32_t from_n = block * p.half;       // this block's columns of the tile
-            const unsigned char* rows[kProductM / 16u];   // forward: this thread's
-            if constexpr (MODE == kForward) {
-#pragma unroll
-                for (uint32_t i = 0; i < kProductM / 16u; ++i) {      // (rows behind the tile's last are anyone's: their columns are not written)
-                    const uint32_t r = min(p.row + from_n + group + 8u * i, p.end - 1u);
-                    rows[i] = static_cast<const unsigned char*>(a.x) + (uint64_t)min(8u * i < p.half ? a.order[r] / a.per_row : 0u, a.x_rows - 1u) * stride + chunk * 16u;
-                }
-            }
-            for (uint32_t step = 0; step < p.steps; ++step, ++it) {
-                if (MODE == kWeights && step % (kProductSources / kProductK) == 0u) product_sources(a, s, p.row + step * kProductK, p.end);
-                fine = __all_sync(kFullMask, mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries));
+            for (uint32_t step = 0; step < p.steps; ++step) {
+                fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
                 if (!fine) break;
-                const uint32_t to_b = stage0 + ring.stage * stage_bytes + kProductM / 2u * 128u + group * 128u + ((chunk ^ group) << 4);
-                if constexpr (MODE == kForward) {
-                    const uint32_t at = step * kProductK * 2u;
-                    const bool there = step * kProductK + chunk * 8u < a.k;
-#pragma unroll
-                    for (uint32_t i = 0; i < kProductM / 16u; ++i) if (8u * i < p.half) copy16_or_zero(to_b + i * 1024u, rows[i] + at, there);
-                } else {
-                    const uint32_t c = p.n0 + from_n + chunk * 8u;
-                    const unsigned char* from = static_cast<const unsigned char*>(a.x) + c * 2ull;
-                    const bool there = c < a.n, there_too = c + 64u < a.n;
-                    const uint32_t* sources = s.sources + step % (kProductSources / kProductK) * kProductK + group;
-#pragma unroll
-                    for (uint32_t i = 0; i < kProductK / 8u; ++i) {
-                        const uint32_t source = sources[8u * i];
-                        const unsigned char* row = from + (uint64_t)min(source, a.x_rows - 1u) * stride;
-                        copy16_or_zero(to_b + i * 1024u, row, there && source != ~0u);
-                        if (p.half > 64u) copy16_or_zero(to_b + i * 1024u + 8192u, row + 128, there_too && source != ~0u);
-                    }
-                    if (warp == 2u && lane == 0u) s.left[ring.stage] = p.end - p.row - step * kProductK;
-                }
-                copies_end_group();
+                if (MODE == kWeights && step + 1u == p.steps)
+                    product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
+                if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
                 ring.next(a.stages);
-                if (it >= kProductLag) {
-                    wait_copies<(int)kProductLag>();
-                    tell();
-                    if (!fine) break;
-                }
             }
         }
-        wait_copies<0>();
-        for (uint32_t i = min(it, kProductLag); i > 0u && fine; --i) tell();
     }
     }
     __syncwarp();
@@ -452,7 +362,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     __syncthreads();
     cluster_meet();                                       // (neither block ends, or frees its accumulators, while the other's products or signals may need it)
     tmem_after_barrier();
-    if (warp == 2u) tmem_free(tmem, columns);
+    if (warp == 3u) tmem_free(tmem, columns);
 }
 
 }  // namespace fsg

@@ -25,10 +25,6 @@ __device__ __forceinline__ void tile_load_3d(uint32_t dst, const CUtensorMap* ma
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-// 16 bytes to shared memory, zeros where not `there` (nothing is read then).  Each thread waits for its own (wait_copies).
-__device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(there ? 16u : 0u) : "memory");
-}
 // what this thread has written to shared memory is seen by copies and matrix instructions that are issued later
 __device__ __forceinline__ void fence_async_reads() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 

@@ -266,6 +266,7 @@ def _check_products(rng, tokens, experts, k, ins, outs, dtype, out, whole, gap=0
     dgy.copy_(torch.from_numpy(gy_held))
     _, dw = _weights(w, dtype, gap, between)
 
+    binding.ensure_products_workspace(rows, ins)
     store, y = _strided(rows, outs, out, gap)
     assert binding.expert_product(dx, dw, starts, y, order=order, per_row=per_row) == 0
     want, size = ref.products(x, source, want_starts, w)
