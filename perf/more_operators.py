@@ -213,13 +213,14 @@ def _run_own(s):
         _done(binding.embedding_backward_pairs(s["grad"], s["ids"], s["order"], s["starts"], s["distinct"], s["number"], s["keys"], s["values"], scale=s["scale"]))
         return {"order": s["order"], "starts": s["starts"], "distinct": s["distinct"], "number": s["number"], "keys": s["keys"], "values": s["values"]}
     if s["kind"] == "forward":
-        binding.ensure_rows_workspace(s["tokens"] * s["chosen"])
+        binding.ensure_products_workspace(s["tokens"] * s["chosen"], s["ins"])
         _done(binding.order_ids(s["selected"], s["order"], s["starts"]))
         _done(binding.expert_product(s["x"], s["w"], s["starts"], s["y"], order=s["order"], per_row=s["chosen"]))
         return {"order": s["order"], "starts": s["starts"], "y": s["y"]}
     if s["kind"] == "input":
         _done(binding.expert_product_backward_input(s["gy"], s["w"], s["starts"], s["gx"]))
         return {"gx": s["gx"]}
+    binding.ensure_products_workspace(s["tokens"] * s["chosen"], s["ins"])
     _done(binding.expert_product_backward_weights(s["gy"], s["x"], s["starts"], s["gw"], order=s["order"], per_row=s["chosen"]))
     return {"gw": s["gw"]}
 
