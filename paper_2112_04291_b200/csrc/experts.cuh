@@ -30,6 +30,7 @@ constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 4u;               // stages between two additions in registers (results of 32 bits)
+constexpr uint32_t kProductTurned     = 2048u;            // bytes of a warp that writes gradients of weights
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
 struct alignas(64) ProductArgs {
@@ -78,8 +79,9 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
         const uint32_t nt = (a.n + a.most_n - 1u) / a.most_n;
         p.expert = t / (mt * nt);
         const uint32_t i = t - p.expert * mt * nt;
-        p.m0 = i % mt * kProductM;
-        p.n0 = i / mt * a.most_n;
+        const uint32_t band = i / (nt * kProductBand), j = i - band * nt * kProductBand, wide = min(kProductBand, mt - band * kProductBand);
+        p.m0 = (band * kProductBand + j % wide) * kProductM;
+        p.n0 = j / wide * a.most_n;
         p.n = min(a.most_n, a.n - p.n0);
         p.row = s.first_row[p.expert];
         p.end = s.first_row[p.expert + 1u];
@@ -185,24 +187,40 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
         uint32_t turn = 0;
         bool fine = true;
         const uint32_t part = warp & 3u, side = (warp - 4u) >> 2;         // lanes; every other 32 columns
+        unsigned char* turned = raw + (stage0 - smem_u32(raw)) + a.stages * stage_bytes + (warp - 4u) * kProductTurned;      // (weights)
         for (uint32_t t = first; t < tiles; t += step_tiles) {
             const ProductTile p = product_tile<MODE>(a, s, t);
-            const uint32_t feature = p.m0 + block * kProductM / 2u + 32u * part + lane;
+            const uint32_t row0 = p.m0 + block * kProductM / 2u + 32u * part;
             const uint32_t from = tmem + (32u * part << 16);
             auto write = [&](const float (&f)[32], uint32_t c0) {
-                if (feature >= a.m) return;
                 if constexpr (MODE == kWeights) {
-                    TO* to = static_cast<TO*>(a.out) + p.expert * a.out_expert + feature * a.out_stride + p.n0 + c0;
-                    constexpr int V = Vec<TO>::N;
+                    // A lane holds 32 columns of a row of its own.  Through shared memory, 64 bytes of a row at a time (in an order of its four
+                    // vectors that keeps rows off one another's banks), four lanes write whole sectors of one row.
+                    constexpr uint32_t V = Vec<TO>::N, COLS = 4u * V;
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; i += V) {
-                        float g[V];
+                    for (uint32_t h = 0; h < 32u; h += COLS) {
 #pragma unroll
-                        for (int j = 0; j < V; ++j) g[j] = f[i + j];
-                        if (c0 + (uint32_t)i < p.n) store_values(to + i, g, true);
+                        for (uint32_t v = 0; v < 4u; ++v) {
+                            const uint32_t i = h + v * V;
+                            uint4 x;
+                            if constexpr (SUMS) x = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
+                            else x = make_uint4(pack_two<TO>(f[i], f[i + 1]), pack_two<TO>(f[i + 2], f[i + 3]), pack_two<TO>(f[i + 4], f[i + 5]), pack_two<TO>(f[i + 6], f[i + 7]));
+                            *reinterpret_cast<uint4*>(turned + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)) = x;
+                        }
+                        __syncwarp();
+                        const uint32_t v = lane & 3u, c = c0 + h + v * V;
+#pragma unroll
+                        for (uint32_t i = 0; i < 4u; ++i) {
+                            const uint32_t r = (lane >> 2) + 8u * i;
+                            const uint4 x = *reinterpret_cast<const uint4*>(turned + r * 64u + ((v ^ (r >> 1 & 3u)) << 4));
+                            if (row0 + r < a.m && c < p.n) store16(static_cast<TO*>(a.out) + p.expert * a.out_expert + (row0 + r) * a.out_stride + p.n0 + c, x);
+                        }
+                        __syncwarp();
                     }
                 } else {
-                    TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + feature;
+                    if (row0 + lane >= a.m) return;
+                    TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + row0 + lane;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) if (c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
                 }
@@ -231,14 +249,15 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                     for (int j = 0; j < 4; ++j) {
                         const uint32_t c0 = 64u * (uint32_t)j + 32u * side;
                         if (c0 >= p.n) continue;
+                        uint32_t r[16], q[16];
+                        tmem_load(from + (turn & 1u) * a.most_n + c0, r);
+                        tmem_wait(r);
+                        tmem_load(from + (turn & 1u) * a.most_n + c0 + 16u, q);
 #pragma unroll
-                        for (int h = 0; h < 32; h += 16) {
-                            uint32_t r[16];
-                            tmem_load(from + (turn & 1u) * a.most_n + c0 + (uint32_t)h, r);
-                            tmem_wait_loads();
+                        for (int i = 0; i < 16; ++i) sum[j][i] += __uint_as_float(r[i]);
+                        tmem_wait(q);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[j][h + i] += __uint_as_float(r[i]);
-                        }
+                        for (int i = 0; i < 16; ++i) sum[j][16 + i] += __uint_as_float(q[i]);
                     }
                     give_back();
                 }
@@ -258,7 +277,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                     uint32_t r[32];
                     if (p.steps && fine) {
                         tmem_load(from + (turn & 1u) * a.most_n + c0, r);
-                        tmem_wait_loads();
+                        tmem_wait(r);
                     }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) f[i] = !p.steps ? 0.f : fine ? __uint_as_float(r[i]) : __uint_as_float(0x7FC00000u);

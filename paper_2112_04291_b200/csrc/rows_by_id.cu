@@ -173,10 +173,11 @@ template <int MODE> const void* product_kernel(uint32_t to) {
 template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t to, const DeviceView& dev, cudaStream_t st) {
     if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
     a.tries = dev.tries;
-    a.stages = (uint32_t)((215u * 1024u) / product_stage_bytes<MODE>(a.most_n));
+    const uint32_t turned = MODE == kWeights ? 8u * kProductTurned : 0u;
+    a.stages = (uint32_t)((215u * 1024u - turned) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
     const void* fn = product_kernel<MODE>(to);
-    const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + 1024u;
+    const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + turned + 1024u;
     uint64_t resident = 0;
     const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);
     if (rc) return rc;
