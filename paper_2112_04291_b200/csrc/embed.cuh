@@ -1,4 +1,8 @@
 // Rows of a table by token (an embedding's lookup), and that table's gradient: the rows of a gradient added up by token.
+//
+// A group of 1 to 32 lanes works on a row, a chunk of eight consecutive columns a lane at a time.  Rows may begin at any element: where
+// they do not all begin on 16 bytes, a lane loads the aligned vectors that its columns lie in and shifts them into place, and stores the
+// aligned vector that begins among its own columns with the first of the next lane's; single elements remain at the two ends of a chunk alone.
 #pragma once
 
 #include "rows.cuh"
@@ -7,61 +11,113 @@ namespace fsg {
 
 constexpr int kEmbedThreads = 256;
 
-// Eight columns of a lane: consecutive ones in vectors of 16 bytes (WIDE: rows begin on 16 bytes), or every G-th of a group of G lanes, one
-// element each, so that lanes next to one another still read next to one another.
-template <bool WIDE> __device__ __forceinline__ uint32_t column_of(uint32_t chunk, uint32_t lane, uint32_t lanes, int i) {
-    return WIDE ? (chunk * lanes + lane) * 8u + (uint32_t)i : chunk * lanes * 8u + (uint32_t)i * lanes + lane;
+struct Group { uint32_t lanes, lane, mask; };             // lanes of a row; this thread's; the warp's lanes that they are
+__device__ __forceinline__ Group row_group(uint32_t lanes_log) {
+    Group g;
+    g.lanes = 1u << lanes_log;
+    g.lane = threadIdx.x & (g.lanes - 1u);
+    g.mask = (g.lanes == 32u ? kFullMask : (1u << g.lanes) - 1u) << (threadIdx.x & 31u & ~(g.lanes - 1u));
+    return g;
 }
-template <class T, bool WIDE> struct Piece {              // as loaded
-    static constexpr int WORDS = WIDE ? 8 / Vec<T>::N : 0;
-    uint4 raw[WIDE ? WORDS : 1];
-    T     one[WIDE ? 1 : 8];
-};
-// (columns beyond the last are zero)
-template <class T, bool WIDE> __device__ __forceinline__ void load_piece(Piece<T, WIDE>& p, const T* row, uint32_t chunk, uint32_t lane, uint32_t lanes, uint32_t cols) {
+
+// 16 bytes from byte `from` (0 .. 15) on of N + 1 vectors next to one another, for each of the first N
+template <int N> __device__ __forceinline__ void shift_words(const uint32_t (&w)[4 * N + 4], uint32_t from, uint32_t (&out)[4 * N]) {
+    uint32_t a[4 * N + 2], b[4 * N + 1];
+    const bool two = from & 8u, one = from & 4u;
+#pragma unroll
+    for (int i = 0; i < 4 * N + 2; ++i) a[i] = two ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4 * N + 1; ++i) b[i] = one ? a[i + 1] : a[i];
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) out[i] = __funnelshift_r(b[i], b[i + 1], (from & 3u) * 8u);
+}
+
+// Eight columns from `c` on, as loaded.  Vectors of which no byte is the row's are not touched; what lies in others behind the row's end
+// comes along and is never written.
+template <class T, bool WIDE> struct Piece { uint4 v[8 / Vec<T>::N + (WIDE ? 0 : 1)]; };
+template <class T, bool WIDE> __device__ __forceinline__ void load_piece(Piece<T, WIDE>& p, const T* row, uint32_t c, uint32_t cols) {
+    constexpr int N = 8 / Vec<T>::N;
     if constexpr (WIDE) {
-        const uint32_t c = column_of<true>(chunk, lane, lanes, 0);
 #pragma unroll
-        for (int w = 0; w < Piece<T, WIDE>::WORDS; ++w) {
-            const uint32_t at = c + (uint32_t)(w * Vec<T>::N);
-            p.raw[w] = make_uint4(0u, 0u, 0u, 0u);
-            if (at + Vec<T>::N <= cols) p.raw[w] = load16(row + at);
-            else if (at < cols) {                         // (the row's last few)
-                T* e = reinterpret_cast<T*>(&p.raw[w]);
-#pragma unroll
-                for (int i = 0; i < Vec<T>::N; ++i) if (at + (uint32_t)i < cols) e[i] = row[at + (uint32_t)i];
-            }
-        }
+        for (int i = 0; i < N; ++i) if (c + (uint32_t)(i * Vec<T>::N) < cols) p.v[i] = load16(row + c + i * Vec<T>::N);
     } else {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), end = reinterpret_cast<uintptr_t>(row + cols), first = at & ~(uintptr_t)15;
+        const int vectors = at != first ? N + 1 : N;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t at = column_of<false>(chunk, lane, lanes, i);
-            p.one[i] = at < cols ? row[at] : from_float<T>(0.f);
-        }
+        for (int i = 0; i <= N; ++i) if (c < cols && i < vectors && first + 16u * i < end) p.v[i] = *reinterpret_cast<const uint4*>(first + 16u * i);
     }
 }
-template <class T, bool WIDE> __device__ __forceinline__ void unpack_piece(const Piece<T, WIDE>& p, float (&f)[8]) {
+template <class T, bool WIDE> __device__ __forceinline__ void unpack_piece(const Piece<T, WIDE>& p, const T* row, float (&f)[8]) {
+    constexpr int N = 8 / Vec<T>::N;
+    uint32_t w[4 * N];
     if constexpr (WIDE) {
-        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                float g[4];
-                Vec<float>::unpack(p.raw[w], g);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f[4 * w + i] = g[i];
-            }
-        } else Vec<T>::unpack(p.raw[0], f);
+        for (int i = 0; i < N; ++i) { w[4 * i] = p.v[i].x; w[4 * i + 1] = p.v[i].y; w[4 * i + 2] = p.v[i].z; w[4 * i + 3] = p.v[i].w; }
     } else {
+        uint32_t all[4 * N + 4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = to_float(p.one[i]);
+        for (int i = 0; i <= N; ++i) { all[4 * i] = p.v[i].x; all[4 * i + 1] = p.v[i].y; all[4 * i + 2] = p.v[i].z; all[4 * i + 3] = p.v[i].w; }
+        shift_words<N>(all, (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u, w);      // (eight columns are whole vectors: the row's own offset)
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float g[Vec<T>::N];
+        Vec<T>::unpack(make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]), g);
+#pragma unroll
+        for (int j = 0; j < Vec<T>::N; ++j) f[i * Vec<T>::N + j] = g[j];
     }
 }
-template <class T, bool WIDE> __device__ __forceinline__ void store_piece(T* row, const float (&f)[8], uint32_t chunk, uint32_t lane, uint32_t lanes, uint32_t cols) {
-    if (WIDE && column_of<true>(chunk, lane, lanes, 7) < cols) { store_values(row + column_of<true>(chunk, lane, lanes, 0), f, true); return; }
+// The words of eight values, rounded to T.
+template <class T> __device__ __forceinline__ void pack_piece(const float (&f)[8], uint32_t (&w)[32 / Vec<T>::N]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t at = column_of<WIDE>(chunk, lane, lanes, i);
-        if (at < cols) row[at] = from_float<T>(f[i]);
+    for (int i = 0; i < 8 * (int)sizeof(T) / 4; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+        else w[i] = pack_two<T>(f[2 * i], f[2 * i + 1]);
+    }
+}
+template <class T> __device__ __forceinline__ void store_element(T* to, const uint32_t* w, uint32_t i) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(to + i) = w[i];
+    else *reinterpret_cast<uint16_t*>(to + i) = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+}
+// Eight columns of each of the group's lanes, all of whose threads come here.
+template <class T, bool WIDE> __device__ __forceinline__ void store_piece(T* row, const uint32_t (&w)[32 / Vec<T>::N], uint32_t c, uint32_t cols, const Group& g) {
+    constexpr int N = 8 / Vec<T>::N;
+    constexpr uint32_t PER = Vec<T>::N;
+    const uint32_t off = WIDE ? 0u : (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;
+    if (off == 0u) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t at = c + i * PER;
+            if (at + PER <= cols) store16(row + at, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            else {
+#pragma unroll
+                for (uint32_t j = 0; j < PER; ++j) if (at + j < cols) store_element(row + c, w, i * PER + j);
+            }
+        }
+        return;
+    }
+    if constexpr (!WIDE) {
+        uint32_t all[4 * N + 4], out[4 * N];
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) all[i] = w[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) all[4 * N + i] = __shfl_down_sync(g.mask, w[i], 1, g.lanes);
+        shift_words<N>(all, 16u - off, out);
+        const uint32_t head = (16u - off) / sizeof(T);    // columns before the first aligned vector
+        if (g.lane == 0u) {
+#pragma unroll
+            for (uint32_t j = 0; j < PER; ++j) if (j < head && c + j < cols) store_element(row + c, w, j);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t at = c + head + i * PER;
+            const uint32_t mine = g.lane + 1u == g.lanes && i + 1 == N ? PER - head : PER;      // (nobody's columns follow those of the last lane)
+            if (mine == PER && at + PER <= cols) store16(row + at, make_uint4(out[4 * i], out[4 * i + 1], out[4 * i + 2], out[4 * i + 3]));
+            else {
+#pragma unroll
+                for (uint32_t j = 0; j < PER; ++j) if (j < mine && at + j < cols) store_element(row + at - i * PER, out, i * PER + j);
+            }
+        }
     }
 }
 
@@ -73,43 +129,47 @@ struct LookupArgs {
     const int32_t* ids;
     uint32_t  per_row;                                    // ids of each of the table's rows: row ids[t] / per_row
     uint32_t  count, vocab, cols;
-    uint32_t  lanes_log;                                  // lanes that share a row's chunk of 8 lanes columns, 1 .. 32
-    uint32_t  chunks;
+    uint32_t  lanes_log;                                  // lanes of a group
+    uint32_t  spans;                                      // pieces of a row that groups take
+    uint64_t  units;                                      // of the groups in all
     float     scale;
     void*     out;
     uint64_t  out_stride;
 };
 
-// A group of lanes per chunk of a row, kLookupAhead chunks in flight.
+// A group takes four chunks of a row (SHORT rows: a chunk of each of four rows), all on their way at once.
 constexpr uint32_t kLookupAhead = 4u;
-template <class T, class TO, bool WIDE> __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_constant__ LookupArgs a) {
+template <class T, class TO, bool WIDE, bool SHORT> __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_constant__ LookupArgs a) {
     wait_for_previous_kernels();
     allow_next_kernel();
-    const uint32_t lanes = 1u << a.lanes_log, lane = threadIdx.x & (lanes - 1u);
-    const uint64_t groups = (uint64_t)gridDim.x * (kEmbedThreads >> a.lanes_log), all = (uint64_t)a.count * a.chunks;
-    for (uint64_t u0 = (uint64_t)blockIdx.x * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log); u0 < all; u0 += groups * kLookupAhead) {
-        Piece<T, WIDE> p[kLookupAhead];
-        uint32_t row[kLookupAhead], chunk[kLookupAhead], id[kLookupAhead];
+    const Group g = row_group(a.lanes_log);
+    const uint64_t u = (uint64_t)blockIdx.x * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
+    if (u >= a.units) return;
+    const uint32_t row0 = SHORT ? (uint32_t)u * kLookupAhead : a.units <= 0xFFFFFFFFull ? (uint32_t)u / a.spans : (uint32_t)(u / a.spans);
+    const uint32_t c0 = SHORT ? g.lane * 8u : ((uint32_t)(u - (uint64_t)row0 * a.spans) * kLookupAhead * g.lanes + g.lane) * 8u, step = SHORT ? 0u : g.lanes * 8u;
+    Piece<T, WIDE> p[kLookupAhead];
+    uint32_t id[kLookupAhead];
 #pragma unroll
-        for (uint32_t j = 0; j < kLookupAhead; ++j) {
-            const uint64_t u = u0 + groups * j;
-            row[j] = (uint32_t)(u / a.chunks); chunk[j] = (uint32_t)(u - (uint64_t)row[j] * a.chunks);
-            id[j] = u < all ? (uint32_t)a.ids[row[j]] / a.per_row : ~0u;
+    for (uint32_t j = 0; j < kLookupAhead; ++j) {
+        if (!SHORT && j) { id[j] = id[0]; continue; }
+        id[j] = row0 + j < a.count ? (uint32_t)a.ids[row0 + j] : ~0u;
+        if (a.per_row != 1u) id[j] /= a.per_row;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kLookupAhead; ++j) if (id[j] < a.vocab) load_piece(p[j], static_cast<const T*>(a.table) + id[j] * a.table_stride, c0 + step * j, a.cols);
+#pragma unroll
+    for (uint32_t j = 0; j < kLookupAhead; ++j) {
+        const uint32_t row = SHORT ? row0 + j : row0;
+        if (row >= a.count || c0 + step * j - g.lane * 8u >= a.cols) continue;       // (of the whole group)
+        float f[8] = {};
+        if (id[j] < a.vocab) {
+            unpack_piece(p[j], static_cast<const T*>(a.table) + id[j] * a.table_stride, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= a.scale;
         }
-#pragma unroll
-        for (uint32_t j = 0; j < kLookupAhead; ++j)
-            if (id[j] < a.vocab) load_piece(p[j], static_cast<const T*>(a.table) + id[j] * a.table_stride, chunk[j], lane, lanes, a.cols);
-#pragma unroll
-        for (uint32_t j = 0; j < kLookupAhead; ++j) {
-            if (u0 + groups * j >= all) continue;
-            float f[8] = {};
-            if (id[j] < a.vocab) {
-                unpack_piece(p[j], f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= a.scale;
-            }
-            store_piece<TO, WIDE>(static_cast<TO*>(a.out) + row[j] * a.out_stride, f, chunk[j], lane, lanes, a.cols);
-        }
+        uint32_t w[32 / Vec<TO>::N];
+        pack_piece<TO>(f, w);
+        store_piece<TO, WIDE>(static_cast<TO*>(a.out) + row * a.out_stride, w, c0 + step * j, a.cols, g);
     }
 }
 
@@ -139,10 +199,23 @@ struct GradientArgs {
     uint32_t  most;                                       // rows that keys and values hold
     uint64_t  part_stride;                                // cols, up to a multiple of 4
     float*    parts;                                      // 2 tiles x part_stride: of a tile's first token (begun earlier), of its last (that goes on)
-    uint64_t  sum_blocks;                                 // blocks that add up; the others clear rows of tokens that do not occur
+    uint32_t  sum_blocks;                                 // blocks that add up; the others clear rows of tokens that do not occur,
+    uint32_t  clear_rows;                                 // so many each
 };
 
-// Where in distinct (ascending, n of them) v is: the first that is not below it.
+// Where in distinct (ascending, n of them) v is: the first that is not below it.  One warp: 32 probes a step.
+__device__ __forceinline__ uint32_t place_among_by_warp(const uint32_t* distinct, uint32_t n, uint32_t v) {
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t lo = 0, hi = n;                              // the answer lies in lo .. hi
+    while (hi - lo > 32u) {
+        const uint32_t each = (hi - lo + 31u) / 32u, at = lo + lane * each;
+        const uint32_t below = __popc(__ballot_sync(kFullMask, at < hi && distinct[at] < v));
+        if (!below) return lo;
+        hi = min(hi, lo + below * each);
+        lo += (below - 1u) * each + 1u;
+    }
+    return lo + __popc(__ballot_sync(kFullMask, lo + lane < hi && distinct[lo + lane] < v));
+}
 __device__ __forceinline__ uint32_t place_among(const uint32_t* distinct, uint32_t n, uint32_t v) {
     uint32_t lo = 0, hi = n;
     while (lo < hi) {
@@ -154,61 +227,84 @@ __device__ __forceinline__ uint32_t place_among(const uint32_t* distinct, uint32
 
 // A finished sum to its row.
 template <class TO, bool WIDE, bool PAIRS>
-__device__ __forceinline__ void write_sum(const GradientArgs& a, uint32_t v, uint32_t row, const float (&sum)[8], uint32_t chunk, uint32_t lane, uint32_t lanes) {
+__device__ __forceinline__ void write_sum(const GradientArgs& a, uint32_t v, uint32_t row, const float (&sum)[8], uint32_t c, const Group& g) {
     float f[8];
+    uint32_t w[32 / Vec<TO>::N];
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = sum[i] * a.scale;
+    pack_piece<TO>(f, w);
     if constexpr (PAIRS) {
         if (row >= a.most) return;
-        store_piece<float, WIDE>(a.values + (uint64_t)row * a.cols, f, chunk, lane, lanes, a.cols);
+        store_piece<float, WIDE>(a.values + (uint64_t)row * a.cols, w, c, a.cols, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v * a.cols + column_of<WIDE>(chunk, lane, lanes, i));
-        store_piece<float, WIDE>(reinterpret_cast<float*>(a.keys) + (uint64_t)row * a.cols, f, chunk, lane, lanes, a.cols);
-    } else store_piece<TO, WIDE>(static_cast<TO*>(a.out) + v * a.out_stride, f, chunk, lane, lanes, a.cols);
+        for (uint32_t i = 0; i < 8u; ++i) w[i] = v * a.cols + c + i;
+        store_piece<float, WIDE>(reinterpret_cast<float*>(a.keys) + (uint64_t)row * a.cols, w, c, a.cols, g);
+    } else store_piece<TO, WIDE>(static_cast<TO*>(a.out) + v * a.out_stride, w, c, a.cols, g);
+}
+__device__ __forceinline__ void write_part(const GradientArgs& a, uint64_t part, const float (&sum)[8], uint32_t c, const Group& g) {
+    uint32_t w[8];
+    pack_piece<float>(sum, w);
+    store_piece<float, true>(a.parts + part * a.part_stride, w, c, a.cols, g);
+}
+
+// Rows of tokens that do not occur become zero: a block's are listed, and gone through vector by vector.
+template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const GradientArgs& a) {
+    __shared__ uint32_t listed[64], some;
+    const uint32_t v0 = (blockIdx.x - a.sum_blocks) * a.clear_rows;
+    if (threadIdx.x == 0) some = 0;
+    __syncthreads();
+    if (threadIdx.x < a.clear_rows && v0 + threadIdx.x < a.vocab && a.starts[v0 + threadIdx.x] == a.starts[v0 + threadIdx.x + 1u]) listed[atomicAdd(&some, 1u)] = v0 + threadIdx.x;
+    __syncthreads();
+    const Group g = row_group(a.lanes_log);
+    const uint32_t zero[32 / Vec<TO>::N] = {};
+    const uint32_t groups = (uint32_t)kEmbedThreads >> a.lanes_log, mine = threadIdx.x >> a.lanes_log;
+    auto clear = [&](uint32_t i, uint32_t chunk) { store_piece<TO, WIDE>(static_cast<TO*>(a.out) + listed[i] * a.out_stride, zero, (chunk * g.lanes + g.lane) * 8u, a.cols, g); };
+    if (a.chunks >= groups) {                             // (a row after the other: nothing to divide)
+        for (uint32_t i = 0; i < some; ++i)
+            for (uint32_t chunk = mine; chunk < a.chunks; chunk += groups) clear(i, chunk);
+    } else {
+        for (uint32_t u = mine; u < some * a.chunks; u += groups) clear(u / a.chunks, u % a.chunks);
+    }
 }
 
 template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads) k_embedding_sum(const __grid_constant__ GradientArgs a) {
-    constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;         // rows in flight
+    constexpr int AHEAD = sizeof(T) == 2 && WIDE ? 8 : 4;         // rows in flight
     wait_for_previous_kernels();
     allow_next_kernel();
-    const uint32_t lanes = 1u << a.lanes_log, lane = threadIdx.x & (lanes - 1u);
-    if (!PAIRS && blockIdx.x >= a.sum_blocks) {           // rows of tokens that do not occur
-        const uint64_t groups = (uint64_t)(gridDim.x - a.sum_blocks) * (kEmbedThreads >> a.lanes_log);
-        const float zero[8] = {};
-        for (uint64_t u = (uint64_t)(blockIdx.x - a.sum_blocks) * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log); u < (uint64_t)a.vocab * a.chunks; u += groups) {
-            const uint32_t v = (uint32_t)(u / a.chunks), chunk = (uint32_t)(u - (uint64_t)v * a.chunks);
-            if (a.starts[v] == a.starts[v + 1u]) store_piece<TO, WIDE>(static_cast<TO*>(a.out) + v * a.out_stride, zero, chunk, lane, lanes, a.cols);
-        }
-        return;
-    }
-    const uint32_t have = min(a.starts[a.vocab], a.count);
-    const uint64_t u = (uint64_t)blockIdx.x * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
-    const uint32_t tile = (uint32_t)(u / a.chunks), chunk = (uint32_t)(u - (uint64_t)tile * a.chunks);
-    const uint32_t begin = min(tile << a.tile_log, have), end = min(begin + (1u << a.tile_log), have);
-    if (tile >= a.tiles || begin >= end) return;
+    if (!PAIRS && blockIdx.x >= a.sum_blocks) { clear_rows<TO, WIDE>(a); return; }
+    const Group g = row_group(a.lanes_log);
+    const uint32_t u = blockIdx.x * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
+    const uint32_t tile = u / a.chunks, c = ((u - tile * a.chunks) * g.lanes + g.lane) * 8u;
+    if (tile >= a.tiles) return;
+    const uint32_t begin = tile << a.tile_log;
+    // the rows and tokens of AHEAD positions (those behind the last are garbage, and of no account)
+    auto look_up = [&](uint32_t p, uint32_t (&at)[AHEAD], uint32_t (&id)[AHEAD]) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) at[j] = p + (uint32_t)j < a.count ? a.order[p + (uint32_t)j] : ~0u;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) id[j] = at[j] < a.count ? (uint32_t)a.ids[at[j]] : ~0u;
+    };
     auto id_at = [&](uint32_t p) { const uint32_t at = a.order[p]; return at < a.count ? (uint32_t)a.ids[at] : ~0u; };
-    uint32_t now = id_at(begin), row = 0;                 // the token whose rows are being added up; pairs: its row
-    bool earlier = begin && id_at(begin - 1u) == now;     // it began in an earlier tile
+    uint32_t at[AHEAD], id[AHEAD], row = 0;
+    look_up(begin, at, id);
+    const uint32_t before = begin ? id_at(begin - 1u) : ~0u;
+    const uint32_t have = min(a.starts[a.vocab], a.count), end = min(begin + (1u << a.tile_log), have);
+    if (begin >= end) return;
+    uint32_t now = id[0];                                 // the token whose rows are being added up; pairs: its row
+    bool earlier = begin && before == now;                // it began in an earlier tile
     const bool goes_on = end < have && id_at(end) == id_at(end - 1u);
-    if constexpr (PAIRS) row = place_among(a.distinct, min(*a.number, a.most), now);
+    if constexpr (PAIRS) row = g.lanes == 32u ? place_among_by_warp(a.distinct, min(*a.number, a.most), now) : place_among(a.distinct, min(*a.number, a.most), now);
     float sum[8] = {};
     auto finish = [&]() {
-        if (earlier) store_piece<float, WIDE>(a.parts + 2ull * tile * a.part_stride, sum, chunk, lane, lanes, a.cols);
-        else if (now < a.vocab) write_sum<TO, WIDE, PAIRS>(a, now, row, sum, chunk, lane, lanes);
+        if (earlier) write_part(a, 2ull * tile, sum, c, g);
+        else if (now < a.vocab) write_sum<TO, WIDE, PAIRS>(a, now, row, sum, c, g);
     };
     for (uint32_t p = begin; p < end; p += AHEAD) {
-        uint32_t at[AHEAD], id[AHEAD];
+        uint32_t next_at[AHEAD], next_id[AHEAD];
         Piece<T, WIDE> piece[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) at[j] = p + (uint32_t)j < end ? a.order[p + (uint32_t)j] : ~0u;
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            id[j] = ~0u;
-            if (at[j] < a.count) {
-                id[j] = (uint32_t)a.ids[at[j]];
-                load_piece(piece[j], static_cast<const T*>(a.grad) + at[j] * a.grad_stride, chunk, lane, lanes, a.cols);
-            }
-        }
+        for (int j = 0; j < AHEAD; ++j) if (p + (uint32_t)j < end && at[j] < a.count) load_piece(piece[j], static_cast<const T*>(a.grad) + at[j] * a.grad_stride, c, a.cols);
+        if (p + AHEAD < end) look_up(p + AHEAD, next_at, next_id);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (p + (uint32_t)j >= end) continue;
@@ -220,12 +316,14 @@ template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bou
             }
             if (at[j] >= a.count) continue;
             float f[8];
-            unpack_piece(piece[j], f);
+            unpack_piece(piece[j], static_cast<const T*>(a.grad) + at[j] * a.grad_stride, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += f[i];
         }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
     }
-    if (goes_on && !earlier) store_piece<float, WIDE>(a.parts + (2ull * tile + 1ull) * a.part_stride, sum, chunk, lane, lanes, a.cols);
+    if (goes_on && !earlier) write_part(a, 2ull * tile + 1ull, sum, c, g);
     else finish();
 }
 
@@ -236,9 +334,10 @@ template <class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEm
     __shared__ float shares[WARPS][32][9];
     wait_for_previous_kernels();
     allow_next_kernel();
-    const uint32_t lanes = 1u << a.lanes_log, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const Group g = row_group(a.lanes_log);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t have = min(a.starts[a.vocab], a.count);
-    const uint32_t tile = (uint32_t)(blockIdx.x / a.chunks), chunk = (uint32_t)(blockIdx.x - (uint64_t)tile * a.chunks);
+    const uint32_t tile = blockIdx.x / a.chunks, c = ((blockIdx.x - tile * a.chunks) * g.lanes + lane) * 8u;
     const uint32_t begin = tile << a.tile_log, end = begin + (1u << a.tile_log);
     if (end >= have) return;                              // (the last tile, or behind it)
     const uint32_t first = a.order[end - 1u], next = a.order[end];
@@ -249,37 +348,37 @@ template <class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEm
     const uint32_t parts = last - tile, each = (parts + WARPS - 1u) / WARPS;
     const uint32_t from = tile + 1u + min(warp * each, parts), to = tile + 1u + min(warp * each + each, parts);
     float sum[8] = {};
-    if (lane < lanes) {
+    auto add = [&](const Piece<float, true>& p) {
+        float f[8];
+        unpack_piece(p, a.parts, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += f[i];
+    };
+    if (lane < g.lanes) {
         if (warp == 0u) {
-            Piece<float, WIDE> p;
-            load_piece(p, a.parts + (2ull * tile + 1ull) * a.part_stride, chunk, lane, lanes, a.cols);
-            unpack_piece(p, sum);
+            Piece<float, true> p;
+            load_piece(p, a.parts + (2ull * tile + 1ull) * a.part_stride, c, a.cols);
+            add(p);
         }
         for (uint32_t t = from; t < to; t += 4u) {
-            Piece<float, WIDE> p[4];
+            Piece<float, true> p[4];
 #pragma unroll
-            for (uint32_t j = 0; j < 4u; ++j) if (t + j < to) load_piece(p[j], a.parts + 2ull * (t + j) * a.part_stride, chunk, lane, lanes, a.cols);
+            for (uint32_t j = 0; j < 4u; ++j) if (t + j < to) load_piece(p[j], a.parts + 2ull * (t + j) * a.part_stride, c, a.cols);
 #pragma unroll
-            for (uint32_t j = 0; j < 4u; ++j) {
-                if (t + j >= to) continue;
-                float f[8];
-                unpack_piece(p[j], f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += f[i];
-            }
+            for (uint32_t j = 0; j < 4u; ++j) if (t + j < to) add(p[j]);
         }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) shares[warp][lane][i] = sum[i];
     __syncthreads();
-    if (warp || lane >= lanes) return;
+    if (warp) return;
     for (uint32_t w = 1; w < WARPS; ++w) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += shares[w][lane][i];
     }
     uint32_t row = 0;
-    if constexpr (PAIRS) row = place_among(a.distinct, min(*a.number, a.most), v);
-    write_sum<TO, WIDE, PAIRS>(a, v, row, sum, chunk, lane, lanes);
+    if constexpr (PAIRS) row = place_among_by_warp(a.distinct, min(*a.number, a.most), v);
+    if (lane < g.lanes) write_sum<TO, WIDE, PAIRS>(a, v, row, sum, c, g);
 }
 
 }  // namespace fsg

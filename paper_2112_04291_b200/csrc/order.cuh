@@ -121,47 +121,101 @@ struct OrderShared {
     uint32_t sums[kOrderMaxBins];                         // this block's, by digit
     uint32_t base[kOrderMaxBins];                         // places of its first element of each digit
     uint32_t warp_sums[32];
-    uint32_t of_block[2];                                 // occurrences and ids that occur in this block's part of the range
+    unsigned long long pair_sums[32];
+    unsigned long long of_block;                          // occurrences and ids that occur in this block's part of the range
     uint32_t pad[2];
     uint32_t keys[2][kOrderTile];
     uint16_t places[2][kOrderTile];
     uint16_t counts[kOrderWarps * kOrderMaxBins];         // by warp and digit (as many digits as there are)
 };
 
-// Where each id's positions begin, from its number of occurrences in starts (one cluster; `slice` ids a block), and the ids that occur.
+// The same of two values that are below 2^32, the second in the upper half.
+__device__ __forceinline__ unsigned long long order_scan_pair(unsigned long long x, unsigned long long* warp_sums, unsigned long long* total) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    unsigned long long y = x;
+#pragma unroll
+    for (uint32_t d = 1; d < 32u; d *= 2u) {
+        const unsigned long long up = __shfl_up_sync(kFullMask, y, d);
+        if (lane >= d) y += up;
+    }
+    if (lane == 31u) warp_sums[warp] = y;
+    __syncthreads();
+    unsigned long long w = warp_sums[lane], before = 0, all = 0;
+#pragma unroll
+    for (uint32_t d = 16; d; d /= 2u) {                   // (every warp sums for itself what lies before it, and all)
+        all = d == 16u ? w : all;
+        all += __shfl_xor_sync(kFullMask, all, d);
+    }
+    before = lane < warp ? w : 0ull;
+#pragma unroll
+    for (uint32_t d = 16; d; d /= 2u) before += __shfl_xor_sync(kFullMask, before, d);
+    *total = all;
+    __syncthreads();
+    return before + y - x;
+}
+
+// Where each id's positions begin, from its number of occurrences in starts (one cluster; a slice of the range a block, sixteen ids a thread at a
+// time), and the ids that occur.
+constexpr uint32_t kOrderEach = 16u;
 __device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, OrderShared& s, uint32_t block) {
-    const uint32_t slice = ((a.range + kOrderBlocks) / kOrderBlocks + 3u) & ~3u;      // (of range + 1 entries)
-    const uint32_t lo = block * slice, hi = min(lo + slice, a.range + 1u);
-    uint32_t sum = 0, occur = 0;
-    for (uint32_t v = lo + threadIdx.x; v < hi; v += kOrderThreads) {
-        const uint32_t n = v < a.range ? __ldcg(a.starts + v) : 0u;
-        sum += n;
-        occur += n != 0u;
-    }
-    uint32_t total = 0, total_occur = 0;
-    order_scan(sum, s.warp_sums, &total);
-    order_scan(occur, s.warp_sums, &total_occur);
-    if (threadIdx.x == 0) { s.of_block[0] = total; s.of_block[1] = total_occur; }
+    constexpr uint32_t ROUND = kOrderThreads * kOrderEach;
+    const uint32_t entries = a.range + 1u, slice = ((entries + kOrderBlocks - 1u) / kOrderBlocks + kOrderEach - 1u) / kOrderEach * kOrderEach;
+    const uint32_t lo = min(block * slice, entries), hi = min(lo + slice, entries);
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.starts) & 15u) == 0u;
+    uint32_t n[kOrderEach];
+    auto load = [&](uint32_t v) {
+        if (aligned && v + kOrderEach <= hi) {
+#pragma unroll
+            for (uint32_t i = 0; i < kOrderEach; i += 4u) {
+                const uint4 x = __ldcg(reinterpret_cast<const uint4*>(a.starts + v + i));
+                n[i] = x.x; n[i + 1] = x.y; n[i + 2] = x.z; n[i + 3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kOrderEach; ++i) n[i] = v + i < hi ? __ldcg(a.starts + v + i) : 0u;
+        }
+        unsigned long long sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kOrderEach; ++i) sum += n[i] + ((unsigned long long)(n[i] != 0u) << 32);
+        return sum;
+    };
+    const bool once = slice <= ROUND;                     // (what a thread has loaded it keeps)
+    unsigned long long mine = 0, total = 0, at = 0, all = 0;
+    for (uint32_t v = lo; v < hi; v += ROUND) mine += load(v + threadIdx.x * kOrderEach);
+    const unsigned long long before_mine = order_scan_pair(mine, s.pair_sums, &total);
+    if (threadIdx.x == 0) s.of_block = total;
     cluster_meet();
-    uint32_t at = 0, at_occur = 0, all_occur = 0;
     for (uint32_t b = 0; b < kOrderBlocks; ++b) {
-        const uint32_t from = address_in(s.of_block, b), n = load_from(from), o = load_from(from + 4u);
-        if (b < block) { at += n; at_occur += o; }
-        all_occur += o;
+        const uint32_t from = address_in(&s.of_block, b);
+        const unsigned long long x = load_from(from) | (unsigned long long)load_from(from + 4u) << 32;
+        if (b < block) at += x;
+        all += x;
     }
-    for (uint32_t v0 = lo; v0 < hi; v0 += kOrderThreads) {
-        const uint32_t v = v0 + threadIdx.x;
-        const uint32_t n = v < hi && v < a.range ? __ldcg(a.starts + v) : 0u;
-        const uint32_t before = order_scan(n, s.warp_sums, &total);
-        if (v < hi) a.starts[v] = at + before;
-        at += total;
-        if (a.distinct) {
-            const uint32_t rank = order_scan(n != 0u, s.warp_sums, &total_occur);
-            if (n) a.distinct[at_occur + rank] = v;
-            at_occur += total_occur;
+    for (uint32_t v0 = lo; v0 < hi; v0 += ROUND) {
+        const uint32_t v = v0 + threadIdx.x * kOrderEach;
+        unsigned long long here = at + before_mine;
+        if (!once) {
+            here = at + order_scan_pair(load(v), s.pair_sums, &total);
+            at += total;
+        }
+        uint32_t first = (uint32_t)here, rank = (uint32_t)(here >> 32);
+        uint32_t first_of[kOrderEach];
+#pragma unroll
+        for (uint32_t i = 0; i < kOrderEach; ++i) {
+            first_of[i] = first;
+            first += n[i];
+            if (n[i]) { if (a.distinct) a.distinct[rank] = v + i; ++rank; }
+        }
+        if (aligned && v + kOrderEach <= hi) {
+#pragma unroll
+            for (uint32_t i = 0; i < kOrderEach; i += 4u)
+                *reinterpret_cast<uint4*>(a.starts + v + i) = make_uint4(first_of[i], first_of[i + 1], first_of[i + 2], first_of[i + 3]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kOrderEach; ++i) if (v + i < hi) a.starts[v + i] = first_of[i];
         }
     }
-    if (a.number && block == 0u && threadIdx.x == 0) *a.number = all_occur;
+    if (a.number && block == 0u && threadIdx.x == 0) *a.number = (uint32_t)(all >> 32);
 }
 
 // One cluster: everything.
@@ -179,10 +233,15 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
     const uint32_t have = first < end ? min(end - first, 1u << per_log) : 0u;
     wait_for_previous_kernels();
     allow_next_kernel();
-    for (uint32_t v = block * kOrderThreads + threadIdx.x; v < a.range; v += kOrderBlocks * kOrderThreads) a.starts[v] = 0u;
+    const bool several = a.passes > 1u;                   // (one digit: its counts are the ids')
+    if (several) {                                        // (the last entry counts nothing)
+        const uint32_t vectors = (reinterpret_cast<uintptr_t>(a.starts) & 15u) == 0u ? (a.range + 1u) / 4u : 0u, thread = block * kOrderThreads + threadIdx.x;
+        for (uint32_t i = thread; i < vectors; i += kOrderBlocks * kOrderThreads) reinterpret_cast<uint4*>(a.starts)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (uint32_t v = 4u * vectors + thread; v <= a.range; v += kOrderBlocks * kOrderThreads) a.starts[v] = 0u;
+    }
     for (uint32_t i = threadIdx.x; i < end - begin; i += kOrderThreads) s.keys[0][i] = order_key(a, begin + i);
-    cluster_meet();
-    for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
+    if (several) cluster_meet(); else __syncthreads();
+    if (several) for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
         const uint32_t i = i0 + threadIdx.x;
         const uint32_t key = i < end - begin ? s.keys[0][i] : a.range;
         const uint32_t same = __match_any_sync(kFullMask, key);
@@ -209,6 +268,13 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
         const uint32_t lower = order_scan(all, s.warp_sums, &total);
         if (threadIdx.x < bins) s.base[threadIdx.x] = lower + before;
         __syncthreads();
+        if (!several && block == 0u) {
+            if (threadIdx.x <= a.range) a.starts[threadIdx.x] = lower;
+            const bool occurs = threadIdx.x < a.range && all != 0u;
+            const uint32_t rank_of = order_scan(occurs, s.warp_sums, &total);
+            if (occurs && a.distinct) a.distinct[rank_of] = threadIdx.x;
+            if (a.number && threadIdx.x == 0) *a.number = total;
+        }
         const bool last = pass + 1u == a.passes;
 #pragma unroll
         for (uint32_t j = 0; j < kOrderRounds; ++j) {
@@ -228,6 +294,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
         from ^= 1u;
         cluster_meet();                                   // (also: the sums have been read before they are formed anew, or their block ends)
     }
+    if (!several) return;
     order_starts_from_counts(a, s, block);
     cluster_meet();                                       // (no block ends while others read its shared memory)
 }

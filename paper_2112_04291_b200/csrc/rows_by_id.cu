@@ -64,26 +64,29 @@ template <bool WIDE, bool PAIRS> const void* join_kernel(uint32_t to) {
     else return to == FASTSGD_F32 ? (const void*)k_embedding_join<float, WIDE, false> : to == FASTSGD_BF16 ? (const void*)k_embedding_join<__nv_bfloat16, WIDE, false>
                                                                                        : (const void*)k_embedding_join<__half, WIDE, false>;
 }
-template <class T, bool WIDE> const void* lookup_kernel_of(uint32_t to) {
-    if (to == FASTSGD_F32) return (const void*)k_embedding<T, float, WIDE>;
-    if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? (const void*)k_embedding<T, __nv_bfloat16, WIDE> : (const void*)k_embedding<T, __half, WIDE>;
-    else return (const void*)k_embedding<T, T, WIDE>;
+template <class T, bool WIDE, bool SHORT> const void* lookup_kernel_of(uint32_t to) {
+    if (to == FASTSGD_F32) return (const void*)k_embedding<T, float, WIDE, SHORT>;
+    if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? (const void*)k_embedding<T, __nv_bfloat16, WIDE, SHORT> : (const void*)k_embedding<T, __half, WIDE, SHORT>;
+    else return (const void*)k_embedding<T, T, WIDE, SHORT>;
 }
-template <bool WIDE> const void* lookup_kernel(uint32_t from, uint32_t to) {
-    return from == FASTSGD_F32 ? lookup_kernel_of<float, WIDE>(to) : from == FASTSGD_BF16 ? lookup_kernel_of<__nv_bfloat16, WIDE>(to) : lookup_kernel_of<__half, WIDE>(to);
+template <bool WIDE, bool SHORT> const void* lookup_kernel(uint32_t from, uint32_t to) {
+    return from == FASTSGD_F32 ? lookup_kernel_of<float, WIDE, SHORT>(to) : from == FASTSGD_BF16 ? lookup_kernel_of<__nv_bfloat16, WIDE, SHORT>(to) : lookup_kernel_of<__half, WIDE, SHORT>(to);
 }
-
 int launch_lookup(const fastsgd_matrix* table, const int32_t* ids, uint32_t per_row, float scale, const fastsgd_matrix* out, const DeviceView& dev, cudaStream_t st) {
     const GradientShape g = gradient_shape(1, table->cols);
     LookupArgs a{};
     a.table = table->data; a.table_stride = table->row_stride; a.ids = ids; a.per_row = per_row;
     a.count = (uint32_t)out->rows; a.vocab = (uint32_t)table->rows; a.cols = (uint32_t)table->cols;
-    a.lanes_log = g.lanes_log; a.chunks = g.chunks; a.scale = scale; a.out = out->data; a.out_stride = out->row_stride;
-    const bool wide = rows_on_16(table) && rows_on_16(out);
-    const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log, all = ((uint64_t)a.count * a.chunks + groups * kLookupAhead - 1) / (groups * kLookupAhead);
-    const uint64_t some = 64ull * (uint64_t)dev.sm_count;
+    a.lanes_log = g.lanes_log; a.scale = scale; a.out = out->data; a.out_stride = out->row_stride;
+    const bool wide = rows_on_16(table) && rows_on_16(out), brief = g.chunks == 1u;
+    a.spans = (g.chunks + kLookupAhead - 1u) / kLookupAhead;
+    a.units = brief ? (out->rows + kLookupAhead - 1u) / kLookupAhead : out->rows * a.spans;
+    const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log, blocks = (a.units + groups - 1) / groups;
+    if (blocks >= 1ull << 31) return FASTSGD_E_BAD_N;
     void* kargs[] = {&a};
-    return launched(launch_overlapped(wide ? lookup_kernel<true>(table->type, out->type) : lookup_kernel<false>(table->type, out->type), (unsigned)(all < some ? all : some), kEmbedThreads, 0, kargs, st));
+    const void* fn = wide ? (brief ? lookup_kernel<true, true>(table->type, out->type) : lookup_kernel<true, false>(table->type, out->type))
+                          : (brief ? lookup_kernel<false, true>(table->type, out->type) : lookup_kernel<false, false>(table->type, out->type));
+    return launched(launch_overlapped(fn, (unsigned)blocks, kEmbedThreads, 0, kargs, st));
 }
 
 template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& g, bool wide, uint32_t from, uint32_t to, const DeviceView& dev, cudaStream_t st) {
@@ -91,11 +94,12 @@ template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& 
     a.lanes_log = g.lanes_log; a.chunks = g.chunks; a.tile_log = g.tile_log; a.tiles = g.tiles; a.part_stride = g.part_stride;
     a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset);
     const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log;
-    a.sum_blocks = ((uint64_t)g.tiles * g.chunks + groups - 1) / groups;
+    a.sum_blocks = (uint32_t)(((uint64_t)g.tiles * g.chunks + groups - 1) / groups);
     uint64_t blocks = a.sum_blocks;
-    if (!PAIRS) {
-        const uint64_t all = ((uint64_t)a.vocab * g.chunks + groups - 1) / groups, some = 16ull * (uint64_t)dev.sm_count;
-        blocks += all < some ? all : some;
+    if (!PAIRS) {                                          // (eight rounds of blocks that clear, of 64 rows at most)
+        a.clear_rows = 1u;
+        while (a.clear_rows < 64u && a.vocab > a.clear_rows * 64ull * (uint64_t)dev.sm_count) a.clear_rows *= 2u;
+        blocks += (a.vocab + a.clear_rows - 1u) / a.clear_rows;
     }
     if (blocks >= 1ull << 31 || (uint64_t)g.tiles * g.chunks >= 1ull << 31) return FASTSGD_E_BAD_N;
     void* kargs[] = {&a};
