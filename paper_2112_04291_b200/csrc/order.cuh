@@ -3,11 +3,11 @@
 //
 // A stable sort by digits, lowest first, of 10 bits at most: one digit for a router's experts, two for a vocabulary.  Ids outside the
 // range become the range itself, the largest key, and are sorted like the others but not written.  Within a warp equal digits find one
-// another by match; each warp counts its digits in shared memory, so that an element's place is the sum of four numbers: elements of lower
+// another by a vote on each of their bits; each warp counts its digits in shared memory, so that an element's place is the sum of four numbers: elements of lower
 // digits, of its digit in earlier blocks, in earlier warps, and before it in its warp.  No place depends on the order in which threads run.
 //
-// Up to 2^16 ids are sorted by one cluster of eight blocks in its shared memory (k_order): no launch between digits and no
-// workspace.  More take three launches a digit (k_order_count, k_order_offsets, k_order_place), with keys and positions in the workspace.
+// Up to 2^16 ids are sorted by one cluster of sixteen blocks in its shared memory (k_order): no launch between digits and no
+// workspace; up to 2^11 are each compared with all others instead.  More take three launches a digit (k_order_count, k_order_offsets, k_order_place), with keys and positions in the workspace.
 #pragma once
 
 #include "async.cuh"
@@ -16,11 +16,13 @@ namespace fsg {
 
 constexpr int      kOrderThreads  = 1024;
 constexpr int      kOrderWarps    = kOrderThreads / 32;
-constexpr uint32_t kOrderBlocks   = 8u;                   // of the cluster
+constexpr uint32_t kOrderBlocks   = 16u;                  // of the cluster
 constexpr uint32_t kOrderMaxBins  = 1024u;
-constexpr uint32_t kOrderRounds   = 8u;                   // elements of a thread
+constexpr uint32_t kOrderRounds   = 4u;                   // elements of a thread of the cluster, at most
 constexpr uint32_t kOrderTile     = kOrderThreads * kOrderRounds;
 constexpr uint32_t kOrderMaxFew   = kOrderTile * kOrderBlocks;      // ids that the cluster takes
+constexpr uint32_t kOrderMaxPairs = 2048u;                // ... by comparing each with all others
+constexpr uint32_t kOrderTileRounds = 8u;                 // elements of a thread of a tile (many ids), at most
 constexpr uint32_t kOrderMaxRange = 1u << 20;
 
 struct OrderArgs {
@@ -32,7 +34,7 @@ struct OrderArgs {
     uint32_t* number;                                     // or nullptr
     uint32_t  passes, bits;                               // digits and their width
     uint32_t  pass;                                       // (many ids) this launch's
-    uint32_t  blocks;                                     // (many ids) tiles
+    uint32_t  blocks, tile;                               // (many ids) tiles, and ids of each
     uint32_t* keys[2];                                    // (many ids) between passes
     uint32_t* places[2];
     uint32_t* table;                                      // (many ids) bins x blocks: counts, then elements of that digit in earlier tiles
@@ -74,15 +76,22 @@ __device__ __forceinline__ uint32_t order_scan(uint32_t x, uint32_t* warp_sums, 
 
 // Each warp's elements of a tile lie next to each other.  Counts the warp's digits in `mine` (bins, zero before) and gives each element the
 // number of those of its digit before it in the warp.  `have` elements of this warp; digits beyond are of no account.
-template <class Key> __device__ __forceinline__ void order_rank(uint16_t* mine, uint32_t have, Key key_at, uint32_t (&digit)[kOrderRounds], uint32_t (&rank)[kOrderRounds]) {
+template <uint32_t ROUNDS, class Key>
+__device__ __forceinline__ void order_rank(uint16_t* mine, uint32_t have, uint32_t bits, Key key_at, uint32_t (&digit)[ROUNDS], uint32_t (&rank)[ROUNDS]) {
     const uint32_t lane = threadIdx.x & 31u;
 #pragma unroll
-    for (uint32_t j = 0; j < kOrderRounds; ++j) {
-        digit[j] = ~0u;
+    for (uint32_t j = 0; j < ROUNDS; ++j) digit[j] = 32u * j + lane < have ? key_at(j) : ~0u;
+#pragma unroll
+    for (uint32_t j = 0; j < ROUNDS; ++j) {
         if (32u * j >= have) continue;
-        const bool in = 32u * j + lane < have;
-        if (in) digit[j] = key_at(j);
-        const uint32_t same = __match_any_sync(kFullMask, digit[j]);
+        const bool in = digit[j] != ~0u;
+        uint32_t same = __ballot_sync(kFullMask, in);
+#pragma unroll
+        for (uint32_t b = 0; b < 10u; ++b) {
+            if (b >= bits) break;
+            const uint32_t set = __ballot_sync(kFullMask, digit[j] >> b & 1u);
+            same &= digit[j] >> b & 1u ? set : ~set;
+        }
         const uint32_t before = __popc(same & ((1u << lane) - 1u));
         uint32_t old = 0;
         if (in) old = mine[digit[j]];
@@ -114,8 +123,7 @@ __device__ __forceinline__ uint32_t address_in(const void* p, uint32_t block) {
     return r;
 }
 __device__ __forceinline__ uint32_t load_from(uint32_t at) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory"); return v; }
-__device__ __forceinline__ void store_to(uint32_t at, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-__device__ __forceinline__ void store_to(uint32_t at, uint16_t v) { asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
+__device__ __forceinline__ void store_to(uint32_t at, uint32_t v, uint32_t w) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(v), "r"(w) : "memory"); }
 
 struct OrderShared {
     uint32_t sums[kOrderMaxBins];                         // this block's, by digit
@@ -124,8 +132,7 @@ struct OrderShared {
     unsigned long long pair_sums[32];
     unsigned long long of_block;                          // occurrences and ids that occur in this block's part of the range
     uint32_t pad[2];
-    uint32_t keys[2][kOrderTile];
-    uint16_t places[2][kOrderTile];
+    uint2    entries[2][kOrderTile];                      // keys and places
     uint16_t counts[kOrderWarps * kOrderMaxBins];         // by warp and digit (as many digits as there are)
 };
 
@@ -185,9 +192,12 @@ __device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, Ord
     const unsigned long long before_mine = order_scan_pair(mine, s.pair_sums, &total);
     if (threadIdx.x == 0) s.of_block = total;
     cluster_meet();
+    uint32_t of[kOrderBlocks][2];
+#pragma unroll
+    for (uint32_t b = 0; b < kOrderBlocks; ++b) { of[b][0] = load_from(address_in(&s.of_block, b)); of[b][1] = load_from(address_in(&s.of_block, b) + 4u); }
+#pragma unroll
     for (uint32_t b = 0; b < kOrderBlocks; ++b) {
-        const uint32_t from = address_in(&s.of_block, b);
-        const unsigned long long x = load_from(from) | (unsigned long long)load_from(from + 4u) << 32;
+        const unsigned long long x = of[b][0] | (unsigned long long)of[b][1] << 32;
         if (b < block) at += x;
         all += x;
     }
@@ -231,40 +241,65 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
     const uint32_t begin = min(a.count, block << slice_log), end = min(a.count, begin + slice);
     const uint32_t first = begin + (warp << per_log);
     const uint32_t have = first < end ? min(end - first, 1u << per_log) : 0u;
+    const bool several = a.passes > 1u;                   // (one digit: its counts are the ids')
+    const bool pairs = several && a.count <= kOrderMaxPairs;
     wait_for_previous_kernels();
     allow_next_kernel();
-    const bool several = a.passes > 1u;                   // (one digit: its counts are the ids')
     if (several) {                                        // (the last entry counts nothing)
         const uint32_t vectors = (reinterpret_cast<uintptr_t>(a.starts) & 15u) == 0u ? (a.range + 1u) / 4u : 0u, thread = block * kOrderThreads + threadIdx.x;
         for (uint32_t i = thread; i < vectors; i += kOrderBlocks * kOrderThreads) reinterpret_cast<uint4*>(a.starts)[i] = make_uint4(0u, 0u, 0u, 0u);
         for (uint32_t v = 4u * vectors + thread; v <= a.range; v += kOrderBlocks * kOrderThreads) a.starts[v] = 0u;
     }
-    for (uint32_t i = threadIdx.x; i < end - begin; i += kOrderThreads) s.keys[0][i] = order_key(a, begin + i);
-    if (several) cluster_meet(); else __syncthreads();
-    if (several) for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
-        const uint32_t i = i0 + threadIdx.x;
-        const uint32_t key = i < end - begin ? s.keys[0][i] : a.range;
-        const uint32_t same = __match_any_sync(kFullMask, key);
-        if (key < a.range && lane == (uint32_t)__ffs((int)same) - 1u) atomicAdd(a.starts + key, (uint32_t)__popc(same));
+    if (pairs) {                                          // eight threads an element, each an eighth of the others
+        uint32_t* keys = reinterpret_cast<uint32_t*>(s.entries);
+        for (uint32_t i = threadIdx.x; i < a.count; i += kOrderThreads) keys[i] = order_key(a, i);
+        cluster_meet();
+        const uint32_t i = block * (kOrderThreads / 8u) + threadIdx.x / 8u, part = threadIdx.x & 7u;
+        const uint32_t key = i < a.count ? keys[i] : ~0u;
+        uint32_t before = 0;
+        for (uint32_t j = part; j < a.count; j += 8u) before += keys[j] < key || (keys[j] == key && j < i);
+#pragma unroll
+        for (uint32_t d = 1; d < 8u; d *= 2u) before += __shfl_xor_sync(kFullMask, before, d);
+        if (part == 0u && key < a.range) {
+            a.order[before] = i;
+            atomicAdd(a.starts + key, 1u);
+        }
+        cluster_meet();
+        order_starts_from_counts(a, s, block);
+        cluster_meet();
+        return;
     }
+    for (uint32_t i = threadIdx.x; i < end - begin; i += kOrderThreads) s.entries[0][i] = make_uint2(order_key(a, begin + i), begin + i);
+    for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
+    if (several) {
+        cluster_meet();
+        for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
+            const uint32_t i = i0 + threadIdx.x;
+            const uint32_t key = i < end - begin ? s.entries[0][i].x : a.range;
+            const uint32_t same = __match_any_sync(kFullMask, key);
+            if (key < a.range && lane == (uint32_t)__ffs((int)same) - 1u) atomicAdd(a.starts + key, (uint32_t)__popc(same));
+        }
+    } else __syncthreads();
     uint32_t from = 0;
     for (uint32_t pass = 0; pass < a.passes; ++pass) {
-        for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
-        __syncthreads();
         uint16_t* mine = s.counts + warp * bins;
         uint32_t digit[kOrderRounds], rank[kOrderRounds];
         const uint32_t local = warp << per_log;
-        order_rank(mine, have, [&](uint32_t j) { return digit_of(a, s.keys[from][local + 32u * j + lane], pass); }, digit, rank);
+        order_rank<kOrderRounds>(mine, have, a.bits, [&](uint32_t j) { return digit_of(a, s.entries[from][local + 32u * j + lane].x, pass); }, digit, rank);
         __syncthreads();
         order_over_warps(s.counts, bins, s.sums);
         cluster_meet();
         uint32_t all = 0, before = 0, total = 0;
-        if (threadIdx.x < bins)
+        if (threadIdx.x < bins) {
+            uint32_t n[kOrderBlocks];
+#pragma unroll
+            for (uint32_t b = 0; b < kOrderBlocks; ++b) n[b] = load_from(address_in(s.sums + threadIdx.x, b));
+#pragma unroll
             for (uint32_t b = 0; b < kOrderBlocks; ++b) {
-                const uint32_t n = load_from(address_in(s.sums + threadIdx.x, b));
-                all += n;
-                if (b < block) before += n;
+                all += n[b];
+                if (b < block) before += n[b];
             }
+        }
         const uint32_t lower = order_scan(all, s.warp_sums, &total);
         if (threadIdx.x < bins) s.base[threadIdx.x] = lower + before;
         __syncthreads();
@@ -279,19 +314,17 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
 #pragma unroll
         for (uint32_t j = 0; j < kOrderRounds; ++j) {
             if (digit[j] == ~0u) continue;
-            const uint32_t i = local + 32u * j + lane;
-            const uint32_t key = s.keys[from][i];
-            const uint32_t place = pass ? s.places[from][i] : begin + i;
+            const uint2 x = s.entries[from][local + 32u * j + lane];
             const uint32_t to = s.base[digit[j]] + mine[digit[j]] + rank[j];
             if (last) {
-                if (key < a.range) a.order[to] = place;
-            } else {
-                const uint32_t there = to >> slice_log, at = to & (slice - 1u);
-                store_to(address_in(&s.keys[from ^ 1u][at], there), key);
-                store_to(address_in(&s.places[from ^ 1u][at], there), (uint16_t)place);
-            }
+                if (x.x < a.range) a.order[to] = x.y;
+            } else store_to(address_in(&s.entries[from ^ 1u][to & (slice - 1u)], to >> slice_log), x.x, x.y);
         }
         from ^= 1u;
+        if (!last) {
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
+        }
         cluster_meet();                                   // (also: the sums have been read before they are formed anew, or their block ends)
     }
     if (!several) return;
@@ -312,15 +345,15 @@ template <int PLACE> __global__ void __launch_bounds__(kOrderThreads, 1) k_order
     extern __shared__ __align__(16) unsigned char raw[];
     OrderTileShared& s = *reinterpret_cast<OrderTileShared*>(raw);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, bins = 1u << a.bits;
-    const uint32_t first = blockIdx.x * kOrderTile + warp * 32u * kOrderRounds;
-    const uint32_t have = first < a.count ? min(a.count - first, 32u * kOrderRounds) : 0u;
+    const uint32_t each = a.tile / kOrderWarps, first = blockIdx.x * a.tile + warp * each;
+    const uint32_t have = first < a.count ? min(a.count - first, each) : 0u;
     for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
     wait_for_previous_kernels();
     allow_next_kernel();
     __syncthreads();
     uint16_t* mine = s.counts + warp * bins;
-    uint32_t digit[kOrderRounds], rank[kOrderRounds], key[kOrderRounds];
-    order_rank(mine, have, [&](uint32_t j) { key[j] = many_key(a, first + 32u * j + lane); return digit_of(a, key[j], a.pass); }, digit, rank);
+    uint32_t digit[kOrderTileRounds], rank[kOrderTileRounds], key[kOrderTileRounds];
+    order_rank<kOrderTileRounds>(mine, have, a.bits, [&](uint32_t j) { key[j] = many_key(a, first + 32u * j + lane); return digit_of(a, key[j], a.pass); }, digit, rank);
     __syncthreads();
     order_over_warps(s.counts, bins, s.sums);
     if constexpr (PLACE == 0) {
@@ -334,7 +367,7 @@ template <int PLACE> __global__ void __launch_bounds__(kOrderThreads, 1) k_order
     const bool last = a.pass + 1u == a.passes;
     const uint32_t to_buffer = (a.pass + 1u) & 1u;
 #pragma unroll
-    for (uint32_t j = 0; j < kOrderRounds; ++j) {
+    for (uint32_t j = 0; j < kOrderTileRounds; ++j) {
         if (digit[j] == ~0u) continue;
         const uint32_t i = first + 32u * j + lane;
         const uint32_t place = a.pass ? a.places[a.pass & 1u][i] : i;
@@ -395,6 +428,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order_distinct(const __gri
     if (threadIdx.x == 0) of_block = total;
     cluster_meet();
     uint32_t at = 0, all = 0;
+#pragma unroll
     for (uint32_t b = 0; b < kOrderBlocks; ++b) {
         const uint32_t n = load_from(address_in(&of_block, b));
         if (b < block) at += n;

@@ -25,9 +25,21 @@ uint64_t up_to(uint64_t x, uint64_t unit) { return (x + unit - 1) / unit * unit;
 
 // ---- ids in order ---------------------------------------------------------------------------------
 
-uint64_t order_blocks(uint64_t count) { return (count + kOrderTile - 1) / kOrderTile; }
+// tiles of 1024 ids where the GPU holds them all at once, of eight times as many at most
+uint64_t order_tile(uint64_t count) {
+    uint64_t rounds = 1;
+    while (rounds < kOrderTileRounds && count > 128u * kOrderThreads * rounds) ++rounds;
+    return kOrderThreads * rounds;
+}
+uint64_t order_blocks(uint64_t count) { return (count + order_tile(count) - 1) / order_tile(count); }
 uint64_t order_bytes(uint64_t count) {                     // behind the workspace's fixed part
     return count <= kOrderMaxFew ? 0 : 4u * up_to(4u * count, 256) + up_to(4ull * kOrderMaxBins * order_blocks(count), 256) + 4u * kOrderMaxBins;
+}
+
+int allow_wide_clusters(const void* fn) {                  // (of more than eight blocks)
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) return FASTSGD_OK;
+    cudaGetLastError();
+    return FASTSGD_E_CUDA;
 }
 
 // ---- an embedding's gradient -------------------------------------------------------------------------
@@ -233,10 +245,12 @@ int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32
     uint64_t resident = 0;
     if (count <= kOrderMaxFew) {
         rc = resident_blocks((const void*)k_order, kOrderThreads, sizeof(OrderShared), dev, &resident);
+        if (!rc) rc = allow_wide_clusters((const void*)k_order);
         return rc ? rc : launched(launch_overlapped((const void*)k_order, kOrderBlocks, kOrderThreads, sizeof(OrderShared), kargs, st, kOrderBlocks));
     }
     if (!dev.ws || dev.ws_bytes < kPartialsOffset + order_bytes(count)) return FASTSGD_E_NO_WORKSPACE;
     a.blocks = (uint32_t)order_blocks(count);
+    a.tile = (uint32_t)order_tile(count);
     unsigned char* at = static_cast<unsigned char*>(dev.ws) + kPartialsOffset;
     for (uint32_t** p : {&a.keys[0], &a.keys[1], &a.places[0], &a.places[1]}) { *p = reinterpret_cast<uint32_t*>(at); at += up_to(4u * count, 256); }
     a.table = reinterpret_cast<uint32_t*>(at);
@@ -253,6 +267,7 @@ int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32
         if (rc) return rc;
     }
     rc = launched(launch_overlapped((const void*)k_order_starts, a.range / 256u + 1u, 256, 0, kargs, st));
+    if (!rc && (distinct || number)) rc = allow_wide_clusters((const void*)k_order_distinct);
     if (rc || (!distinct && !number)) return rc;
     return launched(launch_overlapped((const void*)k_order_distinct, kOrderBlocks, kOrderThreads, 0, kargs, st, kOrderBlocks));
 }
