@@ -199,8 +199,9 @@ struct GradientArgs {
     uint32_t  most;                                       // rows that keys and values hold
     uint64_t  part_stride;                                // cols, up to a multiple of 4
     float*    parts;                                      // 2 tiles x part_stride: of a tile's first token (begun earlier), of its last (that goes on)
-    uint32_t  sum_blocks;                                 // blocks that add up; the others clear rows of tokens that do not occur,
-    uint32_t  clear_rows;                                 // so many each
+    uint4*    follow;                                     // of each tile: in how many of the next its last token goes on, if that begins in it; the token; its row (pairs)
+    uint32_t  sum_blocks, clear_blocks;                   // blocks that add up, and that clear rows of tokens that do not occur (in turn, as long as there are both)
+    uint32_t  clear_rows;                                 // of a block that clears
 };
 
 // Where in distinct (ascending, n of them) v is: the first that is not below it.  One warp: 32 probes a step.
@@ -248,9 +249,9 @@ __device__ __forceinline__ void write_part(const GradientArgs& a, uint64_t part,
 }
 
 // Rows of tokens that do not occur become zero: a block's are listed, and gone through vector by vector.
-template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const GradientArgs& a) {
+template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const GradientArgs& a, uint32_t block) {
     __shared__ uint32_t listed[64], some;
-    const uint32_t v0 = (blockIdx.x - a.sum_blocks) * a.clear_rows;
+    const uint32_t v0 = block * a.clear_rows;
     if (threadIdx.x == 0) some = 0;
     __syncthreads();
     if (threadIdx.x < a.clear_rows && v0 + threadIdx.x < a.vocab && a.starts[v0 + threadIdx.x] == a.starts[v0 + threadIdx.x + 1u]) listed[atomicAdd(&some, 1u)] = v0 + threadIdx.x;
@@ -267,13 +268,19 @@ template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const 
     }
 }
 
-template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads) k_embedding_sum(const __grid_constant__ GradientArgs a) {
-    constexpr int AHEAD = sizeof(T) == 2 && WIDE ? 8 : 4;         // rows in flight
+template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads, 2) k_embedding_sum(const __grid_constant__ GradientArgs a) {
+    constexpr int AHEAD = sizeof(T) == 2 || WIDE ? 8 : 4;         // rows in flight
     wait_for_previous_kernels();
     allow_next_kernel();
-    if (!PAIRS && blockIdx.x >= a.sum_blocks) { clear_rows<TO, WIDE>(a); return; }
+    uint32_t block = blockIdx.x;
+    if constexpr (!PAIRS) {                               // (blocks that wait for rows beside blocks that write)
+        const uint32_t both = min(a.sum_blocks, a.clear_blocks);
+        const bool clears = block < 2u * both ? block & 1u : a.clear_blocks > both;
+        block = block < 2u * both ? block / 2u : block - both;
+        if (clears) { clear_rows<TO, WIDE>(a, block); return; }
+    }
     const Group g = row_group(a.lanes_log);
-    const uint32_t u = blockIdx.x * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
+    const uint32_t u = block * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
     const uint32_t tile = u / a.chunks, c = ((u - tile * a.chunks) * g.lanes + g.lane) * 8u;
     if (tile >= a.tiles) return;
     const uint32_t begin = tile << a.tile_log;
@@ -289,7 +296,11 @@ template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bou
     look_up(begin, at, id);
     const uint32_t before = begin ? id_at(begin - 1u) : ~0u;
     const uint32_t have = min(a.starts[a.vocab], a.count), end = min(begin + (1u << a.tile_log), have);
-    if (begin >= end) return;
+    const bool first_chunk = u == tile * a.chunks && g.lane == 0u;
+    if (begin >= end) {
+        if (first_chunk) a.follow[tile] = make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
     uint32_t now = id[0];                                 // the token whose rows are being added up; pairs: its row
     bool earlier = begin && before == now;                // it began in an earlier tile
     const bool goes_on = end < have && id_at(end) == id_at(end - 1u);
@@ -323,62 +334,68 @@ template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bou
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
     }
-    if (goes_on && !earlier) write_part(a, 2ull * tile + 1ull, sum, c, g);
+    const bool starts_here = goes_on && !earlier;
+    if (first_chunk) a.follow[tile] = make_uint4(starts_here && now < a.vocab ? ((min(a.starts[now + 1u], have) - 1u) >> a.tile_log) - tile : 0u, now, row, 0u);
+    if (starts_here) write_part(a, 2ull * tile + 1ull, sum, c, g);
     else finish();
 }
 
-// Tokens that begin in a tile and go on: a block for each and each chunk of columns (most find nothing to do); its warps each add up an equal
-// share of the parts that follow, in their order, and the shares are added in the warps' order.
+// Tokens that begin in a tile and go on.  A block looks at eight tiles, for a chunk of columns: each of its warps adds up what follows one of
+// them, in the order of the tiles; where that is long all warps add up equal shares, which are added in the warps' order.
+constexpr uint32_t kJoinTiles = 8u, kJoinLong = 32u;
 template <class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads) k_embedding_join(const __grid_constant__ GradientArgs a) {
     constexpr uint32_t WARPS = kEmbedThreads / 32;
+    static_assert(WARPS == kJoinTiles, "a tile a warp");
     __shared__ float shares[WARPS][32][9];
     wait_for_previous_kernels();
     allow_next_kernel();
     const Group g = row_group(a.lanes_log);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t have = min(a.starts[a.vocab], a.count);
-    const uint32_t tile = blockIdx.x / a.chunks, c = ((blockIdx.x - tile * a.chunks) * g.lanes + lane) * 8u;
-    const uint32_t begin = tile << a.tile_log, end = begin + (1u << a.tile_log);
-    if (end >= have) return;                              // (the last tile, or behind it)
-    const uint32_t first = a.order[end - 1u], next = a.order[end];
-    if (first >= a.count || next >= a.count) return;
-    const uint32_t v = (uint32_t)a.ids[first];
-    if (v >= a.vocab || (uint32_t)a.ids[next] != v || a.starts[v] < begin) return;       // nothing goes on, or it began earlier
-    const uint32_t last = (min(a.starts[v + 1u], have) - 1u) >> a.tile_log;              // the tile in which it ends
-    const uint32_t parts = last - tile, each = (parts + WARPS - 1u) / WARPS;
-    const uint32_t from = tile + 1u + min(warp * each, parts), to = tile + 1u + min(warp * each + each, parts);
-    float sum[8] = {};
-    auto add = [&](const Piece<float, true>& p) {
-        float f[8];
-        unpack_piece(p, a.parts, f);
+    const uint32_t tiles = blockIdx.x / a.chunks * kJoinTiles, c = ((blockIdx.x % a.chunks) * g.lanes + lane) * 8u;
+    const uint4 follow = lane < kJoinTiles && tiles + lane < a.tiles ? a.follow[tiles + lane] : make_uint4(0u, 0u, 0u, 0u);
+    float sum[8];
+    // parts of tiles from .. to, behind the first tile's own (where `own`)
+    auto add_up = [&](uint32_t tile, bool own, uint32_t from, uint32_t to) {
+        auto add = [&](const Piece<float, true>& p) {
+            float f[8];
+            unpack_piece(p, a.parts, f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += f[i];
-    };
-    if (lane < g.lanes) {
-        if (warp == 0u) {
-            Piece<float, true> p;
-            load_piece(p, a.parts + (2ull * tile + 1ull) * a.part_stride, c, a.cols);
-            add(p);
-        }
-        for (uint32_t t = from; t < to; t += 4u) {
+            for (int j = 0; j < 8; ++j) sum[j] += f[j];
+        };
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+        if (lane >= g.lanes) return;
+        Piece<float, true> first;
+        if (own) load_piece(first, a.parts + (2ull * tile + 1ull) * a.part_stride, c, a.cols);
+        for (uint32_t t = from; t < to || own; t += 4u) {
             Piece<float, true> p[4];
 #pragma unroll
             for (uint32_t j = 0; j < 4u; ++j) if (t + j < to) load_piece(p[j], a.parts + 2ull * (t + j) * a.part_stride, c, a.cols);
+            if (own) { add(first); own = false; }
 #pragma unroll
             for (uint32_t j = 0; j < 4u; ++j) if (t + j < to) add(p[j]);
         }
+    };
+    const uint32_t mine = __shfl_sync(kFullMask, follow.x, warp), v = __shfl_sync(kFullMask, follow.y, warp), row = __shfl_sync(kFullMask, follow.z, warp);
+    if (mine && mine < kJoinLong) {
+        add_up(tiles + warp, true, tiles + warp + 1u, tiles + warp + 1u + mine);
+        if (lane < g.lanes) write_sum<TO, WIDE, PAIRS>(a, v, row, sum, c, g);
     }
+    for (uint32_t some = __ballot_sync(kFullMask, follow.x >= kJoinLong); some; some &= some - 1u) {
+        const uint32_t i = (uint32_t)__ffs((int)some) - 1u, tile = tiles + i, parts = __shfl_sync(kFullMask, follow.x, i), each = (parts + WARPS - 1u) / WARPS;
+        add_up(tile, warp == 0u, tile + 1u + min(warp * each, parts), tile + 1u + min(warp * each + each, parts));
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) shares[warp][lane][i] = sum[i];
-    __syncthreads();
-    if (warp) return;
-    for (uint32_t w = 1; w < WARPS; ++w) {
+        for (int j = 0; j < 8; ++j) shares[warp][lane][j] = sum[j];
+        __syncthreads();
+        const uint32_t v_of = __shfl_sync(kFullMask, follow.y, i), row_of = __shfl_sync(kFullMask, follow.z, i);
+        if (warp) continue;
+        for (uint32_t w = 1; w < WARPS; ++w) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += shares[w][lane][i];
+            for (int j = 0; j < 8; ++j) sum[j] += shares[w][lane][j];
+        }
+        if (lane < g.lanes) write_sum<TO, WIDE, PAIRS>(a, v_of, row_of, sum, c, g);
     }
-    uint32_t row = 0;
-    if constexpr (PAIRS) row = place_among_by_warp(a.distinct, min(*a.number, a.most), v);
-    if (lane < g.lanes) write_sum<TO, WIDE, PAIRS>(a, v, row, sum, c, g);
 }
 
 }  // namespace fsg

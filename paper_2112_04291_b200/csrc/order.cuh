@@ -192,15 +192,19 @@ __device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, Ord
     const unsigned long long before_mine = order_scan_pair(mine, s.pair_sums, &total);
     if (threadIdx.x == 0) s.of_block = total;
     cluster_meet();
-    uint32_t of[kOrderBlocks][2];
+    if (threadIdx.x < 32u) {                              // (a lane a block)
+        const uint32_t lane = threadIdx.x, from = address_in(&s.of_block, lane % kOrderBlocks);
+        unsigned long long x = load_from(from) | (unsigned long long)load_from(from + 4u) << 32;
+        if (lane >= kOrderBlocks) x = 0;
+        unsigned long long y = lane < block ? x : 0;
 #pragma unroll
-    for (uint32_t b = 0; b < kOrderBlocks; ++b) { of[b][0] = load_from(address_in(&s.of_block, b)); of[b][1] = load_from(address_in(&s.of_block, b) + 4u); }
-#pragma unroll
-    for (uint32_t b = 0; b < kOrderBlocks; ++b) {
-        const unsigned long long x = of[b][0] | (unsigned long long)of[b][1] << 32;
-        if (b < block) at += x;
-        all += x;
+        for (uint32_t d = 16; d; d /= 2u) { x += __shfl_xor_sync(kFullMask, x, d); y += __shfl_xor_sync(kFullMask, y, d); }
+        if (lane == 0u) { s.pair_sums[0] = y; s.pair_sums[1] = x; }
     }
+    __syncthreads();
+    at = s.pair_sums[0];
+    all = s.pair_sums[1];
+    if (!once) __syncthreads();
     for (uint32_t v0 = lo; v0 < hi; v0 += ROUND) {
         const uint32_t v = v0 + threadIdx.x * kOrderEach;
         unsigned long long here = at + before_mine;

@@ -58,7 +58,7 @@ GradientShape gradient_shape(uint64_t count, uint64_t cols) {
     g.part_stride = up_to(cols, 4);
     return g;
 }
-uint64_t part_bytes(const GradientShape& g) { return 8ull * g.tiles * g.part_stride; }
+uint64_t part_bytes(const GradientShape& g) { return up_to(8ull * g.tiles * g.part_stride, 256) + 16ull * g.tiles; }
 
 template <class T, bool WIDE, bool PAIRS> const void* sum_kernel_of(uint32_t to) {
     if constexpr (PAIRS) return (const void*)k_embedding_sum<T, float, WIDE, true>;
@@ -105,13 +105,15 @@ template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& 
     if (part_bytes(g) && (!dev.ws || dev.ws_bytes < kPartialsOffset + part_bytes(g))) return FASTSGD_E_NO_WORKSPACE;
     a.lanes_log = g.lanes_log; a.chunks = g.chunks; a.tile_log = g.tile_log; a.tiles = g.tiles; a.part_stride = g.part_stride;
     a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset);
+    a.follow = reinterpret_cast<uint4*>(static_cast<unsigned char*>(dev.ws) + kPartialsOffset + up_to(8ull * g.tiles * g.part_stride, 256));
     const uint64_t groups = (uint64_t)kEmbedThreads >> g.lanes_log;
     a.sum_blocks = (uint32_t)(((uint64_t)g.tiles * g.chunks + groups - 1) / groups);
     uint64_t blocks = a.sum_blocks;
-    if (!PAIRS) {                                          // (eight rounds of blocks that clear, of 64 rows at most)
+    if (!PAIRS) {                                          // (eight blocks an SM that clear, of 64 rows at most)
         a.clear_rows = 1u;
-        while (a.clear_rows < 64u && a.vocab > a.clear_rows * 64ull * (uint64_t)dev.sm_count) a.clear_rows *= 2u;
-        blocks += (a.vocab + a.clear_rows - 1u) / a.clear_rows;
+        while (a.clear_rows < 64u && a.vocab > a.clear_rows * 8ull * (uint64_t)dev.sm_count) a.clear_rows *= 2u;
+        a.clear_blocks = (a.vocab + a.clear_rows - 1u) / a.clear_rows;
+        blocks += a.clear_blocks;
     }
     if (blocks >= 1ull << 31 || (uint64_t)g.tiles * g.chunks >= 1ull << 31) return FASTSGD_E_BAD_N;
     void* kargs[] = {&a};
@@ -120,7 +122,7 @@ template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& 
         if (rc) return rc;
     }
     if (g.tiles < 2u) return FASTSGD_OK;
-    return launched(launch_overlapped(wide ? join_kernel<true, PAIRS>(to) : join_kernel<false, PAIRS>(to), g.tiles * g.chunks, kEmbedThreads, 0, kargs, st));
+    return launched(launch_overlapped(wide ? join_kernel<true, PAIRS>(to) : join_kernel<false, PAIRS>(to), (g.tiles + kJoinTiles - 1u) / kJoinTiles * g.chunks, kEmbedThreads, 0, kargs, st));
 }
 
 // ---- experts' products ----------------------------------------------------------------------------
