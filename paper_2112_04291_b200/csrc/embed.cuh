@@ -35,16 +35,19 @@ template <int N> __device__ __forceinline__ void shift_words(const uint32_t (&w)
 // Eight columns from `c` on, as loaded.  Vectors of which no byte is the row's are not touched; what lies in others behind the row's end
 // comes along and is never written.
 template <class T, bool WIDE> struct Piece { uint4 v[8 / Vec<T>::N + (WIDE ? 0 : 1)]; };
-template <class T, bool WIDE> __device__ __forceinline__ void load_piece(Piece<T, WIDE>& p, const T* row, uint32_t c, uint32_t cols) {
+// (AGAIN: rows that others will read, too, are kept in the L1)
+template <bool AGAIN = false, class T, bool WIDE> __device__ __forceinline__ void load_piece(Piece<T, WIDE>& p, const T* row, uint32_t c, uint32_t cols) {
     constexpr int N = 8 / Vec<T>::N;
     if constexpr (WIDE) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) if (c + (uint32_t)(i * Vec<T>::N) < cols) p.v[i] = load16(row + c + i * Vec<T>::N);
+        for (int i = 0; i < N; ++i)
+            if (c + (uint32_t)(i * Vec<T>::N) < cols) p.v[i] = AGAIN ? *reinterpret_cast<const uint4*>(row + c + i * Vec<T>::N) : load16(row + c + i * Vec<T>::N);
     } else {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), end = reinterpret_cast<uintptr_t>(row + cols), first = at & ~(uintptr_t)15;
-        const int vectors = at != first ? N + 1 : N;
+        const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;      // (of every lane's columns alike)
+        const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(row + c) - off);
+        const uint32_t bytes = c < cols ? (cols - c) * (uint32_t)sizeof(T) + off : 0u;      // from there to the row's end
 #pragma unroll
-        for (int i = 0; i <= N; ++i) if (c < cols && i < vectors && first + 16u * i < end) p.v[i] = *reinterpret_cast<const uint4*>(first + 16u * i);
+        for (int i = 0; i <= N; ++i) if (16u * (uint32_t)i < bytes && (i < N || off)) p.v[i] = from[i];
     }
 }
 template <class T, bool WIDE> __device__ __forceinline__ void unpack_piece(const Piece<T, WIDE>& p, const T* row, float (&f)[8]) {
@@ -156,7 +159,7 @@ template <class T, class TO, bool WIDE, bool SHORT> __global__ void __launch_bou
         if (a.per_row != 1u) id[j] /= a.per_row;
     }
 #pragma unroll
-    for (uint32_t j = 0; j < kLookupAhead; ++j) if (id[j] < a.vocab) load_piece(p[j], static_cast<const T*>(a.table) + id[j] * a.table_stride, c0 + step * j, a.cols);
+    for (uint32_t j = 0; j < kLookupAhead; ++j) if (id[j] < a.vocab) load_piece<true>(p[j], static_cast<const T*>(a.table) + id[j] * a.table_stride, c0 + step * j, a.cols);
 #pragma unroll
     for (uint32_t j = 0; j < kLookupAhead; ++j) {
         const uint32_t row = SHORT ? row0 + j : row0;
@@ -268,8 +271,11 @@ template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const 
     }
 }
 
-template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads, 2) k_embedding_sum(const __grid_constant__ GradientArgs a) {
-    constexpr int AHEAD = sizeof(T) == 2 || WIDE ? 8 : 4;         // rows in flight
+// FULL: a warp a group.  Its lanes look up the rows and tokens of sixteen positions at once and tell one another; otherwise each lane looks
+// up all of them.
+template <class T, class TO, bool WIDE, bool PAIRS, bool FULL> __global__ void __launch_bounds__(kEmbedThreads, FULL && WIDE && sizeof(T) == 2 ? 3 : 2) k_embedding_sum(const __grid_constant__ GradientArgs a) {
+    constexpr uint32_t AHEAD = sizeof(T) == 2 || WIDE ? 8u : 4u;        // rows in flight
+    constexpr uint32_t WINDOW = FULL ? 16u : AHEAD;                     // positions looked up at a time
     wait_for_previous_kernels();
     allow_next_kernel();
     uint32_t block = blockIdx.x;
@@ -279,20 +285,23 @@ template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bou
         block = block < 2u * both ? block / 2u : block - both;
         if (clears) { clear_rows<TO, WIDE>(a, block); return; }
     }
-    const Group g = row_group(a.lanes_log);
-    const uint32_t u = block * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
+    const Group g = row_group(FULL ? 5u : a.lanes_log);
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t u = FULL ? block * (kEmbedThreads / 32u) + __shfl_sync(kFullMask, threadIdx.x >> 5, 0) : block * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
     const uint32_t tile = u / a.chunks, c = ((u - tile * a.chunks) * g.lanes + g.lane) * 8u;
     if (tile >= a.tiles) return;
     const uint32_t begin = tile << a.tile_log;
-    // the rows and tokens of AHEAD positions (those behind the last are garbage, and of no account)
-    auto look_up = [&](uint32_t p, uint32_t (&at)[AHEAD], uint32_t (&id)[AHEAD]) {
+    // rows and tokens (those behind the last are garbage, and of no account)
+    constexpr uint32_t EACH = FULL ? 1u : AHEAD;
+    auto look_up = [&](uint32_t p, uint32_t (&at)[EACH], uint32_t (&id)[EACH]) {
+        if constexpr (FULL) p += lane & (WINDOW - 1u);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) at[j] = p + (uint32_t)j < a.count ? a.order[p + (uint32_t)j] : ~0u;
+        for (uint32_t j = 0; j < EACH; ++j) at[j] = p + j < a.count ? a.order[p + j] : ~0u;
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) id[j] = at[j] < a.count ? (uint32_t)a.ids[at[j]] : ~0u;
+        for (uint32_t j = 0; j < EACH; ++j) id[j] = at[j] < a.count ? (uint32_t)a.ids[at[j]] : ~0u;
     };
     auto id_at = [&](uint32_t p) { const uint32_t at = a.order[p]; return at < a.count ? (uint32_t)a.ids[at] : ~0u; };
-    uint32_t at[AHEAD], id[AHEAD], row = 0;
+    uint32_t at[EACH], id[EACH], row = 0;
     look_up(begin, at, id);
     const uint32_t before = begin ? id_at(begin - 1u) : ~0u;
     const uint32_t have = min(a.starts[a.vocab], a.count), end = min(begin + (1u << a.tile_log), have);
@@ -301,38 +310,48 @@ template <class T, class TO, bool WIDE, bool PAIRS> __global__ void __launch_bou
         if (first_chunk) a.follow[tile] = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    uint32_t now = id[0];                                 // the token whose rows are being added up; pairs: its row
+    uint32_t now = FULL ? __shfl_sync(kFullMask, id[0], 0) : id[0];      // the token whose rows are being added up; pairs: its row
     bool earlier = begin && before == now;                // it began in an earlier tile
     const bool goes_on = end < have && id_at(end) == id_at(end - 1u);
-    if constexpr (PAIRS) row = g.lanes == 32u ? place_among_by_warp(a.distinct, min(*a.number, a.most), now) : place_among(a.distinct, min(*a.number, a.most), now);
+    if constexpr (PAIRS) row = FULL ? place_among_by_warp(a.distinct, min(*a.number, a.most), now) : place_among(a.distinct, min(*a.number, a.most), now);
     float sum[8] = {};
     auto finish = [&]() {
         if (earlier) write_part(a, 2ull * tile, sum, c, g);
         else if (now < a.vocab) write_sum<TO, WIDE, PAIRS>(a, now, row, sum, c, g);
     };
-    for (uint32_t p = begin; p < end; p += AHEAD) {
-        uint32_t next_at[AHEAD], next_id[AHEAD];
-        Piece<T, WIDE> piece[AHEAD];
+    for (uint32_t p0 = begin; p0 < end; p0 += WINDOW) {
+        uint32_t next_at[EACH], next_id[EACH];
+        if (p0 + WINDOW < end) look_up(p0 + WINDOW, next_at, next_id);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) if (p + (uint32_t)j < end && at[j] < a.count) load_piece(piece[j], static_cast<const T*>(a.grad) + at[j] * a.grad_stride, c, a.cols);
-        if (p + AHEAD < end) look_up(p + AHEAD, next_at, next_id);
+        for (uint32_t w = 0; w < WINDOW; w += AHEAD) {
+            const uint32_t p = p0 + w;
+            if (p >= end) continue;
+            Piece<T, WIDE> piece[AHEAD];
+            uint32_t from[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            if (p + (uint32_t)j >= end) continue;
-            if (id[j] != now) {
-                finish();
-                now = id[j]; earlier = false; ++row;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+            for (uint32_t j = 0; j < AHEAD; ++j) {
+                from[j] = FULL ? __shfl_sync(kFullMask, at[0], w + j) : at[FULL ? 0u : j];
+                if (p + j < end && from[j] < a.count) load_piece(piece[j], static_cast<const T*>(a.grad) + from[j] * a.grad_stride, c, a.cols);
             }
-            if (at[j] >= a.count) continue;
-            float f[8];
-            unpack_piece(piece[j], static_cast<const T*>(a.grad) + at[j] * a.grad_stride, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += f[i];
+            for (uint32_t j = 0; j < AHEAD; ++j) {
+                if (p + j >= end) continue;
+                const uint32_t of = FULL ? __shfl_sync(kFullMask, id[0], w + j) : id[FULL ? 0u : j];
+                if (of != now) {
+                    finish();
+                    now = of; earlier = false; ++row;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+                }
+                if (from[j] >= a.count) continue;
+                float f[8];
+                unpack_piece(piece[j], static_cast<const T*>(a.grad) + from[j] * a.grad_stride, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += f[i];
+            }
         }
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
+        for (uint32_t j = 0; j < EACH; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
     }
     const bool starts_here = goes_on && !earlier;
     if (first_chunk) a.follow[tile] = make_uint4(starts_here && now < a.vocab ? ((min(a.starts[now + 1u], have) - 1u) >> a.tile_log) - tile : 0u, now, row, 0u);
