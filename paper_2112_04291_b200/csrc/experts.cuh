@@ -29,7 +29,7 @@ constexpr uint32_t kProductM          = 256u;             // of a tile; half of 
 constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
-constexpr uint32_t kProductSum        = 4u;               // stages between two additions in registers (results of 32 bits)
+constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers (results of 32 bits)
 constexpr uint32_t kProductTurned     = 2048u;            // bytes of a warp that writes gradients of weights
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
