@@ -30,11 +30,11 @@ constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers (results of 32 bits)
-constexpr uint32_t kProductTurned     = 2048u;            // bytes of a warp that writes gradients of weights
+constexpr uint32_t kProductTurned     = 2048u, kProductTurns = 3u;      // bytes of a box of a gradient of weights, and boxes of a warp on their way
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
 struct alignas(64) ProductArgs {
-    CUtensorMap a_map, b_map;
+    CUtensorMap a_map, b_map, out_map;                    // (the last: weights)
     const uint32_t* starts;
     uint32_t  experts, rows;                              // rows: of the sorted side
     uint32_t  m, n, k;                                    // m: A's rows; n: B's (weights only); k: the contraction (forward, input)
@@ -187,36 +187,38 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
         uint32_t turn = 0;
         bool fine = true;
         const uint32_t part = warp & 3u, side = (warp - 4u) >> 2;         // lanes; every other 32 columns
-        unsigned char* turned = raw + (stage0 - smem_u32(raw)) + a.stages * stage_bytes + (warp - 4u) * kProductTurned;      // (weights)
+        const uint32_t turned = stage0 + a.stages * stage_bytes + (warp - 4u) * kProductTurns * kProductTurned;      // (weights)
+        uint32_t at_turn = 0;
         for (uint32_t t = first; t < tiles; t += step_tiles) {
             const ProductTile p = product_tile<MODE>(a, s, t);
             const uint32_t row0 = p.m0 + block * kProductM / 2u + 32u * part;
             const uint32_t from = tmem + (32u * part << 16);
             auto write = [&](const float (&f)[32], uint32_t c0) {
                 if constexpr (MODE == kWeights) {
-                    // A lane holds 32 columns of a row of its own.  Through shared memory, 64 bytes of a row at a time (in an order of its four
-                    // vectors that keeps rows off one another's banks), four lanes write whole sectors of one row.
+                    // A lane holds 32 columns of a row of its own: 64 bytes of each of 32 rows at a time go through shared memory (in
+                    // the order of vectors that a copy of 64-byte rows has, which keeps rows off one another's banks) and from there by a copy.
                     constexpr uint32_t V = Vec<TO>::N, COLS = 4u * V;
-                    __syncwarp();
 #pragma unroll
                     for (uint32_t h = 0; h < 32u; h += COLS) {
+                        if (c0 + h >= p.n || row0 >= a.m) continue;
+                        if (elect_one()) wait_stores_read<(int)kProductTurns - 1>();      // (the copy that had this place has read it)
+                        __syncwarp();
+                        const uint32_t place = turned + at_turn * kProductTurned;
 #pragma unroll
                         for (uint32_t v = 0; v < 4u; ++v) {
                             const uint32_t i = h + v * V;
                             uint4 x;
                             if constexpr (SUMS) x = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
                             else x = make_uint4(pack_two<TO>(f[i], f[i + 1]), pack_two<TO>(f[i + 2], f[i + 3]), pack_two<TO>(f[i + 4], f[i + 5]), pack_two<TO>(f[i + 6], f[i + 7]));
-                            *reinterpret_cast<uint4*>(turned + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)) = x;
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                         }
+                        fence_async_reads();
                         __syncwarp();
-                        const uint32_t v = lane & 3u, c = c0 + h + v * V;
-#pragma unroll
-                        for (uint32_t i = 0; i < 4u; ++i) {
-                            const uint32_t r = (lane >> 2) + 8u * i;
-                            const uint4 x = *reinterpret_cast<const uint4*>(turned + r * 64u + ((v ^ (r >> 1 & 3u)) << 4));
-                            if (row0 + r < a.m && c < p.n) store16(static_cast<TO*>(a.out) + p.expert * a.out_expert + (row0 + r) * a.out_stride + p.n0 + c, x);
+                        if (elect_one()) {
+                            tile_store_3d(&a.out_map, (int)(p.n0 + c0 + h), (int)row0, (int)p.expert, place);
+                            stores_end_group();
                         }
-                        __syncwarp();
+                        at_turn = at_turn + 1u == kProductTurns ? 0u : at_turn + 1u;
                     }
                 } else {
                     if (row0 + lane >= a.m) return;
@@ -286,6 +288,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                 if (p.steps) give_back();
             }
         }
+        if constexpr (MODE == kWeights) if (elect_one()) wait_stores();
     } else {
     if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 0u) {                                     // copies of tiles

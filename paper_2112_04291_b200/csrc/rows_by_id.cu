@@ -156,6 +156,18 @@ int map_rows(CUtensorMap* map, const void* data, uint32_t type, uint64_t rows, u
     return rc == CUDA_SUCCESS ? FASTSGD_OK : FASTSGD_E_CUDA;
 }
 
+// The map of a gradient of weights for boxes of 32 rows of 64 bytes.
+int map_gradient(CUtensorMap* map, const fastsgd_experts* w) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return FASTSGD_E_CUDA;
+    const uint32_t size = size_of(w->type);
+    const cuuint64_t dims[3] = {w->ins, w->outs, w->experts}, strides[2] = {w->row_stride * size, w->expert_stride * size};
+    const cuuint32_t box[3] = {64u / size, 32u, 1u}, steps[3] = {1u, 1u, 1u};
+    const CUtensorMapDataType type = w->type == FASTSGD_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : w->type == FASTSGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const CUresult rc = encode(map, type, 3u, w->data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? FASTSGD_OK : FASTSGD_E_CUDA;
+}
+
 // Rows of a product: of 16 bits (an output: or of 32), on 16 bytes, in vectors of 8 values.
 int check_product_rows(const fastsgd_matrix* m, bool output) {
     const int rc = check_matrix(m);
@@ -195,7 +207,7 @@ template <int MODE> const void* product_kernel(uint32_t to) {
 template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t to, const DeviceView& dev, cudaStream_t st) {
     if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
     a.tries = dev.tries;
-    const uint32_t turned = MODE == kWeights ? 8u * kProductTurned : 0u;
+    const uint32_t turned = MODE == kWeights ? 8u * kProductTurns * kProductTurned : 0u;
     a.stages = (uint32_t)((215u * 1024u - turned) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
     const void* fn = product_kernel<MODE>(to);
@@ -412,6 +424,8 @@ int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const 
         if (!rc) rc = map_rows(&a.b_map, sorted.data, x->type, sorted.rows, x->cols, sorted.row_stride, kProductK);
         if (rc) return rc;
     }
+    rc = map_gradient(&a.out_map, grad_weights);
+    if (rc) return rc;
     a.starts = starts; a.experts = (uint32_t)grad_weights->experts;
     a.m = (uint32_t)grad_weights->outs; a.n = (uint32_t)grad_weights->ins; a.out = grad_weights->data; a.out_stride = grad_weights->row_stride; a.out_expert = grad_weights->expert_stride;
     a.kind = product_kind(x->type == FASTSGD_BF16, true, true);
