@@ -28,6 +28,7 @@ constexpr int      kProductThreads    = 384;              // four warps that fee
 constexpr uint32_t kProductM          = 256u;             // of a tile; half of it a block's
 constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
+constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their tiles' cost
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers (results of 32 bits)
 constexpr uint32_t kProductTurned     = 2048u, kProductTurns = 3u;      // bytes of a box of a gradient of weights, and boxes of a warp on their way
@@ -59,7 +60,8 @@ struct ProductShared {
     unsigned long long drained;
     uint32_t tmem, tiles;
     uint32_t first_row[kProductMaxExperts + 1];
-    uint32_t first_tile[kProductMaxExperts + 1];
+    uint32_t first_tile[kProductMaxExperts];              // (forward, input) of the experts in their order
+    uint16_t expert_at[kProductMaxExperts];               // that order
 };
 
 // The stages in turn, and the parity of the round.
@@ -72,13 +74,19 @@ struct ProductTile {
     uint32_t expert, m0, n0, n, half, row, end, steps;    // n0: first row (weights: in); half: columns of a block's B; rows row .. end; steps of the contraction
 };
 
+// columns of each of the tiles that an expert's rows make (forward, input): as few tiles as hold them, of equal length
+__device__ __forceinline__ uint32_t product_columns(uint32_t rows, uint32_t most_n) {
+    const uint32_t nt = (rows + most_n - 1u) / most_n;
+    return nt ? ((rows + nt - 1u) / nt + 31u) & ~31u : 0u;
+}
+
 template <int MODE> __device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, const ProductShared& s, uint32_t t) {
     ProductTile p;
     const uint32_t mt = (a.m + kProductM - 1u) / kProductM;
     if constexpr (MODE == kWeights) {
         const uint32_t nt = (a.n + a.most_n - 1u) / a.most_n;
-        p.expert = t / (mt * nt);
-        const uint32_t i = t - p.expert * mt * nt;
+        const uint32_t place = t / (mt * nt), i = t - place * mt * nt;
+        p.expert = s.expert_at[place];
         const uint32_t band = i / (nt * kProductBand), j = i - band * nt * kProductBand, wide = min(kProductBand, mt - band * kProductBand);
         p.m0 = (band * kProductBand + j % wide) * kProductM;
         p.n0 = j / wide * a.most_n;
@@ -92,14 +100,14 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
             const uint32_t mid = (lo + hi) / 2u;
             if (s.first_tile[mid] <= t) lo = mid; else hi = mid;
         }
-        p.expert = lo;
-        const uint32_t i = t - s.first_tile[lo], rows = s.first_row[lo + 1u] - s.first_row[lo];
-        // an expert's rows in tiles of equal length: no tile is empty, since all but one of the fewest tiles that hold them do not
-        const uint32_t nt = (rows + a.most_n - 1u) / a.most_n, each = ((rows + nt - 1u) / nt + 31u) & ~31u;
+        p.expert = s.expert_at[lo];
+        const uint32_t first_row = s.first_row[p.expert], end = s.first_row[p.expert + 1u], rows = end - first_row, i = t - s.first_tile[lo];
+        // (no tile is empty, since all but one of the fewest tiles that hold the rows do not)
+        const uint32_t nt = (rows + a.most_n - 1u) / a.most_n, each = product_columns(rows, a.most_n);
         const uint32_t band = i / (nt * kProductBand), j = i - band * nt * kProductBand, wide = min(kProductBand, mt - band * kProductBand);
         p.m0 = (band * kProductBand + j % wide) * kProductM;
-        p.n0 = s.first_row[lo] + j / wide * each;
-        p.n = min(each, s.first_row[lo + 1u] - p.n0);
+        p.n0 = first_row + j / wide * each;
+        p.n = min(each, end - p.n0);
         p.row = p.n0;
         p.end = p.n0 + p.n;
         p.steps = (a.k + kProductK - 1u) / kProductK;
@@ -110,10 +118,9 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
 
 // Rows and tiles of each expert, from the starts; every thread of the block.
 template <int MODE> __device__ __forceinline__ void product_tables(const ProductArgs& a, ProductShared& s) {
-    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t lane = threadIdx.x & 31u, mt = (a.m + kProductM - 1u) / kProductM;
     if (threadIdx.x < 32u) {                              // (starts that do not ascend, or lie beyond the rows: no rows)
-        const uint32_t mt = (a.m + kProductM - 1u) / kProductM;
-        uint32_t row = 0, tiles = 0;
+        uint32_t row = 0;
         for (uint32_t e0 = 0; e0 <= a.experts; e0 += 32u) {
             const uint32_t e = e0 + lane;
             uint32_t at = e <= a.experts ? min(a.starts[e], a.rows) : 0u;
@@ -123,26 +130,46 @@ template <int MODE> __device__ __forceinline__ void product_tables(const Product
                 if (lane >= d) at = max(at, up);
             }
             at = max(at, row);
-            const uint32_t before = __shfl_up_sync(kFullMask, at, 1);
-            // tiles of the expert before: of row .. at
-            const uint32_t rows = at - (lane ? before : row);
-            uint32_t sum = e && e <= a.experts ? (rows + a.most_n - 1u) / a.most_n * mt : 0u;
+            if (e <= a.experts) s.first_row[e] = at;
+            row = __shfl_sync(kFullMask, at, 31);
+        }
+    }
+    __syncthreads();
+    // (weights) The experts in descending order of their rows, so that pairs of blocks, which take tiles in turn (there and back), have about as much
+    // to do.  (Of more experts each pair has many tiles, whose sums differ little.)
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kProductThreads) {
+        uint32_t place = e;
+        if (MODE == kWeights && a.experts <= kProductSorted) {
+            auto rows = [&](uint32_t i) { return s.first_row[i + 1u] - s.first_row[i]; };
+            const uint32_t mine = rows(e);
+            place = 0;
+            for (uint32_t i = 0; i < a.experts; ++i) { const uint32_t other = rows(i); place += other > mine || (other == mine && i < e); }
+        }
+        s.expert_at[place] = (uint16_t)e;
+    }
+    __syncthreads();
+    if constexpr (MODE == kWeights) {
+        if (threadIdx.x == 0) s.tiles = a.experts * mt * ((a.n + a.most_n - 1u) / a.most_n);
+    } else if (threadIdx.x < 32u) {
+        uint32_t tiles = 0;
+        for (uint32_t i0 = 0; i0 < a.experts; i0 += 32u) {
+            const uint32_t i = i0 + lane, e = i < a.experts ? s.expert_at[i] : 0u;
+            const uint32_t mine = i < a.experts ? (s.first_row[e + 1u] - s.first_row[e] + a.most_n - 1u) / a.most_n * mt : 0u;
+            uint32_t sum = mine;
 #pragma unroll
             for (uint32_t d = 1; d < 32u; d *= 2u) {
                 const uint32_t up = __shfl_up_sync(kFullMask, sum, d);
                 if (lane >= d) sum += up;
             }
-            if (e <= a.experts) { s.first_row[e] = at; s.first_tile[e] = tiles + sum; }
+            if (i < a.experts) s.first_tile[i] = tiles + sum - mine;
             tiles += __shfl_sync(kFullMask, sum, 31);
-            row = __shfl_sync(kFullMask, at, 31);
         }
-        if (lane == 0u) {
-            const uint32_t nt = MODE == kWeights ? (a.n + a.most_n - 1u) / a.most_n : 1u;
-            s.tiles = MODE == kWeights ? a.experts * mt * nt : tiles;
-        }
+        if (lane == 0u) s.tiles = tiles;
     }
     __syncthreads();
 }
+// The tile of a pair's round.
+__device__ __forceinline__ uint32_t product_turn(uint32_t round, uint32_t pair, uint32_t pairs) { return round * pairs + (round & 1u ? pairs - 1u - pair : pair); }
 
 // Rows of a stage's strips from `left` on become zero: what lies behind an expert's last row counts nothing, whatever it holds.  One warp.
 __device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, uint32_t left) {
@@ -159,7 +186,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     __shared__ ProductShared s;
     constexpr bool SUMS = sizeof(TO) == 4;                // accumulators are added up in registers
     const uint32_t warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u, block = blockIdx.x & 1u;
-    const uint32_t first = blockIdx.x / 2u, step_tiles = gridDim.x / 2u;
+    const uint32_t pair = blockIdx.x / 2u, pairs = gridDim.x / 2u;
     const uint32_t stage0 = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t stage_bytes = product_stage_bytes<MODE>(a.most_n);
     uint32_t columns = 32u;
@@ -189,7 +216,8 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
         const uint32_t part = warp & 3u, side = (warp - 4u) >> 2;         // lanes; every other 32 columns
         const uint32_t turned = stage0 + a.stages * stage_bytes + (warp - 4u) * kProductTurns * kProductTurned;      // (weights)
         uint32_t at_turn = 0;
-        for (uint32_t t = first; t < tiles; t += step_tiles) {
+        for (uint32_t t = pair, turns = 0; turns * pairs < tiles; t = product_turn(++turns, pair, pairs)) {
+            if (t >= tiles) continue;
             const ProductTile p = product_tile<MODE>(a, s, t);
             const uint32_t row0 = p.m0 + block * kProductM / 2u + 32u * part;
             const uint32_t from = tmem + (32u * part << 16);
@@ -296,7 +324,8 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
             ProductRing ring;
             uint32_t issued = 0;
             bool fine = true;
-            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                if (t >= tiles) continue;
                 const ProductTile p = product_tile<MODE>(a, s, t);
                 const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
                 const uint32_t bytes = kProductM / 2u * 128u + (MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
@@ -335,7 +364,8 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
             ProductRing ring;
             uint32_t turn = 0;
             bool fine = true;
-            for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                if (t >= tiles) continue;
                 const ProductTile p = product_tile<MODE>(a, s, t);
                 const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
                 uint32_t acc = 0;
@@ -366,7 +396,8 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     } else if (warp == 2u) {                              // what has landed
         ProductRing ring;
         bool fine = true;
-        for (uint32_t t = first; t < tiles && fine; t += step_tiles) {
+        for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                if (t >= tiles) continue;
             const ProductTile p = product_tile<MODE>(a, s, t);
             for (uint32_t step = 0; step < p.steps; ++step) {
                 fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
