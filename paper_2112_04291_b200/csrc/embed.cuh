@@ -354,7 +354,10 @@ template <class T, class TO, bool WIDE, bool PAIRS, bool FULL> __global__ void _
         for (uint32_t j = 0; j < EACH; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
     }
     const bool starts_here = goes_on && !earlier;
-    if (first_chunk) a.follow[tile] = make_uint4(starts_here && now < a.vocab ? ((min(a.starts[now + 1u], have) - 1u) >> a.tile_log) - tile : 0u, now, row, 0u);
+    if (first_chunk) {
+        const uint32_t behind = starts_here && now < a.vocab ? min(a.starts[now + 1u], have) : 0u;
+        a.follow[tile] = make_uint4(behind > end ? ((behind - 1u) >> a.tile_log) - tile : 0u, now, row, 0u);
+    }
     if (starts_here) write_part(a, 2ull * tile + 1ull, sum, c, g);
     else finish();
 }

@@ -48,7 +48,7 @@ inline int launched(cudaError_t err, uint64_t launches = 1) {
     return FASTSGD_OK;
 }
 
-// Blocks of a kernel that stay on the GPU at once (asked for once per device, kernel and size; asking costs as much as a small launch).
+// Blocks of a kernel that stay on the GPU at once; it may then use as much shared memory, and run in clusters of sixteen blocks (asked for once per device, kernel and size; asking costs as much as a small launch).
 struct Residency { int dev; const void* fn; size_t smem; uint64_t blocks; };
 constexpr int kResidencies = 256;
 inline std::mutex g_residency_mu;
@@ -63,7 +63,8 @@ inline int resident_blocks(const void* fn, int threads, size_t smem, const Devic
     int per_sm = 0, most = 0;
     cudaFuncAttributes at;
     if (cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev.device) != cudaSuccess || cudaFuncGetAttributes(&at, fn) != cudaSuccess
-        || cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)at.sharedSizeBytes) != cudaSuccess) {
+        || cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)at.sharedSizeBytes) != cudaSuccess
+        || cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         cudaGetLastError();
         return FASTSGD_E_CUDA;
     }

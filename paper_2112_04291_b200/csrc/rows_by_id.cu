@@ -36,12 +36,6 @@ uint64_t order_bytes(uint64_t count) {                     // behind the workspa
     return count <= kOrderMaxFew ? 0 : 4u * up_to(4u * count, 256) + up_to(4ull * kOrderMaxBins * order_blocks(count), 256) + 4u * kOrderMaxBins;
 }
 
-int allow_wide_clusters(const void* fn) {                  // (of more than eight blocks)
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) return FASTSGD_OK;
-    cudaGetLastError();
-    return FASTSGD_E_CUDA;
-}
-
 // ---- an embedding's gradient -------------------------------------------------------------------------
 
 // Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave 2^13 warps, a few rounds of
@@ -263,7 +257,6 @@ int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32
     uint64_t resident = 0;
     if (count <= kOrderMaxFew) {
         rc = resident_blocks((const void*)k_order, kOrderThreads, sizeof(OrderShared), dev, &resident);
-        if (!rc) rc = allow_wide_clusters((const void*)k_order);
         return rc ? rc : launched(launch_overlapped((const void*)k_order, kOrderBlocks, kOrderThreads, sizeof(OrderShared), kargs, st, kOrderBlocks));
     }
     if (!dev.ws || dev.ws_bytes < kPartialsOffset + order_bytes(count)) return FASTSGD_E_NO_WORKSPACE;
@@ -285,8 +278,9 @@ int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32
         if (rc) return rc;
     }
     rc = launched(launch_overlapped((const void*)k_order_starts, a.range / 256u + 1u, 256, 0, kargs, st));
-    if (!rc && (distinct || number)) rc = allow_wide_clusters((const void*)k_order_distinct);
     if (rc || (!distinct && !number)) return rc;
+    rc = resident_blocks((const void*)k_order_distinct, kOrderThreads, 0, dev, &resident);
+    if (rc) return rc;
     return launched(launch_overlapped((const void*)k_order_distinct, kOrderBlocks, kOrderThreads, 0, kargs, st, kOrderBlocks));
 }
 
@@ -339,7 +333,9 @@ int fastsgd_embedding_backward_pairs(const fastsgd_matrix* grad, const int32_t* 
     if (rc) return rc;
     GradientArgs a{};
     a.grad = grad->data; a.grad_stride = grad->row_stride; a.ids = ids; a.order = order; a.starts = starts; a.distinct = distinct; a.number = number;
-    a.count = (uint32_t)grad->rows; a.vocab = (uint32_t)range; a.cols = (uint32_t)grad->cols; a.scale = scale; a.keys = keys; a.values = values; a.most = (uint32_t)most;
+    a.count = (uint32_t)grad->rows; a.vocab = (uint32_t)range; a.cols = (uint32_t)grad->cols; a.scale = scale; a.keys = keys; a.values = values;
+    a.most = (uint32_t)(most < grad->rows ? most : grad->rows);      // (no more ids occur than there are rows, or ids)
+    if (a.most > a.vocab) a.most = a.vocab;
     const bool wide = rows_on_16(grad) && aligned_to(keys, 16) && aligned_to(values, 16) && grad->cols % 4u == 0;
     return launch_gradient<true>(a, gradient_shape(grad->rows, grad->cols), wide, grad->type, FASTSGD_F32, dev, static_cast<cudaStream_t>(stream));
 }
