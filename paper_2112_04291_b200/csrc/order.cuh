@@ -162,15 +162,16 @@ __device__ __forceinline__ unsigned long long order_scan_pair(unsigned long long
 }
 
 // Where each id's positions begin, from its number of occurrences in starts (one cluster; a slice of the range a block, sixteen ids a thread at a
-// time), and the ids that occur.
+// time), and the ids that occur: first each block's totals, then, once the cluster has met, the rest.
 constexpr uint32_t kOrderEach = 16u;
-__device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, OrderShared& s, uint32_t block) {
-    constexpr uint32_t ROUND = kOrderThreads * kOrderEach;
-    const uint32_t entries = a.range + 1u, slice = ((entries + kOrderBlocks - 1u) / kOrderBlocks + kOrderEach - 1u) / kOrderEach * kOrderEach;
-    const uint32_t lo = min(block * slice, entries), hi = min(lo + slice, entries);
-    const bool aligned = (reinterpret_cast<uintptr_t>(a.starts) & 15u) == 0u;
+struct OrderSlice {
+    static constexpr uint32_t ROUND = kOrderThreads * kOrderEach;
+    uint32_t lo, hi;
+    bool aligned, once;                                   // once: what a thread has loaded it keeps
     uint32_t n[kOrderEach];
-    auto load = [&](uint32_t v) {
+    unsigned long long before;                            // of the block's, before this thread's
+
+    __device__ __forceinline__ unsigned long long load(const OrderArgs& a, uint32_t v) {
         if (aligned && v + kOrderEach <= hi) {
 #pragma unroll
             for (uint32_t i = 0; i < kOrderEach; i += 4u) {
@@ -185,54 +186,59 @@ __device__ __forceinline__ void order_starts_from_counts(const OrderArgs& a, Ord
 #pragma unroll
         for (uint32_t i = 0; i < kOrderEach; ++i) sum += n[i] + ((unsigned long long)(n[i] != 0u) << 32);
         return sum;
-    };
-    const bool once = slice <= ROUND;                     // (what a thread has loaded it keeps)
-    unsigned long long mine = 0, total = 0, at = 0, all = 0;
-    for (uint32_t v = lo; v < hi; v += ROUND) mine += load(v + threadIdx.x * kOrderEach);
-    const unsigned long long before_mine = order_scan_pair(mine, s.pair_sums, &total);
-    if (threadIdx.x == 0) s.of_block = total;
-    cluster_meet();
-    if (threadIdx.x < 32u) {                              // (a lane a block)
-        const uint32_t lane = threadIdx.x, from = address_in(&s.of_block, lane % kOrderBlocks);
-        unsigned long long x = load_from(from) | (unsigned long long)load_from(from + 4u) << 32;
-        if (lane >= kOrderBlocks) x = 0;
-        unsigned long long y = lane < block ? x : 0;
-#pragma unroll
-        for (uint32_t d = 16; d; d /= 2u) { x += __shfl_xor_sync(kFullMask, x, d); y += __shfl_xor_sync(kFullMask, y, d); }
-        if (lane == 0u) { s.pair_sums[0] = y; s.pair_sums[1] = x; }
     }
-    __syncthreads();
-    at = s.pair_sums[0];
-    all = s.pair_sums[1];
-    if (!once) __syncthreads();
-    for (uint32_t v0 = lo; v0 < hi; v0 += ROUND) {
-        const uint32_t v = v0 + threadIdx.x * kOrderEach;
-        unsigned long long here = at + before_mine;
-        if (!once) {
-            here = at + order_scan_pair(load(v), s.pair_sums, &total);
-            at += total;
-        }
-        uint32_t first = (uint32_t)here, rank = (uint32_t)(here >> 32);
-        uint32_t first_of[kOrderEach];
-#pragma unroll
-        for (uint32_t i = 0; i < kOrderEach; ++i) {
-            first_of[i] = first;
-            first += n[i];
-            if (n[i]) { if (a.distinct) a.distinct[rank] = v + i; ++rank; }
-        }
-        if (aligned && v + kOrderEach <= hi) {
-#pragma unroll
-            for (uint32_t i = 0; i < kOrderEach; i += 4u)
-                *reinterpret_cast<uint4*>(a.starts + v + i) = make_uint4(first_of[i], first_of[i + 1], first_of[i + 2], first_of[i + 3]);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < kOrderEach; ++i) if (v + i < hi) a.starts[v + i] = first_of[i];
-        }
+    __device__ __forceinline__ void add_up(const OrderArgs& a, OrderShared& s, uint32_t block) {
+        const uint32_t entries = a.range + 1u, slice = ((entries + kOrderBlocks - 1u) / kOrderBlocks + kOrderEach - 1u) / kOrderEach * kOrderEach;
+        lo = min(block * slice, entries);
+        hi = min(lo + slice, entries);
+        aligned = (reinterpret_cast<uintptr_t>(a.starts) & 15u) == 0u;
+        once = slice <= ROUND;
+        unsigned long long mine = 0, total = 0;
+        for (uint32_t v = lo; v < hi; v += ROUND) mine += load(a, v + threadIdx.x * kOrderEach);
+        before = order_scan_pair(mine, s.pair_sums, &total);
+        if (threadIdx.x == 0) s.of_block = total;
     }
-    if (a.number && block == 0u && threadIdx.x == 0) *a.number = (uint32_t)(all >> 32);
-}
+    __device__ __forceinline__ void finish(const OrderArgs& a, OrderShared& s, uint32_t block) {
+        // (a warp a block: loads of one instruction from different blocks would come one after the other)
+        const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+        if (lane == 0u && warp < kOrderBlocks) {
+            const uint32_t from = address_in(&s.of_block, warp);
+            s.pair_sums[warp] = load_from(from) | (unsigned long long)load_from(from + 4u) << 32;
+        }
+        __syncthreads();
+        unsigned long long all = lane < kOrderBlocks ? s.pair_sums[lane] : 0ull, at = lane < block ? all : 0ull, total = 0;
+#pragma unroll
+        for (uint32_t d = 16; d; d /= 2u) { all += __shfl_xor_sync(kFullMask, all, d); at += __shfl_xor_sync(kFullMask, at, d); }
+        if (!once) __syncthreads();
+        for (uint32_t v0 = lo; v0 < hi; v0 += ROUND) {
+            const uint32_t v = v0 + threadIdx.x * kOrderEach;
+            unsigned long long here = at + before;
+            if (!once) {
+                here = at + order_scan_pair(load(a, v), s.pair_sums, &total);
+                at += total;
+            }
+            uint32_t first = (uint32_t)here, rank = (uint32_t)(here >> 32);
+            uint32_t first_of[kOrderEach];
+#pragma unroll
+            for (uint32_t i = 0; i < kOrderEach; ++i) {
+                first_of[i] = first;
+                first += n[i];
+                if (n[i]) { if (a.distinct) a.distinct[rank] = v + i; ++rank; }
+            }
+            if (aligned && v + kOrderEach <= hi) {
+#pragma unroll
+                for (uint32_t i = 0; i < kOrderEach; i += 4u)
+                    *reinterpret_cast<uint4*>(a.starts + v + i) = make_uint4(first_of[i], first_of[i + 1], first_of[i + 2], first_of[i + 3]);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < kOrderEach; ++i) if (v + i < hi) a.starts[v + i] = first_of[i];
+            }
+        }
+        if (a.number && block == 0u && threadIdx.x == 0) *a.number = (uint32_t)(all >> 32);
+    }
+};
 
-// One cluster: everything.
+// One cluster: everything.  Its blocks meet four times for two digits: what does not depend on the others' is done between the same two meetings.
 __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constant__ OrderArgs a) {
     extern __shared__ __align__(16) unsigned char raw[];
     OrderShared& s = *reinterpret_cast<OrderShared*>(raw);
@@ -247,6 +253,8 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
     const uint32_t have = first < end ? min(end - first, 1u << per_log) : 0u;
     const bool several = a.passes > 1u;                   // (one digit: its counts are the ids')
     const bool pairs = several && a.count <= kOrderMaxPairs;
+    OrderSlice of;
+    if (!pairs) for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
     wait_for_previous_kernels();
     allow_next_kernel();
     if (several) {                                        // (the last entry counts nothing)
@@ -257,42 +265,45 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
     if (pairs) {                                          // eight threads an element, each an eighth of the others
         uint32_t* keys = reinterpret_cast<uint32_t*>(s.entries);
         for (uint32_t i = threadIdx.x; i < a.count; i += kOrderThreads) keys[i] = order_key(a, i);
-        cluster_meet();
+        __syncthreads();
         const uint32_t i = block * (kOrderThreads / 8u) + threadIdx.x / 8u, part = threadIdx.x & 7u;
         const uint32_t key = i < a.count ? keys[i] : ~0u;
         uint32_t before = 0;
         for (uint32_t j = part; j < a.count; j += 8u) before += keys[j] < key || (keys[j] == key && j < i);
 #pragma unroll
         for (uint32_t d = 1; d < 8u; d *= 2u) before += __shfl_xor_sync(kFullMask, before, d);
+        cluster_meet();
         if (part == 0u && key < a.range) {
-            a.order[before] = i;
             atomicAdd(a.starts + key, 1u);
+            a.order[before] = i;
         }
         cluster_meet();
-        order_starts_from_counts(a, s, block);
+        of.add_up(a, s, block);
         cluster_meet();
+        of.finish(a, s, block);
+        cluster_meet();                                   // (no block ends while others read its shared memory)
         return;
     }
     for (uint32_t i = threadIdx.x; i < end - begin; i += kOrderThreads) s.entries[0][i] = make_uint2(order_key(a, begin + i), begin + i);
-    for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
-    if (several) {
-        cluster_meet();
-        for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {      // occurrences, equal ids of a warp together
-            const uint32_t i = i0 + threadIdx.x;
-            const uint32_t key = i < end - begin ? s.entries[0][i].x : a.range;
-            const uint32_t same = __match_any_sync(kFullMask, key);
-            if (key < a.range && lane == (uint32_t)__ffs((int)same) - 1u) atomicAdd(a.starts + key, (uint32_t)__popc(same));
-        }
-    } else __syncthreads();
+    __syncthreads();
     uint32_t from = 0;
     for (uint32_t pass = 0; pass < a.passes; ++pass) {
+        const bool last = pass + 1u == a.passes;
         uint16_t* mine = s.counts + warp * bins;
         uint32_t digit[kOrderRounds], rank[kOrderRounds];
         const uint32_t local = warp << per_log;
         order_rank<kOrderRounds>(mine, have, a.bits, [&](uint32_t j) { return digit_of(a, s.entries[from][local + 32u * j + lane].x, pass); }, digit, rank);
         __syncthreads();
         order_over_warps(s.counts, bins, s.sums);
+        if (several && last) of.add_up(a, s, block);      // (all occurrences have been counted: the cluster has met since)
         cluster_meet();
+        if (several && pass == 0u)                        // occurrences, equal ids of a warp together (all have been cleared)
+            for (uint32_t i0 = 0; i0 < end - begin; i0 += kOrderThreads) {
+                const uint32_t i = i0 + threadIdx.x;
+                const uint32_t key = i < end - begin ? s.entries[0][i].x : a.range;
+                const uint32_t same = __match_any_sync(kFullMask, key);
+                if (key < a.range && lane == (uint32_t)__ffs((int)same) - 1u) atomicAdd(a.starts + key, (uint32_t)__popc(same));
+            }
         uint32_t all = 0, before = 0, total = 0;
         if (threadIdx.x < bins) {
             uint32_t n[kOrderBlocks];
@@ -314,7 +325,6 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
             if (occurs && a.distinct) a.distinct[rank_of] = threadIdx.x;
             if (a.number && threadIdx.x == 0) *a.number = total;
         }
-        const bool last = pass + 1u == a.passes;
 #pragma unroll
         for (uint32_t j = 0; j < kOrderRounds; ++j) {
             if (digit[j] == ~0u) continue;
@@ -325,15 +335,13 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_order(const __grid_constan
             } else store_to(address_in(&s.entries[from ^ 1u][to & (slice - 1u)], to >> slice_log), x.x, x.y);
         }
         from ^= 1u;
+        if (several && last) of.finish(a, s, block);
         if (!last) {
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < kOrderWarps * bins / 2u; i += kOrderThreads) reinterpret_cast<uint32_t*>(s.counts)[i] = 0u;
         }
-        cluster_meet();                                   // (also: the sums have been read before they are formed anew, or their block ends)
+        cluster_meet();                                   // (also: what others read of this block's has been read before it is formed anew, or the block ends)
     }
-    if (!several) return;
-    order_starts_from_counts(a, s, block);
-    cluster_meet();                                       // (no block ends while others read its shared memory)
 }
 
 struct OrderTileShared {
