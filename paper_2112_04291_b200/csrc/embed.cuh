@@ -271,75 +271,100 @@ template <class TO, bool WIDE> __device__ __forceinline__ void clear_rows(const 
     }
 }
 
-// FULL: a warp a group.  Its lanes look up the rows and tokens of sixteen positions at once and tell one another; otherwise each lane looks
-// up all of them.
-template <class T, class TO, bool WIDE, bool PAIRS, bool FULL> __global__ void __launch_bounds__(kEmbedThreads, FULL && WIDE && sizeof(T) == 2 ? 3 : 2) k_embedding_sum(const __grid_constant__ GradientArgs a) {
-    constexpr uint32_t AHEAD = sizeof(T) == 2 || WIDE ? 8u : 4u;        // rows in flight
-    constexpr uint32_t WINDOW = FULL ? 16u : AHEAD;                     // positions looked up at a time
-    wait_for_previous_kernels();
-    allow_next_kernel();
-    uint32_t block = blockIdx.x;
-    if constexpr (!PAIRS) {                               // (blocks that wait for rows beside blocks that write)
+// What a group knows of its tile before it adds up.
+struct SumTile {
+    uint32_t tile, begin, end, have, c, now, row;         // c: this lane's first column; now: the token whose rows are being added up; row: its row (pairs)
+    bool earlier, goes_on, first_chunk;                   // now began in an earlier tile; the last token goes on; this lane writes for the tile
+};
+__device__ __forceinline__ uint32_t id_at(const GradientArgs& a, uint32_t p) {
+    const uint32_t at = a.order[p];
+    return at < a.count ? (uint32_t)a.ids[at] : ~0u;
+}
+// Blocks that add up beside blocks that clear: false where this one clears, and has.
+template <class TO, bool WIDE, bool PAIRS> __device__ __forceinline__ bool sums(const GradientArgs& a, uint32_t& block) {
+    block = blockIdx.x;
+    if constexpr (!PAIRS) {
         const uint32_t both = min(a.sum_blocks, a.clear_blocks);
         const bool clears = block < 2u * both ? block & 1u : a.clear_blocks > both;
         block = block < 2u * both ? block / 2u : block - both;
-        if (clears) { clear_rows<TO, WIDE>(a, block); return; }
+        if (clears) { clear_rows<TO, WIDE>(a, block); return false; }
     }
+    return true;
+}
+template <class TO, bool WIDE, bool PAIRS> __device__ __forceinline__ void finish_token(const GradientArgs& a, const SumTile& t, const float (&sum)[8], const Group& g) {
+    if (t.earlier) write_part(a, 2ull * t.tile, sum, t.c, g);
+    else if (t.now < a.vocab) write_sum<TO, WIDE, PAIRS>(a, t.now, t.row, sum, t.c, g);
+}
+template <class TO, bool WIDE, bool PAIRS> __device__ __forceinline__ void finish_tile(const GradientArgs& a, const SumTile& t, const float (&sum)[8], const Group& g) {
+    const bool starts_here = t.goes_on && !t.earlier;
+    if (t.first_chunk) {
+        const uint32_t behind = starts_here && t.now < a.vocab ? min(a.starts[t.now + 1u], t.have) : 0u;
+        a.follow[t.tile] = make_uint4(behind > t.end ? ((behind - 1u) >> a.tile_log) - t.tile : 0u, t.now, t.row, 0u);
+    }
+    if (starts_here) write_part(a, 2ull * t.tile + 1ull, sum, t.c, g);
+    else finish_token<TO, WIDE, PAIRS>(a, t, sum, g);
+}
+
+// Rows in registers.  FULL: a warp a group, whose lanes look up the rows and tokens of sixteen positions at once and tell one another; otherwise
+// each lane looks up all of them.
+template <class T, class TO, bool WIDE, bool PAIRS, bool FULL> __global__ void __launch_bounds__(kEmbedThreads, FULL && sizeof(T) == 2 ? 3 : 2) k_embedding_sum(const __grid_constant__ GradientArgs a) {
+    constexpr uint32_t AHEAD = sizeof(T) == 2 || WIDE ? 8u : 4u;        // rows in flight
+    constexpr uint32_t WINDOW = FULL ? 16u : AHEAD, EACH = FULL ? 1u : AHEAD;      // positions looked up at a time, and of them a lane's
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    uint32_t block;
+    if (!sums<TO, WIDE, PAIRS>(a, block)) return;
     const Group g = row_group(FULL ? 5u : a.lanes_log);
-    const uint32_t lane = threadIdx.x & 31u;
     const uint32_t u = FULL ? block * (kEmbedThreads / 32u) + __shfl_sync(kFullMask, threadIdx.x >> 5, 0) : block * (kEmbedThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
-    const uint32_t tile = u / a.chunks, c = ((u - tile * a.chunks) * g.lanes + g.lane) * 8u;
-    if (tile >= a.tiles) return;
-    const uint32_t begin = tile << a.tile_log;
+    SumTile t;
+    t.tile = u / a.chunks; t.c = ((u - t.tile * a.chunks) * g.lanes + g.lane) * 8u;
+    if (t.tile >= a.tiles) return;
+    t.begin = t.tile << a.tile_log;
     // rows and tokens (those behind the last are garbage, and of no account)
-    constexpr uint32_t EACH = FULL ? 1u : AHEAD;
     auto look_up = [&](uint32_t p, uint32_t (&at)[EACH], uint32_t (&id)[EACH]) {
-        if constexpr (FULL) p += lane & (WINDOW - 1u);
+        if constexpr (FULL) p += g.lane & (WINDOW - 1u);
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) at[j] = p + j < a.count ? a.order[p + j] : ~0u;
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) id[j] = at[j] < a.count ? (uint32_t)a.ids[at[j]] : ~0u;
     };
-    auto id_at = [&](uint32_t p) { const uint32_t at = a.order[p]; return at < a.count ? (uint32_t)a.ids[at] : ~0u; };
-    uint32_t at[EACH], id[EACH], row = 0;
-    look_up(begin, at, id);
-    const uint32_t before = begin ? id_at(begin - 1u) : ~0u;
-    const uint32_t have = min(a.starts[a.vocab], a.count), end = min(begin + (1u << a.tile_log), have);
-    const bool first_chunk = u == tile * a.chunks && g.lane == 0u;
-    if (begin >= end) {
-        if (first_chunk) a.follow[tile] = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t at[EACH], id[EACH];
+    look_up(t.begin, at, id);
+    const uint32_t before = t.begin ? id_at(a, t.begin - 1u) : ~0u;
+    t.have = min(a.starts[a.vocab], a.count);
+    t.end = min(t.begin + (1u << a.tile_log), t.have);
+    t.first_chunk = u == t.tile * a.chunks && g.lane == 0u;
+    if (t.begin >= t.end) {
+        if (t.first_chunk) a.follow[t.tile] = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    uint32_t now = FULL ? __shfl_sync(kFullMask, id[0], 0) : id[0];      // the token whose rows are being added up; pairs: its row
-    bool earlier = begin && before == now;                // it began in an earlier tile
-    const bool goes_on = end < have && id_at(end) == id_at(end - 1u);
-    if constexpr (PAIRS) row = FULL ? place_among_by_warp(a.distinct, min(*a.number, a.most), now) : place_among(a.distinct, min(*a.number, a.most), now);
+    t.now = FULL ? __shfl_sync(kFullMask, id[0], 0) : id[0];
+    t.row = 0;
+    t.earlier = t.begin && before == t.now;
+    t.goes_on = t.end < t.have && id_at(a, t.end) == id_at(a, t.end - 1u);
+    if constexpr (PAIRS) t.row = FULL ? place_among_by_warp(a.distinct, min(*a.number, a.most), t.now) : place_among(a.distinct, min(*a.number, a.most), t.now);
     float sum[8] = {};
-    auto finish = [&]() {
-        if (earlier) write_part(a, 2ull * tile, sum, c, g);
-        else if (now < a.vocab) write_sum<TO, WIDE, PAIRS>(a, now, row, sum, c, g);
-    };
-    for (uint32_t p0 = begin; p0 < end; p0 += WINDOW) {
+    for (uint32_t p0 = t.begin; p0 < t.end; p0 += WINDOW) {
         uint32_t next_at[EACH], next_id[EACH];
-        if (p0 + WINDOW < end) look_up(p0 + WINDOW, next_at, next_id);
+        if (p0 + WINDOW < t.end) look_up(p0 + WINDOW, next_at, next_id);
 #pragma unroll
         for (uint32_t w = 0; w < WINDOW; w += AHEAD) {
             const uint32_t p = p0 + w;
-            if (p >= end) continue;
+            if (p >= t.end) continue;
             Piece<T, WIDE> piece[AHEAD];
             uint32_t from[AHEAD];
 #pragma unroll
             for (uint32_t j = 0; j < AHEAD; ++j) {
                 from[j] = FULL ? __shfl_sync(kFullMask, at[0], w + j) : at[FULL ? 0u : j];
-                if (p + j < end && from[j] < a.count) load_piece(piece[j], static_cast<const T*>(a.grad) + from[j] * a.grad_stride, c, a.cols);
+                if (p + j < t.end && from[j] < a.count) load_piece(piece[j], static_cast<const T*>(a.grad) + from[j] * a.grad_stride, t.c, a.cols);
             }
 #pragma unroll
             for (uint32_t j = 0; j < AHEAD; ++j) {
-                if (p + j >= end) continue;
-                const uint32_t of = FULL ? __shfl_sync(kFullMask, id[0], w + j) : id[FULL ? 0u : j];
-                if (of != now) {
-                    finish();
-                    now = of; earlier = false; ++row;
+                if (p + j >= t.end) continue;
+                const uint32_t token = FULL ? __shfl_sync(kFullMask, id[0], w + j) : id[FULL ? 0u : j];
+                if (token != t.now) {
+                    finish_token<TO, WIDE, PAIRS>(a, t, sum, g);
+                    t.now = token; t.earlier = false; ++t.row;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
                 }
@@ -353,13 +378,106 @@ template <class T, class TO, bool WIDE, bool PAIRS, bool FULL> __global__ void _
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) { at[j] = next_at[j]; id[j] = next_id[j]; }
     }
-    const bool starts_here = goes_on && !earlier;
-    if (first_chunk) {
-        const uint32_t behind = starts_here && now < a.vocab ? min(a.starts[now + 1u], have) : 0u;
-        a.follow[tile] = make_uint4(behind > end ? ((behind - 1u) >> a.tile_log) - tile : 0u, now, row, 0u);
+    finish_tile<TO, WIDE, PAIRS>(a, t, sum, g);
+}
+
+// Rows of more than 128 columns that begin at any element, a warp a chunk of 256.  Their vectors and what shifts them take registers and
+// instructions for each row in flight above: here the rows are copied to shared memory, 16 or 8 of them ahead of the one that is added up, from the
+// vector that the chunk begins in, and the code for a row stands once.  (30001 x 1001 fp16: 38 us, in registers 45; rows on 16 bytes, 16384 x 2048
+// and 65536 x 512 bf16: 92 and 33 us, in registers 91 and 26.)
+template <class T> struct SumShared {
+    static constexpr uint32_t SLOTS = sizeof(T) == 2 ? 16u : 8u;
+    static constexpr uint32_t VECTORS = 16u * (uint32_t)sizeof(T) + 1u;
+    uint4 rows[kEmbedThreads / 32][SLOTS][VECTORS];
+};
+template <class T, class TO, bool PAIRS> __global__ void __launch_bounds__(kEmbedThreads, 3) k_embedding_sum_shifted(const __grid_constant__ GradientArgs a) {
+    using Shared = SumShared<T>;
+    constexpr uint32_t SLOTS = Shared::SLOTS, N = 8u / Vec<T>::N;       // vectors of a lane
+    extern __shared__ __align__(16) unsigned char raw[];
+    wait_for_previous_kernels();
+    allow_next_kernel();
+    uint32_t block;
+    if (!sums<TO, false, PAIRS>(a, block)) return;
+    const Group g = row_group(5u);
+    const uint32_t lane = threadIdx.x & 31u, warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0);
+    uint4 (&rows)[SLOTS][Shared::VECTORS] = reinterpret_cast<Shared*>(raw)->rows[warp];
+    const uint32_t u = block * (kEmbedThreads / 32u) + warp;
+    SumTile t;
+    t.tile = u / a.chunks;
+    const uint32_t c0 = (u - t.tile * a.chunks) * 256u;
+    t.c = c0 + lane * 8u;
+    if (t.tile >= a.tiles) return;
+    t.begin = t.tile << a.tile_log;
+    // rows and tokens of positions p .. p + 31, a lane each (those behind the last are garbage, and of no account)
+    auto look_up = [&](uint32_t p, uint32_t& at, uint32_t& id) {
+        at = p + lane < a.count ? a.order[p + lane] : ~0u;
+        id = at < a.count ? (uint32_t)a.ids[at] : ~0u;
+    };
+    uint32_t at, id, next_at = ~0u, next_id = ~0u;
+    look_up(t.begin, at, id);
+    const uint32_t before = t.begin ? id_at(a, t.begin - 1u) : ~0u;
+    t.have = min(a.starts[a.vocab], a.count);
+    t.end = min(t.begin + (1u << a.tile_log), t.have);
+    t.first_chunk = c0 == 0u && lane == 0u;
+    if (t.begin >= t.end) {
+        if (t.first_chunk) a.follow[t.tile] = make_uint4(0u, 0u, 0u, 0u);
+        return;
     }
-    if (starts_here) write_part(a, 2ull * tile + 1ull, sum, c, g);
-    else finish();
+    uint32_t window = t.begin;                            // the first position of those that at and id are of
+    if (window + 32u < t.end) look_up(window + 32u, next_at, next_id);
+    const T* const grad = static_cast<const T*>(a.grad) + c0;
+    const uint32_t bytes = min(256u, a.cols - c0) * (uint32_t)sizeof(T);
+    // position p's row on its way to its place (one group of copies, whether or not there is one)
+    auto fetch = [&](uint32_t p, uint32_t slot) {
+        const uint32_t ahead = p - window, of = __shfl_sync(kFullMask, ahead < 32u ? at : next_at, ahead & 31u);
+        if (p < t.end && of < a.count) {
+            const T* from = grad + of * a.grad_stride;
+            const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(from) & 15u, vectors = (off + bytes + 15u) / 16u;
+            const unsigned char* first = reinterpret_cast<const unsigned char*>(from) - off;
+#pragma unroll
+            for (uint32_t i = 0; i < Shared::VECTORS; i += 32u) if (i + lane < vectors && i + lane < Shared::VECTORS) copy16_async(&rows[slot][i + lane], first + 16u * (i + lane));
+        }
+        copies_end_group();
+    };
+#pragma unroll 1
+    for (uint32_t i = 0; i < SLOTS; ++i) fetch(t.begin + i, i);
+    t.now = __shfl_sync(kFullMask, id, 0); t.row = 0;
+    t.earlier = t.begin && before == t.now;
+    t.goes_on = t.end < t.have && id_at(a, t.end) == id_at(a, t.end - 1u);
+    if constexpr (PAIRS) t.row = place_among_by_warp(a.distinct, min(*a.number, a.most), t.now);
+    float sum[8] = {};
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (uint32_t p = t.begin; p < t.end; ++p) {
+        const uint32_t of = __shfl_sync(kFullMask, at, p - window), token = __shfl_sync(kFullMask, id, p - window);
+        if (token != t.now) {
+            finish_token<TO, false, PAIRS>(a, t, sum, g);
+            t.now = token; t.earlier = false; ++t.row;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+        }
+        wait_copies<(int)SLOTS - 1>();
+        __syncwarp();                                     // (a lane reads what others have copied)
+        if (of < a.count) {
+            Piece<T, false> piece;
+#pragma unroll
+            for (uint32_t i = 0; i <= N; ++i) piece.v[i] = rows[slot][lane * N + i];
+            float f[8];
+            unpack_piece(piece, grad + of * a.grad_stride, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += f[i];
+        }
+        __syncwarp();
+        fetch(p + SLOTS, slot);
+        slot = slot + 1u == SLOTS ? 0u : slot + 1u;
+        if (p + 1u == window + 32u) {
+            window += 32u;
+            at = next_at; id = next_id;
+            if (window + 32u < t.end) look_up(window + 32u, next_at, next_id);
+        }
+    }
+    wait_copies<0>();
+    finish_tile<TO, false, PAIRS>(a, t, sum, g);
 }
 
 // Tokens that begin in a tile and go on.  A block looks at eight tiles, for a chunk of columns: each of its warps adds up what follows one of

@@ -54,20 +54,22 @@ GradientShape gradient_shape(uint64_t count, uint64_t cols) {
 }
 uint64_t part_bytes(const GradientShape& g) { return up_to(8ull * g.tiles * g.part_stride, 256) + 16ull * g.tiles; }
 
-template <class T, bool WIDE, bool PAIRS, bool FULL> const void* sum_kernel_of(uint32_t to) {
-    if constexpr (PAIRS) return (const void*)k_embedding_sum<T, float, WIDE, true, FULL>;
+struct SumKernel { const void* fn; size_t smem; };
+template <class T, class TO, bool WIDE, bool PAIRS> SumKernel sum_kernel_as(bool full) {
+    if (!full) return {(const void*)k_embedding_sum<T, TO, WIDE, PAIRS, false>, 0};
+    if constexpr (WIDE) return {(const void*)k_embedding_sum<T, TO, true, PAIRS, true>, 0};
+    else return {(const void*)k_embedding_sum_shifted<T, TO, PAIRS>, sizeof(SumShared<T>)};
+}
+template <class T, bool WIDE, bool PAIRS> SumKernel sum_kernel_of(uint32_t to, bool full) {
+    if constexpr (PAIRS) return sum_kernel_as<T, float, WIDE, true>(full);
     else {
-        if (to == FASTSGD_F32) return (const void*)k_embedding_sum<T, float, WIDE, false, FULL>;
-        if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? (const void*)k_embedding_sum<T, __nv_bfloat16, WIDE, false, FULL> : (const void*)k_embedding_sum<T, __half, WIDE, false, FULL>;
-        else return (const void*)k_embedding_sum<T, T, WIDE, false, FULL>;
+        if (to == FASTSGD_F32) return sum_kernel_as<T, float, WIDE, false>(full);
+        if constexpr (sizeof(T) == 4) return to == FASTSGD_BF16 ? sum_kernel_as<T, __nv_bfloat16, WIDE, false>(full) : sum_kernel_as<T, __half, WIDE, false>(full);
+        else return sum_kernel_as<T, T, WIDE, false>(full);
     }
 }
-template <bool WIDE, bool PAIRS, bool FULL> const void* sum_kernel_for(uint32_t from, uint32_t to) {
-    return from == FASTSGD_F32 ? sum_kernel_of<float, WIDE, PAIRS, FULL>(to) : from == FASTSGD_BF16 ? sum_kernel_of<__nv_bfloat16, WIDE, PAIRS, FULL>(to) : sum_kernel_of<__half, WIDE, PAIRS, FULL>(to);
-}
-template <bool PAIRS> const void* sum_kernel(bool wide, bool full, uint32_t from, uint32_t to) {
-    return wide ? (full ? sum_kernel_for<true, PAIRS, true>(from, to) : sum_kernel_for<true, PAIRS, false>(from, to))
-                : (full ? sum_kernel_for<false, PAIRS, true>(from, to) : sum_kernel_for<false, PAIRS, false>(from, to));
+template <bool WIDE, bool PAIRS> SumKernel sum_kernel_for(uint32_t from, uint32_t to, bool full) {
+    return from == FASTSGD_F32 ? sum_kernel_of<float, WIDE, PAIRS>(to, full) : from == FASTSGD_BF16 ? sum_kernel_of<__nv_bfloat16, WIDE, PAIRS>(to, full) : sum_kernel_of<__half, WIDE, PAIRS>(to, full);
 }
 template <bool WIDE, bool PAIRS> const void* join_kernel(uint32_t to) {
     if constexpr (PAIRS) return (const void*)k_embedding_join<float, WIDE, true>;
@@ -116,7 +118,10 @@ template <bool PAIRS> int launch_gradient(GradientArgs& a, const GradientShape& 
     if (blocks >= 1ull << 31 || (uint64_t)g.tiles * g.chunks >= 1ull << 31) return FASTSGD_E_BAD_N;
     void* kargs[] = {&a};
     if (blocks) {
-        const int rc = launched(launch_overlapped(sum_kernel<PAIRS>(wide, g.lanes_log == 5u, from, to), (unsigned)blocks, kEmbedThreads, 0, kargs, st));
+        const SumKernel k = wide ? sum_kernel_for<true, PAIRS>(from, to, g.lanes_log == 5u) : sum_kernel_for<false, PAIRS>(from, to, g.lanes_log == 5u);
+        uint64_t resident = 0;
+        int rc = resident_blocks(k.fn, kEmbedThreads, k.smem, dev, &resident);
+        if (!rc) rc = launched(launch_overlapped(k.fn, (unsigned)blocks, kEmbedThreads, k.smem, kargs, st));
         if (rc) return rc;
     }
     if (g.tiles < 2u) return FASTSGD_OK;
