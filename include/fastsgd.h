@@ -442,7 +442,7 @@ int fastsgd_embedding_backward(const fastsgd_matrix* grad, const int32_t* ids, c
 
 /*
  * The same gradient as key-value pairs, the rows of the ids that occur alone: what fastsgd_compress_kv takes (count = *number * cols,
- * n = range * cols).
+ * n = range * cols).  The values are those of the dense gradient in fp32, bit for bit.
  *   distinct, number  as fastsgd_order_ids wrote them
  *   range             of the ids; range * cols < 2^31
  *   keys, values      device, room for most * cols each: row i holds the keys distinct[i] * cols + c and their values; rows from *number on

@@ -10,12 +10,16 @@
 //
 // A pair of blocks (two SMs) works on a tile: each copies half of A and half of B, so that an operand byte in shared memory serves twice as many
 // products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products, a third tells it what has
-// landed; eight write results, while the next tile's products go into the other half of the
-// accumulators.
+// landed; eight write results, while the next tile's products go into the other half of the accumulators.  A single thread issues copies and
+// products: what bounds the rate is then the tensor cores (and the GPU's power) alone.  Bounds, measured, with sorted rows and one GPU to itself:
+//   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1390 us each way (1380 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
+//   49152 x 2048 x 1408, 64 experts: 205 to 230 us (1230 to 1390 TFLOP/s; 19 rounds of tiles, the last partly filled, 5.5 tiles of 256 outs)
+//   32 x 4096 x 14336, 8 experts: 142 to 155 us, the weights' 940 MB at a copy's rate
+//   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 305 to 340 us, 738 MB written while 340 MB are read; bf16 235
 //
-// The tensor cores cut off each addition to an accumulator where it exceeds 32 bits: over n values of the contraction the result loses about
-// n / 16 halves of its last bit, always towards zero (770 rows: 1.6e-6 of the result).  Where the result is wanted in 32 bits, accumulators
-// begin anew every 256 values, and the warps that write add them up in registers, rounding to nearest.
+// The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero: a sum of 512 values of the contraction loses
+// 4.7e-7 of the result, of 768 about 1.6e-6.  Where the result is wanted in 32 bits, accumulators begin anew every 512 values, and the warps that
+// write add them up in registers, rounding to nearest: 4.8e-7 for 4096 values (plain sums in fp32: 6.1e-7).
 #pragma once
 
 #include "rows.cuh"
@@ -28,7 +32,7 @@ constexpr int      kProductThreads    = 384;              // four warps that fee
 constexpr uint32_t kProductM          = 256u;             // of a tile; half of it a block's
 constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
-constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their tiles' cost
+constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their rows (weights)
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers (results of 32 bits)
 constexpr uint32_t kProductTurned     = 2048u, kProductTurns = 3u;      // bytes of a box of a gradient of weights, and boxes of a warp on their way
@@ -318,97 +322,97 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
         }
         if constexpr (MODE == kWeights) if (elect_one()) wait_stores();
     } else {
-    if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == 0u) {                                     // copies of tiles
-        if (elect_one()) {
-            ProductRing ring;
-            uint32_t issued = 0;
-            bool fine = true;
-            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
-                if (t >= tiles) continue;
-                const ProductTile p = product_tile<MODE>(a, s, t);
-                const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
-                const uint32_t bytes = kProductM / 2u * 128u + (MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
-                const int m0 = (int)(p.m0 + block * kProductM / 2u);
-                const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
-                int at = MODE == kWeights ? (int)p.row : 0;            // in the contraction
-                for (uint32_t step = 0; step < p.steps; ++step, at += (int)kProductK) {
-                    fine = mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
-                    if (!fine) break;
-                    const uint32_t bar = smem_u32(&s.landed[ring.stage]), to_a = stage0 + ring.stage * stage_bytes, to_b = to_a + kProductM / 2u * 128u;
-                    mbar_expect_tx(&s.landed[ring.stage], bytes);
-                    if constexpr (MODE == kForward) tile_load_3d(to_a, &a.a_map, at, m0, (int)p.expert, bar);
-                    else if constexpr (MODE == kInput) {
-                        tile_load_3d(to_a, &a.a_map, m0, at, (int)p.expert, bar);
-                        tile_load_3d(to_a + 8192u, &a.a_map, m0 + 64, at, (int)p.expert, bar);
-                    } else {
-                        tile_load_2d(to_a, &a.a_map, m0, at, bar);
-                        tile_load_2d(to_a + 8192u, &a.a_map, m0 + 64, at, bar);
+        if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        if (warp == 0u) {                                     // copies of tiles
+            if (elect_one()) {
+                ProductRing ring;
+                uint32_t issued = 0;
+                bool fine = true;
+                for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                    if (t >= tiles) continue;
+                    const ProductTile p = product_tile<MODE>(a, s, t);
+                    const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
+                    const uint32_t bytes = kProductM / 2u * 128u + (MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
+                    const int m0 = (int)(p.m0 + block * kProductM / 2u);
+                    const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
+                    int at = MODE == kWeights ? (int)p.row : 0;            // in the contraction
+                    for (uint32_t step = 0; step < p.steps; ++step, at += (int)kProductK) {
+                        fine = mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
+                        if (!fine) break;
+                        const uint32_t bar = smem_u32(&s.landed[ring.stage]), to_a = stage0 + ring.stage * stage_bytes, to_b = to_a + kProductM / 2u * 128u;
+                        mbar_expect_tx(&s.landed[ring.stage], bytes);
+                        if constexpr (MODE == kForward) tile_load_3d(to_a, &a.a_map, at, m0, (int)p.expert, bar);
+                        else if constexpr (MODE == kInput) {
+                            tile_load_3d(to_a, &a.a_map, m0, at, (int)p.expert, bar);
+                            tile_load_3d(to_a + 8192u, &a.a_map, m0 + 64, at, (int)p.expert, bar);
+                        } else {
+                            tile_load_2d(to_a, &a.a_map, m0, at, bar);
+                            tile_load_2d(to_a + 8192u, &a.a_map, m0 + 64, at, bar);
+                        }
+                        if constexpr (MODE == kWeights) {
+                            tile_load_2d(to_b, &a.b_map, n0, at, bar);
+                            if (strips > 1u) tile_load_2d(to_b + 8192u, &a.b_map, n0 + 64, at, bar);
+                        } else for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, n0 + (int)(j * a.box), bar);
+                        ring.next(a.stages);
+                        ++issued;
                     }
-                    if constexpr (MODE == kWeights) {
-                        tile_load_2d(to_b, &a.b_map, n0, at, bar);
-                        if (strips > 1u) tile_load_2d(to_b + 8192u, &a.b_map, n0 + 64, at, bar);
-                    } else for (uint32_t j = 0; j < boxes; ++j) tile_load_2d(to_b + j * a.box * 128u, &a.b_map, at, n0 + (int)(j * a.box), bar);
-                    ring.next(a.stages);
-                    ++issued;
+                }
+                // what is still on its way lands before the block ends, whoever has given up: the last round of each stage
+                for (uint32_t i = min(issued, a.stages); i > 0u; --i) {
+                    const uint32_t back = ring.stage >= i ? ring.stage - i : ring.stage + a.stages - i;
+                    mbar_wait(&s.landed[back], back < ring.stage ? ring.round : ring.round ^ 1u);
                 }
             }
-            // what is still on its way lands before the block ends, whoever has given up: the last round of each stage
-            for (uint32_t i = min(issued, a.stages); i > 0u; --i) {
-                const uint32_t back = ring.stage >= i ? ring.stage - i : ring.stage + a.stages - i;
-                mbar_wait(&s.landed[back], back < ring.stage ? ring.round : ring.round ^ 1u);
-            }
-        }
-    } else if (warp == 1u && block == 0u) {               // products
-        if (elect_one()) {
-            ProductRing ring;
-            uint32_t turn = 0;
-            bool fine = true;
-            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
-                if (t >= tiles) continue;
-                const ProductTile p = product_tile<MODE>(a, s, t);
-                const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
-                uint32_t acc = 0;
-                for (uint32_t step = 0; step < p.steps; ++step) {
-                    const bool begins = SUMS ? step % kProductSum == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && (step + 1u) % kProductSum == 0u);
-                    if (begins) {
-                        fine = mbar_wait(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
-                        acc = tmem + (turn & 1u) * a.most_n;
-                    }
-                    fine = fine && mbar_wait(&s.full[ring.stage], ring.round, a.tries);
-                    if (!fine) break;
-                    tmem_after_barrier();
-                    const uint32_t from_a = stage0 + ring.stage * stage_bytes, from_b = from_a + kProductM / 2u * 128u;
-                    const uint32_t da = operand_at(from_a, MODE == kForward ? 0u : 8192u), db = operand_at(from_b, MODE == kWeights ? 8192u : 0u);
-                    constexpr uint32_t STEP_A = (MODE == kForward ? 32u : 2048u) >> 4, STEP_B = (MODE == kWeights ? 2048u : 32u) >> 4;
+        } else if (warp == 1u && block == 0u) {               // products
+            if (elect_one()) {
+                ProductRing ring;
+                uint32_t turn = 0;
+                bool fine = true;
+                for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                    if (t >= tiles) continue;
+                    const ProductTile p = product_tile<MODE>(a, s, t);
+                    const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
+                    uint32_t acc = 0;
+                    for (uint32_t step = 0; step < p.steps; ++step) {
+                        const bool begins = SUMS ? step % kProductSum == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && (step + 1u) % kProductSum == 0u);
+                        if (begins) {
+                            fine = mbar_wait(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
+                            acc = tmem + (turn & 1u) * a.most_n;
+                        }
+                        fine = fine && mbar_wait(&s.full[ring.stage], ring.round, a.tries);
+                        if (!fine) break;
+                        tmem_after_barrier();
+                        const uint32_t from_a = stage0 + ring.stage * stage_bytes, from_b = from_a + kProductM / 2u * 128u;
+                        const uint32_t da = operand_at(from_a, MODE == kForward ? 0u : 8192u), db = operand_at(from_b, MODE == kWeights ? 8192u : 0u);
+                        constexpr uint32_t STEP_A = (MODE == kForward ? 32u : 2048u) >> 4, STEP_B = (MODE == kWeights ? 2048u : 32u) >> 4;
 #pragma unroll
-                    for (uint32_t i = 0; i < kProductK / 16u; ++i) multiply(acc, da + STEP_A * i, db + STEP_B * i, shape, !begins || i);
-                    products_arrive(&s.empty[ring.stage]);
-                    if (ends) { products_arrive(&s.ready[turn & 1u]); ++turn; }
+                        for (uint32_t i = 0; i < kProductK / 16u; ++i) multiply(acc, da + STEP_A * i, db + STEP_B * i, shape, !begins || i);
+                        products_arrive(&s.empty[ring.stage]);
+                        if (ends) { products_arrive(&s.ready[turn & 1u]); ++turn; }
+                        ring.next(a.stages);
+                    }
+                }
+                products_arrive(&s.drained);                  // no product is under way any more when the accumulators are given back
+                mbar_wait(&s.drained, 0u);
+            }
+        } else if (warp == 1u) {
+            mbar_wait(&s.drained, 0u);                        // (every signal of the other block's products has come)
+        } else if (warp == 2u) {                              // what has landed
+            ProductRing ring;
+            bool fine = true;
+            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+                if (t >= tiles) continue;
+                const ProductTile p = product_tile<MODE>(a, s, t);
+                for (uint32_t step = 0; step < p.steps; ++step) {
+                    fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
+                    if (!fine) break;
+                    if (MODE == kWeights && step + 1u == p.steps)
+                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
+                    if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
                     ring.next(a.stages);
                 }
             }
-            products_arrive(&s.drained);                  // no product is under way any more when the accumulators are given back
-            mbar_wait(&s.drained, 0u);
         }
-    } else if (warp == 1u) {
-        mbar_wait(&s.drained, 0u);                        // (every signal of the other block's products has come)
-    } else if (warp == 2u) {                              // what has landed
-        ProductRing ring;
-        bool fine = true;
-        for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
-                if (t >= tiles) continue;
-            const ProductTile p = product_tile<MODE>(a, s, t);
-            for (uint32_t step = 0; step < p.steps; ++step) {
-                fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
-                if (!fine) break;
-                if (MODE == kWeights && step + 1u == p.steps)
-                    product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
-                if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
-                ring.next(a.stages);
-            }
-        }
-    }
     }
     __syncwarp();
     tmem_before_barrier();

@@ -38,8 +38,10 @@ uint64_t order_bytes(uint64_t count) {                     // behind the workspa
 
 // ---- an embedding's gradient -------------------------------------------------------------------------
 
-// Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave 2^13 warps, a few rounds of
-// what the GPU holds at once.
+// Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave so many warps, one or two rounds of
+// what the GPU holds at once.  (us with 2^12, 2^13, 2^14 warps: 65536 x 768 bf16 of 2 rows 33, 45, 65; 65536 x 512 of 1000 rows 23, 26, 34; 30001 x 1001
+// fp16 37.5, 38.5, 44.7; 49152 x 2048 bf16 52, 52, 58; pairs of 16384 x 2048 bf16 57, 49, 53: but their sums are those of the dense gradient, bit for bit.)
+constexpr uint32_t kSumWarpsLog = 12u;
 struct GradientShape { uint32_t lanes_log, chunks, tile_log, tiles; uint64_t part_stride; };
 GradientShape gradient_shape(uint64_t count, uint64_t cols) {
     GradientShape g{};
@@ -47,7 +49,7 @@ GradientShape gradient_shape(uint64_t count, uint64_t cols) {
     const uint64_t chunks = (cols + (8ull << g.lanes_log) - 1) / (8ull << g.lanes_log);
     g.chunks = (uint32_t)chunks;
     g.tile_log = 4;
-    while ((((count + (1ull << g.tile_log) - 1) >> g.tile_log) * chunks << g.lanes_log) > (1ull << 13) * 32u && (1ull << g.tile_log) < count) ++g.tile_log;
+    while ((((count + (1ull << g.tile_log) - 1) >> g.tile_log) * chunks << g.lanes_log) > (32ull << kSumWarpsLog) && (1ull << g.tile_log) < count) ++g.tile_log;
     g.tiles = (uint32_t)((count + (1ull << g.tile_log) - 1) >> g.tile_log);
     g.part_stride = up_to(cols, 4);
     return g;
