@@ -19,7 +19,8 @@
 //
 // The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero: a sum of 512 values of the contraction loses
 // 4.7e-7 of the result, of 768 about 1.6e-6.  Where the result is wanted in 32 bits, accumulators begin anew every 512 values, and the warps that
-// write add them up in registers, rounding to nearest: 4.8e-7 for 4096 values (plain sums in fp32: 6.1e-7).
+// write add them up in registers, rounding to nearest (SUMS): 4.8e-7 for 4096 values (plain sums in fp32: 6.1e-7).  So they do for results of 16 bits
+// where the contraction may have more than 2^16 values, which would lose a third of half a step of fp16.
 #pragma once
 
 #include "rows.cuh"
@@ -34,7 +35,8 @@ constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their rows (weights)
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
-constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers (results of 32 bits)
+constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers
+constexpr uint64_t kProductLong       = 1ull << 16;       // values of a contraction that results of 16 bits are not added up for
 constexpr uint32_t kProductTurned     = 2048u, kProductTurns = 3u;      // bytes of a box of a gradient of weights, and boxes of a warp on their way
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
@@ -185,10 +187,9 @@ __device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, ui
     __syncwarp();
 }
 
-template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads, 1) k_product(const __grid_constant__ ProductArgs a) {
+template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProductThreads, 1) k_product(const __grid_constant__ ProductArgs a) {
     extern __shared__ unsigned char raw[];
     __shared__ ProductShared s;
-    constexpr bool SUMS = sizeof(TO) == 4;                // accumulators are added up in registers
     const uint32_t warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u, block = blockIdx.x & 1u;
     const uint32_t pair = blockIdx.x / 2u, pairs = gridDim.x / 2u;
     const uint32_t stage0 = (smem_u32(raw) + 1023u) & ~1023u;
@@ -212,7 +213,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
     allow_next_kernel();
     product_tables<MODE>(a, s);
     const uint32_t tiles = s.tiles;
-    // (results of 32 bits: of 168 registers a thread at launch 96 x 128 + 200 x 256 are less than 168 x 384)
+    // (SUMS: of 168 registers a thread at launch 96 x 128 + 200 x 256 are less than 168 x 384)
     if (warp >= 4u) {                                     // results
         if constexpr (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         uint32_t turn = 0;
@@ -240,7 +241,7 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                         for (uint32_t v = 0; v < 4u; ++v) {
                             const uint32_t i = h + v * V;
                             uint4 x;
-                            if constexpr (SUMS) x = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
+                            if constexpr (sizeof(TO) == 4) x = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
                             else x = make_uint4(pack_two<TO>(f[i], f[i + 1]), pack_two<TO>(f[i + 2], f[i + 3]), pack_two<TO>(f[i + 4], f[i + 5]), pack_two<TO>(f[i + 6], f[i + 7]));
                             asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                         }
@@ -406,9 +407,10 @@ template <class TO, int MODE> __global__ void __launch_bounds__(kProductThreads,
                 for (uint32_t step = 0; step < p.steps; ++step) {
                     fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
                     if (!fine) break;
-                    if (MODE == kWeights && step + 1u == p.steps)
+                    const bool clear = MODE == kWeights && step + 1u == p.steps;
+                    if (clear)
                         product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
-                    if (lane == 0u) mbar_tell(&s.full[ring.stage], 0u);
+                    if (lane == 0u) { if (clear) mbar_tell<true>(&s.full[ring.stage], 0u); else mbar_tell(&s.full[ring.stage], 0u); }
                     ring.next(a.stages);
                 }
             }

@@ -200,8 +200,10 @@ int sort_rows(const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, 
 }
 uint64_t span_bytes(const fastsgd_experts* w) { return ((w->experts - 1) * w->expert_stride + (w->outs - 1) * w->row_stride + w->ins) * size_of(w->type); }
 
-template <int MODE> const void* product_kernel(uint32_t to) {
-    return to == FASTSGD_F32 ? (const void*)k_product<float, MODE> : to == FASTSGD_BF16 ? (const void*)k_product<__nv_bfloat16, MODE> : (const void*)k_product<__half, MODE>;
+template <int MODE> const void* product_kernel(uint32_t to, bool sums) {
+    if (to == FASTSGD_F32) return (const void*)k_product<float, MODE, true>;
+    if (to == FASTSGD_BF16) return sums ? (const void*)k_product<__nv_bfloat16, MODE, true> : (const void*)k_product<__nv_bfloat16, MODE, false>;
+    return sums ? (const void*)k_product<__half, MODE, true> : (const void*)k_product<__half, MODE, false>;
 }
 
 // `tiles`: at most
@@ -211,7 +213,7 @@ template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t 
     const uint32_t turned = MODE == kWeights ? 8u * kProductTurns * kProductTurned : 0u;
     a.stages = (uint32_t)((215u * 1024u - turned) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
-    const void* fn = product_kernel<MODE>(to);
+    const void* fn = product_kernel<MODE>(to, (MODE == kWeights ? a.rows : a.k) > kProductLong);
     const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + turned + 1024u;
     uint64_t resident = 0;
     const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);

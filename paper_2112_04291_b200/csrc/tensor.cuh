@@ -37,10 +37,13 @@ __device__ __forceinline__ void wait_stores() { asm volatile("cp.async.bulk.wait
 __device__ __forceinline__ void fence_async_reads() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // One more arrival on a barrier of another block of the pair, about operands and accumulators alone: what copies and matrix instructions have
-// written is complete when its own barrier says so, what threads have written to shared memory once they have fenced it.  (A release and
-// an acquire of the cluster's scope would order this thread's accesses to global memory, too, and cost a microsecond each.)
-__device__ __forceinline__ void mbar_tell(unsigned long long* bar, uint32_t block) {
-    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
+// written is complete when its own barrier says so, and what threads have written to shared memory once they have fenced it (RELEASE: they have).
+// An order of the cluster's scope would be one for this thread's accesses to global memory, too, and cost a microsecond each time.
+template <bool RELEASE = false> __device__ __forceinline__ void mbar_tell(unsigned long long* bar, uint32_t block) {
+    if constexpr (RELEASE)
+        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.release.cta.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
+    else
+        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
 }
 
 // ---- tensor memory, of a pair of blocks ---------------------------------------------------------

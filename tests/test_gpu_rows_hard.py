@@ -184,6 +184,26 @@ def test_products_are_the_same_every_time():
         assert i == 0 or all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("length", [512, 776, 4_096, 70_016])
+def test_long_contractions_lose_no_more_than_short_ones(length):
+    """Results of 32 bits against 64: relative, in the 2-norm.  512 values of a contraction are 32 steps of the tensor cores, each of which cuts off at
+    most the last bit of the accumulator (2^-23 of it), towards zero; an accumulator that grows evenly is half its last value on average: at most
+    32 2^-24 = 1.9e-6 of the sum of 512, and the sums of such pieces, whose signs differ, keep that share."""
+    g = torch.Generator(device="cuda").manual_seed(length)
+    a, c = (torch.randn((length, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    gw = _full((1, 128, 128), torch.float32)
+    assert binding.expert_product_backward_weights(a, c, torch.tensor([0, length], dtype=torch.int32, device="cuda"), gw) == 0
+    want = a.double().t() @ c.double()
+    assert (gw[0].double() - want).norm() <= 1.9e-6 * want.norm()
+    x, w, y = a.t().contiguous(), c.t().contiguous()[None], _full((128, 128), torch.float32)
+    assert binding.expert_product(x, w, torch.tensor([0, 128], dtype=torch.int32, device="cuda"), y) == 0
+    assert (y.double() - want).norm() <= 1.9e-6 * want.norm()
+    half = _full((128, 128), torch.float16)
+    assert binding.expert_product(x.half(), w.half(), torch.tensor([0, 128], dtype=torch.int32, device="cuda"), half) == 0
+    want = x.half().double() @ w[0].half().double().t()
+    assert (half.double() - want).abs().max() <= ref.rounding(want.abs().max().item(), "fp16") + 1.9e-6 * want.norm()
+
+
 @pytest.mark.parametrize("rows", [2_000, 40])
 def test_products_of_rows_with_infinities_and_nan_elsewhere(rows):
     """What a row holds shows in its own results, and in its own expert's gradient, alone."""
