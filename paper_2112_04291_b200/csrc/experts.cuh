@@ -271,6 +271,10 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
                 ++turn;
             };
             // (no rows: zero; a wait that ran out: not a number)
+            auto not_a_number = [&](float (&f)[32]) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(0x7FC00000u);
+            };
             if constexpr (SUMS) {
                 float sum[4][32];
 #pragma unroll
@@ -299,26 +303,28 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t c0 = 64u * (uint32_t)j + 32u * side;
-                    if (!fine) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) sum[j][i] = __uint_as_float(0x7FC00000u);
-                    }
+                    if (!fine) not_a_number(sum[j]);
                     if (c0 < p.n) write(sum[j], c0);
                 }
             } else {
+                // 64 columns at a time; the accumulator is given back before the last of them are written
                 if (p.steps) wait();
-                for (uint32_t c0 = 32u * side; c0 < p.n; c0 += 64u) {
-                    float f[32];
-                    uint32_t r[32];
-                    if (p.steps && fine) {
-                        tmem_load(from + (turn & 1u) * a.most_n + c0, r);
-                        tmem_wait(r);
+                const uint32_t at = from + (turn & 1u) * a.most_n + 32u * side;
+                for (uint32_t c0 = 32u * side; c0 < p.n || c0 == 32u * side; c0 += 128u) {
+                    float f[2][32] = {};
+                    if (p.steps) {
+#pragma unroll
+                        for (uint32_t j = 0; j < 2u; ++j) if (c0 + 64u * j < p.n) tmem_load(at + (c0 - 32u * side) + 64u * j, reinterpret_cast<uint32_t (&)[32]>(f[j]));
+#pragma unroll
+                        for (uint32_t j = 0; j < 2u; ++j) tmem_wait(reinterpret_cast<uint32_t (&)[32]>(f[j]));
+                        if (c0 + 128u >= p.n) give_back();
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = !p.steps ? 0.f : fine ? __uint_as_float(r[i]) : __uint_as_float(0x7FC00000u);
-                    write(f, c0);
+                    for (uint32_t j = 0; j < 2u; ++j) {
+                        if (!fine) not_a_number(f[j]);
+                        if (c0 + 64u * j < p.n) write(f[j], c0 + 64u * j);
+                    }
                 }
-                if (p.steps) give_back();
             }
         }
         if constexpr (MODE == kWeights) if (elect_one()) wait_stores();
