@@ -45,7 +45,7 @@ template <bool AGAIN = false, class T, bool WIDE> __device__ __forceinline__ voi
     } else {
         const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;      // (of every lane's columns alike)
         const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(row + c) - off);
-        const uint32_t bytes = c < cols ? (cols - c) * (uint32_t)sizeof(T) + off : 0u;      // from there to the row's end
+        const uint32_t bytes = c < cols ? min(cols - c, 64u) * (uint32_t)sizeof(T) + off : 0u;      // from there to the row's end, or more than there is to load
 #pragma unroll
         for (int i = 0; i <= N; ++i) if (16u * (uint32_t)i < bytes && (i < N || off)) p.v[i] = from[i];
     }
