@@ -58,6 +58,23 @@ __device__ __forceinline__ uint32_t cluster_block() { uint32_t r; asm("mov.u32 %
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Shared memory of the cluster's other blocks.
+__device__ __forceinline__ uint32_t address_in(const void* p, uint32_t block) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(block));
+    return r;
+}
+__device__ __forceinline__ uint32_t address_in_cluster(uint32_t at, uint32_t block) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(block));
+    return r;
+}
+__device__ __forceinline__ float4 load_four_from(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load_from(uint32_t at) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory"); return v; }
 
 // ---- dynamic rows -----------------------------------------------------------------------------
 // A grid has a block (or cluster) per piece of work.  One that is running asks for the launch of another to be cancelled and, when that

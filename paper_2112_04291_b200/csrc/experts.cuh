@@ -10,7 +10,8 @@
 //
 // A pair of blocks (two SMs) works on a tile: each copies half of A and half of B, so that an operand byte in shared memory serves twice as many
 // products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products, a third tells it what has
-// landed; eight write results, while the next tile's products go into the other half of the accumulators.  A single thread issues copies and
+// landed; eight write results, while the next tile's products go into the other half of the accumulators.  Where there are few tiles of a long
+// contraction, up to eight pairs of a cluster share each, and add up what they have through their shared memory.  A single thread issues copies and
 // products: what bounds the rate is then the tensor cores (and the GPU's power) alone.  Bounds, measured, with sorted rows and one GPU to itself:
 //   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1390 us each way (1380 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
 //   49152 x 2048 x 1408, 64 experts: 205 to 230 us (1230 to 1390 TFLOP/s; 19 rounds of tiles, the last partly filled, 5.5 tiles of 256 outs)
@@ -48,6 +49,7 @@ struct alignas(64) ProductArgs {
     void*     out;
     uint64_t  out_stride, out_expert;
     uint32_t  most_n, box, stages;                        // columns of a tile at most; rows of a copy of B
+    uint32_t  splits;                                     // pairs of blocks that share a tile's contraction (a cluster; then a tile each)
     uint32_t  kind;
     uint32_t  tries;
 };
@@ -64,7 +66,7 @@ struct ProductShared {
     unsigned long long ready[2];                          // an accumulator's products are done
     unsigned long long taken[2];                          // (first block) ... and have been read, by both blocks
     unsigned long long drained;
-    uint32_t tmem, tiles;
+    uint32_t tmem, tiles, lost;                           // lost: (a shared contraction) a wait of this block's has run out
     uint32_t first_row[kProductMaxExperts + 1];
     uint32_t first_tile[kProductMaxExperts];              // (forward, input) of the experts in their order
     uint16_t expert_at[kProductMaxExperts];               // that order
@@ -77,7 +79,8 @@ struct ProductRing {
 };
 
 struct ProductTile {
-    uint32_t expert, m0, n0, n, half, row, end, steps;    // n0: first row (weights: in); half: columns of a block's B; rows row .. end; steps of the contraction
+    uint32_t expert, m0, n0, n, half, row, end;           // n0: first row (weights: in); half: columns of a block's B; rows row .. end
+    uint32_t step0, steps, all_steps;                     // of the contraction: this pair's, and all
 };
 
 // columns of each of the tiles that an expert's rows make (forward, input): as few tiles as hold them, of equal length
@@ -86,7 +89,7 @@ __device__ __forceinline__ uint32_t product_columns(uint32_t rows, uint32_t most
     return nt ? ((rows + nt - 1u) / nt + 31u) & ~31u : 0u;
 }
 
-template <int MODE> __device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, const ProductShared& s, uint32_t t) {
+template <int MODE, bool SPLIT> __device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, const ProductShared& s, uint32_t t, uint32_t share) {
     ProductTile p;
     const uint32_t mt = (a.m + kProductM - 1u) / kProductM;
     if constexpr (MODE == kWeights) {
@@ -99,7 +102,7 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
         p.n = min(a.most_n, a.n - p.n0);
         p.row = s.first_row[p.expert];
         p.end = s.first_row[p.expert + 1u];
-        p.steps = (p.end - p.row + kProductK - 1u) / kProductK;
+        p.all_steps = (p.end - p.row + kProductK - 1u) / kProductK;
     } else {
         uint32_t lo = 0, hi = a.experts;                  // the last expert whose tiles begin at t or before
         while (hi - lo > 1u) {
@@ -116,9 +119,14 @@ template <int MODE> __device__ __forceinline__ ProductTile product_tile(const Pr
         p.n = min(each, end - p.n0);
         p.row = p.n0;
         p.end = p.n0 + p.n;
-        p.steps = (a.k + kProductK - 1u) / kProductK;
+        p.all_steps = (a.k + kProductK - 1u) / kProductK;
     }
     p.half = ((p.n + 31u) & ~31u) / 2u;
+    p.step0 = 0; p.steps = p.all_steps;
+    if constexpr (SPLIT) {
+        p.step0 = (uint32_t)((uint64_t)p.all_steps * share / a.splits);
+        p.steps = (uint32_t)((uint64_t)p.all_steps * (share + 1u) / a.splits) - p.step0;
+    }
     return p;
 }
 
@@ -187,11 +195,40 @@ __device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, ui
     __syncwarp();
 }
 
-template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProductThreads, 1) k_product(const __grid_constant__ ProductArgs a) {
+// A shared contraction: a block keeps its sums in lines that lie as those of the result do, a line a column of the tile (forward, input) or a row of it.
+// Words of a line (weights: a vector more than 256, which keeps rows off one another's banks).
+template <int MODE> __device__ __forceinline__ constexpr uint32_t product_line() { return MODE == kWeights ? 260u : kProductM / 2u; }
+// Each of the cluster's blocks adds up every splits-th line of its half of the tile, in the order of the shares: a warp a line, four values a lane.  The
+// eight warps that write (they have the registers).
+template <class TO, int MODE> __device__ __forceinline__ void product_join(const ProductArgs& a, ProductShared& s, const ProductTile& p, uint32_t stage0, uint32_t share, uint32_t block) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32u - 4u;
+    bool lost = lane < 2u * a.splits && load_from(address_in(&s.lost, lane % (2u * a.splits))) != 0u;
+    lost = __any_sync(kFullMask, lost);
+    const uint32_t along = MODE == kWeights ? p.n : kProductM / 2u, lines = MODE == kWeights ? kProductM / 2u : p.n, row0 = p.m0 + block * (kProductM / 2u);
+    for (uint32_t line = share + a.splits * warp; line < lines; line += a.splits * 8u)
+        for (uint32_t i = 4u * lane; i < along; i += 128u) {
+            if (MODE == kWeights ? row0 + line >= a.m : row0 + i >= a.m) continue;      // (a.m is a multiple of 8)
+            float4 part[8];
+            float sum[4] = {};
+#pragma unroll
+            for (uint32_t j = 0; j < 8u; ++j) if (j < a.splits) part[j] = load_four_from(address_in_cluster(stage0 + 4u * (line * product_line<MODE>() + i), 2u * j + block));
+#pragma unroll
+            for (uint32_t j = 0; j < 8u; ++j) if (j < a.splits) { sum[0] += part[j].x; sum[1] += part[j].y; sum[2] += part[j].z; sum[3] += part[j].w; }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (lost) sum[j] = __uint_as_float(0x7FC00000u);
+            TO* to = static_cast<TO*>(a.out) + (MODE == kWeights ? p.expert * a.out_expert + (row0 + line) * a.out_stride + p.n0 + i : (uint64_t)(p.n0 + line) * a.out_stride + row0 + i);
+            if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(to) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            else *reinterpret_cast<uint2*>(to) = make_uint2(pack_two<TO>(sum[0], sum[1]), pack_two<TO>(sum[2], sum[3]));
+        }
+}
+
+template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bounds__(kProductThreads, 1) k_product(const __grid_constant__ ProductArgs a) {
     extern __shared__ unsigned char raw[];
     __shared__ ProductShared s;
-    const uint32_t warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u, block = blockIdx.x & 1u;
-    const uint32_t pair = blockIdx.x / 2u, pairs = gridDim.x / 2u;
+    const uint32_t warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+    // the pair's first block, this one of the two, the pair's share of a contraction (pairs of a cluster), and the pair, or cluster, among all
+    const uint32_t leader = SPLIT ? cluster_block() & ~1u : 0u, block = blockIdx.x & 1u, share = leader / 2u, both = 3u << leader;
+    const uint32_t splits = SPLIT ? a.splits : 1u, pair = blockIdx.x / (2u * splits), pairs = gridDim.x / (2u * splits);
     const uint32_t stage0 = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t stage_bytes = product_stage_bytes<MODE>(a.most_n);
     uint32_t columns = 32u;
@@ -200,6 +237,7 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
         for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.landed[i], 1u); mbar_init(&s.full[i], 2u); mbar_init(&s.empty[i], 1u); }
         for (uint32_t i = 0; i < 2u; ++i) { mbar_init(&s.ready[i], 1u); mbar_init(&s.taken[i], 16u); }
         mbar_init(&s.drained, 1u);
+        s.lost = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -223,11 +261,23 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
         uint32_t at_turn = 0;
         for (uint32_t t = pair, turns = 0; turns * pairs < tiles; t = product_turn(++turns, pair, pairs)) {
             if (t >= tiles) continue;
-            const ProductTile p = product_tile<MODE>(a, s, t);
+            const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
             const uint32_t row0 = p.m0 + block * kProductM / 2u + 32u * part;
             const uint32_t from = tmem + (32u * part << 16);
             auto write = [&](const float (&f)[32], uint32_t c0) {
-                if constexpr (MODE == kWeights) {
+                if constexpr (SPLIT) {                    // (a shared contraction: this pair's sums, where its operands were, for all to add up)
+                    const uint32_t row = 32u * part + lane;
+                    if constexpr (MODE == kWeights) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(stage0 + 4u * (row * product_line<MODE>() + c0 + (uint32_t)i)), "f"(f[i]), "f"(f[i + 1]), "f"(f[i + 2]), "f"(f[i + 3]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (c0 + (uint32_t)i < p.n) asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage0 + 4u * ((c0 + (uint32_t)i) * product_line<MODE>() + row)), "f"(f[i]) : "memory");
+                    }
+                    if (!fine) s.lost = 1u;
+                } else if constexpr (MODE == kWeights) {
                     // A lane holds 32 columns of a row of its own: 64 bytes of each of 32 rows at a time go through shared memory (in
                     // the order of vectors that a copy of 64-byte rows has, which keeps rows off one another's banks) and from there by a copy.
                     constexpr uint32_t V = Vec<TO>::N, COLS = 4u * V;
@@ -267,7 +317,7 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
             auto give_back = [&]() {
                 tmem_before_barrier();
                 __syncwarp();
-                if (lane == 0u) mbar_tell(&s.taken[turn & 1u], 0u);
+                if (lane == 0u) mbar_tell(&s.taken[turn & 1u], leader);
                 ++turn;
             };
             // (no rows: zero; a wait that ran out: not a number)
@@ -327,7 +377,7 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
                 }
             }
         }
-        if constexpr (MODE == kWeights) if (elect_one()) wait_stores();
+        if constexpr (MODE == kWeights && !SPLIT) if (elect_one()) wait_stores();
     } else {
         if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         if (warp == 0u) {                                     // copies of tiles
@@ -337,12 +387,12 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
                 bool fine = true;
                 for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
                     if (t >= tiles) continue;
-                    const ProductTile p = product_tile<MODE>(a, s, t);
+                    const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
                     const uint32_t boxes = (p.half + a.box - 1u) / a.box, strips = (p.half + 63u) / 64u;
                     const uint32_t bytes = kProductM / 2u * 128u + (MODE == kWeights ? strips * 8192u : boxes * a.box * 128u);
                     const int m0 = (int)(p.m0 + block * kProductM / 2u);
                     const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
-                    int at = MODE == kWeights ? (int)p.row : 0;            // in the contraction
+                    int at = (int)((MODE == kWeights ? p.row : 0u) + p.step0 * kProductK);      // in the contraction
                     for (uint32_t step = 0; step < p.steps; ++step, at += (int)kProductK) {
                         fine = mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
                         if (!fine) break;
@@ -377,7 +427,7 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
                 bool fine = true;
                 for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
                     if (t >= tiles) continue;
-                    const ProductTile p = product_tile<MODE>(a, s, t);
+                    const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
                     const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
                     uint32_t acc = 0;
                     for (uint32_t step = 0; step < p.steps; ++step) {
@@ -394,12 +444,12 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
                         constexpr uint32_t STEP_A = (MODE == kForward ? 32u : 2048u) >> 4, STEP_B = (MODE == kWeights ? 2048u : 32u) >> 4;
 #pragma unroll
                         for (uint32_t i = 0; i < kProductK / 16u; ++i) multiply(acc, da + STEP_A * i, db + STEP_B * i, shape, !begins || i);
-                        products_arrive(&s.empty[ring.stage]);
-                        if (ends) { products_arrive(&s.ready[turn & 1u]); ++turn; }
+                        products_arrive(&s.empty[ring.stage], both);
+                        if (ends) { products_arrive(&s.ready[turn & 1u], both); ++turn; }
                         ring.next(a.stages);
                     }
                 }
-                products_arrive(&s.drained);                  // no product is under way any more when the accumulators are given back
+                products_arrive(&s.drained, both);                  // no product is under way any more when the accumulators are given back
                 mbar_wait(&s.drained, 0u);
             }
         } else if (warp == 1u) {
@@ -409,14 +459,14 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
             bool fine = true;
             for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
                 if (t >= tiles) continue;
-                const ProductTile p = product_tile<MODE>(a, s, t);
+                const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
                 for (uint32_t step = 0; step < p.steps; ++step) {
                     fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
                     if (!fine) break;
-                    const bool clear = MODE == kWeights && step + 1u == p.steps;
+                    const bool clear = MODE == kWeights && p.step0 + step + 1u == p.all_steps;
                     if (clear)
-                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - step * kProductK);
-                    if (lane == 0u) { if (clear) mbar_tell<true>(&s.full[ring.stage], 0u); else mbar_tell(&s.full[ring.stage], 0u); }
+                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - (p.step0 + step) * kProductK);
+                    if (lane == 0u) { if (clear) mbar_tell<true>(&s.full[ring.stage], leader); else mbar_tell(&s.full[ring.stage], leader); }
                     ring.next(a.stages);
                 }
             }
@@ -428,6 +478,11 @@ template <class TO, int MODE, bool SUMS> __global__ void __launch_bounds__(kProd
     cluster_meet();                                       // (neither block ends, or frees its accumulators, while the other's products or signals may need it)
     tmem_after_barrier();
     if (warp == 3u) tmem_free(tmem, columns);
+    if constexpr (SPLIT) {
+        if (warp >= 4u && pair < tiles) product_join<TO, MODE>(a, s, product_tile<MODE, SPLIT>(a, s, pair, share), stage0, share, block);
+        __syncwarp();
+        cluster_meet();                                   // (no block ends while others read its sums)
+    }
 }
 
 }  // namespace fsg

@@ -117,12 +117,6 @@ __device__ __forceinline__ void order_over_warps(uint16_t* counts, uint32_t bins
     }
 }
 
-__device__ __forceinline__ uint32_t address_in(const void* p, uint32_t block) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(block));
-    return r;
-}
-__device__ __forceinline__ uint32_t load_from(uint32_t at) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory"); return v; }
 __device__ __forceinline__ void store_to(uint32_t at, uint32_t v, uint32_t w) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(v), "r"(w) : "memory"); }
 
 struct OrderShared {

@@ -200,29 +200,42 @@ int sort_rows(const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, 
 }
 uint64_t span_bytes(const fastsgd_experts* w) { return ((w->experts - 1) * w->expert_stride + (w->outs - 1) * w->row_stride + w->ins) * size_of(w->type); }
 
-template <int MODE> const void* product_kernel(uint32_t to, bool sums) {
-    if (to == FASTSGD_F32) return (const void*)k_product<float, MODE, true>;
-    if (to == FASTSGD_BF16) return sums ? (const void*)k_product<__nv_bfloat16, MODE, true> : (const void*)k_product<__nv_bfloat16, MODE, false>;
-    return sums ? (const void*)k_product<__half, MODE, true> : (const void*)k_product<__half, MODE, false>;
+template <class TO, int MODE> const void* product_kernel_of(bool sums, bool split) {
+    if (split) return (const void*)k_product<TO, MODE, true, true>;
+    if constexpr (sizeof(TO) == 4) return (const void*)k_product<TO, MODE, true, false>;
+    else return sums ? (const void*)k_product<TO, MODE, true, false> : (const void*)k_product<TO, MODE, false, false>;
+}
+template <int MODE> const void* product_kernel(uint32_t to, bool sums, bool split) {
+    return to == FASTSGD_F32 ? product_kernel_of<float, MODE>(sums, split) : to == FASTSGD_BF16 ? product_kernel_of<__nv_bfloat16, MODE>(sums, split) : product_kernel_of<__half, MODE>(sums, split);
 }
 
-// `tiles`: at most
-template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint32_t to, const DeviceView& dev, cudaStream_t st) {
+// `tiles`: at most; `steps`: of a contraction, about
+template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint64_t steps, uint32_t to, const DeviceView& dev, cudaStream_t st) {
     if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
     a.tries = dev.tries;
     const uint32_t turned = MODE == kWeights ? 8u * kProductTurns * kProductTurned : 0u;
     a.stages = (uint32_t)((215u * 1024u - turned) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
-    const void* fn = product_kernel<MODE>(to, (MODE == kWeights ? a.rows : a.k) > kProductLong);
+    // Few tiles of a contraction of at least `least` stages: up to eight pairs of blocks share it, as long as each has eight stages, and as clusters
+    // of them all find room at once (of sixteen blocks one in each of the GPU's groups of 16 to 20 SMs, of eight and four two and four).  Adding up
+    // wide tiles takes as long as some 30 stages, and those of the weights' gradients are 256 wide.  Unshared and shared, us:
+    //   8 rows, 1024 / 2048 / 4096 -> 512: 7.7, 11.0, 17.5 and 7.5, 7.5, 7.9;  200 rows, 2048 -> 1024: 13.7 and 11.1, 1024 -> 2048: 9.8 and 12.1
+    //   gradient of 512 x 512 weights, 2000 / 4096 / 60000 rows: 16.3, 24.9, 290 and 18.2, 16.5, 69
+    const uint64_t least = a.most_n <= 64u ? 16u : MODE == kWeights ? 48u : 32u;
+    a.splits = 1u;
+    while (a.splits < 8u && tiles * a.splits * 2u <= 8ull * ((uint64_t)dev.sm_count / 20u) && steps >= (a.splits > 1u ? a.splits * 16ull : least)) a.splits *= 2u;
+    const void* fn = product_kernel<MODE>(to, (MODE == kWeights ? a.rows : a.k) > kProductLong, a.splits > 1u);
     const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + turned + 1024u;
     uint64_t resident = 0;
     const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);
     if (rc) return rc;
-    const uint64_t pairs = tiles < resident / 2u ? tiles : resident / 2u;
+    const uint64_t clusters = a.splits > 1u || tiles < resident / 2u ? tiles : resident / 2u;
     void* kargs[] = {&a};
-    return launched(launch_overlapped(fn, (unsigned)(2u * pairs), kProductThreads, smem, kargs, st, 2u));
+    return launched(launch_overlapped(fn, (unsigned)(2u * a.splits * clusters), kProductThreads, smem, kargs, st, 2u * a.splits));
 }
 
+// tiles of the rows, at most: every expert that has any may have one that is not full
+uint64_t row_tiles(uint64_t rows, uint64_t experts, uint32_t most_n) { return rows / most_n + (experts < rows ? experts : rows); }
 // Columns of a tile where the rows' side is ragged: enough for most experts' rows in one.
 uint32_t columns_for(uint64_t rows, uint64_t experts) {
     uint32_t n = 32u;
@@ -375,7 +388,7 @@ int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint3
     a.starts = starts; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)y->rows;
     a.m = (uint32_t)weights->outs; a.k = (uint32_t)weights->ins; a.out = y->data; a.out_stride = y->row_stride;
     a.kind = product_kind(x->type == FASTSGD_BF16, false, false);
-    return launch_product<kForward>(a, (y->rows / a.most_n + weights->experts) * ((weights->outs + kProductM - 1) / kProductM), y->type, dev, static_cast<cudaStream_t>(stream));
+    return launch_product<kForward>(a, row_tiles(y->rows, weights->experts, a.most_n) * ((weights->outs + kProductM - 1) / kProductM), weights->ins / kProductK, y->type, dev, static_cast<cudaStream_t>(stream));
 }
 
 int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const uint32_t* starts, const fastsgd_experts* weights, const fastsgd_matrix* grad_x, void* stream) {
@@ -401,7 +414,7 @@ int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const ui
     a.starts = starts; a.experts = (uint32_t)weights->experts; a.rows = (uint32_t)grad_y->rows;
     a.m = (uint32_t)weights->ins; a.k = (uint32_t)weights->outs; a.out = grad_x->data; a.out_stride = grad_x->row_stride;
     a.kind = product_kind(grad_y->type == FASTSGD_BF16, true, false);
-    return launch_product<kInput>(a, (grad_y->rows / a.most_n + weights->experts) * ((weights->ins + kProductM - 1) / kProductM), grad_x->type, dev, static_cast<cudaStream_t>(stream));
+    return launch_product<kInput>(a, row_tiles(grad_y->rows, weights->experts, a.most_n) * ((weights->ins + kProductM - 1) / kProductM), weights->outs / kProductK, grad_x->type, dev, static_cast<cudaStream_t>(stream));
 }
 
 int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row, const uint32_t* starts, const fastsgd_experts* grad_weights,
@@ -434,7 +447,8 @@ int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const 
     a.starts = starts; a.experts = (uint32_t)grad_weights->experts;
     a.m = (uint32_t)grad_weights->outs; a.n = (uint32_t)grad_weights->ins; a.out = grad_weights->data; a.out_stride = grad_weights->row_stride; a.out_expert = grad_weights->expert_stride;
     a.kind = product_kind(x->type == FASTSGD_BF16, true, true);
-    return launch_product<kWeights>(a, grad_weights->experts * ((grad_weights->outs + kProductM - 1) / kProductM) * ((grad_weights->ins + a.most_n - 1) / a.most_n), grad_weights->type, dev,
+    return launch_product<kWeights>(a, grad_weights->experts * ((grad_weights->outs + kProductM - 1) / kProductM) * ((grad_weights->ins + a.most_n - 1) / a.most_n), a.rows / grad_weights->experts / kProductK,
+                                    grad_weights->type, dev,
                                     static_cast<cudaStream_t>(stream));
 }
 

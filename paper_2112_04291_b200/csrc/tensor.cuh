@@ -100,9 +100,9 @@ __device__ __forceinline__ void multiply(uint32_t acc, uint32_t a, uint32_t b, u
                  " tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n}"
                  ::"r"(acc), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandWord) : "memory");
 }
-// arrives on the barrier, in both blocks, once the products that this thread has issued are done
-__device__ __forceinline__ void products_arrive(unsigned long long* bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+// arrives on the barrier, in both blocks of the pair (`pair`: their bits among the cluster's), once the products that this thread has issued are done
+__device__ __forceinline__ void products_arrive(unsigned long long* bar, uint32_t pair) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)pair) : "memory");
 }
 
 }  // namespace fsg

@@ -302,6 +302,14 @@ def test_products(dtype, out, tokens, experts, k, ins, outs, whole):
     _check_products(np.random.default_rng(tokens + ins), tokens, experts, k, ins, outs, dtype, out, whole)
 
 
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("tokens,experts,k,ins,outs", [(1, 1, 1, 4096, 264), (8, 1, 1, 8200, 520), (3, 4, 2, 2056, 1032), (40, 2, 1, 1032, 3080), (300, 1, 1, 2048, 1288), (5000, 1, 1, 64, 72), (9000, 3, 1, 272, 136),
+                                                       (20_000, 2, 2, 8, 264)])
+@pytest.mark.parametrize("whole", [True, False])
+def test_products_of_few_tiles_and_long_contractions(dtype, out, tokens, experts, k, ins, outs, whole):
+    _check_products(np.random.default_rng(tokens + ins), tokens, experts, k, ins, outs, dtype, out, whole)
+
+
 @pytest.mark.parametrize("tokens,experts,k,ins,outs", [(3, 8, 2, 72, 136), (257, 2, 2, 320, 1000), (700, 60, 4, 120, 88)])
 @pytest.mark.parametrize("gap,between", [(8, 0), (0, 8), (24, 16)])
 def test_products_of_strided_matrices(tokens, experts, k, ins, outs, gap, between):
