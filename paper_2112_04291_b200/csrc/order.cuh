@@ -7,7 +7,7 @@
 // digits, of its digit in earlier blocks, in earlier warps, and before it in its warp.  No place depends on the order in which threads run.
 //
 // Up to 2^16 ids are sorted by one cluster of sixteen blocks in its shared memory (k_order): no launch between digits and no
-// workspace; up to 2^11 are each compared with all others instead.  More take three launches a digit (k_order_count, k_order_offsets, k_order_place), with keys and positions in the workspace.
+// workspace; up to 2^11 are each compared with all others instead.  More take three launches a digit (k_order_tile counts, k_order_offsets, k_order_tile places), with keys and positions in the workspace.
 #pragma once
 
 #include "async.cuh"
