@@ -38,7 +38,10 @@ constexpr uint32_t kProductSorted     = 256u;             // experts that are pu
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers
 constexpr uint64_t kProductLong       = 1ull << 16;       // values of a contraction that results of 16 bits are not added up for
-constexpr uint32_t kProductTurned     = 2048u, kProductTurns = 3u;      // bytes of a box of a gradient of weights, and boxes of a warp on their way
+// Bytes of a box of a gradient of weights; each warp that writes has one.  With two or three, which it would wait for less, or with boxes of rows of
+// 128 bytes, there is room for five or four stages instead of six: 49152 x 2048 x 1408 of 64 experts 239 us as it is, 246, 245 (128) and 259 (two of
+// 128); to fp32 288, 298, 297, 319; 8192 x 2048 x 2048 of 8 52, 54, 54.5, 58; 4096 x 1016 x 680 of 60 30.6, 31.2, 29.8, 30.0.
+constexpr uint32_t kProductTurned     = 2048u;
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 
 struct alignas(64) ProductArgs {
@@ -257,8 +260,7 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
         uint32_t turn = 0;
         bool fine = true;
         const uint32_t part = warp & 3u, side = (warp - 4u) >> 2;         // lanes; every other 32 columns
-        const uint32_t turned = stage0 + a.stages * stage_bytes + (warp - 4u) * kProductTurns * kProductTurned;      // (weights)
-        uint32_t at_turn = 0;
+        const uint32_t turned = stage0 + a.stages * stage_bytes + (warp - 4u) * kProductTurned;      // (weights)
         for (uint32_t t = pair, turns = 0; turns * pairs < tiles; t = product_turn(++turns, pair, pairs)) {
             if (t >= tiles) continue;
             const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
@@ -284,24 +286,22 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
 #pragma unroll
                     for (uint32_t h = 0; h < 32u; h += COLS) {
                         if (c0 + h >= p.n || row0 >= a.m) continue;
-                        if (elect_one()) wait_stores_read<(int)kProductTurns - 1>();      // (the copy that had this place has read it)
+                        if (elect_one()) wait_stores_read<0>();      // (the copy before has read it)
                         __syncwarp();
-                        const uint32_t place = turned + at_turn * kProductTurned;
 #pragma unroll
                         for (uint32_t v = 0; v < 4u; ++v) {
                             const uint32_t i = h + v * V;
                             uint4 x;
                             if constexpr (sizeof(TO) == 4) x = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
                             else x = make_uint4(pack_two<TO>(f[i], f[i + 1]), pack_two<TO>(f[i + 2], f[i + 3]), pack_two<TO>(f[i + 4], f[i + 5]), pack_two<TO>(f[i + 6], f[i + 7]));
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(turned + lane * 64u + ((v ^ (lane >> 1 & 3u)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                         }
                         fence_async_reads();
                         __syncwarp();
                         if (elect_one()) {
-                            tile_store_3d(&a.out_map, (int)(p.n0 + c0 + h), (int)row0, (int)p.expert, place);
+                            tile_store_3d(&a.out_map, (int)(p.n0 + c0 + h), (int)row0, (int)p.expert, turned);
                             stores_end_group();
                         }
-                        at_turn = at_turn + 1u == kProductTurns ? 0u : at_turn + 1u;
                     }
                 } else {
                     if (row0 + lane >= a.m) return;

@@ -213,7 +213,7 @@ template <int MODE> const void* product_kernel(uint32_t to, bool sums, bool spli
 template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint64_t steps, uint32_t to, const DeviceView& dev, cudaStream_t st) {
     if (tiles >= 1ull << 31) return FASTSGD_E_BAD_N;
     a.tries = dev.tries;
-    const uint32_t turned = MODE == kWeights ? 8u * kProductTurns * kProductTurned : 0u;
+    const uint32_t turned = MODE == kWeights ? 8u * kProductTurned : 0u;
     a.stages = (uint32_t)((215u * 1024u - turned) / product_stage_bytes<MODE>(a.most_n));
     if (a.stages > kProductMaxStages) a.stages = kProductMaxStages;
     // Few tiles of a contraction of at least `least` stages: up to eight pairs of blocks share it, as long as each has eight stages, and as clusters
