@@ -16,7 +16,7 @@
 //   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1390 us each way (1380 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
 //   49152 x 2048 x 1408, 64 experts: 205 to 230 us (1230 to 1390 TFLOP/s; 19 rounds of tiles, the last partly filled, 5.5 tiles of 256 outs)
 //   32 x 4096 x 14336, 8 experts: 142 to 155 us, the weights' 940 MB at a copy's rate
-//   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 305 to 340 us, 738 MB written while 340 MB are read; bf16 235
+//   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 281 to 340 us, 738 MB written while 340 MB are read; bf16 234 to 270
 //
 // The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero: a sum of 512 values of the contraction loses
 // 4.7e-7 of the result, of 768 about 1.6e-6.  Where the result is wanted in 32 bits, accumulators begin anew every 512 values, and the warps that
