@@ -55,7 +55,9 @@ __device__ __forceinline__ void bulk_load(void* dst_smem, const void* src_global
 // ---- clusters ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_block() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 // Every thread of the cluster's blocks; what they wrote before, to shared or global memory, is visible behind it.
+// (The instructions want each warp as one: its lanes come together first, wherever they have been.)
 __device__ __forceinline__ void cluster_meet() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Shared memory of the cluster's other blocks.

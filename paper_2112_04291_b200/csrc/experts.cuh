@@ -304,14 +304,15 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                         }
                     }
                 } else {
-                    if (row0 + lane >= a.m) return;
+                    const bool in = row0 + lane < a.m;
                     TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + row0 + lane;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) if (c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
+                    for (int i = 0; i < 32; ++i) if (in && c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
                 }
             };
             auto wait = [&]() {
                 if (fine) fine = __all_sync(kFullMask, mbar_wait(&s.ready[turn & 1u], turn / 2u & 1u, a.tries));
+                __syncwarp();
                 tmem_after_barrier();
             };
             auto give_back = [&]() {
@@ -363,6 +364,7 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                 for (uint32_t c0 = 32u * side; c0 < p.n || c0 == 32u * side; c0 += 128u) {
                     float f[2][32] = {};
                     if (p.steps) {
+                        __syncwarp();                     // (a warp reads an accumulator as one: its lanes, or the one that copies, may have written apart)
 #pragma unroll
                         for (uint32_t j = 0; j < 2u; ++j) if (c0 + 64u * j < p.n) tmem_load(at + (c0 - 32u * side) + 64u * j, reinterpret_cast<uint32_t (&)[32]>(f[j]));
 #pragma unroll

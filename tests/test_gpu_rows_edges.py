@@ -1,0 +1,35 @@
+"""The operators on rows chosen by an id where a part of a warp, a block of a pair, a workspace or a rounding could go wrong.
+
+Values are small whole numbers where nothing else is said, so that every sum is exact in fp32 and fp16 whatever its order."""
+import pytest
+import torch
+
+from paper_2112_04291_b200 import binding
+
+pytestmark = pytest.mark.gpu
+MARK = -77.0
+
+
+def _whole(shape, most, dtype, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda").to(dtype)
+
+
+def _full(shape, dtype=torch.int32, value=-9):
+    return torch.full(shape, value, dtype=dtype, device="cuda")
+
+
+@pytest.mark.parametrize("ins,outs", [(40, 264), (264, 40), (72, 1000), (8, 8), (136, 488), (776, 520)])
+@pytest.mark.parametrize("rows", [129, 200, 256, 700, 5_000])
+def test_products_whose_last_lanes_have_nothing_to_write(rows, ins, outs):
+    """Outs and ins that are a multiple of 8 but not of 32, in tiles of more than 128 rows: some lanes of a warp write nothing and all of them read the next columns."""
+    x, w, gy = _whole((rows, ins), 1, torch.float16, 1), _whole((2, outs, ins), 1, torch.float16, 2), _whole((rows, outs), 1, torch.float16, 3)
+    starts = torch.tensor([0, rows // 5, rows], dtype=torch.int32, device="cuda")
+    for dtype in (torch.float16, torch.float32):
+        y, gx, gw = _full((rows, outs), dtype, MARK), _full((rows, ins), dtype, MARK), _full(w.shape, dtype, MARK)
+        assert binding.expert_product(x, w, starts, y) == 0 and binding.expert_product_backward_input(gy, w, starts, gx) == 0
+        assert binding.expert_product_backward_weights(gy, x, starts, gw) == 0
+        for e, part in enumerate((slice(0, rows // 5), slice(rows // 5, rows))):
+            assert torch.equal(y[part].double(), x[part].double() @ w[e].double().t())
+            assert torch.equal(gx[part].double(), gy[part].double() @ w[e].double())
+            assert torch.equal(gw[e].double(), gy[part].double().t() @ x[part].double())
