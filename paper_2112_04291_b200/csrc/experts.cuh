@@ -304,10 +304,11 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                         }
                     }
                 } else {
-                    const bool in = row0 + lane < a.m;
-                    TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + row0 + lane;
+                    if (row0 + lane < a.m) {
+                        TO* to = static_cast<TO*>(a.out) + (uint64_t)(p.n0 + c0) * a.out_stride + row0 + lane;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) if (in && c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
+                        for (int i = 0; i < 32; ++i) if (c0 + (uint32_t)i < p.n) to[(uint64_t)i * a.out_stride] = from_float<TO>(f[i]);
+                    }
                 }
             };
             auto wait = [&]() {
