@@ -9,8 +9,12 @@
 // which bound the time where rows are few, fill whole tiles.
 //
 // A pair of blocks (two SMs) works on a tile: each copies half of A and half of B, so that an operand byte in shared memory serves twice as many
-// products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products, a third tells it what has
-// landed; eight write results, while the next tile's products go into the other half of the accumulators.  Where there are few tiles of a long
+// products as with one block.  In each block a warp copies tiles, a second (the first block's) issues the products; eight write results, while the
+// next tile's products go into the other half of the accumulators.  What both blocks copy completes on a barrier of the first block, where the
+// products wait.  (A thread that told it what has landed in the second block would have to release at the cluster's scope, which takes a microsecond
+// a stage: 16384 x 4096 x 14336 in 3290 us.)  Only where rows behind an expert's last are cleared, once a tile of the weights' gradients, do two
+// further warps of each block so (with one, 40 rows, 8 experts, 14336 x 4096: 249 us, with two 163; 512 rows, nothing to clear, 160).  Waits for what
+// the other block's threads, copies or products signal are of the cluster's scope; that costs nothing that could be measured.  Where there are few tiles of a long
 // contraction, up to eight pairs of a cluster share each, and add up what they have through their shared memory.  A single thread issues copies and
 // products: what bounds the rate is then the tensor cores (and the GPU's power) alone.  Bounds, measured, with sorted rows and one GPU to itself:
 //   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1390 us each way (1380 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
@@ -63,13 +67,15 @@ template <int MODE> __host__ __device__ constexpr uint32_t product_stage_bytes(u
 }
 
 struct ProductShared {
-    unsigned long long landed[kProductMaxStages];         // this block's copies
+    unsigned long long landed[kProductMaxStages];         // (weights) this block's copies of a stage whose last rows are to be cleared
     unsigned long long full[kProductMaxStages];           // (first block) both blocks' operands
     unsigned long long empty[kProductMaxStages];          // the products that read them are done
     unsigned long long ready[2];                          // an accumulator's products are done
     unsigned long long taken[2];                          // (first block) ... and have been read, by both blocks
     unsigned long long drained;
     uint32_t tmem, tiles, lost;                           // lost: (a shared contraction) a wait of this block's has run out
+    uint32_t gave_up;                                     // a thread of the pair's that copies or multiplies has
+    uint32_t issued[2], cleared[2];                       // of each block: stages copied; those whose last copies are its own `landed`'s (bits)
     uint32_t first_row[kProductMaxExperts + 1];
     uint32_t first_tile[kProductMaxExperts];              // (forward, input) of the experts in their order
     uint16_t expert_at[kProductMaxExperts];               // that order
@@ -84,6 +90,7 @@ struct ProductRing {
 struct ProductTile {
     uint32_t expert, m0, n0, n, half, row, end;           // n0: first row (weights: in); half: columns of a block's B; rows row .. end
     uint32_t step0, steps, all_steps;                     // of the contraction: this pair's, and all
+    bool     clears;                                      // (weights) the last of this pair's stages holds rows behind `end`
 };
 
 // columns of each of the tiles that an expert's rows make (forward, input): as few tiles as hold them, of equal length
@@ -130,6 +137,7 @@ template <int MODE, bool SPLIT> __device__ __forceinline__ ProductTile product_t
         p.step0 = (uint32_t)((uint64_t)p.all_steps * share / a.splits);
         p.steps = (uint32_t)((uint64_t)p.all_steps * (share + 1u) / a.splits) - p.step0;
     }
+    p.clears = MODE == kWeights && p.steps && p.step0 + p.steps == p.all_steps && (p.end - p.row) % kProductK != 0u;
     return p;
 }
 
@@ -188,9 +196,9 @@ template <int MODE> __device__ __forceinline__ void product_tables(const Product
 // The tile of a pair's round.
 __device__ __forceinline__ uint32_t product_turn(uint32_t round, uint32_t pair, uint32_t pairs) { return round * pairs + (round & 1u ? pairs - 1u - pair : pair); }
 
-// Rows of a stage's strips from `left` on become zero: what lies behind an expert's last row counts nothing, whatever it holds.  One warp.
+// Rows of a stage's strips from `left` on become zero: what lies behind an expert's last row counts nothing, whatever it holds.  One warp; the
+// products may be issued by the other block, which learns of it by an arrival that releases at the cluster's scope.
 __device__ __forceinline__ void product_clear(uint32_t from, uint32_t strips, uint32_t left) {
-    if (left >= kProductK) return;
     for (uint32_t j = 0; j < strips; ++j)
         for (uint32_t c = left * 8u + (threadIdx.x & 31u); c < kProductK * 8u; c += 32u)
             asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(from + j * 8192u + c * 16u), "r"(0u) : "memory");
@@ -240,7 +248,7 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
         for (uint32_t i = 0; i < a.stages; ++i) { mbar_init(&s.landed[i], 1u); mbar_init(&s.full[i], 2u); mbar_init(&s.empty[i], 1u); }
         for (uint32_t i = 0; i < 2u; ++i) { mbar_init(&s.ready[i], 1u); mbar_init(&s.taken[i], 16u); }
         mbar_init(&s.drained, 1u);
-        s.lost = 0u;
+        s.lost = 0u; s.gave_up = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -312,7 +320,7 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                 }
             };
             auto wait = [&]() {
-                if (fine) fine = __all_sync(kFullMask, mbar_wait(&s.ready[turn & 1u], turn / 2u & 1u, a.tries));
+                if (fine) fine = __all_sync(kFullMask, mbar_wait_cluster(&s.ready[turn & 1u], turn / 2u & 1u, a.tries));
                 __syncwarp();
                 tmem_after_barrier();
             };
@@ -383,11 +391,15 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
         if constexpr (MODE == kWeights && !SPLIT) if (elect_one()) wait_stores();
     } else {
         if constexpr (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        auto give_up = [&]() {                            // (both blocks of the pair know before they meet at the end)
+            for (uint32_t i = 0; i < 2u; ++i) store_word_to(address_in(&s.gave_up, leader + i), 1u);
+        };
         if (warp == 0u) {                                     // copies of tiles
             if (elect_one()) {
                 ProductRing ring;
-                uint32_t issued = 0;
+                uint32_t issued = 0, cleared = 0, parity = 0;         // (weights, a bit a stage) its last copies are `landed`'s; of that barrier
                 bool fine = true;
+                const uint32_t full0 = address_in(s.full, leader), landed0 = address_in(s.landed, leader + block);
                 for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
                     if (t >= tiles) continue;
                     const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
@@ -397,10 +409,18 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                     const int n0 = (int)((MODE == kWeights ? p.n0 : p.row) + block * p.half);
                     int at = (int)((MODE == kWeights ? p.row : 0u) + p.step0 * kProductK);      // in the contraction
                     for (uint32_t step = 0; step < p.steps; ++step, at += (int)kProductK) {
-                        fine = mbar_wait(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
+                        fine = mbar_wait_cluster(&s.empty[ring.stage], ring.round ^ 1u, a.tries);
                         if (!fine) break;
-                        const uint32_t bar = smem_u32(&s.landed[ring.stage]), to_a = stage0 + ring.stage * stage_bytes, to_b = to_a + kProductM / 2u * 128u;
-                        mbar_expect_tx(&s.landed[ring.stage], bytes);
+                        const uint32_t to_a = stage0 + ring.stage * stage_bytes, to_b = to_a + kProductM / 2u * 128u;
+                        // Both blocks' copies complete on the first block's barrier, for the products that read them; where rows are to be
+                        // cleared, on one of their own block's.
+                        uint32_t bar = full0 + 8u * ring.stage;
+                        if constexpr (MODE == kWeights) {
+                            const uint32_t bit = 1u << ring.stage;
+                            cleared &= ~bit;
+                            if (p.clears && step + 1u == p.steps) { bar = landed0 + 8u * ring.stage; cleared |= bit; parity ^= bit; }
+                        }
+                        mbar_expect_tx_at(bar, bytes);
                         if constexpr (MODE == kForward) tile_load_3d(to_a, &a.a_map, at, m0, (int)p.expert, bar);
                         else if constexpr (MODE == kInput) {
                             tile_load_3d(to_a, &a.a_map, m0, at, (int)p.expert, bar);
@@ -417,11 +437,13 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                         ++issued;
                     }
                 }
-                // what is still on its way lands before the block ends, whoever has given up: the last round of each stage
-                for (uint32_t i = min(issued, a.stages); i > 0u; --i) {
-                    const uint32_t back = ring.stage >= i ? ring.stage - i : ring.stage + a.stages - i;
-                    mbar_wait(&s.landed[back], back < ring.stage ? ring.round : ring.round ^ 1u);
+                // what is still on its way to a barrier of this block's alone lands before it ends
+                for (uint32_t i = 0; i < a.stages; ++i) if (cleared >> i & 1u) mbar_wait(&s.landed[i], (parity >> i & 1u) ^ 1u);
+                for (uint32_t i = 0; i < 2u; ++i) {
+                    store_word_to(address_in(&s.issued[block], leader + i), issued);
+                    store_word_to(address_in(&s.cleared[block], leader + i), cleared);
                 }
+                if (!fine) give_up();
             }
         } else if (warp == 1u && block == 0u) {               // products
             if (elect_one()) {
@@ -436,11 +458,11 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                     for (uint32_t step = 0; step < p.steps; ++step) {
                         const bool begins = SUMS ? step % kProductSum == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && (step + 1u) % kProductSum == 0u);
                         if (begins) {
-                            fine = mbar_wait(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
+                            fine = mbar_wait_cluster(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
                             acc = tmem + (turn & 1u) * a.most_n;
                         }
-                        fine = fine && mbar_wait(&s.full[ring.stage], ring.round, a.tries);
-                        if (!fine) break;
+                        fine = fine && mbar_wait_cluster(&s.full[ring.stage], ring.round, a.tries);
+                        if (!fine) { give_up(); break; }
                         tmem_after_barrier();
                         const uint32_t from_a = stage0 + ring.stage * stage_bytes, from_b = from_a + kProductM / 2u * 128u;
                         const uint32_t da = operand_at(from_a, MODE == kForward ? 0u : 8192u), db = operand_at(from_b, MODE == kWeights ? 8192u : 0u);
@@ -457,21 +479,21 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
             }
         } else if (warp == 1u) {
             mbar_wait(&s.drained, 0u);                        // (every signal of the other block's products has come)
-        } else if (warp == 2u) {                              // what has landed
-            ProductRing ring;
-            bool fine = true;
-            for (uint32_t t = pair, turns = 0; turns * pairs < tiles && fine; t = product_turn(++turns, pair, pairs)) {
+        } else if (MODE == kWeights && warp >= 2u) {          // rows behind an expert's last: two warps, each with stages of its own
+            uint32_t issued = 0, parity = 0;
+            for (uint32_t t = pair, turns = 0; turns * pairs < tiles; t = product_turn(++turns, pair, pairs)) {
                 if (t >= tiles) continue;
                 const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
-                for (uint32_t step = 0; step < p.steps; ++step) {
-                    fine = __all_sync(kFullMask, mbar_wait(&s.landed[ring.stage], ring.round, a.tries));
-                    if (!fine) break;
-                    const bool clear = MODE == kWeights && p.step0 + step + 1u == p.all_steps;
-                    if (clear)
-                        product_clear(stage0 + ring.stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, p.end - p.row - (p.step0 + step) * kProductK);
-                    if (lane == 0u) { if (clear) mbar_tell<true>(&s.full[ring.stage], leader); else mbar_tell(&s.full[ring.stage], leader); }
-                    ring.next(a.stages);
-                }
+                issued += p.steps;
+                if (!p.clears) continue;
+                const uint32_t stage = (issued - 1u) % a.stages;
+                // a warp's stages: of six or eight, and of every other one of them, about half (whoever waits for a barrier waits for each of its
+                // rounds: a parity tells no more than two apart)
+                if ((stage ^ stage / 2u ^ warp) & 1u) continue;
+                if (!__all_sync(kFullMask, mbar_wait(&s.landed[stage], parity >> stage & 1u, a.tries))) break;
+                parity ^= 1u << stage;
+                product_clear(stage0 + stage * stage_bytes, kProductM / 128u + (p.half + 63u) / 64u, (p.end - p.row) % kProductK);
+                if (lane == 0u) mbar_arrive_at(&s.full[stage], leader);
             }
         }
     }
@@ -481,11 +503,22 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
     cluster_meet();                                       // (neither block ends, or frees its accumulators, while the other's products or signals may need it)
     tmem_after_barrier();
     if (warp == 3u) tmem_free(tmem, columns);
+    // Where a thread gave up, copies may still be on their way to either block: the first block waits for the last of each stage, in the place of a
+    // block that did not come so far.  (One that did has seen the products of the round before, so the other was there, too.)
+    const bool gave_up = s.gave_up != 0u;
+    if (gave_up && warp == 0u && block == 0u && elect_one()) {
+        const uint32_t most = max(s.issued[0], s.issued[1]), least = min(s.issued[0], s.issued[1]), cleared = s.cleared[s.issued[0] < s.issued[1]];
+        for (uint32_t i = 0; i < min(most, a.stages); ++i) {
+            const uint32_t round = (most - 1u - i) / a.stages;
+            if (cleared >> i & 1u) continue;
+            if (least <= i + round * a.stages) mbar_arrive(&s.full[i]);
+            mbar_wait_cluster(&s.full[i], round & 1u);
+        }
+    }
     if constexpr (SPLIT) {
         if (warp >= 4u && pair < tiles) product_join<TO, MODE>(a, s, product_tile<MODE, SPLIT>(a, s, pair, share), stage0, share, block);
-        __syncwarp();
-        cluster_meet();                                   // (no block ends while others read its sums)
     }
+    if (SPLIT || gave_up) cluster_meet();                 // (no block ends while others read its sums, or its copies are on their way)
 }
 
 }  // namespace fsg

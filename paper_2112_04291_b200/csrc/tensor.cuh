@@ -17,13 +17,19 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 // ---- tiled copies -----------------------------------------------------------------------------
+// To this block's shared memory; the barrier (an address of the cluster's shared memory) may be this block's or the other's of the pair.
 __device__ __forceinline__ void tile_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void tile_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// One arrival on a barrier of the pair's, at an address of the cluster's shared memory, and the bytes that copies will bring: the thread itself
+// has written nothing that whoever waits would read, and the copies' own completion orders what they write.
+__device__ __forceinline__ void mbar_expect_tx_at(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 // A box of shared memory to a map's place; what of it lies outside the map is not written.  Boxes of a thread complete in groups.
 __device__ __forceinline__ void tile_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
@@ -36,14 +42,11 @@ __device__ __forceinline__ void wait_stores() { asm volatile("cp.async.bulk.wait
 // what this thread has written to shared memory is seen by copies and matrix instructions that are issued later
 __device__ __forceinline__ void fence_async_reads() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// One more arrival on a barrier of another block of the pair, about operands and accumulators alone: what copies and matrix instructions have
-// written is complete when its own barrier says so, and what threads have written to shared memory once they have fenced it (RELEASE: they have).
-// An order of the cluster's scope would be one for this thread's accesses to global memory, too, and cost a microsecond each time.
-template <bool RELEASE = false> __device__ __forceinline__ void mbar_tell(unsigned long long* bar, uint32_t block) {
-    if constexpr (RELEASE)
-        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.release.cta.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
-    else
-        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
+// One more arrival on a barrier of another block of the pair, about accumulators alone: what was read of them is ordered by the fences of tensor
+// memory on both sides (tmem_before_barrier here, tmem_after_barrier behind the wait, which is one of the cluster's scope), not by the arrival,
+// which would otherwise wait for this thread's stores to global memory.
+__device__ __forceinline__ void mbar_tell(unsigned long long* bar, uint32_t block) {
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [r];\n}" ::"r"(smem_u32(bar)), "r"(block) : "memory");
 }
 
 // ---- tensor memory, of a pair of blocks ---------------------------------------------------------

@@ -33,3 +33,24 @@ def test_products_whose_last_lanes_have_nothing_to_write(rows, ins, outs):
             assert torch.equal(y[part].double(), x[part].double() @ w[e].double().t())
             assert torch.equal(gx[part].double(), gy[part].double() @ w[e].double())
             assert torch.equal(gw[e].double(), gy[part].double().t() @ x[part].double())
+
+
+@pytest.mark.parametrize("experts,ins,outs,most", [(256, 72, 136, 70), (40, 520, 1_032, 300), (9, 2_056, 264, 1_500), (1, 264, 264, 5_000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_behind_an_experts_last_count_nothing_in_either_block(experts, ins, outs, most, dtype):
+    """The last stage of an expert's rows holds the next expert's, or NaN, in both blocks' operands: each gradient is that of its own rows, again and again."""
+    g = torch.Generator().manual_seed(experts)
+    lengths = torch.randint(0, most, (experts,), generator=g)
+    rows = int(lengths.sum())
+    starts = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    x, gy = _whole((rows + 70, ins), 1, torch.bfloat16, 1), _whole((rows + 70, outs), 1, torch.bfloat16, 2)
+    want = _full((experts, outs, ins), torch.float64, 0.0)
+    for e in range(experts):
+        part = slice(int(starts[e]), int(starts[e + 1]))
+        want[e] = gy[part].double().t() @ x[part].double()
+    x[rows:], gy[rows:] = float("nan"), float("inf")
+    at = starts.int().cuda()
+    for _ in range(20):
+        gw = _full((experts, outs, ins), dtype, MARK)
+        assert binding.expert_product_backward_weights(gy, x, at, gw) == 0
+        assert torch.equal(gw, want.to(gw.dtype))
