@@ -497,8 +497,9 @@ int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const ui
 int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const fastsgd_matrix* x, const uint32_t* order, uint32_t per_row,
                                             const uint32_t* starts, const fastsgd_experts* grad_weights, void* stream);
 
-/* bytes of workspace for fastsgd_order_ids and fastsgd_embedding_backward(_pairs) of `count` ids or rows of `cols` columns, and for products of
- * `rows` rows of `ins` columns by an order, which is made in it, too; 0 for invalid arguments */
+/* bytes of workspace for fastsgd_order_ids and fastsgd_embedding_backward(_pairs) of `count` ids or rows of `cols` columns or fewer, and for products
+ * of `rows` rows of `ins` columns or fewer by an order, which is made in it, too: one for the largest batch serves every smaller one; 0 for
+ * invalid arguments */
 uint64_t fastsgd_rows_workspace_bytes(uint64_t count, uint64_t cols);
 uint64_t fastsgd_products_workspace_bytes(uint64_t rows, uint64_t ins);
 

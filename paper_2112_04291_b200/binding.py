@@ -426,7 +426,7 @@ def rows_workspace_bytes(count: int, cols: int = 1) -> int:
 
 
 def ensure_rows_workspace(count: int, cols: int = 1, device="cuda") -> torch.Tensor:
-    """Allocates (torch) and registers a workspace large enough for order_ids and embedding_backward(_pairs) of `count` ids or rows of `cols` columns, if needed."""
+    """Allocates (torch) and registers a workspace large enough for order_ids and embedding_backward(_pairs) of `count` ids or rows of `cols` columns or fewer, if needed."""
     return _ensure(rows_workspace_bytes(count, cols), device)
 
 

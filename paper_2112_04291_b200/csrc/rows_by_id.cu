@@ -32,8 +32,14 @@ uint64_t order_tile(uint64_t count) {
     return kOrderThreads * rounds;
 }
 uint64_t order_blocks(uint64_t count) { return (count + order_tile(count) - 1) / order_tile(count); }
-uint64_t order_bytes(uint64_t count) {                     // behind the workspace's fixed part
-    return count <= kOrderMaxFew ? 0 : 4u * up_to(4u * count, 256) + up_to(4ull * kOrderMaxBins * order_blocks(count), 256) + 4u * kOrderMaxBins;
+uint64_t order_bytes(uint64_t count, uint64_t blocks) {    // behind the workspace's fixed part
+    return count <= kOrderMaxFew ? 0 : 4u * up_to(4u * count, 256) + up_to(4ull * kOrderMaxBins * blocks, 256) + 4u * kOrderMaxBins;
+}
+uint64_t order_bytes(uint64_t count) { return order_bytes(count, order_blocks(count)); }
+// ... of so many ids or fewer.  (Blocks become fewer where tiles become longer: 128 before each step.)
+uint64_t most_order_bytes(uint64_t count) {
+    const uint64_t blocks = order_blocks(count);
+    return order_bytes(count, count > 128u * kOrderThreads && blocks < 128u ? 128u : blocks);
 }
 
 // ---- an embedding's gradient -------------------------------------------------------------------------
@@ -55,6 +61,17 @@ GradientShape gradient_shape(uint64_t count, uint64_t cols) {
     return g;
 }
 uint64_t part_bytes(const GradientShape& g) { return up_to(8ull * g.tiles * g.part_stride, 256) + 16ull * g.tiles; }
+// ... of so many rows and columns or fewer: tiles become longer, and fewer, where rows or columns become more.  Tiles x chunks x lanes are no more than
+// the warps allow, a lane has eight columns, and there is always one tile.
+uint64_t most_part_bytes(uint64_t count, uint64_t cols) {
+    const uint64_t lanes = 32ull << kSumWarpsLog, stride = up_to(cols, 4);
+    uint64_t tiles = (count + 15u) / 16u;
+    if (tiles > lanes) tiles = lanes;
+    uint64_t values = tiles * stride;
+    if (values > 8u * lanes) values = 8u * lanes;
+    if (count && values < stride) values = stride;
+    return up_to(8u * values, 256) + 16u * tiles;
+}
 
 struct SumKernel { const void* fn; size_t smem; };
 template <class T, class TO, bool WIDE, bool PAIRS> SumKernel sum_kernel_as(bool full) {
@@ -249,13 +266,13 @@ extern "C" {
 
 uint64_t fastsgd_rows_workspace_bytes(uint64_t count, uint64_t cols) {
     if (count >= (1ull << 31) || cols < 1 || cols >= (1ull << 31)) return 0;
-    const uint64_t order = order_bytes(count), parts = part_bytes(gradient_shape(count, cols));
+    const uint64_t order = most_order_bytes(count), parts = most_part_bytes(count, cols);
     return up_to(kPartialsOffset + (order > parts ? order : parts), 256);
 }
 
 uint64_t fastsgd_products_workspace_bytes(uint64_t rows, uint64_t ins) {
     if (rows >= (1ull << 31) || ins < 1 || ins >= (1ull << 31)) return 0;
-    const uint64_t order = order_bytes(rows), sorted = sorted_bytes(rows, ins);
+    const uint64_t order = most_order_bytes(rows), sorted = sorted_bytes(rows, ins);
     return up_to(kPartialsOffset + (order > sorted ? order : sorted), 256);
 }
 

@@ -54,3 +54,25 @@ def test_rows_behind_an_experts_last_count_nothing_in_either_block(experts, ins,
         gw = _full((experts, outs, ins), dtype, MARK)
         assert binding.expert_product_backward_weights(gy, x, at, gw) == 0
         assert torch.equal(gw, want.to(gw.dtype))
+
+
+def test_a_workspace_for_the_largest_batch_serves_every_smaller_one():
+    """Tiles become longer at 8193 and 16385 rows of 2048 columns, and at 131073 ids: fewer rows then take more parts of sums, or counts."""
+    keep = binding._workspace_keepalive
+
+    def run(tokens, cols, vocab):
+        ids, grad = torch.arange(tokens, dtype=torch.int32, device="cuda") % vocab, _full((tokens, cols), torch.bfloat16, 1)
+        order, starts, table = _full((tokens,)), _full((vocab + 1,)), _full((vocab, cols), torch.float32)
+        assert binding.order_ids(ids, order, starts) == 0 and binding.embedding_backward(grad, ids, order, starts, table) == 0
+        assert torch.equal(table, torch.bincount(ids, minlength=vocab).float()[:, None].expand(vocab, cols))
+    try:
+        for tokens, cols, fewer in ((16_385, 2_048, (16_385, 16_384, 16_383, 8_193, 8_192, 4_100, 17, 1)), (131_073, 8, (131_073, 131_072, 131_071, 65_537, 65_536))):
+            torch.cuda.synchronize()
+            binding.set_workspace(torch.zeros(binding.rows_workspace_bytes(tokens, cols), dtype=torch.uint8, device="cuda"))
+            for n in fewer:
+                for c in (cols, cols - 1, cols // 2):
+                    run(n, c, 40)
+    finally:
+        torch.cuda.synchronize()
+        binding.set_workspace(keep if keep is not None else torch.zeros(64 << 20, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
