@@ -526,7 +526,8 @@ uint64_t fastsgd_workspace_bytes(uint64_t n, const fastsgd_params* params);
 
 /* Registers caller-owned device memory (256-byte aligned) as the library's
  * scratch and initialises it on `stream`.  The memory must stay valid until
- * another workspace is registered. */
+ * another workspace is registered, and as long as a graph is replayed that was
+ * captured while it was: a graph goes on using the one of its capture. */
 int fastsgd_set_workspace(void* dev_ptr, uint64_t bytes, void* stream);
 
 /* Synchronises `stream`, then copies total_bytes, d and status out of a

@@ -202,29 +202,40 @@ def workspace_bytes(n: int, p: Params) -> int:
     return int(lib().fastsgd_workspace_bytes(n, C.byref(p)))
 
 
-_workspace_keepalive = None
+_workspace_keepalive = None         # the last that was registered
+_workspaces = {}                    # by device: the one that the library uses there
+_allocated = {}                     # by device: those of the ensure_... functions; a graph captured with one goes on using it after another is registered
+_outgrown = []                      # a caller's own that they found too small
 
 
 def set_workspace(ws: torch.Tensor, stream=None) -> None:
-    """Registers a uint8 CUDA tensor as the library's scratch (kept alive here)."""
+    """Registers a uint8 CUDA tensor as the library's scratch on its device (kept alive here until another is registered by this call).  A graph
+    that was captured before goes on using the one that was registered then: whoever replays it keeps that tensor."""
     global _workspace_keepalive
     assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
-    _check(lib().fastsgd_set_workspace(ws.data_ptr(), ws.numel(), _stream_handle(stream)), "fastsgd_set_workspace")
-    _workspace_keepalive = ws
+    with torch.cuda.device(ws.device):
+        _check(lib().fastsgd_set_workspace(ws.data_ptr(), ws.numel(), _stream_handle(stream)), "fastsgd_set_workspace")
+    _workspaces[ws.get_device()] = _workspace_keepalive = ws
 
 
 def ensure_workspace(n: int, p: Params, device="cuda") -> torch.Tensor:
-    """Allocates (torch) and registers a workspace large enough for n entries, if needed."""
+    """Allocates (torch) and registers a workspace large enough for n entries, if needed.  One that becomes too small is kept, for graphs that were
+    captured with it."""
     return _ensure(workspace_bytes(n, p), device)
 
 
 def _ensure(need: int, device) -> torch.Tensor:
-    ws = _workspace_keepalive
     dev = torch.device(device)
-    if dev.index is None:
-        dev = torch.device(dev.type, torch.cuda.current_device())
-    if ws is None or ws.numel() < need or ws.device != dev:
-        ws = torch.empty(max(need, 4096), dtype=torch.uint8, device=dev)
+    index = torch.cuda.current_device() if dev.index is None else dev.index
+    ws = _workspaces.get(index)
+    if ws is None or ws.numel() < need:
+        mine = _allocated.setdefault(index, [])               # (ascending; each half as large again as the one before, at least)
+        if ws is not None and all(ws is not w for w in mine + _outgrown):
+            _outgrown.append(ws)
+        if not mine or mine[-1].numel() < need:
+            grown = mine[-1].numel() * 3 // 2 if mine else 0
+            mine.append(torch.empty(max(need, grown, 4096), dtype=torch.uint8, device=torch.device(dev.type, index)))
+        ws = mine[-1]
         set_workspace(ws)
     return ws
 

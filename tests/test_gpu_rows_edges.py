@@ -76,3 +76,39 @@ def test_a_workspace_for_the_largest_batch_serves_every_smaller_one():
         torch.cuda.synchronize()
         binding.set_workspace(keep if keep is not None else torch.zeros(64 << 20, dtype=torch.uint8, device="cuda"))
         torch.cuda.synchronize()
+
+
+def test_a_graph_replays_after_its_workspace_was_outgrown():
+    """A product by an order lays its rows out in the workspace of its capture, whatever has been registered and allocated since."""
+    x, w, ids = _whole((400, 264), 1, torch.float16, 1), _whole((6, 72, 264), 1, torch.float16, 2), _whole((400, 2), 1, torch.int32, 3).abs() * 3
+    order, starts, y = _full((800,)), _full((7,)), _full((800, 72), torch.float32)
+
+    def run():
+        assert binding.order_ids(ids, order, starts) == 0 and binding.expert_product(x, w, starts, y, order=order, per_row=2) == 0
+    binding.ensure_products_workspace(800, 264)
+    before = binding._workspace_keepalive
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        run()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            run()
+    torch.cuda.synchronize()
+    binding.ensure_products_workspace(before.numel() // 512, 264)               # one that is larger
+    address, size = before.data_ptr(), before.numel()
+    assert binding._workspace_keepalive.data_ptr() != address
+    del before
+    others = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    assert all(o.data_ptr() >= address + size or o.data_ptr() + size <= address for o in others)
+    for seed in (5, 6):
+        x.copy_(_whole(x.shape, 1, torch.float16, seed))
+        y.fill_(MARK)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        torch.cuda.synchronize()
+        at = starts.tolist()
+        for e in range(6):
+            part = slice(at[e], at[e + 1])
+            assert torch.equal(y[part].double(), x[order[part].long() // 2].double() @ w[e].double().t())
+    assert all((o == 255).all() for o in others)
