@@ -22,10 +22,12 @@
 //   32 x 4096 x 14336, 8 experts: 142 to 155 us, the weights' 940 MB at a copy's rate
 //   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 281 to 340 us, 738 MB written while 340 MB are read; bf16 234 to 270
 //
-// The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero: a sum of 512 values of the contraction loses
-// 4.7e-7 of the result, of 768 about 1.6e-6.  Where the result is wanted in 32 bits, accumulators begin anew every 512 values, and the warps that
-// write add them up in registers, rounding to nearest (SUMS): 4.8e-7 for 4096 values (plain sums in fp32: 6.1e-7).  So they do for results of 16 bits
-// where the contraction may have more than 2^16 values, which would lose a third of half a step of fp16.
+// The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero.  Measured, in proportion to the contraction's
+// length: 5.9e-9 of the result for each value where all have one sign (512 values 2.4e-6, 8192 4.8e-5, 65536 3.9e-4), 1e-9 where signs are random
+// (512 5.5e-7, 8192 8.4e-6, 65536 6.6e-5).  So accumulators begin anew after a while, and the warps that write add them up in registers, rounding to
+// nearest (SUMS): results of 32 bits every 512 values, whatever the length (plain sums in fp32 of 4096 values of random signs: 6.1e-7).  Results
+// of 16 bits may lose a quarter of half a step, which just below a power of two is 2^-12 of the value in fp16, 2^-9 in bf16: contractions that may
+// have more than 2^13 values (fp16) or 2^16 (bf16) are added up every 2^13.
 #pragma once
 
 #include "rows.cuh"
@@ -40,8 +42,9 @@ constexpr uint32_t kProductK          = 64u;              // of a stage
 constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their rows (weights)
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
-constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers
-constexpr uint64_t kProductLong       = 1ull << 16;       // values of a contraction that results of 16 bits are not added up for
+constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers: results of 32 bits, and shared contractions
+constexpr uint32_t kProductLongSum    = 128u;             // ... results of 16 bits, of contractions that may have more values than
+constexpr uint64_t kProductLongF16    = 1ull << 13, kProductLongBF16 = 1ull << 16;
 // Bytes of a box of a gradient of weights; each warp that writes has one.  With two or three, which it would wait for less, or with boxes of rows of
 // 128 bytes, there is room for five or four stages instead of six: 49152 x 2048 x 1408 of 64 experts 239 us as it is, 246, 245 (128) and 259 (two of
 // 128); to fp32 288, 298, 297, 319; 8192 x 2048 x 2048 of 8 52, 54, 54.5, 58; 4096 x 1016 x 680 of 60 30.6, 31.2, 29.8, 30.0.
@@ -56,6 +59,7 @@ struct alignas(64) ProductArgs {
     void*     out;
     uint64_t  out_stride, out_expert;
     uint32_t  most_n, box, stages;                        // columns of a tile at most; rows of a copy of B
+    uint32_t  sum_stages;                                 // (SUMS) of an accumulator
     uint32_t  splits;                                     // pairs of blocks that share a tile's contraction (a cluster; then a tile each)
     uint32_t  kind;
     uint32_t  tries;
@@ -342,7 +346,7 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum[j][i] = 0.f;
                 }
-                for (uint32_t step = 0; step < p.steps; step += kProductSum) {
+                for (uint32_t step = 0; step < p.steps; step += a.sum_stages) {
                     wait();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -454,9 +458,10 @@ template <class TO, int MODE, bool SUMS, bool SPLIT> __global__ void __launch_bo
                     if (t >= tiles) continue;
                     const ProductTile p = product_tile<MODE, SPLIT>(a, s, t, share);
                     const uint32_t shape = product_shape(a.kind, kProductM, 2u * p.half);
-                    uint32_t acc = 0;
+                    uint32_t acc = 0, piece = 0;
                     for (uint32_t step = 0; step < p.steps; ++step) {
-                        const bool begins = SUMS ? step % kProductSum == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && (step + 1u) % kProductSum == 0u);
+                        const bool begins = SUMS ? piece == 0u : step == 0u, ends = step + 1u == p.steps || (SUMS && piece + 1u == a.sum_stages);
+                        piece = ends ? 0u : piece + 1u;
                         if (begins) {
                             fine = mbar_wait_cluster(&s.taken[turn & 1u], (turn >> 1 & 1u) ^ 1u, a.tries);
                             acc = tmem + (turn & 1u) * a.most_n;

@@ -241,7 +241,9 @@ template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint64_t 
     const uint64_t least = a.most_n <= 64u ? 16u : MODE == kWeights ? 48u : 32u;
     a.splits = 1u;
     while (a.splits < 8u && tiles * a.splits * 2u <= 8ull * ((uint64_t)dev.sm_count / 20u) && steps >= (a.splits > 1u ? a.splits * 16ull : least)) a.splits *= 2u;
-    const void* fn = product_kernel<MODE>(to, (MODE == kWeights ? a.rows : a.k) > kProductLong, a.splits > 1u);
+    const uint64_t longest = MODE == kWeights ? a.rows : a.k;
+    const void* fn = product_kernel<MODE>(to, longest > (to == FASTSGD_F16 ? kProductLongF16 : kProductLongBF16), a.splits > 1u);
+    a.sum_stages = to == FASTSGD_F32 || a.splits > 1u ? kProductSum : kProductLongSum;
     const size_t smem = (size_t)a.stages * product_stage_bytes<MODE>(a.most_n) + turned + 1024u;
     uint64_t resident = 0;
     const int rc = resident_blocks(fn, kProductThreads, smem, dev, &resident);

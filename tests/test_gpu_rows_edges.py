@@ -112,3 +112,40 @@ def test_a_graph_replays_after_its_workspace_was_outgrown():
             part = slice(at[e], at[e + 1])
             assert torch.equal(y[part].double(), x[order[part].long() // 2].double() @ w[e].double().t())
     assert all((o == 255).all() for o in others)
+
+
+LENGTHS = [512, 8_192, 8_200, 20_000, 65_536, 65_544, 70_016]
+
+
+def _losses(got, want):
+    """What the sums of positive values lose, on average and at most, of the value."""
+    off = want - got.double()
+    return (off.mean() / want.mean()).item(), (off.abs() / want).max().item()
+
+
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_long_sums_of_one_sign_lose_no_more_than_is_said(length, dtype):
+    """Values of one sign show best what the tensor cores cut off towards zero.  16 bits: a quarter of half a step just below a power of two, 2^-14 of the
+    value in fp16 and 2^-11 in bf16, on average, since roundings of two million results are off by half a step at random (2^-11 / 1000 on average); a
+    single one by half a step more (finfo.eps / 2).  32 bits: 2^-18, and half a step for each addition of two sums of 512 values.  More than 28 tiles: no
+    contraction is shared."""
+    g = torch.Generator(device="cuda").manual_seed(length)
+    a = (torch.rand((4_096, length), generator=g, device="cuda") + 0.5).to(dtype)
+    c = ((torch.rand((512, length), generator=g, device="cuda") + 0.5) * (1000.0 / length)).to(dtype)
+    want = torch.cat([a[i:i + 512].double() @ c.double().t() for i in range(0, 4_096, 512)])
+    most = 2.0 ** -14 if dtype == torch.float16 else 2.0 ** -11
+    starts, rows = torch.tensor([0, 4_096], dtype=torch.int32, device="cuda"), torch.tensor([0, length], dtype=torch.int32, device="cuda")
+    y, wide = _full((4_096, 512), dtype, MARK), _full((4_096, 512), torch.float32, MARK)
+    assert binding.expert_product(a, c[None], starts, y) == 0 and binding.expert_product(a, c[None], starts, wide) == 0
+    at, ct = a.t().contiguous(), c.t().contiguous()
+    gx = _full((4_096, 512), dtype, MARK)
+    assert binding.expert_product_backward_input(a, ct[None], starts, gx) == 0
+    gw, wide_gw = _full((1, 4_096, 512), dtype, MARK), _full((1, 4_096, 512), torch.float32, MARK)
+    assert binding.expert_product_backward_weights(at, ct, rows, gw) == 0 and binding.expert_product_backward_weights(at, ct, rows, wide_gw) == 0
+    for got in (y, gx, gw[0]):
+        mean, worst = _losses(got, want)
+        assert abs(mean) <= most and worst <= most + torch.finfo(dtype).eps / 2
+    for got in (wide, wide_gw[0]):
+        mean, worst = _losses(got, want)
+        assert abs(mean) <= 2.0 ** -18 and worst <= 2.0 ** -18 + (length / 512 + 1) * 2.0 ** -24
