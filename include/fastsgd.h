@@ -403,6 +403,7 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
  * tokens that occur.  The experts whose selections fastsgd_expert_counts counts have products of their own.  Both work through
  * rows in the order of an id (token, expert), which fastsgd_order_ids makes once for all of them.  All calls only enqueue kernels on `stream`;
  * those that use the workspace say so and are serialised with the others that do, the rest may run on several streams at once.
+ * What a call writes lies apart from everything that it reads, and from what else it writes (else FASTSGD_E_BAD_PARAM).
  */
 
 /*

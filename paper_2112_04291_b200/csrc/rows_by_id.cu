@@ -1,6 +1,7 @@
 // C-ABI entries of the operators on rows that are chosen by an id: ids in order, an embedding's lookup and gradient, a router's
 // experts' products.  Argument checks and launches on the caller's stream, as in losses.cu.
 #include <atomic>
+#include <initializer_list>
 
 #include "host.cuh"
 #include "order.cuh"
@@ -14,6 +15,12 @@ using namespace fsg;
 bool apart(const void* p, uint64_t p_bytes, const void* q, uint64_t q_bytes) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
     return !p || !q || a + p_bytes <= b || b + q_bytes <= a;
+}
+// What a call writes lies apart from the whole numbers that it reads: blocks read them while others write.
+struct Words { const void* data; uint64_t count; };
+bool apart(const void* p, uint64_t p_bytes, std::initializer_list<Words> words) {
+    for (const Words& w : words) if (!apart(p, p_bytes, w.data, 4u * w.count)) return false;
+    return true;
 }
 bool apart(const fastsgd_matrix* p, const fastsgd_matrix* q) { return apart(p->data, span_bytes(p), q->data, span_bytes(q)); }
 
@@ -284,6 +291,9 @@ int fastsgd_order_ids(const int32_t* ids, uint64_t count, uint64_t range, uint32
     if ((count && (!ids || !order)) || !starts) return FASTSGD_E_NULL;
     if (!aligned_to(ids, 4) || !aligned_to(order, 4) || !aligned_to(starts, 4) || !aligned_to(distinct, 4) || !aligned_to(number, 4)) return FASTSGD_E_ALIGN;
     if (range > kOrderMaxRange) return FASTSGD_E_NOT_IMPLEMENTED;
+    const uint64_t some = count < range ? count : range;
+    if (!apart(order, 4u * count, {{ids, count}, {starts, range + 1u}, {distinct, some}, {number, 1u}}) || !apart(starts, 4u * (range + 1u), {{ids, count}, {distinct, some}, {number, 1u}})
+        || !apart(distinct, 4u * some, {{ids, count}, {number, 1u}}) || !apart(number, 4u, {{ids, count}})) return FASTSGD_E_BAD_PARAM;
     DeviceView dev;
     int rc = device_view(&dev);
     if (rc) return rc;
@@ -333,6 +343,7 @@ int fastsgd_embedding(const fastsgd_matrix* table, const int32_t* ids, float sca
     if (table->cols != out->cols || !types_go(table->type, out->type) || !apart(table, out)) return FASTSGD_E_BAD_PARAM;
     if (out->rows && !ids) return FASTSGD_E_NULL;
     if (!aligned_to(ids, 4)) return FASTSGD_E_ALIGN;
+    if (!apart(out->data, span_bytes(out), {{ids, out->rows}})) return FASTSGD_E_BAD_PARAM;
     if (!out->rows) return FASTSGD_OK;
     DeviceView dev;
     rc = device_view(&dev);
@@ -349,6 +360,7 @@ int fastsgd_embedding_backward(const fastsgd_matrix* grad, const int32_t* ids, c
     if ((grad->rows && (!ids || !order)) || !starts) return FASTSGD_E_NULL;
     if (!aligned_to(ids, 4) || !aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
     if (!table_grad->rows) return FASTSGD_E_BAD_N;
+    if (!apart(table_grad->data, span_bytes(table_grad), {{ids, grad->rows}, {order, grad->rows}, {starts, table_grad->rows + 1u}})) return FASTSGD_E_BAD_PARAM;
     DeviceView dev;
     rc = device_view(&dev);
     if (rc) return rc;
@@ -368,6 +380,9 @@ int fastsgd_embedding_backward_pairs(const fastsgd_matrix* grad, const int32_t* 
         return FASTSGD_E_ALIGN;
     const uint64_t bytes = 4u * most * grad->cols;
     if (!apart(grad->data, span_bytes(grad), keys, bytes) || !apart(grad->data, span_bytes(grad), values, bytes) || !apart(keys, bytes, values, bytes)) return FASTSGD_E_BAD_PARAM;
+    const uint64_t some = grad->rows < range ? grad->rows : range;
+    for (const void* written : {static_cast<const void*>(keys), static_cast<const void*>(values)})
+        if (!apart(written, bytes, {{ids, grad->rows}, {order, grad->rows}, {starts, range + 1u}, {distinct, some}, {number, 1u}})) return FASTSGD_E_BAD_PARAM;
     if (!grad->rows) return FASTSGD_OK;
     DeviceView dev;
     rc = device_view(&dev);
@@ -391,6 +406,7 @@ int fastsgd_expert_product(const fastsgd_matrix* x, const uint32_t* order, uint3
     if (!apart(x, y) || !apart(weights->data, span_bytes(weights), y->data, span_bytes(y))) return FASTSGD_E_BAD_PARAM;
     if (!starts) return FASTSGD_E_NULL;
     if (!aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!apart(y->data, span_bytes(y), {{order, y->rows}, {starts, weights->experts + 1u}})) return FASTSGD_E_BAD_PARAM;
     if (!y->rows || !x->rows) return FASTSGD_OK;
     DeviceView dev;
     rc = device_view(&dev);
@@ -420,6 +436,7 @@ int fastsgd_expert_product_backward_input(const fastsgd_matrix* grad_y, const ui
     if (!apart(grad_y, grad_x) || !apart(weights->data, span_bytes(weights), grad_x->data, span_bytes(grad_x))) return FASTSGD_E_BAD_PARAM;
     if (!starts) return FASTSGD_E_NULL;
     if (!aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!apart(grad_x->data, span_bytes(grad_x), {{starts, weights->experts + 1u}})) return FASTSGD_E_BAD_PARAM;
     if (!grad_y->rows) return FASTSGD_OK;
     DeviceView dev;
     rc = device_view(&dev);
@@ -447,6 +464,7 @@ int fastsgd_expert_product_backward_weights(const fastsgd_matrix* grad_y, const 
     if (!apart(grad_weights->data, span_bytes(grad_weights), grad_y->data, span_bytes(grad_y)) || !apart(grad_weights->data, span_bytes(grad_weights), x->data, span_bytes(x))) return FASTSGD_E_BAD_PARAM;
     if (!starts) return FASTSGD_E_NULL;
     if (!aligned_to(order, 4) || !aligned_to(starts, 4)) return FASTSGD_E_ALIGN;
+    if (!apart(grad_weights->data, span_bytes(grad_weights), {{order, grad_y->rows}, {starts, grad_weights->experts + 1u}})) return FASTSGD_E_BAD_PARAM;
     DeviceView dev;
     rc = device_view(&dev);
     if (rc) return rc;

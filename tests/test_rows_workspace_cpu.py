@@ -62,3 +62,49 @@ def test_sizes_stay_near_what_is_needed(lib):
         for c in COLS:
             if c <= 65_537:
                 assert lib.fastsgd_rows_workspace_bytes(n, c) <= lib.fastsgd_rows_workspace_bytes(0, 1) + _need(n, c) + 64 * 131_072 + 16 * 131_072 + 512
+
+
+# ---- outputs on top of whole numbers that the call reads -------------------------------------------
+
+A, B, C, D, E, F = (1 << 20 | i << 24 for i in range(1, 7))      # never dereferenced: the checks fail before any launch
+
+
+def _matrix(data, rows, cols, kind=binding.BF16):
+    return binding.Matrix(data, rows, cols, cols, kind, 0)
+
+
+def test_an_order_does_not_lie_on_its_ids_or_its_starts(lib):
+    def call(ids=A, order=B, starts=C, distinct=D, number=E):
+        return lib.fastsgd_order_ids(ids, 70_000, 500, order, starts, distinct, number, None)
+    at = dict(ids=A, order=B, starts=C, distinct=D, number=E)
+    size = dict(ids=70_000, order=70_000, starts=501, distinct=500, number=1)
+    for one in at:
+        for other in at:
+            if one != other:
+                assert call(**{one: at[other] + 4 * (size[other] - 1)}) == binding.E_BAD_PARAM
+                assert call(**{one: at[other] - 4 * (size[one] - 1)}) == binding.E_BAD_PARAM
+    assert call(order=A, distinct=None, number=None) == binding.E_BAD_PARAM
+
+
+def test_rows_do_not_lie_on_the_ids_that_choose_them(lib):
+    table, grad = _matrix(A, 100, 16), _matrix(B, 10, 16)
+    for ids in (B, B + 16 * 2 * 10 - 4):
+        assert lib.fastsgd_embedding(table, ids, 1.0, grad, None) == binding.E_BAD_PARAM
+    for i in range(3):
+        words = [C, D, E]
+        words[i] = A + 100 * 32 - 4
+        assert lib.fastsgd_embedding_backward(grad, *words, 1.0, table, None) == binding.E_BAD_PARAM
+    for on in (A, F):
+        for i in range(5):
+            words = [C, C + 4096, D, D + 4096, E]
+            words[i] = on + 4 * 10 * 16 - 4
+            assert lib.fastsgd_embedding_backward_pairs(grad, *words, 100, 1.0, A, F, 10, None) == binding.E_BAD_PARAM
+
+
+def test_products_do_not_lie_on_the_order_or_the_starts(lib):
+    x, y, w = _matrix(A, 10, 16), _matrix(B, 20, 24), binding.Experts(C, 4, 24, 16, 16, 24 * 16, binding.BF16, 0)
+    for order, starts in ((B + 4, D), (D, B + 20 * 48 - 4)):
+        assert lib.fastsgd_expert_product(x, order, 2, starts, w, y, None) == binding.E_BAD_PARAM
+    assert lib.fastsgd_expert_product_backward_input(y, E + 20 * 32 - 4, w, _matrix(E, 20, 16), None) == binding.E_BAD_PARAM
+    for order, starts in ((C + 4, D), (D, C + 4 * 24 * 32 - 4)):
+        assert lib.fastsgd_expert_product_backward_weights(y, x, order, 2, starts, w, None) == binding.E_BAD_PARAM
