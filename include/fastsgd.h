@@ -411,7 +411,8 @@ int fastsgd_balance_loss(const fastsgd_matrix* logits, const uint8_t* mask, cons
  *   ids       device, count < 2^31; one outside [0, range) was padded or dropped and is left out
  *   range     1 .. 2^20 (above: FASTSGD_E_NOT_IMPLEMENTED)
  *   order     device, room for count: the positions of the ids that are not left out, in ascending order of the ids, equal ids in
- *             ascending order of their positions; what lies behind the last of them is not written
+ *             ascending order of their positions; what lies behind the last of them is not written (who goes on to make tokens of the whole
+ *             order writes -1 there before)
  *   starts    device, range + 1: positions of id v are order[starts[v]] .. order[starts[v + 1] - 1]
  *   distinct  device, room for min(count, range), or NULL: the ids that occur, ascending
  *   number    device, one, or NULL: how many these are

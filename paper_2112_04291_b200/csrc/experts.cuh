@@ -16,11 +16,11 @@
 // further warps of each block so (with one, 40 rows, 8 experts, 14336 x 4096: 249 us, with two 163; 512 rows, nothing to clear, 160).  Waits for what
 // the other block's threads, copies or products signal are of the cluster's scope; that costs nothing that could be measured.  Where there are few tiles of a long
 // contraction, up to eight pairs of a cluster share each, and add up what they have through their shared memory.  A single thread issues copies and
-// products: what bounds the rate is then the tensor cores (and the GPU's power) alone.  Bounds, measured, with sorted rows and one GPU to itself:
-//   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1390 us each way (1380 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
-//   49152 x 2048 x 1408, 64 experts: 205 to 230 us (1230 to 1390 TFLOP/s; 19 rounds of tiles, the last partly filled, 5.5 tiles of 256 outs)
-//   32 x 4096 x 14336, 8 experts: 142 to 155 us, the weights' 940 MB at a copy's rate
-//   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 281 to 340 us, 738 MB written while 340 MB are read; bf16 234 to 270
+// products: what bounds the rate is then the tensor cores (and the GPU's power) alone.  Measured, with sorted rows, by the GPU and its clocks:
+//   16384 x 4096 x 14336 bf16, 8 experts: 1160 to 1460 us each way (1320 to 1650 TFLOP/s; a library's product of one matrix of that size, 1590)
+//   49152 x 2048 x 1408, 64 experts: 205 to 286 us (990 to 1390 TFLOP/s; 19 rounds of tiles, the last partly filled, 5.5 tiles of 256 outs); to fp32 273 to 290
+//   32 x 4096 x 14336, 8 experts: 142 to 156 us, the weights' 940 MB at a copy's rate
+//   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 281 to 384 us, 738 MB written while 340 MB are read; bf16 234 to 302, fp16 277 to 340
 //
 // The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero.  Measured, in proportion to the contraction's
 // length: 5.9e-9 of the result for each value where all have one sign (512 values 2.4e-6, 8192 4.8e-5, 65536 3.9e-4), 1e-9 where signs are random

@@ -51,8 +51,8 @@ uint64_t most_order_bytes(uint64_t count) {
 
 // ---- an embedding's gradient -------------------------------------------------------------------------
 
-// Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave so many warps, one or two rounds of
-// what the GPU holds at once.  (us with 2^12, 2^13, 2^14 warps: 65536 x 768 bf16 of 2 rows 33, 45, 65; 65536 x 512 of 1000 rows 23, 26, 34; 30001 x 1001
+// Lanes that share a chunk of a row, chunks of a row, and positions of a tile: from 16 on as many as leave so many warps or fewer; of those with
+// 24 warps an SM the GPU holds 3552 at once.  (us with 2^12, 2^13, 2^14 warps: 65536 x 768 bf16 of 2 rows 33, 45, 65; 65536 x 512 of 1000 rows 23, 26, 34; 30001 x 1001
 // fp16 37.5, 38.5, 44.7; 49152 x 2048 bf16 52, 52, 58; pairs of 16384 x 2048 bf16 57, 49, 53: but their sums are those of the dense gradient, bit for bit.)
 constexpr uint32_t kSumWarpsLog = 12u;
 struct GradientShape { uint32_t lanes_log, chunks, tile_log, tiles; uint64_t part_stride; };
@@ -243,8 +243,8 @@ template <int MODE> int launch_product(ProductArgs& a, uint64_t tiles, uint64_t 
     // Few tiles of a contraction of at least `least` stages: up to eight pairs of blocks share it, as long as each has eight stages, and as clusters
     // of them all find room at once (of sixteen blocks one in each of the GPU's groups of 16 to 20 SMs, of eight and four two and four).  Adding up
     // wide tiles takes as long as some 30 stages, and those of the weights' gradients are 256 wide.  Unshared and shared, us:
-    //   8 rows, 1024 / 2048 / 4096 -> 512: 7.7, 11.0, 17.5 and 7.5, 7.5, 7.9;  200 rows, 2048 -> 1024: 13.7 and 11.1, 1024 -> 2048: 9.8 and 12.1
-    //   gradient of 512 x 512 weights, 2000 / 4096 / 60000 rows: 16.3, 24.9, 290 and 18.2, 16.5, 69
+    //   8 rows, 1024 / 2048 / 4096 -> 512: 7.3, 10.5, 16.9 and 7.3, 7.4, 7.7;  200 rows, 2048 -> 1024: 13.5 and 11.0, 1024 -> 2048: 9.7 and 12.1
+    //   gradient of 512 x 512 weights, 2000 / 3000 / 4096 / 60000 rows: 14.4, 18.1, 22.9, 267 and 16.1, 13.1, 14.0, 48
     const uint64_t least = a.most_n <= 64u ? 16u : MODE == kWeights ? 48u : 32u;
     a.splits = 1u;
     while (a.splits < 8u && tiles * a.splits * 2u <= 8ull * ((uint64_t)dev.sm_count / 20u) && steps >= (a.splits > 1u ? a.splits * 16ull : least)) a.splits *= 2u;
