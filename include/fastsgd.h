@@ -475,9 +475,9 @@ typedef struct fastsgd_experts {
  *            the weights
  * Matrices begin on 16 bytes; their columns and strides are multiples of 8 (else FASTSGD_E_ALIGN); x and the weights are of 16 bits (fp32:
  * FASTSGD_E_NOT_IMPLEMENTED).  Products are summed in 32 bits by the tensor cores, which cut off towards zero what an addition has beyond them, and
- * every 512 values of the contraction (results of 16 bits: every 8192 where it may have more than 8192, fp16, or 65536, bf16) rounding to nearest:
- * results of 32 bits lose less than 2^-18 of the sum of magnitudes, those of 16 bits less than a quarter of half a step of their type before they are
- * rounded once.  (fastsgd_expert_product_backward_weights: the contraction is over the rows; "may have" goes by all rows.)  One launch and no workspace for sorted rows; with an order x's
+ * every 512 values of the contraction (results of 16 bits: every 4096 where it may have more than 4096, fp16, or 32768, bf16) rounding to nearest.
+ * Of the sum of magnitudes, results of 32 bits lose less than 2^-16 so (2^-18 where the values are alike), those of 16 bits less than 2^-13 (fp16) or
+ * 2^-10 (bf16), half of half a step, before they are rounded once.  (fastsgd_expert_product_backward_weights: the contraction is over the rows; "may have" goes by all rows.)  One launch and no workspace for sorted rows; with an order x's
  * rows are sorted first: a launch more, and a workspace of fastsgd_products_workspace_bytes(y->rows, x->cols).
  * The kernel's waits have a limit of some seconds; where one ran out, what its block had not yet written is NaN.
  */

@@ -23,11 +23,12 @@
 //   gradients of 64 experts' 1408 x 2048 weights of 49152 rows, fp32: 281 to 384 us, 738 MB written while 340 MB are read; bf16 234 to 302, fp16 277 to 340
 //
 // The tensor cores cut off what an addition to an accumulator has beyond 32 bits, always towards zero.  Measured, in proportion to the contraction's
-// length: 5.9e-9 of the result for each value where all have one sign (512 values 2.4e-6, 8192 4.8e-5, 65536 3.9e-4), 1e-9 where signs are random
-// (512 5.5e-7, 8192 8.4e-6, 65536 6.6e-5).  So accumulators begin anew after a while, and the warps that write add them up in registers, rounding to
-// nearest (SUMS): results of 32 bits every 512 values, whatever the length (plain sums in fp32 of 4096 values of random signs: 6.1e-7).  Results
-// of 16 bits may lose a quarter of half a step, which just below a power of two is 2^-12 of the value in fp16, 2^-9 in bf16: contractions that may
-// have more than 2^13 values (fp16) or 2^16 (bf16) are added up every 2^13.
+// length, of the sum of magnitudes: 5.9e-9 for each value where all have one sign (512 values 2.4e-6, 8192 4.8e-5, 65536 3.9e-4), up to 2.6 times
+// that where the first values outweigh the others (512 6.4e-6, 1.1e-5 at most; 8192 1.0e-4); 1e-9 of the result where signs are random (512 5.5e-7, 8192
+// 8.4e-6).  So accumulators begin anew after a while, and the warps that write add them up in registers, rounding to nearest (SUMS): results of 32 bits
+// every 512 values, whatever the length (plain sums in fp32 of 4096 values of random signs: 6.1e-7).  Results of 16 bits may lose a quarter of half
+// a step on average, which just below a power of two is 2^-12 of the value in fp16, 2^-9 in bf16: contractions that may have more than 2^12 values
+// (fp16) or 2^15 (bf16) are added up every 2^12.
 #pragma once
 
 #include "rows.cuh"
@@ -43,8 +44,8 @@ constexpr uint32_t kProductMaxStages  = 12u;
 constexpr uint32_t kProductSorted     = 256u;             // experts that are put in order of their rows (weights)
 constexpr uint32_t kProductBand       = 8u;               // tiles of weights that are gone through together
 constexpr uint32_t kProductSum        = 8u;               // stages between two additions in registers: results of 32 bits, and shared contractions
-constexpr uint32_t kProductLongSum    = 128u;             // ... results of 16 bits, of contractions that may have more values than
-constexpr uint64_t kProductLongF16    = 1ull << 13, kProductLongBF16 = 1ull << 16;
+constexpr uint32_t kProductLongSum    = 64u;              // ... results of 16 bits, of contractions that may have more values than
+constexpr uint64_t kProductLongF16    = 1ull << 12, kProductLongBF16 = 1ull << 15;
 // Bytes of a box of a gradient of weights; each warp that writes has one.  With two or three, which it would wait for less, or with boxes of rows of
 // 128 bytes, there is room for five or four stages instead of six: 49152 x 2048 x 1408 of 64 experts 239 us as it is, 246, 245 (128) and 259 (two of
 // 128); to fp32 288, 298, 297, 319; 8192 x 2048 x 2048 of 8 52, 54, 54.5, 58; 4096 x 1016 x 680 of 60 30.6, 31.2, 29.8, 30.0.

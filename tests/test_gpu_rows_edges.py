@@ -149,3 +149,25 @@ def test_long_sums_of_one_sign_lose_no_more_than_is_said(length, dtype):
     for got in (wide, wide_gw[0]):
         mean, worst = _losses(got, want)
         assert abs(mean) <= 2.0 ** -18 and worst <= 2.0 ** -18 + (length / 512 + 1) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("length", [512, 4_096, 4_104, 8_192, 32_768, 32_776])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_sums_whose_first_value_outweighs_the_others_lose_no_more_than_is_said(length, dtype):
+    """An accumulator that is large from the first step on cuts off most.  Of the sum: a quarter of half a step (2^-14 fp16, 2^-11 bf16) on average, half of
+    it for a single result of 16 bits, and half a step for its rounding; 2^-16 for one of 32 bits, and half a step for each addition of two sums."""
+    g = torch.Generator(device="cuda").manual_seed(length)
+    a, c = (torch.rand((n, length), generator=g, device="cuda") + 0.5 for n in (4_096, 512))
+    a[:, 0] *= 300.0
+    c[:, 0] *= length / 3.0
+    c *= 10.0 / length
+    a, c = a.to(dtype), c.to(dtype)
+    want = torch.cat([a[i:i + 512].double() @ c.double().t() for i in range(0, 4_096, 512)])
+    assert want.max() < 60_000
+    starts, mean_most = torch.tensor([0, 4_096], dtype=torch.int32, device="cuda"), 2.0 ** -14 if dtype == torch.float16 else 2.0 ** -11
+    y, wide = _full((4_096, 512), dtype, MARK), _full((4_096, 512), torch.float32, MARK)
+    assert binding.expert_product(a, c[None], starts, y) == 0 and binding.expert_product(a, c[None], starts, wide) == 0
+    mean, worst = _losses(y, want)
+    assert abs(mean) <= mean_most and worst <= 2.0 * mean_most + torch.finfo(dtype).eps / 2
+    _, worst = _losses(wide, want)
+    assert worst <= 2.0 ** -16 + (length / 512 + 1) * 2.0 ** -24
