@@ -628,7 +628,7 @@ def debug_layout() -> dict:
 def workspace_u32(field: str, count: int):
     """`count` 32-bit words of the registered workspace at a field of debug_layout(), as a torch view
     (reads and writes go to device memory; synchronise before relying on them)."""
-    ws = _workspace_keepalive
+    ws = _workspaces.get(torch.cuda.current_device())
     assert ws is not None, "no workspace registered through this module"
     off = debug_layout()[field]
     return ws[off:off + 4 * count].view(torch.int32)
